@@ -307,6 +307,57 @@ int profk_debug_sae_sample(const profk_plan_t* plan, const void* x, const void* 
                            uint64_t seed, uint32_t* keys_dev, void* ws, size_t ws_bytes,
                            void* stream);
 
+/* ---- Rows of logits: token log probabilities and their gradient ----
+ *
+ * With x one row of V logits, lse = log sum_j exp(x_j), p_j = exp(x_j - lse)
+ * and y the row's token:
+ *   logprob = x_y - lse
+ *   entropy = -sum_j p_j log p_j  (terms with p_j = 0 are 0)
+ *   alternatives: the n_top largest x_j in the total order, as (x_j - lse, j).
+ * All sums are fp32; a row's last step is taken in 64 bits.
+ *
+ *   logits   fp32 or bf16 [T, V], rows row_stride elements apart.  T = 0 is
+ *            accepted and does nothing; 1 <= V <= 2^31 - 1.
+ *   tokens   int64 [T].  Negative: the row has no token; its logprob is 0 and
+ *            has no gradient.  V or more: logprob and gradient are NaN.
+ *   -inf     a logit of -inf has p = 0 and is never an alternative.  Where
+ *            fewer than n_top remain, the rest is (-inf, -1).  A row of
+ *            nothing but -inf has lse = logprob = -inf, entropy 0 and a zero
+ *            gradient.  The lowest finite value is a value like any other.
+ *   NaN, +inf  a row with either has NaN for lse, logprob and entropy (and
+ *            log probabilities of alternatives, whose order stays the total
+ *            order; -NaN is never one), and a NaN gradient.
+ *   outputs  logprob, entropy, lse fp32 [T]; alternatives fp32 and int64
+ *            [T, n_top], 0 <= n_top <= 64 (NULL for n_top = 0).
+ *   ws       profk_token_logprobs_workspace_size(T, V, n_top) bytes, 16-byte
+ *            aligned, for few rows, which are split over several workgroups;
+ *            0 (and NULL) otherwise.
+ * Errors: PROFK_EDTYPE, PROFK_EINVAL (sizes, strides, alignment),
+ * PROFK_ENULL, PROFK_EWORKSPACE, PROFK_EHIP. */
+size_t profk_token_logprobs_workspace_size(int64_t T, int64_t V, int64_t n_top);
+int profk_token_logprobs(int32_t dtype, const void* logits, int64_t T, int64_t V, int64_t row_stride,
+                         const int64_t* tokens, int64_t n_top, float* out_logprob, float* out_entropy,
+                         float* out_lse, float* out_top_logprob, int64_t* out_top_idx, void* ws,
+                         size_t ws_bytes, void* stream);
+
+/* The gradient of sum_r g_logprob[r] logprob[r] + g_entropy[r] entropy[r] +
+ * sum_i g_top[r, i] top_logprob[r, i] with respect to the logits:
+ *   out_j = g ([j = y] - p_j) - h p_j (log p_j + H) + sum_i t_i ([j = a_i] - p_j)
+ * rounded once to the logits' dtype.  lse and entropy are the forward call's;
+ * where an lse is 16384 or more in size, too coarse in fp32 for p, it is taken
+ * from the row again (slowly).
+ * top_idx may be the call's alternatives or any other indices.  g_logprob (with
+ * tokens), g_entropy (with entropy) and the alternatives (n_top = 0) may each
+ * be left out as NULL.  top_idx entries that are negative or V and more take
+ * no gradient; an index may occur more than once, or be the token's.  `out`
+ * has rows out_stride elements apart; the memory from its first element to its
+ * last must not overlap the logits' (PROFK_EINVAL).  No workspace. */
+int profk_token_logprobs_grad(int32_t dtype, const void* logits, int64_t T, int64_t V, int64_t row_stride,
+                              const int64_t* tokens, const float* lse, const float* entropy,
+                              const float* g_logprob, const float* g_entropy, int64_t n_top,
+                              const int64_t* top_idx, const float* g_top, void* out, int64_t out_stride,
+                              void* stream);
+
 /* profk_topk with stages 1-2 replaced by a caller-given threshold key, to
  * drive the underflow and overflow paths on purpose.  A key alone names no
  * threshold pair, so this entry point filters with key >= tau_key also for

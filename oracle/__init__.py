@@ -16,6 +16,9 @@ Modules
   exact  -- O1: exact top-k by a full stable sort (Sec. 3 problem statement).
   profk  -- O2: the four stages of Prof-K (Sec. 3) step by step on the CPU,
             for the flat, per-row and flattened-BatchTopK forms.
+  sae    -- O3: the SAE encoder and decoder around the selection.
+  logprobs -- O4: token log probabilities, entropy and alternatives of rows
+            of logits, and their gradient.
 
 Floating point is fp64 throughout the planner; every other step is integer
 or bit-copy work and therefore exact.

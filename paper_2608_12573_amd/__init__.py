@@ -8,6 +8,8 @@ built, every call raises instead of computing anything on the CPU.
     vals, idx, info = topk(x, k)                  # x: 1-D fp32/bf16 CUDA tensor
     vals, idx, info = topk_rows(x, k)             # x: [B, D]
     vals, idx, info = batchtopk(x, k_row)         # global top-(B*k_row) of [B, D]
+    logprob, entropy, lse, top_logprob, top_idx = token_logprobs(logits, tokens, n_top)
+    d_logits = token_logprobs_grad(logits, tokens, lse, entropy, g_logprob)
 """
 
 import ctypes
@@ -110,6 +112,10 @@ def lib():
         L.profk_sae_decode_workspace_size.argtypes = [i64, i64]
         L.profk_sae_decode_workspace_size.restype = sz
         L.profk_sae_decode.argtypes = [vp, vp, i64, vp, vp, i64, i64, i64, vp, vp, sz, vp]
+        L.profk_token_logprobs_workspace_size.argtypes = [i64, i64, i64]
+        L.profk_token_logprobs_workspace_size.restype = sz
+        L.profk_token_logprobs.argtypes = [i32, vp, i64, i64, i64, vp, i64, vp, vp, vp, vp, vp, vp, sz, vp]
+        L.profk_token_logprobs_grad.argtypes = [i32, vp, i64, i64, i64, vp, vp, vp, vp, vp, i64, vp, vp, vp, i64, vp]
         L.profk_debug_sae_sample.argtypes = [P(Plan), vp, vp, vp, i64, i64, i64, u64, vp, vp, sz, vp]
         _lib = L
     return _lib
@@ -530,3 +536,106 @@ def debug_sae_sample(x, w_enc, b_enc, p, seed=0, ws=None):
                                         seed, _ptr(keys), _ptr(ws), _nbytes(ws), _stream()))
     return keys.to(torch.int64) & 0xFFFFFFFF
 
+
+
+# ------------------------------------------- rows of logits: probabilities ---
+
+MAX_TOP = 64                       # most alternatives of a row
+
+
+def _vector(t, name, dtype, shape, device):
+    """A contiguous input of exactly this dtype and shape, on `device`."""
+    torch = _torch()
+    if not isinstance(t, torch.Tensor):
+        raise ProfkError(f"{name} must be a torch tensor")
+    if t.dtype != dtype or tuple(t.shape) != shape or not t.is_contiguous():
+        raise ProfkError(f"{name} must be contiguous {dtype} of shape {shape}, got {t.dtype} {tuple(t.shape)}")
+    _on_device(t, name, device)
+
+
+def _logits(x):
+    """Checks logits [T, V] (rows may be strided): dtype code, T, V, stride."""
+    dt = _input(x, "logits", 2, layout="rows")
+    T, V = x.shape
+    return dt, T, V, max(x.stride(0), V) if T > 1 else V
+
+
+def token_logprobs_workspace(T, V, n_top=0, device="cuda"):
+    """A workspace for token_logprobs of T rows of V logits (may be empty)."""
+    torch = _torch()
+    return torch.empty(int(lib().profk_token_logprobs_workspace_size(T, V, n_top)), dtype=torch.uint8, device=device)
+
+
+def token_logprobs_outputs(T, n_top=0, device="cuda"):
+    """New outputs of token_logprobs: (logprob, entropy, lse) fp32 [T], and
+    the alternatives' log probabilities fp32 and indices int64 [T, n_top]."""
+    torch = _torch()
+    f32 = dict(dtype=torch.float32, device=device)
+    return (torch.empty(T, **f32), torch.empty(T, **f32), torch.empty(T, **f32), torch.empty((T, n_top), **f32),
+            torch.empty((T, n_top), dtype=torch.int64, device=device))
+
+
+def token_logprobs(logits, tokens, n_top=0, ws=None, out=None):
+    """Log probabilities of the given tokens under softmax(logits), with each
+    row's entropy, log-sum-exp and n_top most probable alternatives:
+    (logprob [T], entropy [T], lse [T], top_logprob [T, n_top],
+    top_idx [T, n_top]).
+
+    logits: fp32 or bf16 [T, V], rows may be strided.  tokens: int64 [T];
+    negative for rows without a token (logprob 0), NaN results from V up.
+    Alternatives are most probable first, equal ones by smaller index; logits
+    of -inf are never among them ((-inf, -1) where too few are left)."""
+    torch = _torch()
+    dt, T, V, stride = _logits(logits)
+    _vector(tokens, "tokens", torch.int64, (T,), logits.device)
+    if not 0 <= n_top <= MAX_TOP:
+        raise ProfkError(f"n_top must be from 0 to {MAX_TOP}, got {n_top}")
+    n = int(lib().profk_token_logprobs_workspace_size(T, V, n_top))
+    if ws is None:
+        ws = torch.empty(n, dtype=torch.uint8, device=logits.device)
+    else:
+        _bytes_buffer(ws, "ws", n, logits.device)
+    if out is None:
+        out = token_logprobs_outputs(T, n_top, logits.device)
+    else:
+        for i, t in enumerate(out):
+            _vector(t, f"out[{i}]", torch.int64 if i == 4 else torch.float32, (T,) if i < 3 else (T, n_top),
+                    logits.device)
+    lp, h, lse, top, idx = out
+    _check(lib().profk_token_logprobs(dt, _ptr(logits), T, V, stride, _ptr(tokens), n_top, _ptr(lp), _ptr(h),
+                                      _ptr(lse), _ptr(top), _ptr(idx), _ptr(ws) if n else None, n, _stream()))
+    return out
+
+
+def token_logprobs_grad(logits, tokens, lse, entropy, g_logprob, g_entropy=None, top_idx=None, g_top=None, out=None):
+    """The gradient with respect to the logits of token_logprobs' outputs,
+    given theirs: g_logprob [T], g_entropy [T] or None, and g_top [T, n] for
+    the alternatives at top_idx [T, n] or None.  lse and entropy are
+    token_logprobs'.  out: the logits' dtype and shape, rows may be strided;
+    it must not overlap the logits."""
+    torch = _torch()
+    dt, T, V, stride = _logits(logits)
+    dev = logits.device
+    _vector(tokens, "tokens", torch.int64, (T,), dev)
+    for t, name in ((lse, "lse"), (entropy, "entropy"), (g_logprob, "g_logprob"), (g_entropy, "g_entropy")):
+        if t is not None or name == "lse":
+            _vector(t, name, torch.float32, (T,), dev)
+    if g_entropy is not None and entropy is None:
+        raise ProfkError("g_entropy needs the rows' entropy")
+    n = 0
+    if g_top is not None:
+        if not isinstance(top_idx, torch.Tensor) or top_idx.dim() != 2 or top_idx.shape[1] > MAX_TOP:
+            raise ProfkError(f"top_idx must be [T, n] with n at most {MAX_TOP}")
+        n = top_idx.shape[1]
+        _vector(top_idx, "top_idx", torch.int64, (T, n), dev)
+        _vector(g_top, "g_top", torch.float32, (T, n), dev)
+    if out is None:
+        out = torch.empty((T, V), dtype=logits.dtype, device=dev)
+    ot, oT, oV, ostride = _logits(out)
+    if (ot, oT, oV) != (dt, T, V):
+        raise ProfkError("out must have the logits' dtype and shape")
+    _on_device(out, "out", dev)
+    _check(lib().profk_token_logprobs_grad(dt, _ptr(logits), T, V, stride, _ptr(tokens), _ptr(lse), _ptr(entropy),
+                                           _ptr(g_logprob), _ptr(g_entropy), n, _ptr(top_idx), _ptr(g_top),
+                                           _ptr(out), ostride, _stream()))
+    return out

@@ -305,6 +305,96 @@ int profk_topk_rows(const profk_plan_t* plan, int32_t dtype, const void* values,
   return PROFK_OK;
 }
 
+// ---- Token log probabilities ----
+
+namespace {
+
+// Shapes of the log probability calls; T = 0 is a call without rows.
+int check_logits(int32_t dtype, int64_t T, int64_t V, int64_t row_stride, int64_t n_top) {
+  if (!dtype_ok(dtype)) return PROFK_EDTYPE;
+  if (T < 0 || T > static_cast<int64_t>(INT32_MAX) || V < 1 || V > static_cast<int64_t>(INT32_MAX)) return PROFK_EINVAL;
+  if (row_stride < V || n_top < 0 || n_top > profk::kLpMaxTop) return PROFK_EINVAL;
+  // the rows' byte offsets fit 63 bits
+  if (row_stride > INT64_MAX / 8 / (T > 0 ? T : 1)) return PROFK_EINVAL;
+  return PROFK_OK;
+}
+
+bool aligned(const void* p, uintptr_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
+
+}  // namespace
+
+size_t profk_token_logprobs_workspace_size(int64_t T, int64_t V, int64_t n_top) {
+  if (T < 1 || check_logits(PROFK_F32, T, V, V, n_top) != PROFK_OK) return 0;
+  return profk::lp_layout(T, V, n_top, profk::device_cu_count()).bytes;
+}
+
+int profk_token_logprobs(int32_t dtype, const void* logits, int64_t T, int64_t V, int64_t row_stride,
+                         const int64_t* tokens, int64_t n_top, float* out_logprob, float* out_entropy,
+                         float* out_lse, float* out_top_logprob, int64_t* out_top_idx, void* ws, size_t ws_bytes,
+                         void* stream) {
+  const int rc = check_logits(dtype, T, V, row_stride, n_top);
+  if (rc != PROFK_OK || T == 0) return rc;
+  if (!logits || !tokens || !out_logprob || !out_entropy || !out_lse) return PROFK_ENULL;
+  if (n_top > 0 && (!out_top_logprob || !out_top_idx)) return PROFK_ENULL;
+  if (!aligned(logits, elem_size(dtype)) || !aligned(ws, 16)) return PROFK_EINVAL;
+  const profk::LpLayout L = profk::lp_layout(T, V, n_top, profk::device_cu_count());
+  if (L.bytes > 0 && !ws) return PROFK_ENULL;
+  if (ws_bytes < L.bytes) return PROFK_EWORKSPACE;
+  profk::LpCall c{};
+  c.dtype = dtype;
+  c.T = T;
+  c.a.x = logits;
+  c.a.stride = static_cast<uint64_t>(row_stride);
+  c.a.V = static_cast<uint32_t>(V);
+  c.a.n = static_cast<uint32_t>(n_top);
+  c.a.tokens = tokens;
+  c.a.logprob = out_logprob;
+  c.a.entropy = out_entropy;
+  c.a.lse = out_lse;
+  c.a.top = out_top_logprob;
+  c.a.top_idx = out_top_idx;
+  c.L = L;
+  c.ws = static_cast<uint8_t*>(ws);
+  c.stream = static_cast<hipStream_t>(stream);
+  const hipError_t e = profk::launch_logprobs(c);
+  return e == hipSuccess ? PROFK_OK : hip_fail(e);
+}
+
+int profk_token_logprobs_grad(int32_t dtype, const void* logits, int64_t T, int64_t V, int64_t row_stride,
+                              const int64_t* tokens, const float* lse, const float* entropy,
+                              const float* g_logprob, const float* g_entropy, int64_t n_top,
+                              const int64_t* top_idx, const float* g_top, void* out, int64_t out_stride,
+                              void* stream) {
+  const int rc = check_logits(dtype, T, V, row_stride, n_top);
+  if (rc != PROFK_OK) return rc;
+  if (check_logits(dtype, T, V, out_stride, n_top) != PROFK_OK) return PROFK_EINVAL;
+  if (T == 0) return PROFK_OK;
+  if (!logits || !lse || !out || (g_logprob && !tokens) || (g_entropy && !entropy)) return PROFK_ENULL;
+  if (n_top > 0 && (!top_idx || !g_top)) return PROFK_ENULL;
+  if (!aligned(logits, elem_size(dtype)) || !aligned(out, elem_size(dtype))) return PROFK_EINVAL;
+  const auto extent = [&](int64_t stride) {
+    return static_cast<uintptr_t>(((T - 1) * stride + V) * static_cast<int64_t>(elem_size(dtype)));
+  };
+  const uintptr_t xb = reinterpret_cast<uintptr_t>(logits), ob = reinterpret_cast<uintptr_t>(out);
+  if (xb < ob + extent(out_stride) && ob < xb + extent(row_stride)) return PROFK_EINVAL;
+  profk::LpGradArgs a{};
+  a.x = logits;
+  a.stride = static_cast<uint64_t>(row_stride);
+  a.V = static_cast<uint32_t>(V);
+  a.n = static_cast<uint32_t>(n_top);
+  a.tokens = g_logprob ? tokens : nullptr;
+  a.lse = lse;
+  a.entropy = entropy;
+  a.g_logprob = g_logprob;
+  a.g_entropy = g_entropy;
+  a.g_top = g_top;
+  a.top_idx = top_idx;
+  a.out = out;
+  a.out_stride = static_cast<uint64_t>(out_stride);
+  const hipError_t e = profk::launch_logprobs_grad(a, dtype, T, static_cast<hipStream_t>(stream));
+  return e == hipSuccess ? PROFK_OK : hip_fail(e);
+}
+
 int profk_debug_sample_indices(uint64_t seed, int64_t row, int64_t S, int64_t N, int64_t* out_dev,
                                void* stream) {
   if (!out_dev) return PROFK_ENULL;
