@@ -358,6 +358,50 @@ int profk_token_logprobs_grad(int32_t dtype, const void* logits, int64_t T, int6
                               const int64_t* top_idx, const float* g_top, void* out, int64_t out_stride,
                               void* stream);
 
+/* ---- Microscaled 4-bit floating point (MXFP4) ----
+ *
+ * Each 32 consecutive values of a row share a scale 2^s, held as the byte
+ * s + 127; a value is 4 bits, a sign and one of 0, 0.5, 1, 1.5, 2, 3, 4, 6
+ * times the scale.  With m the block's largest magnitude, s = floor(log2 m) -
+ * 2 within [-127, 127] (byte 0 for m = 0); v / 2^s is rounded to nearest, ties
+ * to the even code, magnitudes past 6 to 6.  A block that holds an infinity
+ * or NaN has the byte 255 and stands for NaN.
+ *
+ * Layout.  K is padded with zeros to Kp, a multiple of 128.  Codes: Kp / 2
+ * bytes a row, value 2 i in the low half of byte i; scales: Kp / 32 bytes a
+ * row.  Rows are contiguous; codes are 16-byte aligned, scales 4-byte.
+ * profk_mx4_codes_size and profk_mx4_scales_size give the bytes of R rows (0
+ * for invalid sizes).  1 <= K <= 2^20, 0 <= R <= 2^31 - 1; a call without rows
+ * does nothing. */
+size_t profk_mx4_codes_size(int64_t R, int64_t K);
+size_t profk_mx4_scales_size(int64_t R, int64_t K);
+
+/* x fp32 or bf16 [R, K], rows row_stride elements apart, to codes and scales
+ * (the padding included). */
+int profk_mx4_quantize(int32_t dtype, const void* x, int64_t R, int64_t K, int64_t row_stride,
+                       uint8_t* codes, uint8_t* scales, void* stream);
+
+/* The values that codes and scales stand for, out contiguous [R, K] of
+ * `dtype` (each is exact in either). */
+int profk_mx4_dequantize(int32_t dtype, const uint8_t* codes, const uint8_t* scales, int64_t R, int64_t K,
+                         void* out, void* stream);
+
+/* out[m, n] = sum_k a[m, k] b[n, k] over quantised a [M, K] and b [N, K]:
+ * exact products, fp32 sums on the matrix cores (64 products a step), rounded
+ * once to out_dtype.  out: contiguous [M, N].  A NaN block makes its whole
+ * row or column NaN. */
+int profk_mx4_matmul(const uint8_t* a_codes, const uint8_t* a_scales, int64_t M, const uint8_t* b_codes,
+                     const uint8_t* b_scales, int64_t N, int64_t K, int32_t out_dtype, void* out,
+                     void* stream);
+
+/* x W^T with x fp32 or bf16 [M, K] quantised in the call (into ws) and W
+ * [N, K] quantised before.  ws: profk_mx4_linear_workspace_size(M, K, N)
+ * bytes, 16-byte aligned.  Errors as above and PROFK_EWORKSPACE. */
+size_t profk_mx4_linear_workspace_size(int64_t M, int64_t K, int64_t N);
+int profk_mx4_linear(int32_t dtype, const void* x, int64_t M, int64_t K, int64_t row_stride,
+                     const uint8_t* w_codes, const uint8_t* w_scales, int64_t N, int32_t out_dtype, void* out,
+                     void* ws, size_t ws_bytes, void* stream);
+
 /* profk_topk with stages 1-2 replaced by a caller-given threshold key, to
  * drive the underflow and overflow paths on purpose.  A key alone names no
  * threshold pair, so this entry point filters with key >= tau_key also for

@@ -19,6 +19,7 @@ Modules
   sae    -- O3: the SAE encoder and decoder around the selection.
   logprobs -- O4: token log probabilities, entropy and alternatives of rows
             of logits, and their gradient.
+  mx4    -- O5: microscaled 4-bit floating point.
 
 Floating point is fp64 throughout the planner; every other step is integer
 or bit-copy work and therefore exact.

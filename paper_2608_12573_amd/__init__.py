@@ -10,6 +10,8 @@ built, every call raises instead of computing anything on the CPU.
     vals, idx, info = batchtopk(x, k_row)         # global top-(B*k_row) of [B, D]
     logprob, entropy, lse, top_logprob, top_idx = token_logprobs(logits, tokens, n_top)
     d_logits = token_logprobs_grad(logits, tokens, lse, entropy, g_logprob)
+    codes, scales = mx4_quantize(w)               # 4-bit microscaled weights
+    logits = mx4_linear(x, codes, scales)         # x w^T
 """
 
 import ctypes
@@ -116,6 +118,14 @@ def lib():
         L.profk_token_logprobs_workspace_size.restype = sz
         L.profk_token_logprobs.argtypes = [i32, vp, i64, i64, i64, vp, i64, vp, vp, vp, vp, vp, vp, sz, vp]
         L.profk_token_logprobs_grad.argtypes = [i32, vp, i64, i64, i64, vp, vp, vp, vp, vp, i64, vp, vp, vp, i64, vp]
+        for f in (L.profk_mx4_codes_size, L.profk_mx4_scales_size):
+            f.argtypes, f.restype = [i64, i64], sz
+        L.profk_mx4_linear_workspace_size.argtypes = [i64, i64, i64]
+        L.profk_mx4_linear_workspace_size.restype = sz
+        L.profk_mx4_quantize.argtypes = [i32, vp, i64, i64, i64, vp, vp, vp]
+        L.profk_mx4_dequantize.argtypes = [i32, vp, vp, i64, i64, vp, vp]
+        L.profk_mx4_matmul.argtypes = [vp, vp, i64, vp, vp, i64, i64, i32, vp, vp]
+        L.profk_mx4_linear.argtypes = [i32, vp, i64, i64, i64, vp, vp, i64, i32, vp, vp, sz, vp]
         L.profk_debug_sae_sample.argtypes = [P(Plan), vp, vp, vp, i64, i64, i64, u64, vp, vp, sz, vp]
         _lib = L
     return _lib
@@ -638,4 +648,111 @@ def token_logprobs_grad(logits, tokens, lse, entropy, g_logprob, g_entropy=None,
     _check(lib().profk_token_logprobs_grad(dt, _ptr(logits), T, V, stride, _ptr(tokens), _ptr(lse), _ptr(entropy),
                                            _ptr(g_logprob), _ptr(g_entropy), n, _ptr(top_idx), _ptr(g_top),
                                            _ptr(out), ostride, _stream()))
+    return out
+
+
+# ------------------------------------------------- microscaled 4-bit values ---
+
+MX4_MAX_K = 1 << 20
+
+
+def _mx4_shapes(R, K):
+    """Shapes of the codes and scales of R rows of K values."""
+    if not 1 <= K <= MX4_MAX_K:
+        raise ProfkError(f"rows must hold from 1 to {MX4_MAX_K} values, got {K}")
+    steps = -(-K // 128)
+    return (R, 64 * steps), (R, 4 * steps)
+
+
+def _mx4(codes, scales, name, K, device=None):
+    """Checks a quantised matrix of K columns; returns its rows."""
+    torch = _torch()
+    if not isinstance(codes, torch.Tensor) or codes.dim() != 2:
+        raise ProfkError(f"{name} codes must be a 2-dimensional torch tensor")
+    R = codes.shape[0]
+    c, s = _mx4_shapes(R, K)
+    _vector(codes, f"{name} codes", torch.uint8, c, device)
+    _vector(scales, f"{name} scales", torch.uint8, s, codes.device)
+    return R
+
+
+def mx4_outputs(R, K, device="cuda"):
+    """New (codes, scales) for R rows of K values."""
+    torch = _torch()
+    c, s = _mx4_shapes(R, K)
+    return torch.empty(c, dtype=torch.uint8, device=device), torch.empty(s, dtype=torch.uint8, device=device)
+
+
+def mx4_quantize(x, out=None):
+    """fp32 or bf16 x [R, K] (rows may be strided) in 4 bits a value with one
+    power-of-two scale per 32: (codes uint8 [R, Kp/2], scales uint8
+    [R, Kp/32]), Kp = K rounded up to a multiple of 128."""
+    dt = _input(x, "x", 2, layout="rows")
+    R, K = x.shape
+    if out is None:
+        out = mx4_outputs(R, K, x.device)
+    elif _mx4(*out, "out", K, x.device) != R:
+        raise ProfkError(f"out must have {R} rows")
+    _check(lib().profk_mx4_quantize(dt, _ptr(x), R, K, max(x.stride(0), K) if R > 1 else K, _ptr(out[0]), _ptr(out[1]),
+                                    _stream()))
+    return out
+
+
+def mx4_dequantize(codes, scales, K, dtype=None, out=None):
+    """The values [R, K] that codes and scales stand for, in fp32 or bf16
+    (the default; every value is exact in it), or into `out`."""
+    torch = _torch()
+    R = _mx4(codes, scales, "the", K)
+    if out is None:
+        out = torch.empty((R, K), dtype=dtype or torch.bfloat16, device=codes.device)
+    elif dtype is not None and out.dtype != dtype:
+        raise ProfkError(f"out is {out.dtype}, not {dtype}")
+    dt = _input(out, "out", 2)
+    _vector(out, "out", out.dtype, (R, K), codes.device)
+    _check(lib().profk_mx4_dequantize(dt, _ptr(codes), _ptr(scales), R, K, _ptr(out), _stream()))
+    return out
+
+
+def _mx4_out(M, N, dtype, out, device):
+    torch = _torch()
+    if out is None:
+        out = torch.empty((M, N), dtype=dtype or torch.float32, device=device)
+    elif dtype is not None and out.dtype != dtype:
+        raise ProfkError(f"out is {out.dtype}, not {dtype}")
+    dt = _input(out, "out", 2)
+    _vector(out, "out", out.dtype, (M, N), device)
+    return out, dt
+
+
+def mx4_matmul(a_codes, a_scales, b_codes, b_scales, K, dtype=None, out=None):
+    """a b^T of quantised a [M, K] and b [N, K]: fp32 (the default) or bf16
+    [M, N], fp32 sums."""
+    M = _mx4(a_codes, a_scales, "a's", K)
+    N = _mx4(b_codes, b_scales, "b's", K, a_codes.device)
+    out, dt = _mx4_out(M, N, dtype, out, a_codes.device)
+    _check(lib().profk_mx4_matmul(_ptr(a_codes), _ptr(a_scales), M, _ptr(b_codes), _ptr(b_scales), N, K, dt, _ptr(out),
+                                  _stream()))
+    return out
+
+
+def mx4_linear_workspace(M, K, N, device="cuda"):
+    """A workspace for mx4_linear."""
+    torch = _torch()
+    return torch.empty(int(lib().profk_mx4_linear_workspace_size(M, K, N)), dtype=torch.uint8, device=device)
+
+
+def mx4_linear(x, w_codes, w_scales, dtype=None, ws=None, out=None):
+    """x W^T: fp32 or bf16 x [M, K] (rows may be strided), quantised in the
+    call, and W [N, K] from mx4_quantize; fp32 (the default) or bf16 [M, N]."""
+    dt = _input(x, "x", 2, layout="rows")
+    M, K = x.shape
+    N = _mx4(w_codes, w_scales, "the weights'", K, x.device)
+    out, odt = _mx4_out(M, N, dtype, out, x.device)
+    n = int(lib().profk_mx4_linear_workspace_size(M, K, N))
+    if ws is None:
+        ws = mx4_linear_workspace(M, K, N, x.device)
+    else:
+        _bytes_buffer(ws, "ws", n, x.device)
+    _check(lib().profk_mx4_linear(dt, _ptr(x), M, K, max(x.stride(0), K) if M > 1 else K, _ptr(w_codes), _ptr(w_scales),
+                                  N, odt, _ptr(out), _ptr(ws), n, _stream()))
     return out

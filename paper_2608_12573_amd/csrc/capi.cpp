@@ -395,6 +395,88 @@ int profk_token_logprobs_grad(int32_t dtype, const void* logits, int64_t T, int6
   return e == hipSuccess ? PROFK_OK : hip_fail(e);
 }
 
+// ---- Microscaled 4-bit values ----
+
+namespace {
+
+int check_mx(int64_t R, int64_t K) {
+  return R < 0 || R > static_cast<int64_t>(INT32_MAX) || K < 1 || K > profk::kMxMaxK ? PROFK_EINVAL : PROFK_OK;
+}
+bool mx_aligned(const void* codes, const void* scales) { return aligned(codes, 16) && aligned(scales, 4); }
+size_t align256(size_t n) { return (n + 255) / 256 * 256; }
+
+}  // namespace
+
+size_t profk_mx4_codes_size(int64_t R, int64_t K) {
+  return check_mx(R, K) == PROFK_OK ? static_cast<size_t>(R) * profk::mx_steps(K) * 64 : 0;
+}
+
+size_t profk_mx4_scales_size(int64_t R, int64_t K) {
+  return check_mx(R, K) == PROFK_OK ? static_cast<size_t>(R) * profk::mx_steps(K) * 4 : 0;
+}
+
+int profk_mx4_quantize(int32_t dtype, const void* x, int64_t R, int64_t K, int64_t row_stride, uint8_t* codes,
+                       uint8_t* scales, void* stream) {
+  if (!dtype_ok(dtype)) return PROFK_EDTYPE;
+  if (check_mx(R, K) != PROFK_OK || row_stride < K || row_stride > INT64_MAX / 8 / (R > 0 ? R : 1)) return PROFK_EINVAL;
+  if (R == 0) return PROFK_OK;
+  if (!x || !codes || !scales) return PROFK_ENULL;
+  if (!aligned(x, elem_size(dtype)) || !mx_aligned(codes, scales)) return PROFK_EINVAL;
+  const hipError_t e = profk::launch_mx_quantize(dtype, x, static_cast<uint64_t>(row_stride), R, K, codes, scales,
+                                                 static_cast<hipStream_t>(stream));
+  return e == hipSuccess ? PROFK_OK : hip_fail(e);
+}
+
+int profk_mx4_dequantize(int32_t dtype, const uint8_t* codes, const uint8_t* scales, int64_t R, int64_t K, void* out,
+                         void* stream) {
+  if (!dtype_ok(dtype)) return PROFK_EDTYPE;
+  if (check_mx(R, K) != PROFK_OK) return PROFK_EINVAL;
+  if (R == 0) return PROFK_OK;
+  if (!codes || !scales || !out) return PROFK_ENULL;
+  if (!aligned(out, elem_size(dtype)) || !mx_aligned(codes, scales)) return PROFK_EINVAL;
+  const hipError_t e =
+      profk::launch_mx_dequantize(dtype, codes, scales, R, K, out, static_cast<hipStream_t>(stream));
+  return e == hipSuccess ? PROFK_OK : hip_fail(e);
+}
+
+int profk_mx4_matmul(const uint8_t* a_codes, const uint8_t* a_scales, int64_t M, const uint8_t* b_codes,
+                     const uint8_t* b_scales, int64_t N, int64_t K, int32_t out_dtype, void* out, void* stream) {
+  if (!dtype_ok(out_dtype)) return PROFK_EDTYPE;
+  if (check_mx(M, K) != PROFK_OK || check_mx(N, K) != PROFK_OK) return PROFK_EINVAL;
+  if (M == 0 || N == 0) return PROFK_OK;
+  if (!a_codes || !a_scales || !b_codes || !b_scales || !out) return PROFK_ENULL;
+  if (!mx_aligned(a_codes, a_scales) || !mx_aligned(b_codes, b_scales) || !aligned(out, elem_size(out_dtype)))
+    return PROFK_EINVAL;
+  const profk::MxMatmulCall c{a_codes, a_scales, b_codes, b_scales, M, N, K, out_dtype, out,
+                              static_cast<hipStream_t>(stream)};
+  const hipError_t e = profk::launch_mx_matmul(c);
+  return e == hipSuccess ? PROFK_OK : hip_fail(e);
+}
+
+size_t profk_mx4_linear_workspace_size(int64_t M, int64_t K, int64_t N) {
+  if (check_mx(M, K) != PROFK_OK || check_mx(N, K) != PROFK_OK || M == 0 || N == 0) return 0;
+  return align256(profk_mx4_codes_size(M, K)) + profk_mx4_scales_size(M, K);
+}
+
+int profk_mx4_linear(int32_t dtype, const void* x, int64_t M, int64_t K, int64_t row_stride, const uint8_t* w_codes,
+                     const uint8_t* w_scales, int64_t N, int32_t out_dtype, void* out, void* ws, size_t ws_bytes,
+                     void* stream) {
+  if (!dtype_ok(dtype) || !dtype_ok(out_dtype)) return PROFK_EDTYPE;
+  if (check_mx(M, K) != PROFK_OK || check_mx(N, K) != PROFK_OK) return PROFK_EINVAL;
+  if (row_stride < K || row_stride > INT64_MAX / 8 / (M > 0 ? M : 1)) return PROFK_EINVAL;
+  if (M == 0 || N == 0) return PROFK_OK;
+  if (!x || !w_codes || !w_scales || !out || !ws) return PROFK_ENULL;
+  if (!aligned(x, elem_size(dtype)) || !mx_aligned(w_codes, w_scales) || !aligned(out, elem_size(out_dtype)) ||
+      !aligned(ws, 16))
+    return PROFK_EINVAL;
+  if (ws_bytes < profk_mx4_linear_workspace_size(M, K, N)) return PROFK_EWORKSPACE;
+  uint8_t* const codes = static_cast<uint8_t*>(ws);
+  uint8_t* const scales = codes + align256(profk_mx4_codes_size(M, K));
+  const int rc = profk_mx4_quantize(dtype, x, M, K, row_stride, codes, scales, stream);
+  if (rc != PROFK_OK) return rc;
+  return profk_mx4_matmul(codes, scales, M, w_codes, w_scales, N, K, out_dtype, out, stream);
+}
+
 int profk_debug_sample_indices(uint64_t seed, int64_t row, int64_t S, int64_t N, int64_t* out_dev,
                                void* stream) {
   if (!out_dev) return PROFK_ENULL;

@@ -356,6 +356,26 @@ struct LpGradArgs {
 
 hipError_t launch_logprobs_grad(LpGradArgs a, int dtype, int64_t T, hipStream_t s);
 
+// Microscaled 4-bit values (kernels_mx4.hip): K padded to whole steps of 128,
+// 64 bytes of codes and 4 of scales each.
+uint64_t mx_steps(int64_t K);
+constexpr int64_t kMxMaxK = 1 << 20;
+hipError_t launch_mx_quantize(int dtype, const void* x, uint64_t stride, int64_t R, int64_t K, uint8_t* codes,
+                              uint8_t* scales, hipStream_t s);
+hipError_t launch_mx_dequantize(int dtype, const uint8_t* codes, const uint8_t* scales, int64_t R, int64_t K,
+                                void* out, hipStream_t s);
+
+struct MxMatmulCall {
+  const uint8_t *a, *as;      // codes and scales [M, ..]
+  const uint8_t *b, *bs;      // ... [N, ..]
+  int64_t M, N, K;
+  int out_dtype;
+  void* out;                  // [M, N]
+  hipStream_t stream;
+};
+
+hipError_t launch_mx_matmul(const MxMatmulCall& c);
+
 // Inspection helpers.
 hipError_t launch_sample_indices(uint64_t seed, uint64_t row, uint32_t S, uint64_t N,
                                  int64_t* out, hipStream_t s);
