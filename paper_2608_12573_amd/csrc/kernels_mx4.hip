@@ -188,35 +188,283 @@ template <int DT> __device__ __forceinline__ void mx_store4(void* out, size_t ro
   }
 }
 
-// A simple product: a wave computes 32 x 128 outputs straight from memory.
-// Column n = 128 w + 4 (lane % 32) + j is in fragment j, so that a lane's four
-// results of a row are neighbours.
-template <int DT> __global__ __launch_bounds__(256) void k_mx_simple(MxGemmArgs g) {
-  const uint32_t lane = threadIdx.x & (kWave - 1), w = threadIdx.x / kWave;
-  const uint32_t c = lane & 31, h = lane >> 5;
-  const uint32_t m0 = blockIdx.y * 32, n0 = (blockIdx.x * 4 + w) * 128;
-  if (n0 >= g.N) return;
+// s_waitcnt vmcnt(N) lgkmcnt(0) (gfx9 encoding: vmcnt in bits 3:0 and 15:14,
+// expcnt in 6:4, lgkmcnt in 11:8): all but this wave's N newest loads are
+// done, and so are its LDS reads.
+template <int N> __device__ __forceinline__ void wait_loads_lds() {
+  static_assert(N >= 0 && N < 64, "vmcnt");
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt((N & 0xF) | ((N >> 4) << 14) | (0x7 << 4));
+}
+// A workgroup barrier that waits for nothing else, across which the compiler
+// moves no memory access.
+__device__ __forceinline__ void bare_barrier() {
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+
+// The tiled product.  A workgroup of WM x WN waves computes a tile of BM x BN
+// outputs, a wave MI x NJ accumulators of 32 x 32.  A step (128 values of K)
+// of a tile is 64 bytes of codes a row and a word of four scales, loaded
+// straight to LDS, four stages deep; every wait is for the oldest stage, so
+// that the others stay in flight.  16-byte granule g of a row r is at
+// position g ^ (r / 4 % 4) of its four: sixteen neighbouring rows' granules
+// g then cover all 64 banks once.
+//
+// Output column n of a wave's slab is in fragment n % NJ, lane n / NJ (the
+// LDS rows of b are in that order), so that a lane's NJ results of a row are
+// neighbours and are stored together.
+//
+// Rows past M or N are read as the last one and not stored.
+
+template <int WM, int WN, int MI, int NJ> struct MxTile {
+  static constexpr int BS = WM * WN * kWave, BM = WM * MI * 32, BN = WN * NJ * 32;
+  static constexpr int QA = BM * 4 / BS, QB = BN * 4 / BS, QS = (BM + BN) / BS;   // loads of a lane
+  static constexpr int kLoads = QA + QB + QS;
+  static constexpr int kB = BM * 4, kS = (BM + BN) * 4;        // first granule of b, of the scales
+  static constexpr int kGran = kS + (BM + BN) / 4;             // granules of a stage
+  static_assert(BM * 4 % BS == 0 && BN * 4 % BS == 0 && (BM + BN) % BS == 0, "whole loads");
+  static_assert(NJ == 4, "four neighbouring results a lane");
+};
+
+template <int DT, int WM, int WN, int MI, int NJ>
+__device__ __forceinline__ void mx_gemm_body(const MxGemmArgs& g, uint32_t tiles_m, uint32_t tiles, uint32_t per) {
+  using T = MxTile<WM, WN, MI, NJ>;
+  // distinct arrays, so that the compiler can tell the stage being read from
+  // those being filled
+  __shared__ __align__(16) uint4 s0[T::kGran], s1[T::kGran], s2[T::kGran], s3[T::kGran];
+  // workgroup b runs on XCD b % 8: each XCD takes a run of tiles, the row
+  // tiles of a column tile one after the other, so that its L2 holds what
+  // they share
+  const uint32_t tile = (blockIdx.x % kXcds) * per + blockIdx.x / kXcds;
+  if (blockIdx.x / kXcds >= per || tile >= tiles) return;
+  const uint32_t m0 = tile % tiles_m * T::BM, n0 = tile / tiles_m * T::BN;
+  const uint32_t tid = threadIdx.x, lane = tid & (kWave - 1);
+  const uint32_t w = __builtin_amdgcn_readfirstlane(tid / kWave);
+  const uint32_t c = lane & 31, h = lane >> 5, wm = w / WN, wn = w % WN;
   const size_t cb = static_cast<size_t>(g.steps) * 64, sb = static_cast<size_t>(g.steps) * 4;
-  const uint32_t m = min(m0 + c, g.M - 1);
-  const uint8_t* const pa = g.a + m * cb + h * 16;
-  f32x16 acc[4] = {};
-  for (uint32_t k = 0; k < g.steps; ++k) {
-    const int sa = static_cast<int>(reinterpret_cast<const uint32_t*>(g.as + m * sb)[k] >> (8 * h));
-    const u32x4 a0 = *reinterpret_cast<const u32x4*>(pa + k * 64), a1 = *reinterpret_cast<const u32x4*>(pa + k * 64 + 32);
+
+  auto col_of = [](uint32_t r) { return r / (NJ * 32) * (NJ * 32) + r % 32 * NJ + r % (NJ * 32) / 32; };
+  // a lane's loads: offsets from the tile's first row, which a step adds to
+  // (within 256 rows of at most 2^19 bytes)
+  const uint8_t *base_a = g.a + m0 * cb, *base_b = g.b + n0 * cb, *base_as = g.as + m0 * sb, *base_bs = g.bs + n0 * sb;
+  const uint32_t last_m = g.M - 1 - m0, last_n = g.N - 1 - n0;
+  uint32_t oa[T::QA], ob[T::QB], os[T::QS];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const uint32_t n = min(n0 + 4 * c + j, g.N - 1);
-      const uint8_t* const pb = g.b + n * cb + h * 16 + k * 64;
-      const int sw = static_cast<int>(reinterpret_cast<const uint32_t*>(g.bs + n * sb)[k] >> (8 * h));
-      acc[j] = mx_mma<0>(a0, *reinterpret_cast<const u32x4*>(pb), acc[j], sa, sw);
-      acc[j] = mx_mma<1>(a1, *reinterpret_cast<const u32x4*>(pb + 32), acc[j], sa, sw);
+  for (int q = 0; q < T::QA; ++q) {
+    const uint32_t p = (w * T::QA + q) * kWave + lane, r = p / 4, gr = (p & 3) ^ (r >> 2 & 3);
+    oa[q] = min(r, last_m) * static_cast<uint32_t>(cb) + gr * 16;
+  }
+#pragma unroll
+  for (int q = 0; q < T::QB; ++q) {
+    const uint32_t p = (w * T::QB + q) * kWave + lane, r = p / 4, gr = (p & 3) ^ (r >> 2 & 3);
+    ob[q] = min(col_of(r), last_n) * static_cast<uint32_t>(cb) + gr * 16;
+  }
+  // (a wave's scale loads are all of a or all of b)
+  static_assert(T::BM % kWave == 0, "scale loads of one matrix a wave");
+  const uint8_t* base_s[T::QS];
+#pragma unroll
+  for (int q = 0; q < T::QS; ++q) {
+    const uint32_t r0 = (w * T::QS + q) * kWave, r = r0 + lane;
+    base_s[q] = r0 < T::BM ? base_as : base_bs;
+    os[q] = (r0 < T::BM ? min(r, last_m) : min(col_of(r - T::BM), last_n)) * static_cast<uint32_t>(sb);
+  }
+  // the next step, or the last one again, into a stage
+  uint32_t next = 0;
+  auto issue = [&](uint4* st) {
+#pragma unroll
+    for (int q = 0; q < T::QA; ++q) __builtin_amdgcn_global_load_lds(reinterpret_cast<const uint32_t*>(base_a + oa[q]), st + (w * T::QA + q) * kWave, 16, 0, 0);
+#pragma unroll
+    for (int q = 0; q < T::QB; ++q) __builtin_amdgcn_global_load_lds(reinterpret_cast<const uint32_t*>(base_b + ob[q]), st + T::kB + (w * T::QB + q) * kWave, 16, 0, 0);
+#pragma unroll
+    for (int q = 0; q < T::QS; ++q) __builtin_amdgcn_global_load_lds(reinterpret_cast<const uint32_t*>(base_s[q] + os[q]), st + T::kS + (w * T::QS + q) * (kWave / 4), 4, 0, 0);
+    if (++next < g.steps) {
+      base_a += 64;
+      base_b += 64;
+#pragma unroll
+      for (int q = 0; q < T::QS; ++q) base_s[q] += 4;
+    }
+  };
+  f32x16 acc[MI][NJ] = {};
+  auto compute = [&](const uint4* st) {
+    const uint32_t* const sc = reinterpret_cast<const uint32_t*>(st + T::kS);
+    int sa[MI], sw[NJ];
+#pragma unroll
+    for (int i = 0; i < MI; ++i) sa[i] = static_cast<int>(sc[wm * MI * 32 + i * 32 + c] >> (8 * h));
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) sw[j] = static_cast<int>(sc[T::BM + wn * NJ * 32 + j * 32 + c] >> (8 * h));
+    auto half = [&](auto KS) {
+      constexpr int ks = decltype(KS)::value;
+      u32x4 fa[MI], fb[NJ];
+#pragma unroll
+      for (int i = 0; i < MI; ++i) {
+        const uint32_t r = wm * MI * 32 + i * 32 + c;
+        fa[i] = __builtin_bit_cast(u32x4, st[r * 4 + ((2 * ks + h) ^ (r >> 2 & 3))]);
+      }
+#pragma unroll
+      for (int j = 0; j < NJ; ++j) {
+        const uint32_t r = wn * NJ * 32 + j * 32 + c;
+        fb[j] = __builtin_bit_cast(u32x4, st[T::kB + r * 4 + ((2 * ks + h) ^ (r >> 2 & 3))]);
+      }
+#pragma unroll
+      for (int i = 0; i < MI; ++i)
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) acc[i][j] = mx_mma<ks>(fa[i], fb[j], acc[i][j], sa[i], sw[j]);
+    };
+    half(std::integral_constant<int, 0>{});
+    half(std::integral_constant<int, 1>{});
+  };
+  issue(s0);
+  issue(s1);
+  issue(s2);
+  // step k: its stage has arrived (this wave's loads, then by the barrier the
+  // others'), and everyone has read the stage before it, which is refilled
+  auto step = [&](uint4* cur, uint4* old) {
+    wait_loads_lds<2 * T::kLoads>();
+    bare_barrier();
+    issue(old);
+    compute(cur);
+  };
+  uint32_t k = 0;
+  for (; k + 4 <= g.steps; k += 4) {
+    step(s0, s3);
+    step(s1, s0);
+    step(s2, s1);
+    step(s3, s2);
+  }
+  if (k < g.steps) step(s0, s3);
+  if (k + 1 < g.steps) step(s1, s0);
+  if (k + 2 < g.steps) step(s2, s1);
+  wait_loads_lds<0>();   // (no load may reach LDS after the workgroup's end)
+#pragma unroll
+  for (int i = 0; i < MI; ++i)
+#pragma unroll
+    for (int v = 0; v < 16; ++v) {
+      const uint32_t r = m0 + wm * MI * 32 + i * 32 + 8 * (v / 4) + 4 * h + (v % 4), n = n0 + wn * NJ * 32 + NJ * c;
+      if (r < g.M) mx_store4<DT>(g.out, r, n, g.N, f32x4{acc[i][0][v], acc[i][1][v], acc[i][2][v], acc[i][3][v]});
+    }
+}
+
+template <int DT, int WM, int WN, int MI, int NJ>
+__global__ __launch_bounds__(WM * WN * 64, 2) void k_mx_gemm(MxGemmArgs g, uint32_t tiles_m, uint32_t tiles, uint32_t per) {
+  mx_gemm_body<DT, WM, WN, MI, NJ>(g, tiles_m, tiles, per);
+}
+
+// The product of few rows (M <= 32), bound by reading b once.  A wave takes
+// 32 rows of b, straight from memory to registers, two groups of kMxFewU
+// steps in flight; a sits in LDS, its rows 16 bytes apart from a whole number
+// of banks.  KSPLIT: the workgroup's waves take the steps of the same 32 rows
+// in turn and add their sums at the end, in wave order.
+constexpr int kMxFewBS = 256;
+constexpr int kMxFewU = 4;
+constexpr uint32_t kMxFewLds = 72 * 1024;
+__host__ __device__ constexpr uint32_t mx_few_row(uint32_t steps) { return steps * 64 + 16; }   // LDS bytes of a row of a
+__host__ __device__ constexpr uint32_t mx_few_lds(uint32_t M, uint32_t steps) { return M * (mx_few_row(steps) + steps * 4); }
+
+template <int DT, bool KSPLIT> __global__ __launch_bounds__(kMxFewBS) void k_mx_few(MxGemmArgs g) {
+  constexpr int NW = kMxFewBS / kWave, U = kMxFewU;
+  extern __shared__ __align__(16) uint8_t smem[];
+  __shared__ float s_sum[KSPLIT ? (NW - 1) * 16 * kWave : 1];
+  const uint32_t tid = threadIdx.x, lane = tid & (kWave - 1);
+  const uint32_t w = __builtin_amdgcn_readfirstlane(tid / kWave);
+  const uint32_t c = lane & 31, h = lane >> 5;
+  const uint32_t rb = mx_few_row(g.steps);
+  uint32_t* const s_scale = reinterpret_cast<uint32_t*>(smem + g.M * rb);
+  for (uint32_t i = tid; i < g.M * g.steps * 4; i += kMxFewBS) {
+    const uint32_t r = i / (g.steps * 4), q = i - r * g.steps * 4;
+    *reinterpret_cast<uint4*>(smem + r * rb + q * 16) = reinterpret_cast<const uint4*>(g.a)[i];
+  }
+  for (uint32_t i = tid; i < g.M * g.steps; i += kMxFewBS) s_scale[i] = reinterpret_cast<const uint32_t*>(g.as)[i];
+  __syncthreads();
+
+  const uint32_t n0 = (KSPLIT ? blockIdx.x : blockIdx.x * NW + w) * 32;
+  const uint32_t n = min(n0 + c, g.N - 1);
+  // steps first, first + stride, ...
+  const uint32_t first = KSPLIT ? w : 0, stride = KSPLIT ? NW : 1;
+  const uint32_t count = g.steps > first ? (g.steps - first + stride - 1) / stride : 0;
+  const uint8_t* const pb = g.b + n * (static_cast<size_t>(g.steps) * 64) + h * 16;
+  const uint32_t* const ps = reinterpret_cast<const uint32_t*>(g.bs) + n * static_cast<size_t>(g.steps);
+  const uint32_t m = min(c, g.M - 1);
+  const uint8_t* const xa = smem + m * rb + h * 16;
+  const uint32_t* const xs = s_scale + m * g.steps;
+  f32x16 acc = {};
+  struct Group {
+    u32x4 v[2 * U];
+    uint32_t s[U];
+  };
+  // steps t .. t + U - 1 of this wave (past its last: the last again)
+  auto load = [&](uint32_t t, Group& q) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const uint32_t k = first + min(t + u, count - 1) * stride;
+      q.v[2 * u] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(pb + k * 64));
+      q.v[2 * u + 1] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(pb + k * 64 + 32));
+      q.s[u] = ps[k];
+    }
+  };
+  auto use = [&](uint32_t t, const Group& q) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (t + u >= count) break;
+      const uint32_t k = first + (t + u) * stride;
+      const u32x4 a0 = *reinterpret_cast<const u32x4*>(xa + k * 64), a1 = *reinterpret_cast<const u32x4*>(xa + k * 64 + 32);
+      const int sa = static_cast<int>(xs[k] >> (8 * h)), sw = static_cast<int>(q.s[u] >> (8 * h));
+      acc = mx_mma<0>(a0, q.v[2 * u], acc, sa, sw);
+      acc = mx_mma<1>(a1, q.v[2 * u + 1], acc, sa, sw);
+    }
+  };
+  if (count && n0 < g.N) {
+    Group q0, q1;
+    load(0, q0);
+    for (uint32_t t = 0; t < count; t += 2 * U) {
+      load(t + U, q1);
+      use(t, q0);
+      if (t + U >= count) break;
+      load(t + 2 * U, q0);
+      use(t + U, q1);
     }
   }
+  if (KSPLIT) {
+    if (w > 0) {
+#pragma unroll
+      for (int v = 0; v < 16; ++v) s_sum[((w - 1) * 16 + v) * kWave + lane] = acc[v];
+    }
+    __syncthreads();
+    if (w > 0) return;
+#pragma unroll
+    for (int o = 0; o < NW - 1; ++o)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) acc[v] += s_sum[(o * 16 + v) * kWave + lane];
+  }
+  if (n0 + c >= g.N) return;
 #pragma unroll
   for (int v = 0; v < 16; ++v) {
-    const uint32_t r = m0 + 8 * (v / 4) + 4 * h + (v % 4);
-    if (r < g.M) mx_store4<DT>(g.out, r, n0 + 4 * c, g.N, f32x4{acc[0][v], acc[1][v], acc[2][v], acc[3][v]});
+    const uint32_t r = 8 * (v / 4) + 4 * h + (v % 4);
+    if (r < g.M) {
+      const size_t o = static_cast<size_t>(r) * g.N + n0 + c;
+      if constexpr (DT == PROFK_F32) static_cast<float*>(g.out)[o] = acc[v];
+      else static_cast<__bf16*>(g.out)[o] = static_cast<__bf16>(acc[v]);
+    }
   }
+}
+
+template <int DT, int WM, int WN, int MI, int NJ> void launch_gemm(const MxGemmArgs& g, hipStream_t s) {
+  using T = MxTile<WM, WN, MI, NJ>;
+  const uint32_t tm = (g.M + T::BM - 1) / T::BM, tn = (g.N + T::BN - 1) / T::BN;
+  const uint32_t tiles = tm * tn, per = (tiles + kXcds - 1) / kXcds;
+  k_mx_gemm<DT, WM, WN, MI, NJ><<<per * kXcds, T::BS, 0, s>>>(g, tm, tiles, per);
+}
+
+template <int DT> void launch_product(const MxGemmArgs& g, hipStream_t s) {
+  const uint32_t lds = mx_few_lds(g.M, g.steps);
+  if (g.M <= 32 && lds <= kMxFewLds) {
+    if (g.steps >= 16) k_mx_few<DT, true><<<(g.N + 31) / 32, kMxFewBS, lds, s>>>(g);
+    else k_mx_few<DT, false><<<(g.N + 127) / 128, kMxFewBS, lds, s>>>(g);
+    return;
+  }
+  const uint64_t big = static_cast<uint64_t>((g.M + 255) / 256) * ((g.N + 255) / 256);
+  if (g.M > 128 && big >= 128) launch_gemm<DT, 4, 2, 2, 4>(g, s);
+  else launch_gemm<DT, 4, 1, 1, 4>(g, s);
 }
 
 }  // namespace
@@ -265,9 +513,8 @@ hipError_t launch_mx_matmul(const MxMatmulCall& c) {
   const MxGemmArgs g{c.a, c.b, c.as, c.bs, static_cast<uint32_t>(c.M), static_cast<uint32_t>(c.N),
                      static_cast<uint32_t>(mx_steps(c.K)), c.out};
   (void)hipGetLastError();
-  const dim3 grid((g.N + 511) / 512, (g.M + 31) / 32);
-  if (c.out_dtype == PROFK_F32) k_mx_simple<PROFK_F32><<<grid, 256, 0, c.stream>>>(g);
-  else k_mx_simple<PROFK_BF16><<<grid, 256, 0, c.stream>>>(g);
+  if (c.out_dtype == PROFK_F32) launch_product<PROFK_F32>(g, c.stream);
+  else launch_product<PROFK_BF16>(g, c.stream);
   return hipGetLastError();
 }
 
