@@ -351,24 +351,68 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void k_mx_gemm(MxGemmArgs g, uint3
 }
 
 // The product of few rows (M <= 32), bound by reading b once.  A wave takes
-// 32 rows of b, straight from memory to registers, two groups of kMxFewU
-// steps in flight; a sits in LDS, its rows 16 bytes apart from a whole number
-// of banks.  KSPLIT: the workgroup's waves take the steps of the same 32 rows
-// in turn and add their sums at the end, in wave order.
+// groups of 32 rows of b, two steps (128 bytes a row) at a time: whole lines,
+// loaded straight to a part of LDS of its own, four stages deep, so that no
+// barrier is needed and the loads of the next group start before this one
+// ends.  Granule g of row r is at position g ^ (r / 2 % 8) of its eight.  a
+// sits in LDS, its rows 16 bytes apart from a whole number of banks.
+// KSPLIT: the workgroup's waves each take a part of the steps of the same
+// groups, and their sums are added in wave order.
 constexpr int kMxFewBS = 256;
-constexpr int kMxFewU = 4;
-constexpr uint32_t kMxFewLds = 72 * 1024;
+constexpr uint32_t kMxFewStage = 32 * 128 + 32 * 8;   // bytes of a wave's stage: codes, then scales
+constexpr int kMxFewLoads = 5;                        // loads of a stage
+// LDS for a: two workgroups a CU, or one.
+constexpr uint32_t kMxFewLdsSmall = 10 * 1024, kMxFewLds = 72 * 1024;
 __host__ __device__ constexpr uint32_t mx_few_row(uint32_t steps) { return steps * 64 + 16; }   // LDS bytes of a row of a
 __host__ __device__ constexpr uint32_t mx_few_lds(uint32_t M, uint32_t steps) { return M * (mx_few_row(steps) + steps * 4); }
 
-template <int DT, bool KSPLIT> __global__ __launch_bounds__(kMxFewBS) void k_mx_few(MxGemmArgs g) {
-  constexpr int NW = kMxFewBS / kWave, U = kMxFewU;
-  extern __shared__ __align__(16) uint8_t smem[];
+template <int DT, bool KSPLIT, int LDS> __device__ __forceinline__ void mx_few_body(const MxGemmArgs& g) {
+  constexpr int NW = kMxFewBS / kWave;
+  constexpr uint32_t kQ = kMxFewStage / 16;
+  __shared__ __align__(16) uint8_t smem[LDS];   // a: codes, then scales
+  __shared__ __align__(16) uint4 s0[NW * kQ], s1[NW * kQ], s2[NW * kQ], s3[NW * kQ];
   __shared__ float s_sum[KSPLIT ? (NW - 1) * 16 * kWave : 1];
   const uint32_t tid = threadIdx.x, lane = tid & (kWave - 1);
   const uint32_t w = __builtin_amdgcn_readfirstlane(tid / kWave);
   const uint32_t c = lane & 31, h = lane >> 5;
+  const uint32_t groups = (g.N + 31) / 32, pairs = (g.steps + 1) / 2;
+  // this wave's groups and its pairs of steps
+  const uint32_t g0 = KSPLIT ? blockIdx.x : blockIdx.x * NW + w, gs = KSPLIT ? gridDim.x : gridDim.x * NW;
+  const uint32_t p0 = KSPLIT ? pairs * w / NW : 0, p1 = KSPLIT ? pairs * (w + 1) / NW : pairs;
+  const uint32_t mine = g0 < groups ? (groups - g0 + gs - 1) / gs : 0;
+  const uint32_t total = mine * (p1 - p0);
   const uint32_t rb = mx_few_row(g.steps);
+  const size_t cb = static_cast<size_t>(g.steps) * 64, sb = static_cast<size_t>(g.steps) * 4;
+
+  // the pair to load next: group ig, pair ip
+  uint32_t ig = g0, ip = p0, issued = 0;
+  auto issue = [&](uint4* stage) {
+    uint4* const st = stage + w * kQ;
+    const uint32_t n0 = ig * 32, last = g.N - 1 - n0;
+    const uint32_t half = 2 * ip + 1 < g.steps ? 1u : 0u;   // 0: the pair's second step is past the end
+    const uint8_t* const codes = g.b + n0 * cb + ip * 128;
+    const uint8_t* const scales = g.bs + n0 * sb + ip * 8;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const uint32_t r = q * 8 + lane / 8, gr = (lane & 7) ^ (r >> 1 & 7);
+      const uint32_t o = min(r, last) * static_cast<uint32_t>(cb) + (half ? gr : gr & 3) * 16;
+      __builtin_amdgcn_global_load_lds(reinterpret_cast<const uint32_t*>(codes + o), st + q * kWave, 16, 0, 0);
+    }
+    const uint32_t o = min(lane / 2, last) * static_cast<uint32_t>(sb) + (lane & half) * 4;
+    __builtin_amdgcn_global_load_lds(reinterpret_cast<const uint32_t*>(scales + o), st + 4 * kWave, 4, 0, 0);
+    if (++issued < total) {
+      if (++ip == p1) {
+        ip = p0;
+        ig += gs;
+      }
+    }
+  };
+  if (total) {
+    issue(s0);
+    issue(s1);
+    issue(s2);
+  }
+  // a to LDS meanwhile
   uint32_t* const s_scale = reinterpret_cast<uint32_t*>(smem + g.M * rb);
   for (uint32_t i = tid; i < g.M * g.steps * 4; i += kMxFewBS) {
     const uint32_t r = i / (g.steps * 4), q = i - r * g.steps * 4;
@@ -377,75 +421,74 @@ template <int DT, bool KSPLIT> __global__ __launch_bounds__(kMxFewBS) void k_mx_
   for (uint32_t i = tid; i < g.M * g.steps; i += kMxFewBS) s_scale[i] = reinterpret_cast<const uint32_t*>(g.as)[i];
   __syncthreads();
 
-  const uint32_t n0 = (KSPLIT ? blockIdx.x : blockIdx.x * NW + w) * 32;
-  const uint32_t n = min(n0 + c, g.N - 1);
-  // steps first, first + stride, ...
-  const uint32_t first = KSPLIT ? w : 0, stride = KSPLIT ? NW : 1;
-  const uint32_t count = g.steps > first ? (g.steps - first + stride - 1) / stride : 0;
-  const uint8_t* const pb = g.b + n * (static_cast<size_t>(g.steps) * 64) + h * 16;
-  const uint32_t* const ps = reinterpret_cast<const uint32_t*>(g.bs) + n * static_cast<size_t>(g.steps);
   const uint32_t m = min(c, g.M - 1);
   const uint8_t* const xa = smem + m * rb + h * 16;
   const uint32_t* const xs = s_scale + m * g.steps;
   f32x16 acc = {};
-  struct Group {
-    u32x4 v[2 * U];
-    uint32_t s[U];
-  };
-  // steps t .. t + U - 1 of this wave (past its last: the last again)
-  auto load = [&](uint32_t t, Group& q) {
+  uint32_t cg = g0, cp = p0;      // the pair at hand
+  auto finish = [&]() {
+    const uint32_t n = cg * 32 + c;
+    if (KSPLIT) {
+      if (w > 0) {
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const uint32_t k = first + min(t + u, count - 1) * stride;
-      q.v[2 * u] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(pb + k * 64));
-      q.v[2 * u + 1] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(pb + k * 64 + 32));
-      q.s[u] = ps[k];
+        for (int v = 0; v < 16; ++v) s_sum[((w - 1) * 16 + v) * kWave + lane] = acc[v];
+      }
+      __syncthreads();
+      if (w == 0) {
+#pragma unroll
+        for (int o = 0; o < NW - 1; ++o)
+#pragma unroll
+          for (int v = 0; v < 16; ++v) acc[v] += s_sum[(o * 16 + v) * kWave + lane];
+      }
+      __syncthreads();
     }
-  };
-  auto use = [&](uint32_t t, const Group& q) {
+    if ((!KSPLIT || w == 0) && n < g.N) {
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      if (t + u >= count) break;
-      const uint32_t k = first + (t + u) * stride;
+      for (int v = 0; v < 16; ++v) {
+        const uint32_t r = 8 * (v / 4) + 4 * h + (v % 4);
+        if (r < g.M) {
+          const size_t o = static_cast<size_t>(r) * g.N + n;
+          if constexpr (DT == PROFK_F32) static_cast<float*>(g.out)[o] = acc[v];
+          else static_cast<__bf16*>(g.out)[o] = static_cast<__bf16>(acc[v]);
+        }
+      }
+    }
+    acc = f32x16{};
+  };
+  auto step = [&](uint4* cur, uint4* old) {
+    // (this wave's own loads and reads: no barrier)
+    wait_loads_lds<2 * kMxFewLoads>();
+    issue(old);
+    const uint4* const st = cur + w * kQ;
+    const uint2 sc = reinterpret_cast<const uint2*>(st + 4 * kWave)[c];
+    const uint32_t x = c >> 1 & 7;
+    auto one = [&](uint32_t k, uint32_t hi, uint32_t scale) {
+      const u32x4 b0 = __builtin_bit_cast(u32x4, st[c * 8 + ((4 * hi + h) ^ x)]);
+      const u32x4 b1 = __builtin_bit_cast(u32x4, st[c * 8 + ((4 * hi + 2 + h) ^ x)]);
       const u32x4 a0 = *reinterpret_cast<const u32x4*>(xa + k * 64), a1 = *reinterpret_cast<const u32x4*>(xa + k * 64 + 32);
-      const int sa = static_cast<int>(xs[k] >> (8 * h)), sw = static_cast<int>(q.s[u] >> (8 * h));
-      acc = mx_mma<0>(a0, q.v[2 * u], acc, sa, sw);
-      acc = mx_mma<1>(a1, q.v[2 * u + 1], acc, sa, sw);
+      const int sa = static_cast<int>(xs[k] >> (8 * h)), sw = static_cast<int>(scale >> (8 * h));
+      acc = mx_mma<0>(a0, b0, acc, sa, sw);
+      acc = mx_mma<1>(a1, b1, acc, sa, sw);
+    };
+    one(2 * cp, 0, sc.x);
+    if (2 * cp + 1 < g.steps) one(2 * cp + 1, 1, sc.y);
+    if (++cp == p1) {
+      finish();
+      cp = p0;
+      cg += gs;
     }
   };
-  if (count && n0 < g.N) {
-    Group q0, q1;
-    load(0, q0);
-    for (uint32_t t = 0; t < count; t += 2 * U) {
-      load(t + U, q1);
-      use(t, q0);
-      if (t + U >= count) break;
-      load(t + 2 * U, q0);
-      use(t + U, q1);
-    }
+  for (uint32_t t = 0; t < total; t += 4) {
+    step(s0, s3);
+    if (t + 1 < total) step(s1, s0);
+    if (t + 2 < total) step(s2, s1);
+    if (t + 3 < total) step(s3, s2);
   }
-  if (KSPLIT) {
-    if (w > 0) {
-#pragma unroll
-      for (int v = 0; v < 16; ++v) s_sum[((w - 1) * 16 + v) * kWave + lane] = acc[v];
-    }
-    __syncthreads();
-    if (w > 0) return;
-#pragma unroll
-    for (int o = 0; o < NW - 1; ++o)
-#pragma unroll
-      for (int v = 0; v < 16; ++v) acc[v] += s_sum[(o * 16 + v) * kWave + lane];
-  }
-  if (n0 + c >= g.N) return;
-#pragma unroll
-  for (int v = 0; v < 16; ++v) {
-    const uint32_t r = 8 * (v / 4) + 4 * h + (v % 4);
-    if (r < g.M) {
-      const size_t o = static_cast<size_t>(r) * g.N + n0 + c;
-      if constexpr (DT == PROFK_F32) static_cast<float*>(g.out)[o] = acc[v];
-      else static_cast<__bf16*>(g.out)[o] = static_cast<__bf16>(acc[v]);
-    }
-  }
+  wait_loads_lds<0>();   // (no load may reach LDS after the workgroup's end)
+}
+
+template <int DT, bool KSPLIT, int LDS> __global__ __launch_bounds__(kMxFewBS) void k_mx_few(MxGemmArgs g) {
+  mx_few_body<DT, KSPLIT, LDS>(g);
 }
 
 template <int DT, int WM, int WN, int MI, int NJ> void launch_gemm(const MxGemmArgs& g, hipStream_t s) {
@@ -455,11 +498,18 @@ template <int DT, int WM, int WN, int MI, int NJ> void launch_gemm(const MxGemmA
   k_mx_gemm<DT, WM, WN, MI, NJ><<<per * kXcds, T::BS, 0, s>>>(g, tm, tiles, per);
 }
 
-template <int DT> void launch_product(const MxGemmArgs& g, hipStream_t s) {
+template <int DT, int LDS> void launch_few(const MxGemmArgs& g, uint32_t cus, uint32_t per_cu, hipStream_t s) {
+  // few groups: the waves of a workgroup share one
+  const uint32_t groups = (g.N + 31) / 32, most = per_cu * cus;
+  if (groups < 4 * cus && g.steps >= 8) k_mx_few<DT, true, LDS><<<groups < most ? groups : most, kMxFewBS, 0, s>>>(g);
+  else k_mx_few<DT, false, LDS><<<(groups + 3) / 4 < most ? (groups + 3) / 4 : most, kMxFewBS, 0, s>>>(g);
+}
+
+template <int DT> void launch_product(const MxGemmArgs& g, uint32_t cus, hipStream_t s) {
   const uint32_t lds = mx_few_lds(g.M, g.steps);
   if (g.M <= 32 && lds <= kMxFewLds) {
-    if (g.steps >= 16) k_mx_few<DT, true><<<(g.N + 31) / 32, kMxFewBS, lds, s>>>(g);
-    else k_mx_few<DT, false><<<(g.N + 127) / 128, kMxFewBS, lds, s>>>(g);
+    if (lds <= kMxFewLdsSmall) launch_few<DT, kMxFewLdsSmall>(g, cus, 2, s);
+    else launch_few<DT, kMxFewLds>(g, cus, 1, s);
     return;
   }
   const uint64_t big = static_cast<uint64_t>((g.M + 255) / 256) * ((g.N + 255) / 256);
@@ -512,9 +562,10 @@ hipError_t launch_mx_dequantize(int dtype, const uint8_t* codes, const uint8_t* 
 hipError_t launch_mx_matmul(const MxMatmulCall& c) {
   const MxGemmArgs g{c.a, c.b, c.as, c.bs, static_cast<uint32_t>(c.M), static_cast<uint32_t>(c.N),
                      static_cast<uint32_t>(mx_steps(c.K)), c.out};
+  const uint32_t cus = static_cast<uint32_t>(device_cu_count());
   (void)hipGetLastError();
-  if (c.out_dtype == PROFK_F32) launch_product<PROFK_F32>(g, c.stream);
-  else launch_product<PROFK_BF16>(g, c.stream);
+  if (c.out_dtype == PROFK_F32) launch_product<PROFK_F32>(g, cus, c.stream);
+  else launch_product<PROFK_BF16>(g, cus, c.stream);
   return hipGetLastError();
 }
 
