@@ -368,8 +368,10 @@ int profk_token_logprobs_grad(int32_t dtype, const void* logits, int64_t T, int6
  * or NaN has the byte 255 and stands for NaN.
  *
  * Layout.  K is padded with zeros to Kp, a multiple of 128.  Codes: Kp / 2
- * bytes a row, value 2 i in the low half of byte i; scales: Kp / 32 bytes a
- * row.  Rows are contiguous; codes are 16-byte aligned, scales 4-byte.
+ * bytes a row, value 2 i in the low half of byte i.  Scales: bytes
+ * [R / 32, Kp / 128, 32, 4], R rounded up to a multiple of 32, that of row r
+ * and block b at [r / 32, b / 4, r % 32, b % 4] (0 past the last row).  Both
+ * contiguous; codes are 16-byte aligned, scales 4-byte.
  * profk_mx4_codes_size and profk_mx4_scales_size give the bytes of R rows (0
  * for invalid sizes).  1 <= K <= 2^20, 0 <= R <= 2^31 - 1; a call without rows
  * does nothing. */
@@ -394,9 +396,9 @@ int profk_mx4_matmul(const uint8_t* a_codes, const uint8_t* a_scales, int64_t M,
                      const uint8_t* b_scales, int64_t N, int64_t K, int32_t out_dtype, void* out,
                      void* stream);
 
-/* x W^T with x fp32 or bf16 [M, K] quantised in the call (into ws) and W
- * [N, K] quantised before.  ws: profk_mx4_linear_workspace_size(M, K, N)
- * bytes, 16-byte aligned.  Errors as above and PROFK_EWORKSPACE. */
+/* x W^T with x fp32 or bf16 [M, K] quantised in the call and W [N, K]
+ * quantised before.  ws: profk_mx4_linear_workspace_size(M, K, N) bytes (0 for
+ * few rows: NULL is accepted), 16-byte aligned.  Errors as above and PROFK_EWORKSPACE. */
 size_t profk_mx4_linear_workspace_size(int64_t M, int64_t K, int64_t N);
 int profk_mx4_linear(int32_t dtype, const void* x, int64_t M, int64_t K, int64_t row_stride,
                      const uint8_t* w_codes, const uint8_t* w_scales, int64_t N, int32_t out_dtype, void* out,

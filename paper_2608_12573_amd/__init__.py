@@ -661,7 +661,7 @@ def _mx4_shapes(R, K):
     if not 1 <= K <= MX4_MAX_K:
         raise ProfkError(f"rows must hold from 1 to {MX4_MAX_K} values, got {K}")
     steps = -(-K // 128)
-    return (R, 64 * steps), (R, 4 * steps)
+    return (R, 64 * steps), (-(-R // 32), steps, 32, 4)
 
 
 def _mx4(codes, scales, name, K, device=None):
@@ -686,7 +686,8 @@ def mx4_outputs(R, K, device="cuda"):
 def mx4_quantize(x, out=None):
     """fp32 or bf16 x [R, K] (rows may be strided) in 4 bits a value with one
     power-of-two scale per 32: (codes uint8 [R, Kp/2], scales uint8
-    [R, Kp/32]), Kp = K rounded up to a multiple of 128."""
+    [R/32, Kp/128, 32, 4]), K rounded up to a multiple of 128 and, in the
+    scales, R to one of 32."""
     dt = _input(x, "x", 2, layout="rows")
     R, K = x.shape
     if out is None:

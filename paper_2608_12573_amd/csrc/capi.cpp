@@ -412,7 +412,7 @@ size_t profk_mx4_codes_size(int64_t R, int64_t K) {
 }
 
 size_t profk_mx4_scales_size(int64_t R, int64_t K) {
-  return check_mx(R, K) == PROFK_OK ? static_cast<size_t>(R) * profk::mx_steps(K) * 4 : 0;
+  return check_mx(R, K) == PROFK_OK ? (static_cast<size_t>(R) + 31) / 32 * profk::mx_steps(K) * 128 : 0;
 }
 
 int profk_mx4_quantize(int32_t dtype, const void* x, int64_t R, int64_t K, int64_t row_stride, uint8_t* codes,
@@ -448,13 +448,14 @@ int profk_mx4_matmul(const uint8_t* a_codes, const uint8_t* a_scales, int64_t M,
   if (!mx_aligned(a_codes, a_scales) || !mx_aligned(b_codes, b_scales) || !aligned(out, elem_size(out_dtype)))
     return PROFK_EINVAL;
   const profk::MxMatmulCall c{a_codes, a_scales, b_codes, b_scales, M, N, K, out_dtype, out,
-                              static_cast<hipStream_t>(stream)};
+                              static_cast<hipStream_t>(stream), nullptr, 0, 0};
   const hipError_t e = profk::launch_mx_matmul(c);
   return e == hipSuccess ? PROFK_OK : hip_fail(e);
 }
 
 size_t profk_mx4_linear_workspace_size(int64_t M, int64_t K, int64_t N) {
   if (check_mx(M, K) != PROFK_OK || check_mx(N, K) != PROFK_OK || M == 0 || N == 0) return 0;
+  if (profk::mx_quantizes_x(M, K)) return 0;
   return align256(profk_mx4_codes_size(M, K)) + profk_mx4_scales_size(M, K);
 }
 
@@ -465,11 +466,18 @@ int profk_mx4_linear(int32_t dtype, const void* x, int64_t M, int64_t K, int64_t
   if (check_mx(M, K) != PROFK_OK || check_mx(N, K) != PROFK_OK) return PROFK_EINVAL;
   if (row_stride < K || row_stride > INT64_MAX / 8 / (M > 0 ? M : 1)) return PROFK_EINVAL;
   if (M == 0 || N == 0) return PROFK_OK;
-  if (!x || !w_codes || !w_scales || !out || !ws) return PROFK_ENULL;
+  const size_t need = profk_mx4_linear_workspace_size(M, K, N);
+  if (!x || !w_codes || !w_scales || !out || (need && !ws)) return PROFK_ENULL;
   if (!aligned(x, elem_size(dtype)) || !mx_aligned(w_codes, w_scales) || !aligned(out, elem_size(out_dtype)) ||
       !aligned(ws, 16))
     return PROFK_EINVAL;
-  if (ws_bytes < profk_mx4_linear_workspace_size(M, K, N)) return PROFK_EWORKSPACE;
+  if (ws_bytes < need) return PROFK_EWORKSPACE;
+  if (need == 0) {
+    const profk::MxMatmulCall c{nullptr, nullptr, w_codes, w_scales, M, N, K, out_dtype, out,
+                                static_cast<hipStream_t>(stream), x, static_cast<uint64_t>(row_stride), dtype};
+    const hipError_t e = profk::launch_mx_matmul(c);
+    return e == hipSuccess ? PROFK_OK : hip_fail(e);
+  }
   uint8_t* const codes = static_cast<uint8_t*>(ws);
   uint8_t* const scales = codes + align256(profk_mx4_codes_size(M, K));
   const int rc = profk_mx4_quantize(dtype, x, M, K, row_stride, codes, scales, stream);

@@ -10,10 +10,14 @@
 // to even.  Byte 255 is NaN: a block that holds an infinity or NaN.
 //
 // Layout: K is padded to Kp, whole steps of 128 values (zero codes).  Codes
-// [R, Kp / 2] bytes, the even value of a pair in the low half; scales
-// [R, Kp / 32] bytes.  A row's codes start at a multiple of 64 bytes, and the
-// four scales of a step are one word: a lane of the 32x32x64 matrix
-// instruction takes 32 values of a row (16 bytes) and their scale.
+// [R, Kp / 2] bytes, the even value of a pair in the low half: a row's codes
+// start at a multiple of 64 bytes, and a lane of the 32x32x64 matrix
+// instruction takes 32 values of a row (16 bytes) and their scale.  Scales
+// [R / 32, Kp / 128, 32, 4] bytes, R padded to whole groups of 32 rows: the
+// four scales of a row's step are a word, and a group's step is one line of 128
+// bytes.  (With a row's scales one after the other, a step's loads of a 256 x
+// 256 tile touched 512 lines for 2 KB, as many as its 32 KB of codes did, and
+// a product of 4096 x 4096 x 65536 took 805 us.)
 #include <type_traits>
 
 #include "device_common.h"
@@ -93,37 +97,70 @@ __device__ __forceinline__ uint32_t mx_quant8(const float (&v)[8], uint32_t& byt
   return c;
 }
 
+// A workgroup takes 32 rows and kMxPairs steps: whole lines of scales.
+constexpr uint32_t kMxPairs = 2;
+
 struct MxQuantArgs {
   const void* x;
   uint64_t stride;
-  uint32_t rows, K, lanes;   // lanes of a row (Kp / 8)
-  uint32_t* codes;
-  uint8_t* scales;
+  uint32_t rows, K, steps;
+  uint8_t *codes, *scales;
 };
 
+// Word of a row's four scales of step k, in words from the first.
+__device__ __forceinline__ size_t mx_scale_word(uint32_t r, uint32_t k, uint32_t steps) {
+  return (static_cast<size_t>(r >> 5) * steps + k) * 32 + (r & 31);
+}
+
 template <int DT> __global__ __launch_bounds__(kMxBS) void k_mx_quantize(MxQuantArgs a) {
-  const uint32_t t = blockIdx.x * kMxBS + threadIdx.x;
-  const uint32_t r = t / a.lanes, c = t - r * a.lanes;
-  if (r >= a.rows) return;                          // (whole quads: a row has a multiple of 16 lanes)
-  float v[8];
-  mx_load8<DT>(static_cast<const char*>(a.x) + r * a.stride * (DT == PROFK_F32 ? 4 : 2), 8 * c, a.K, v);
-  uint32_t byte;
-  a.codes[t] = mx_quant8(v, byte);
-  if ((c & 3) == 0) a.scales[t >> 2] = static_cast<uint8_t>(byte);
+  constexpr int P = 32 * 16 / kMxBS;                 // turns to 32 rows of a step, 16 lanes a row
+  const uint32_t parts = (a.steps + kMxPairs - 1) / kMxPairs;
+  const uint32_t group = blockIdx.x / parts, k0 = (blockIdx.x - group * parts) * kMxPairs;
+  const uint32_t c = threadIdx.x & 15;
+  float v[kMxPairs][P][8];
+#pragma unroll
+  for (uint32_t u = 0; u < kMxPairs; ++u)
+#pragma unroll
+    for (int p = 0; p < P; ++p) {
+      const uint32_t r = group * 32 + p * (kMxBS / 16) + threadIdx.x / 16, k = (k0 + u) * 128 + 8 * c;
+      // (past the rows or the row's values: zeros)
+      const bool in = r < a.rows;
+      mx_load8<DT>(static_cast<const char*>(a.x) + (in ? r : 0) * a.stride * (DT == PROFK_F32 ? 4 : 2), k,
+                   in ? a.K : 0, v[u][p]);
+    }
+#pragma unroll
+  for (uint32_t u = 0; u < kMxPairs; ++u) {
+    const uint32_t k = k0 + u;
+    if (k >= a.steps) break;
+#pragma unroll
+    for (int p = 0; p < P; ++p) {
+      const uint32_t r = group * 32 + p * (kMxBS / 16) + threadIdx.x / 16;
+      uint32_t byte;
+      const uint32_t code = mx_quant8(v[u][p], byte);
+      if (r < a.rows)
+        *reinterpret_cast<uint32_t*>(a.codes + (static_cast<size_t>(r) * a.steps + k) * 64 + 4 * c) = code;
+      // the row's four bytes, from lanes 0, 4, 8 and 12 of its sixteen
+      uint32_t word = byte;
+      word |= static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, static_cast<int>(byte), 0x104, 0xF, 0xF, false)) << 8;
+      word |= static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, static_cast<int>(byte), 0x108, 0xF, 0xF, false)) << 16;
+      word |= static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, static_cast<int>(byte), 0x10C, 0xF, 0xF, false)) << 24;
+      if (c == 0) reinterpret_cast<uint32_t*>(a.scales)[mx_scale_word(r, k, a.steps)] = word;
+    }
+  }
 }
 
 struct MxDequantArgs {
   const uint32_t* codes;
   const uint8_t* scales;
-  uint32_t rows, K, lanes;
+  uint32_t rows, K, lanes;   // lanes of a row (Kp / 8)
   void* out;
 };
 
 template <int DT> __global__ __launch_bounds__(kMxBS) void k_mx_dequantize(MxDequantArgs a) {
   const uint32_t t = blockIdx.x * kMxBS + threadIdx.x;
-  const uint32_t r = t / a.lanes, k = 8 * (t - r * a.lanes);
+  const uint32_t r = t / a.lanes, c = t - r * a.lanes, k = 8 * c;
   if (r >= a.rows || k >= a.K) return;
-  const uint32_t code = a.codes[t], byte = a.scales[t >> 2];
+  const uint32_t code = a.codes[t], byte = a.scales[4 * mx_scale_word(r, c / 16, a.lanes / 16) + c % 16 / 4];
   const bool small = byte < kMxSmall;
   const float scale = __uint_as_float((small ? byte + 64 : byte) << 23);
   const float f = byte == 255 ? __builtin_nanf("") : small ? 0x1p-64f : 1.0f;
@@ -167,9 +204,12 @@ template <int KS> __device__ __forceinline__ f32x16 mx_mma(const u32x4& a, const
 
 struct MxGemmArgs {
   const uint8_t *a, *b;       // codes [M, Kp / 2], [N, Kp / 2]
-  const uint8_t *as, *bs;     // scales [M, Kp / 32], [N, Kp / 32]
+  const uint8_t *as, *bs;     // scales [M / 32, steps, 32, 4], [N / 32, steps, 32, 4]
   uint32_t M, N, steps;       // steps of 128 values
   void* out;                  // [M, N]
+  const void* x;              // few rows: a before it is quantised (a, as unused)
+  uint64_t x_stride;
+  uint32_t K;
 };
 
 // Values n .. n + 3 of an output row.
@@ -242,12 +282,13 @@ __device__ __forceinline__ void mx_gemm_body(const MxGemmArgs& g, uint32_t tiles
   const uint32_t tid = threadIdx.x, lane = tid & (kWave - 1);
   const uint32_t w = __builtin_amdgcn_readfirstlane(tid / kWave);
   const uint32_t c = lane & 31, h = lane >> 5, wm = w / WN, wn = w % WN;
-  const size_t cb = static_cast<size_t>(g.steps) * 64, sb = static_cast<size_t>(g.steps) * 4;
+  const size_t cb = static_cast<size_t>(g.steps) * 64;
 
   auto col_of = [](uint32_t r) { return r / (NJ * 32) * (NJ * 32) + r % 32 * NJ + r % (NJ * 32) / 32; };
   // a lane's loads: offsets from the tile's first row, which a step adds to
   // (within 256 rows of at most 2^19 bytes)
-  const uint8_t *base_a = g.a + m0 * cb, *base_b = g.b + n0 * cb, *base_as = g.as + m0 * sb, *base_bs = g.bs + n0 * sb;
+  const uint8_t *base_a = g.a + m0 * cb, *base_b = g.b + n0 * cb, *base_as = g.as + m0 * (cb / 16),
+                *base_bs = g.bs + n0 * (cb / 16);
   const uint32_t last_m = g.M - 1 - m0, last_n = g.N - 1 - n0;
   uint32_t oa[T::QA], ob[T::QB], os[T::QS];
 #pragma unroll
@@ -260,14 +301,16 @@ __device__ __forceinline__ void mx_gemm_body(const MxGemmArgs& g, uint32_t tiles
     const uint32_t p = (w * T::QB + q) * kWave + lane, r = p / 4, gr = (p & 3) ^ (r >> 2 & 3);
     ob[q] = min(col_of(r), last_n) * static_cast<uint32_t>(cb) + gr * 16;
   }
-  // (a wave's scale loads are all of a or all of b)
+  // (a wave's scale loads are all of a or all of b; rows past the last group
+  // read the last one)
   static_assert(T::BM % kWave == 0, "scale loads of one matrix a wave");
   const uint8_t* base_s[T::QS];
 #pragma unroll
   for (int q = 0; q < T::QS; ++q) {
     const uint32_t r0 = (w * T::QS + q) * kWave, r = r0 + lane;
     base_s[q] = r0 < T::BM ? base_as : base_bs;
-    os[q] = (r0 < T::BM ? min(r, last_m) : min(col_of(r - T::BM), last_n)) * static_cast<uint32_t>(sb);
+    const uint32_t row = r0 < T::BM ? r : col_of(r - T::BM), last = r0 < T::BM ? last_m : last_n;
+    os[q] = (min(row / 32, last / 32) * g.steps * 32 + row % 32) * 4;
   }
   // the next step, or the last one again, into a stage
   uint32_t next = 0;
@@ -282,7 +325,7 @@ __device__ __forceinline__ void mx_gemm_body(const MxGemmArgs& g, uint32_t tiles
       base_a += 64;
       base_b += 64;
 #pragma unroll
-      for (int q = 0; q < T::QS; ++q) base_s[q] += 4;
+      for (int q = 0; q < T::QS; ++q) base_s[q] += 128;
     }
   };
   f32x16 acc[MI][NJ] = {};
@@ -359,14 +402,18 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void k_mx_gemm(MxGemmArgs g, uint3
 // KSPLIT: the workgroup's waves each take a part of the steps of the same
 // groups, and their sums are added in wave order.
 constexpr int kMxFewBS = 256;
+constexpr int kMxCodes = -1;                          // a's type where it is quantised already
 constexpr uint32_t kMxFewStage = 32 * 128 + 32 * 8;   // bytes of a wave's stage: codes, then scales
 constexpr int kMxFewLoads = 5;                        // loads of a stage
 // LDS for a: two workgroups a CU, or one.
 constexpr uint32_t kMxFewLdsSmall = 10 * 1024, kMxFewLds = 72 * 1024;
 __host__ __device__ constexpr uint32_t mx_few_row(uint32_t steps) { return steps * 64 + 16; }   // LDS bytes of a row of a
 __host__ __device__ constexpr uint32_t mx_few_lds(uint32_t M, uint32_t steps) { return M * (mx_few_row(steps) + steps * 4); }
+constexpr bool mx_few(uint64_t M, uint64_t steps) {
+  return M <= 32 && steps <= kMxFewLds / 64 && mx_few_lds(static_cast<uint32_t>(M), static_cast<uint32_t>(steps)) <= kMxFewLds;
+}
 
-template <int DT, bool KSPLIT, int LDS> __device__ __forceinline__ void mx_few_body(const MxGemmArgs& g) {
+template <int DT, int XDT, bool KSPLIT, int LDS> __device__ __forceinline__ void mx_few_body(const MxGemmArgs& g) {
   constexpr int NW = kMxFewBS / kWave;
   constexpr uint32_t kQ = kMxFewStage / 16;
   __shared__ __align__(16) uint8_t smem[LDS];   // a: codes, then scales
@@ -382,7 +429,7 @@ template <int DT, bool KSPLIT, int LDS> __device__ __forceinline__ void mx_few_b
   const uint32_t mine = g0 < groups ? (groups - g0 + gs - 1) / gs : 0;
   const uint32_t total = mine * (p1 - p0);
   const uint32_t rb = mx_few_row(g.steps);
-  const size_t cb = static_cast<size_t>(g.steps) * 64, sb = static_cast<size_t>(g.steps) * 4;
+  const size_t cb = static_cast<size_t>(g.steps) * 64;
 
   // the pair to load next: group ig, pair ip
   uint32_t ig = g0, ip = p0, issued = 0;
@@ -391,14 +438,14 @@ template <int DT, bool KSPLIT, int LDS> __device__ __forceinline__ void mx_few_b
     const uint32_t n0 = ig * 32, last = g.N - 1 - n0;
     const uint32_t half = 2 * ip + 1 < g.steps ? 1u : 0u;   // 0: the pair's second step is past the end
     const uint8_t* const codes = g.b + n0 * cb + ip * 128;
-    const uint8_t* const scales = g.bs + n0 * sb + ip * 8;
+    const uint8_t* const scales = g.bs + (static_cast<size_t>(ig) * g.steps + 2 * ip) * 128;
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
       const uint32_t r = q * 8 + lane / 8, gr = (lane & 7) ^ (r >> 1 & 7);
       const uint32_t o = min(r, last) * static_cast<uint32_t>(cb) + (half ? gr : gr & 3) * 16;
       __builtin_amdgcn_global_load_lds(reinterpret_cast<const uint32_t*>(codes + o), st + q * kWave, 16, 0, 0);
     }
-    const uint32_t o = min(lane / 2, last) * static_cast<uint32_t>(sb) + (lane & half) * 4;
+    const uint32_t o = (half ? lane : lane & 31) * 4;
     __builtin_amdgcn_global_load_lds(reinterpret_cast<const uint32_t*>(scales + o), st + 4 * kWave, 4, 0, 0);
     if (++issued < total) {
       if (++ip == p1) {
@@ -412,13 +459,26 @@ template <int DT, bool KSPLIT, int LDS> __device__ __forceinline__ void mx_few_b
     issue(s1);
     issue(s2);
   }
-  // a to LDS meanwhile
+  // a to LDS meanwhile, quantised here where it is not yet
   uint32_t* const s_scale = reinterpret_cast<uint32_t*>(smem + g.M * rb);
-  for (uint32_t i = tid; i < g.M * g.steps * 4; i += kMxFewBS) {
-    const uint32_t r = i / (g.steps * 4), q = i - r * g.steps * 4;
-    *reinterpret_cast<uint4*>(smem + r * rb + q * 16) = reinterpret_cast<const uint4*>(g.a)[i];
+  if constexpr (XDT == kMxCodes) {
+    for (uint32_t i = tid; i < g.M * g.steps * 4; i += kMxFewBS) {
+      const uint32_t r = i / (g.steps * 4), q = i - r * g.steps * 4;
+      *reinterpret_cast<uint4*>(smem + r * rb + q * 16) = reinterpret_cast<const uint4*>(g.a)[i];
+    }
+    for (uint32_t i = tid; i < g.steps * 32; i += kMxFewBS)
+      if ((i & 31) < g.M) s_scale[(i & 31) * g.steps + (i >> 5)] = reinterpret_cast<const uint32_t*>(g.as)[i];
+  } else {
+    const uint32_t lanes = g.steps * 16;
+    for (uint32_t i = tid; i < g.M * lanes; i += kMxFewBS) {   // (whole quads of lanes)
+      const uint32_t r = i / lanes, q = i - r * lanes;
+      float v[8];
+      mx_load8<XDT>(static_cast<const char*>(g.x) + r * g.x_stride * (XDT == PROFK_F32 ? 4 : 2), 8 * q, g.K, v);
+      uint32_t byte;
+      *reinterpret_cast<uint32_t*>(smem + r * rb + q * 4) = mx_quant8(v, byte);
+      if ((q & 3) == 0) reinterpret_cast<uint8_t*>(s_scale)[i >> 2] = static_cast<uint8_t>(byte);
+    }
   }
-  for (uint32_t i = tid; i < g.M * g.steps; i += kMxFewBS) s_scale[i] = reinterpret_cast<const uint32_t*>(g.as)[i];
   __syncthreads();
 
   const uint32_t m = min(c, g.M - 1);
@@ -460,7 +520,7 @@ template <int DT, bool KSPLIT, int LDS> __device__ __forceinline__ void mx_few_b
     wait_loads_lds<2 * kMxFewLoads>();
     issue(old);
     const uint4* const st = cur + w * kQ;
-    const uint2 sc = reinterpret_cast<const uint2*>(st + 4 * kWave)[c];
+    const uint32_t* const sc = reinterpret_cast<const uint32_t*>(st + 4 * kWave);
     const uint32_t x = c >> 1 & 7;
     auto one = [&](uint32_t k, uint32_t hi, uint32_t scale) {
       const u32x4 b0 = __builtin_bit_cast(u32x4, st[c * 8 + ((4 * hi + h) ^ x)]);
@@ -470,8 +530,8 @@ template <int DT, bool KSPLIT, int LDS> __device__ __forceinline__ void mx_few_b
       acc = mx_mma<0>(a0, b0, acc, sa, sw);
       acc = mx_mma<1>(a1, b1, acc, sa, sw);
     };
-    one(2 * cp, 0, sc.x);
-    if (2 * cp + 1 < g.steps) one(2 * cp + 1, 1, sc.y);
+    one(2 * cp, 0, sc[c]);
+    if (2 * cp + 1 < g.steps) one(2 * cp + 1, 1, sc[32 + c]);
     if (++cp == p1) {
       finish();
       cp = p0;
@@ -487,8 +547,8 @@ template <int DT, bool KSPLIT, int LDS> __device__ __forceinline__ void mx_few_b
   wait_loads_lds<0>();   // (no load may reach LDS after the workgroup's end)
 }
 
-template <int DT, bool KSPLIT, int LDS> __global__ __launch_bounds__(kMxFewBS) void k_mx_few(MxGemmArgs g) {
-  mx_few_body<DT, KSPLIT, LDS>(g);
+template <int DT, int XDT, bool KSPLIT, int LDS> __global__ __launch_bounds__(kMxFewBS) void k_mx_few(MxGemmArgs g) {
+  mx_few_body<DT, XDT, KSPLIT, LDS>(g);
 }
 
 template <int DT, int WM, int WN, int MI, int NJ> void launch_gemm(const MxGemmArgs& g, hipStream_t s) {
@@ -498,18 +558,23 @@ template <int DT, int WM, int WN, int MI, int NJ> void launch_gemm(const MxGemmA
   k_mx_gemm<DT, WM, WN, MI, NJ><<<per * kXcds, T::BS, 0, s>>>(g, tm, tiles, per);
 }
 
-template <int DT, int LDS> void launch_few(const MxGemmArgs& g, uint32_t cus, uint32_t per_cu, hipStream_t s) {
+template <int DT, int XDT, int LDS> void launch_few(const MxGemmArgs& g, uint32_t cus, uint32_t per_cu, hipStream_t s) {
   // few groups: the waves of a workgroup share one
   const uint32_t groups = (g.N + 31) / 32, most = per_cu * cus;
-  if (groups < 4 * cus && g.steps >= 8) k_mx_few<DT, true, LDS><<<groups < most ? groups : most, kMxFewBS, 0, s>>>(g);
-  else k_mx_few<DT, false, LDS><<<(groups + 3) / 4 < most ? (groups + 3) / 4 : most, kMxFewBS, 0, s>>>(g);
+  if (groups < 4 * cus && g.steps >= 8) k_mx_few<DT, XDT, true, LDS><<<groups < most ? groups : most, kMxFewBS, 0, s>>>(g);
+  else k_mx_few<DT, XDT, false, LDS><<<(groups + 3) / 4 < most ? (groups + 3) / 4 : most, kMxFewBS, 0, s>>>(g);
 }
 
-template <int DT> void launch_product(const MxGemmArgs& g, uint32_t cus, hipStream_t s) {
-  const uint32_t lds = mx_few_lds(g.M, g.steps);
-  if (g.M <= 32 && lds <= kMxFewLds) {
-    if (lds <= kMxFewLdsSmall) launch_few<DT, kMxFewLdsSmall>(g, cus, 2, s);
-    else launch_few<DT, kMxFewLds>(g, cus, 1, s);
+template <int DT, int XDT> void launch_few_any(const MxGemmArgs& g, uint32_t cus, hipStream_t s) {
+  if (mx_few_lds(g.M, g.steps) <= kMxFewLdsSmall) launch_few<DT, XDT, kMxFewLdsSmall>(g, cus, 2, s);
+  else if constexpr (XDT == kMxCodes) launch_few<DT, XDT, kMxFewLds>(g, cus, 1, s);
+}
+
+template <int DT> void launch_product(const MxGemmArgs& g, int x_dtype, uint32_t cus, hipStream_t s) {
+  if (mx_few(g.M, g.steps)) {
+    if (!g.x) launch_few_any<DT, kMxCodes>(g, cus, s);
+    else if (x_dtype == PROFK_F32) launch_few_any<DT, PROFK_F32>(g, cus, s);
+    else launch_few_any<DT, PROFK_BF16>(g, cus, s);
     return;
   }
   const uint64_t big = static_cast<uint64_t>((g.M + 255) / 256) * ((g.N + 255) / 256);
@@ -523,15 +588,15 @@ uint64_t mx_steps(int64_t K) { return (static_cast<uint64_t>(K) + 127) / 128; }
 
 hipError_t launch_mx_quantize(int dtype, const void* x, uint64_t stride, int64_t R, int64_t K, uint8_t* codes,
                               uint8_t* scales, hipStream_t s) {
-  const uint64_t lanes = mx_steps(K) * 16;
-  const int64_t step = static_cast<int64_t>((uint64_t{1} << 31) / lanes);
+  const uint64_t steps = mx_steps(K), parts = (steps + kMxPairs - 1) / kMxPairs;
+  const int64_t step = static_cast<int64_t>(rows_per_launch(kMxBS) / static_cast<int64_t>(parts)) * 32;
   (void)hipGetLastError();
   for (int64_t r = 0; r < R; r += step) {
     const uint64_t rows = static_cast<uint64_t>(R - r < step ? R - r : step);
     const MxQuantArgs a{static_cast<const uint8_t*>(x) + static_cast<uint64_t>(r) * stride * (dtype == PROFK_F32 ? 4 : 2),
-                        stride, static_cast<uint32_t>(rows), static_cast<uint32_t>(K), static_cast<uint32_t>(lanes),
-                        reinterpret_cast<uint32_t*>(codes + r * lanes * 4), scales + r * (lanes / 4)};
-    const uint32_t grid = static_cast<uint32_t>((rows * lanes + kMxBS - 1) / kMxBS);
+                        stride, static_cast<uint32_t>(rows), static_cast<uint32_t>(K), static_cast<uint32_t>(steps),
+                        codes + r * steps * 64, scales + r * steps * 4};
+    const uint32_t grid = static_cast<uint32_t>((rows + 31) / 32 * parts);
     if (dtype == PROFK_F32) k_mx_quantize<PROFK_F32><<<grid, kMxBS, 0, s>>>(a);
     else k_mx_quantize<PROFK_BF16><<<grid, kMxBS, 0, s>>>(a);
     const hipError_t e = hipGetLastError();
@@ -543,7 +608,7 @@ hipError_t launch_mx_quantize(int dtype, const void* x, uint64_t stride, int64_t
 hipError_t launch_mx_dequantize(int dtype, const uint8_t* codes, const uint8_t* scales, int64_t R, int64_t K, void* out,
                                 hipStream_t s) {
   const uint64_t lanes = mx_steps(K) * 16;
-  const int64_t step = static_cast<int64_t>((uint64_t{1} << 31) / lanes);
+  const int64_t step = static_cast<int64_t>((uint64_t{1} << 31) / lanes / 32 * 32);   // (whole groups of rows)
   (void)hipGetLastError();
   for (int64_t r = 0; r < R; r += step) {
     const uint64_t rows = static_cast<uint64_t>(R - r < step ? R - r : step);
@@ -559,13 +624,22 @@ hipError_t launch_mx_dequantize(int dtype, const uint8_t* codes, const uint8_t* 
   return hipSuccess;
 }
 
+// A workgroup that quantises a for itself saves a launch (about 4 us); where a
+// is larger, that every workgroup does so costs more (K = 4096, N = 131072:
+// M = 4 59.2 us against 55.2 and the launch, M = 16 77.9 against 63.7 and it).
+bool mx_quantizes_x(int64_t M, int64_t K) {
+  const uint64_t steps = mx_steps(K);
+  return mx_few(static_cast<uint64_t>(M), steps) &&
+         mx_few_lds(static_cast<uint32_t>(M), static_cast<uint32_t>(steps)) <= kMxFewLdsSmall;
+}
+
 hipError_t launch_mx_matmul(const MxMatmulCall& c) {
   const MxGemmArgs g{c.a, c.b, c.as, c.bs, static_cast<uint32_t>(c.M), static_cast<uint32_t>(c.N),
-                     static_cast<uint32_t>(mx_steps(c.K)), c.out};
+                     static_cast<uint32_t>(mx_steps(c.K)), c.out, c.x, c.x_stride, static_cast<uint32_t>(c.K)};
   const uint32_t cus = static_cast<uint32_t>(device_cu_count());
   (void)hipGetLastError();
-  if (c.out_dtype == PROFK_F32) launch_product<PROFK_F32>(g, cus, c.stream);
-  else launch_product<PROFK_BF16>(g, cus, c.stream);
+  if (c.out_dtype == PROFK_F32) launch_product<PROFK_F32>(g, c.x_dtype, cus, c.stream);
+  else launch_product<PROFK_BF16>(g, c.x_dtype, cus, c.stream);
   return hipGetLastError();
 }
 

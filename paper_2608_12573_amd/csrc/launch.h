@@ -357,7 +357,7 @@ struct LpGradArgs {
 hipError_t launch_logprobs_grad(LpGradArgs a, int dtype, int64_t T, hipStream_t s);
 
 // Microscaled 4-bit values (kernels_mx4.hip): K padded to whole steps of 128,
-// 64 bytes of codes and 4 of scales each.
+// 64 bytes of codes and 4 of scales each (of rows padded to groups of 32).
 uint64_t mx_steps(int64_t K);
 constexpr int64_t kMxMaxK = 1 << 20;
 hipError_t launch_mx_quantize(int dtype, const void* x, uint64_t stride, int64_t R, int64_t K, uint8_t* codes,
@@ -372,8 +372,13 @@ struct MxMatmulCall {
   int out_dtype;
   void* out;                  // [M, N]
   hipStream_t stream;
+  const void* x;              // set: a is not quantised yet (mx_quantizes_x)
+  uint64_t x_stride;
+  int x_dtype;
 };
 
+// The product's kernel for this shape quantises a itself.
+bool mx_quantizes_x(int64_t M, int64_t K);
 hipError_t launch_mx_matmul(const MxMatmulCall& c);
 
 // Inspection helpers.

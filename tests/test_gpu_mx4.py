@@ -46,7 +46,10 @@ def _check_quantize(x, dtype, pad=0, offset=0):
     g, v = _rows(x, dtype, pad, offset)
     codes, scales = pk.mx4_quantize(g)
     code, byte = omx.quantize(v)
-    assert np.array_equal(scales.cpu().numpy(), byte.astype(np.uint8))
+    # [R / 32, Kp / 128, 32, 4]: rows in groups of 32, the last one's rest 0
+    groups = -(-R // 32)
+    got = scales.cpu().numpy().transpose(0, 2, 1, 3).reshape(groups * 32, -1)
+    assert np.array_equal(got[:R], byte.astype(np.uint8)) and not got[R:].any()
     got, ref = codes.cpu().numpy(), omx.pack(code)
     # (codes of a NaN block have no meaning)
     ok = np.repeat(byte != 255, 16, axis=1)
@@ -203,7 +206,7 @@ def test_no_rows():
     t = torch()
     e = t.empty((0, 70), device="cuda")
     q = pk.mx4_quantize(e)
-    assert q[0].shape == (0, 64) and q[1].shape == (0, 4)
+    assert q[0].shape == (0, 64) and q[1].shape == (0, 1, 32, 4)
     assert pk.mx4_dequantize(*q, 70).shape == (0, 70)
     w = pk.mx4_quantize(t.ones((5, 70), device="cuda"))
     assert pk.mx4_linear(e, *w).shape == (0, 5)
@@ -260,10 +263,10 @@ def test_refusals_on_the_device():
     x = t.zeros(4, 64, device="cuda")
     c, s = pk.mx4_quantize(x)
     bad = [lambda: pk.mx4_quantize(x, out=pk.mx4_outputs(5, 64)), lambda: pk.mx4_quantize(x, out=pk.mx4_outputs(4, 129)),
-           lambda: pk.mx4_dequantize(c, s[:3], 64), lambda: pk.mx4_dequantize(c, s, 64, t.float16),
+           lambda: pk.mx4_dequantize(c, s[:, :, :3], 64), lambda: pk.mx4_dequantize(c, s, 64, t.float16),
            lambda: pk.mx4_dequantize(c, s.cpu(), 64), lambda: pk.mx4_matmul(c, s, c, s, 129),
            lambda: pk.mx4_matmul(c, s, c, s, 64, out=t.zeros(4, 5, device="cuda")),
-           lambda: pk.mx4_linear(x, c, s, ws=t.zeros(8, dtype=t.uint8, device="cuda")),
+           lambda: pk.mx4_linear(x, c, s, ws=t.zeros(8, dtype=t.uint8)),
            lambda: pk.mx4_linear(x, c, s, dtype=t.bfloat16, out=t.zeros(4, 4, device="cuda")),
            lambda: pk.mx4_linear(t.zeros(4, 200, device="cuda"), c, s)]
     for call in bad:

@@ -16,18 +16,19 @@ def _raises(fn, match):
 
 def test_sizes():
     L = pk.lib()
-    assert L.profk_mx4_codes_size(3, 1) == 3 * 64 and L.profk_mx4_scales_size(3, 1) == 12
-    assert L.profk_mx4_codes_size(5, 129) == 5 * 128 and L.profk_mx4_scales_size(5, 128) == 20
+    assert L.profk_mx4_codes_size(3, 1) == 3 * 64 and L.profk_mx4_scales_size(3, 1) == 128
+    assert L.profk_mx4_codes_size(5, 129) == 5 * 128 and L.profk_mx4_scales_size(33, 129) == 512
     assert L.profk_mx4_codes_size(2**31 - 1, 2**20) == (2**31 - 1) * 2**19
     for R, K in ((-1, 5), (5, 0), (5, 2**20 + 1), (2**31, 5)):
         assert L.profk_mx4_codes_size(R, K) == 0 and L.profk_mx4_scales_size(R, K) == 0
-    assert L.profk_mx4_linear_workspace_size(3, 129, 7) == 512 + 24
+    assert L.profk_mx4_linear_workspace_size(33, 129, 7) == (33 * 128 + 255) // 256 * 256 + 512
+    assert L.profk_mx4_linear_workspace_size(3, 129, 7) == 0      # few rows: none
     assert L.profk_mx4_linear_workspace_size(0, 129, 7) == 0
 
 
 def test_binding_refusals():
     x = torch.zeros(4, 64)
-    c, s = torch.zeros(4, 64, dtype=torch.uint8), torch.zeros(4, 4, dtype=torch.uint8)
+    c, s = torch.zeros(4, 64, dtype=torch.uint8), torch.zeros(1, 1, 32, 4, dtype=torch.uint8)
     _raises(lambda: pk.mx4_quantize(x), "CUDA tensor")
     _raises(lambda: pk.mx4_quantize(x.half()), "unsupported dtype")
     _raises(lambda: pk.mx4_quantize(x[0]), "2 dimension")
@@ -80,6 +81,6 @@ def test_matmul_refusals(kw, rc):
     (dict(x=None), pk.ENULL), (dict(ws=None), pk.ENULL), (dict(nb=7), pk.EWORKSPACE), (dict(ws=ctypes.c_void_p(4104)), pk.EINVAL),
     (dict(w=ODD), pk.EINVAL), (dict(M=0, x=None), pk.OK), (dict(st=2**62), pk.EINVAL)])
 def test_linear_refusals(kw, rc):
-    def call(dt=0, x=P, M=4, K=100, st=100, w=P, s=P, N=8, od=0, o=P, ws=P, nb=1 << 20):
+    def call(dt=0, x=P, M=40, K=100, st=100, w=P, s=P, N=8, od=0, o=P, ws=P, nb=1 << 20):
         return pk.lib().profk_mx4_linear(dt, x, M, K, st, w, s, N, od, o, ws, nb, None)
     assert call(**kw) == rc
