@@ -212,22 +212,6 @@ struct MxGemmArgs {
   uint32_t K;
 };
 
-// Values n .. n + 3 of an output row.
-template <int DT> __device__ __forceinline__ void mx_store4(void* out, size_t row, uint32_t n, uint32_t N, f32x4 v) {
-  const size_t o = row * N + n;
-  if (n + 4 <= N) {
-    if constexpr (DT == PROFK_F32) *reinterpret_cast<f32x4u*>(static_cast<float*>(out) + o) = v;
-    else *reinterpret_cast<u32x2u*>(static_cast<uint16_t*>(out) + o) = u32x2u{pack_bf16(v.x, v.y), pack_bf16(v.z, v.w)};
-  } else {
-#pragma unroll
-    for (int e = 0; e < 4; ++e)
-      if (n + e < N) {
-        if constexpr (DT == PROFK_F32) static_cast<float*>(out)[o + e] = v[e];
-        else static_cast<__bf16*>(out)[o + e] = static_cast<__bf16>(v[e]);
-      }
-  }
-}
-
 // s_waitcnt vmcnt(N) lgkmcnt(0) (gfx9 encoding: vmcnt in bits 3:0 and 15:14,
 // expcnt in 6:4, lgkmcnt in 11:8): all but this wave's N newest loads are
 // done, and so are its LDS reads.
@@ -243,11 +227,13 @@ __device__ __forceinline__ void bare_barrier() {
   asm volatile("" ::: "memory");
 }
 
-// The tiled product.  A workgroup of WM x WN waves computes a tile of BM x BN
+// The tiled product.  A workgroup of WM x WN waves computes tiles of BM x BN
 // outputs, a wave MI x NJ accumulators of 32 x 32.  A step (128 values of K)
 // of a tile is 64 bytes of codes a row and a word of four scales, loaded
 // straight to LDS, four stages deep; every wait is for the oldest stage, so
-// that the others stay in flight.  16-byte granule g of a row r is at
+// that the others stay in flight, and the loads run on into the workgroup's
+// next tile.  Fragments are read one half step ahead, under the matrix
+// instructions of the half before.  16-byte granule g of a row r is at
 // position g ^ (r / 4 % 4) of its four: sixteen neighbouring rows' granules
 // g then cover all 64 banks once.
 //
@@ -256,7 +242,6 @@ __device__ __forceinline__ void bare_barrier() {
 // neighbours and are stored together.
 //
 // Rows past M or N are read as the last one and not stored.
-
 template <int WM, int WN, int MI, int NJ> struct MxTile {
   static constexpr int BS = WM * WN * kWave, BM = WM * MI * 32, BN = WN * NJ * 32;
   static constexpr int QA = BM * 4 / BS, QB = BN * 4 / BS, QS = (BM + BN) / BS;   // loads of a lane
@@ -264,11 +249,14 @@ template <int WM, int WN, int MI, int NJ> struct MxTile {
   static constexpr int kB = BM * 4, kS = (BM + BN) * 4;        // first granule of b, of the scales
   static constexpr int kGran = kS + (BM + BN) / 4;             // granules of a stage
   static_assert(BM * 4 % BS == 0 && BN * 4 % BS == 0 && (BM + BN) % BS == 0, "whole loads");
+  static_assert(BM % kWave == 0, "scale loads of one matrix a wave");
   static_assert(NJ == 4, "four neighbouring results a lane");
 };
 
-template <int DT, int WM, int WN, int MI, int NJ>
-__device__ __forceinline__ void mx_gemm_body(const MxGemmArgs& g, uint32_t tiles_m, uint32_t tiles, uint32_t per) {
+// WHOLE: the steps are a multiple of four, so that no stage is skipped and the
+// reads and the matrix instructions of a half step are one run of code.
+template <int DT, int WM, int WN, int MI, int NJ, bool WHOLE>
+__device__ __forceinline__ void mx_gemm_body(const MxGemmArgs& g, uint32_t tiles_m, uint32_t tiles) {
   using T = MxTile<WM, WN, MI, NJ>;
   // distinct arrays, so that the compiler can tell the stage being read from
   // those being filled
@@ -276,121 +264,222 @@ __device__ __forceinline__ void mx_gemm_body(const MxGemmArgs& g, uint32_t tiles
   // workgroup b runs on XCD b % 8: each XCD takes a run of tiles, the row
   // tiles of a column tile one after the other, so that its L2 holds what
   // they share
-  const uint32_t tile = (blockIdx.x % kXcds) * per + blockIdx.x / kXcds;
-  if (blockIdx.x / kXcds >= per || tile >= tiles) return;
-  const uint32_t m0 = tile % tiles_m * T::BM, n0 = tile / tiles_m * T::BN;
+  const uint32_t xcd = blockIdx.x % kXcds, per_xcd = gridDim.x / kXcds;   // (the grid is a multiple of 8)
+  const uint32_t end = static_cast<uint32_t>(static_cast<uint64_t>(tiles) * (xcd + 1) / kXcds);
+  const uint32_t tile0 = static_cast<uint32_t>(static_cast<uint64_t>(tiles) * xcd / kXcds) + blockIdx.x / kXcds;
+  if (tile0 >= end) return;
+  // a tile takes a multiple of four stages, so that each starts at the same
+  // one; those past its last step are not multiplied
+  const uint32_t slots = WHOLE ? g.steps : (g.steps + 3) / 4 * 4;
   const uint32_t tid = threadIdx.x, lane = tid & (kWave - 1);
   const uint32_t w = __builtin_amdgcn_readfirstlane(tid / kWave);
   const uint32_t c = lane & 31, h = lane >> 5, wm = w / WN, wn = w % WN;
-  const size_t cb = static_cast<size_t>(g.steps) * 64;
+  const uint32_t cb = g.steps * 64;
 
   auto col_of = [](uint32_t r) { return r / (NJ * 32) * (NJ * 32) + r % 32 * NJ + r % (NJ * 32) / 32; };
-  // a lane's loads: offsets from the tile's first row, which a step adds to
-  // (within 256 rows of at most 2^19 bytes)
-  const uint8_t *base_a = g.a + m0 * cb, *base_b = g.b + n0 * cb, *base_as = g.as + m0 * (cb / 16),
-                *base_bs = g.bs + n0 * (cb / 16);
-  const uint32_t last_m = g.M - 1 - m0, last_n = g.N - 1 - n0;
+  // The step to load next: a lane's offsets from the first row of its tile
+  // (within 256 rows of at most 2^19 bytes), to which a step adds.
+  const uint8_t *base_a, *base_b, *base_s[T::QS];
   uint32_t oa[T::QA], ob[T::QB], os[T::QS];
+  auto start = [&](uint32_t tile) {
+    const uint32_t m0 = tile % tiles_m * T::BM, n0 = tile / tiles_m * T::BN;
+    const uint32_t last_m = g.M - 1 - m0, last_n = g.N - 1 - n0;
+    base_a = g.a + static_cast<size_t>(m0) * cb;
+    base_b = g.b + static_cast<size_t>(n0) * cb;
 #pragma unroll
-  for (int q = 0; q < T::QA; ++q) {
-    const uint32_t p = (w * T::QA + q) * kWave + lane, r = p / 4, gr = (p & 3) ^ (r >> 2 & 3);
-    oa[q] = min(r, last_m) * static_cast<uint32_t>(cb) + gr * 16;
-  }
+    for (int q = 0; q < T::QA; ++q) {
+      const uint32_t p = (w * T::QA + q) * kWave + lane, r = p / 4, gr = (p & 3) ^ (r >> 2 & 3);
+      oa[q] = min(r, last_m) * cb + gr * 16;
+    }
 #pragma unroll
-  for (int q = 0; q < T::QB; ++q) {
-    const uint32_t p = (w * T::QB + q) * kWave + lane, r = p / 4, gr = (p & 3) ^ (r >> 2 & 3);
-    ob[q] = min(col_of(r), last_n) * static_cast<uint32_t>(cb) + gr * 16;
-  }
-  // (a wave's scale loads are all of a or all of b; rows past the last group
-  // read the last one)
-  static_assert(T::BM % kWave == 0, "scale loads of one matrix a wave");
-  const uint8_t* base_s[T::QS];
+    for (int q = 0; q < T::QB; ++q) {
+      const uint32_t p = (w * T::QB + q) * kWave + lane, r = p / 4, gr = (p & 3) ^ (r >> 2 & 3);
+      ob[q] = min(col_of(r), last_n) * cb + gr * 16;
+    }
+    // (a wave's scale loads are all of a or all of b; rows past the last group
+    // read the last one)
 #pragma unroll
-  for (int q = 0; q < T::QS; ++q) {
-    const uint32_t r0 = (w * T::QS + q) * kWave, r = r0 + lane;
-    base_s[q] = r0 < T::BM ? base_as : base_bs;
-    const uint32_t row = r0 < T::BM ? r : col_of(r - T::BM), last = r0 < T::BM ? last_m : last_n;
-    os[q] = (min(row / 32, last / 32) * g.steps * 32 + row % 32) * 4;
-  }
-  // the next step, or the last one again, into a stage
-  uint32_t next = 0;
-  auto issue = [&](uint4* st) {
+    for (int q = 0; q < T::QS; ++q) {
+      const uint32_t r0 = (w * T::QS + q) * kWave, r = r0 + lane;
+      const bool of_a = r0 < T::BM;
+      base_s[q] = of_a ? g.as + static_cast<size_t>(m0) * (cb / 16) : g.bs + static_cast<size_t>(n0) * (cb / 16);
+      const uint32_t row = of_a ? r : col_of(r - T::BM), last = of_a ? last_m : last_n;
+      os[q] = (min(row / 32, last / 32) * g.steps * 32 + row % 32) * 4;
+    }
+  };
+  uint32_t next_k = 0, next_tile = tile0;
+  // (past a tile's last step, and the last tile: the last again; a tile's
+  // stages end with the fourth)
+  auto issue = [&](uint4* st, auto fourth) {
 #pragma unroll
-    for (int q = 0; q < T::QA; ++q) __builtin_amdgcn_global_load_lds(reinterpret_cast<const uint32_t*>(base_a + oa[q]), st + (w * T::QA + q) * kWave, 16, 0, 0);
+    for (int q = 0; q < T::QA; ++q)
+      __builtin_amdgcn_global_load_lds(reinterpret_cast<const uint32_t*>(base_a + oa[q]), st + (w * T::QA + q) * kWave,
+                                       16, 0, 0);
 #pragma unroll
-    for (int q = 0; q < T::QB; ++q) __builtin_amdgcn_global_load_lds(reinterpret_cast<const uint32_t*>(base_b + ob[q]), st + T::kB + (w * T::QB + q) * kWave, 16, 0, 0);
+    for (int q = 0; q < T::QB; ++q)
+      __builtin_amdgcn_global_load_lds(reinterpret_cast<const uint32_t*>(base_b + ob[q]),
+                                       st + T::kB + (w * T::QB + q) * kWave, 16, 0, 0);
 #pragma unroll
-    for (int q = 0; q < T::QS; ++q) __builtin_amdgcn_global_load_lds(reinterpret_cast<const uint32_t*>(base_s[q] + os[q]), st + T::kS + (w * T::QS + q) * (kWave / 4), 4, 0, 0);
-    if (++next < g.steps) {
+    for (int q = 0; q < T::QS; ++q)
+      __builtin_amdgcn_global_load_lds(reinterpret_cast<const uint32_t*>(base_s[q] + os[q]),
+                                       st + T::kS + (w * T::QS + q) * (kWave / 4), 4, 0, 0);
+    ++next_k;
+    if (next_k < g.steps) {
       base_a += 64;
       base_b += 64;
 #pragma unroll
       for (int q = 0; q < T::QS; ++q) base_s[q] += 128;
     }
+    if (decltype(fourth)::value && next_k == slots && next_tile + per_xcd < end) {
+      next_k = 0;
+      next_tile += per_xcd;
+      start(next_tile);
+    }
   };
-  f32x16 acc[MI][NJ] = {};
-  auto compute = [&](const uint4* st) {
-    const uint32_t* const sc = reinterpret_cast<const uint32_t*>(st + T::kS);
-    int sa[MI], sw[NJ];
-#pragma unroll
-    for (int i = 0; i < MI; ++i) sa[i] = static_cast<int>(sc[wm * MI * 32 + i * 32 + c] >> (8 * h));
-#pragma unroll
-    for (int j = 0; j < NJ; ++j) sw[j] = static_cast<int>(sc[T::BM + wn * NJ * 32 + j * 32 + c] >> (8 * h));
-    auto half = [&](auto KS) {
-      constexpr int ks = decltype(KS)::value;
-      u32x4 fa[MI], fb[NJ];
-#pragma unroll
-      for (int i = 0; i < MI; ++i) {
-        const uint32_t r = wm * MI * 32 + i * 32 + c;
-        fa[i] = __builtin_bit_cast(u32x4, st[r * 4 + ((2 * ks + h) ^ (r >> 2 & 3))]);
-      }
-#pragma unroll
-      for (int j = 0; j < NJ; ++j) {
-        const uint32_t r = wn * NJ * 32 + j * 32 + c;
-        fb[j] = __builtin_bit_cast(u32x4, st[T::kB + r * 4 + ((2 * ks + h) ^ (r >> 2 & 3))]);
-      }
-#pragma unroll
-      for (int i = 0; i < MI; ++i)
-#pragma unroll
-        for (int j = 0; j < NJ; ++j) acc[i][j] = mx_mma<ks>(fa[i], fb[j], acc[i][j], sa[i], sw[j]);
-    };
-    half(std::integral_constant<int, 0>{});
-    half(std::integral_constant<int, 1>{});
+  struct Frag {
+    u32x4 a[MI], b[NJ];
   };
-  issue(s0);
-  issue(s1);
-  issue(s2);
-  // step k: its stage has arrived (this wave's loads, then by the barrier the
-  // others'), and everyone has read the stage before it, which is refilled
-  auto step = [&](uint4* cur, uint4* old) {
+  struct Scale {
+    int a[MI], b[NJ];
+  };
+  // byte offsets of a lane's fragments and scales in a stage; taken anew at
+  // each read, or the compiler keeps one for each stage
+  uint32_t la = (wm * MI * 32 + c) * 64 + (h ^ (c >> 2 & 3)) * 16, lb = T::kB * 16 + (wn * NJ * 32 + c) * 64 + (h ^ (c >> 2 & 3)) * 16;
+  uint32_t lsa = T::kS * 16 + (wm * MI * 32 + c) * 4, lsb = T::kS * 16 + (T::BM + wn * NJ * 32 + c) * 4;
+  auto rd = [&](const uint4* st, uint32_t ks, Frag& f) {
+    asm volatile("" : "+v"(la), "+v"(lb));
+    const uint8_t* const p = reinterpret_cast<const uint8_t*>(st);
+#pragma unroll
+    for (int i = 0; i < MI; ++i) f.a[i] = *reinterpret_cast<const u32x4*>(p + (la ^ (ks * 32)) + i * 2048);
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) f.b[j] = *reinterpret_cast<const u32x4*>(p + (lb ^ (ks * 32)) + j * 2048);
+  };
+  auto rd_scale = [&](const uint4* st, Scale& sc) {
+    asm volatile("" : "+v"(lsa), "+v"(lsb));
+    const uint8_t* const p = reinterpret_cast<const uint8_t*>(st);
+#pragma unroll
+    for (int i = 0; i < MI; ++i) sc.a[i] = *reinterpret_cast<const int*>(p + lsa + i * 128);
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) sc.b[j] = *reinterpret_cast<const int*>(p + lsb + j * 128);
+  };
+  // the scales that this half of the wave takes, to bytes 0 and 2
+  auto own_scale = [&](const Scale& raw, Scale& sc) {
+#pragma unroll
+    for (int i = 0; i < MI; ++i) sc.a[i] = static_cast<int>(static_cast<uint32_t>(raw.a[i]) >> (8 * h));
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) sc.b[j] = static_cast<int>(static_cast<uint32_t>(raw.b[j]) >> (8 * h));
+  };
+  f32x16 acc[MI][NJ];
+  auto mma = [&](auto KS, const Frag& f, const Scale& sc) {
+#pragma unroll
+    for (int i = 0; i < MI; ++i)
+#pragma unroll
+      for (int j = 0; j < NJ; ++j)
+        acc[i][j] = mx_mma<decltype(KS)::value>(f.a[i], f.b[j], acc[i][j], sc.a[i], sc.b[j]);
+  };
+  // The accumulators exist here: a half step's instructions, which touch no
+  // memory, would else be moved past the barriers to where they are stored.
+  auto pin = [&]() {
+#pragma unroll
+    for (int i = 0; i < MI; ++i)
+#pragma unroll
+      for (int j = 0; j < NJ; ++j) asm volatile("" : "+v"(acc[i][j]));
+  };
+  using I0 = std::integral_constant<int, 0>;
+  using I1 = std::integral_constant<int, 1>;
+  auto clear = [&]() {
+#pragma unroll
+    for (int i = 0; i < MI; ++i)
+#pragma unroll
+      for (int j = 0; j < NJ; ++j) acc[i][j] = f32x16{};
+  };
+  auto store = [&](uint32_t tile) {
+    using O = std::conditional_t<DT == PROFK_F32, float, __bf16>;
+    const uint32_t m = tile % tiles_m * T::BM + wm * MI * 32 + 4 * h, n = tile / tiles_m * T::BN + wn * NJ * 32 + NJ * c;
+    if (n >= g.N) return;
+    O* p = static_cast<O*>(g.out) + static_cast<size_t>(m) * g.N + n;
+    const bool whole = n + NJ <= g.N;
+#pragma unroll
+    for (int i = 0; i < MI; ++i) {
+      // (no row's address or mask is kept through the steps)
+      asm volatile("" : "+v"(p));
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int v = 0; v < 16; ++v) {
+        const uint32_t r = i * 32 + 8 * (v / 4) + (v % 4);
+        if (m + r >= g.M) continue;
+        O* const o = p + static_cast<size_t>(r) * g.N;
+        if (whole) {
+          if constexpr (DT == PROFK_F32)
+            *reinterpret_cast<f32x4u*>(o) = f32x4{acc[i][0][v], acc[i][1][v], acc[i][2][v], acc[i][3][v]};
+          else
+            *reinterpret_cast<u32x2u*>(o) = u32x2u{pack_bf16(acc[i][0][v], acc[i][1][v]), pack_bf16(acc[i][2][v], acc[i][3][v])};
+        } else {
+          o[0] = static_cast<O>(acc[i][0][v]);
+          if (n + 1 < g.N) o[1] = static_cast<O>(acc[i][1][v]);
+          if (n + 2 < g.N) o[2] = static_cast<O>(acc[i][2][v]);
+        }
+      }
+    }
+  };
+  start(tile0);
+  issue(s0, std::false_type{});
+  issue(s1, std::false_type{});
+  issue(s2, std::false_type{});
+  issue(s3, std::true_type{});
+  Frag f0, f1;
+  Scale sc, raw;
+  wait_loads_lds<3 * T::kLoads>();
+  bare_barrier();
+  rd_scale(s0, raw);
+  rd(s0, 0, f0);
+  // LDS reads between the matrix instructions of a half step, from the second
+  // on: the first one waits for the reads before
+  auto weave = [&](auto reads) {
+    constexpr int R = decltype(reads)::value, M = MI * NJ, per = (R + M - 2) / (M - 1);
+#pragma unroll
+    for (int i = 0; i < M; ++i) {
+      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(0x100, per, 0);
+    }
+  };
+  // One step; its first half's fragments are in f0.
+  auto step = [&](uint4* cur, uint4* nxt, bool real, auto fourth) {
+    __builtin_amdgcn_sched_barrier(0);
+    own_scale(raw, sc);
+    rd(cur, 1, f1);
+    if (real) mma(I0{}, f0, sc);
+    pin();
+    weave(std::integral_constant<int, MI + NJ>{});
+    __builtin_amdgcn_sched_barrier(0);
+    // this wave has read its stage and its loads of the next have arrived;
+    // by the barrier, so have the others
     wait_loads_lds<2 * T::kLoads>();
     bare_barrier();
-    issue(old);
-    compute(cur);
+    issue(cur, fourth);
+    rd_scale(nxt, raw);
+    rd(nxt, 0, f0);
+    if (real) mma(I1{}, f1, sc);
+    pin();
+    weave(std::integral_constant<int, 2 * (MI + NJ)>{});
+    __builtin_amdgcn_sched_barrier(0);
   };
-  uint32_t k = 0;
-  for (; k + 4 <= g.steps; k += 4) {
-    step(s0, s3);
-    step(s1, s0);
-    step(s2, s1);
-    step(s3, s2);
-  }
-  if (k < g.steps) step(s0, s3);
-  if (k + 1 < g.steps) step(s1, s0);
-  if (k + 2 < g.steps) step(s2, s1);
-  wait_loads_lds<0>();   // (no load may reach LDS after the workgroup's end)
-#pragma unroll
-  for (int i = 0; i < MI; ++i)
-#pragma unroll
-    for (int v = 0; v < 16; ++v) {
-      const uint32_t r = m0 + wm * MI * 32 + i * 32 + 8 * (v / 4) + 4 * h + (v % 4), n = n0 + wn * NJ * 32 + NJ * c;
-      if (r < g.M) mx_store4<DT>(g.out, r, n, g.N, f32x4{acc[i][0][v], acc[i][1][v], acc[i][2][v], acc[i][3][v]});
+  for (uint32_t tile = tile0; tile < end; tile += per_xcd) {
+    clear();
+    for (uint32_t k = 0; k < slots; k += 4) {
+      step(s0, s1, true, std::false_type{});
+      step(s1, s2, WHOLE || k + 1 < g.steps, std::false_type{});
+      step(s2, s3, WHOLE || k + 2 < g.steps, std::false_type{});
+      step(s3, s0, WHOLE || k + 3 < g.steps, std::true_type{});
     }
+    store(tile);
+  }
+  wait_loads_lds<0>();   // (no load may reach LDS after the workgroup's end)
 }
 
-template <int DT, int WM, int WN, int MI, int NJ>
-__global__ __launch_bounds__(WM * WN * 64, 2) void k_mx_gemm(MxGemmArgs g, uint32_t tiles_m, uint32_t tiles, uint32_t per) {
-  mx_gemm_body<DT, WM, WN, MI, NJ>(g, tiles_m, tiles, per);
+template <int DT, int WM, int WN, int MI, int NJ, int WAVES, bool WHOLE>
+__global__ __launch_bounds__(WM * WN * 64, WAVES) void k_mx_gemm(MxGemmArgs g, uint32_t tiles_m, uint32_t tiles) {
+  mx_gemm_body<DT, WM, WN, MI, NJ, WHOLE>(g, tiles_m, tiles);
 }
 
 // The product of few rows (M <= 32), bound by reading b once.  A wave takes
@@ -551,11 +640,15 @@ template <int DT, int XDT, bool KSPLIT, int LDS> __global__ __launch_bounds__(kM
   mx_few_body<DT, XDT, KSPLIT, LDS>(g);
 }
 
-template <int DT, int WM, int WN, int MI, int NJ> void launch_gemm(const MxGemmArgs& g, hipStream_t s) {
+// PER: workgroups a CU holds.
+template <int DT, int WM, int WN, int MI, int NJ, int PER> void launch_gemm(const MxGemmArgs& g, uint32_t cus, hipStream_t s) {
   using T = MxTile<WM, WN, MI, NJ>;
-  const uint32_t tm = (g.M + T::BM - 1) / T::BM, tn = (g.N + T::BN - 1) / T::BN;
-  const uint32_t tiles = tm * tn, per = (tiles + kXcds - 1) / kXcds;
-  k_mx_gemm<DT, WM, WN, MI, NJ><<<per * kXcds, T::BS, 0, s>>>(g, tm, tiles, per);
+  const uint32_t tm = (g.M + T::BM - 1) / T::BM, tn = (g.N + T::BN - 1) / T::BN, tiles = tm * tn;
+  uint32_t grid = (tiles + kXcds - 1) / kXcds * kXcds;
+  if (grid > PER * cus) grid = PER * cus / kXcds * kXcds;
+  constexpr int kWaves = PER * WM * WN / 4;
+  if (g.steps % 4 == 0) k_mx_gemm<DT, WM, WN, MI, NJ, kWaves, true><<<grid, T::BS, 0, s>>>(g, tm, tiles);
+  else k_mx_gemm<DT, WM, WN, MI, NJ, kWaves, false><<<grid, T::BS, 0, s>>>(g, tm, tiles);
 }
 
 template <int DT, int XDT, int LDS> void launch_few(const MxGemmArgs& g, uint32_t cus, uint32_t per_cu, hipStream_t s) {
@@ -578,8 +671,8 @@ template <int DT> void launch_product(const MxGemmArgs& g, int x_dtype, uint32_t
     return;
   }
   const uint64_t big = static_cast<uint64_t>((g.M + 255) / 256) * ((g.N + 255) / 256);
-  if (g.M > 128 && big >= 128) launch_gemm<DT, 4, 2, 2, 4>(g, s);
-  else launch_gemm<DT, 4, 1, 1, 4>(g, s);
+  if (g.M > 128 && big >= 128) launch_gemm<DT, 4, 2, 2, 4, 1>(g, cus, s);
+  else launch_gemm<DT, 4, 1, 1, 4, 2>(g, cus, s);
 }
 
 }  // namespace
