@@ -228,39 +228,38 @@ __device__ __forceinline__ void bare_barrier() {
 }
 
 // The tiled product.  A workgroup of WM x WN waves computes tiles of BM x BN
-// outputs, a wave MI x NJ accumulators of 32 x 32.  A step (128 values of K)
-// of a tile is 64 bytes of codes a row and a word of four scales, loaded
-// straight to LDS, four stages deep; every wait is for the oldest stage, so
-// that the others stay in flight, and the loads run on into the workgroup's
-// next tile.  Fragments are read one half step ahead, under the matrix
-// instructions of the half before.  16-byte granule g of a row r is at
-// position g ^ (r / 4 % 4) of its four: sixteen neighbouring rows' granules
-// g then cover all 64 banks once.
+// outputs, a wave MI x NJ accumulators of 32 x 32.  A stage, two steps (256
+// values of K), is 128 bytes of codes a row, whole lines, and two words of
+// four scales, loaded straight to LDS; there are two, and one is filled, on
+// into the workgroup's next tile, while the other is multiplied.  Fragments
+// are read half a step ahead, under the matrix instructions of the half
+// before.  16-byte granule g of a row r is at position g ^ (r / 2 % 8) of its
+// eight: sixteen neighbouring rows' granules g then cover all 64 banks once.
 //
 // Output column n of a wave's slab is in fragment n % NJ, lane n / NJ (the
-// LDS rows of b are in that order), so that a lane's NJ results of a row are
+// codes of b are in LDS in that order), so that a lane's NJ results of a row are
 // neighbours and are stored together.
 //
 // Rows past M or N are read as the last one and not stored.
 template <int WM, int WN, int MI, int NJ> struct MxTile {
-  static constexpr int BS = WM * WN * kWave, BM = WM * MI * 32, BN = WN * NJ * 32;
-  static constexpr int QA = BM * 4 / BS, QB = BN * 4 / BS, QS = (BM + BN) / BS;   // loads of a lane
-  static constexpr int kLoads = QA + QB + QS;
-  static constexpr int kB = BM * 4, kS = (BM + BN) * 4;        // first granule of b, of the scales
-  static constexpr int kGran = kS + (BM + BN) / 4;             // granules of a stage
-  static_assert(BM * 4 % BS == 0 && BN * 4 % BS == 0 && (BM + BN) % BS == 0, "whole loads");
-  static_assert(BM % kWave == 0, "scale loads of one matrix a wave");
+  static constexpr int NW = WM * WN, BS = NW * kWave, BM = WM * MI * 32, BN = WN * NJ * 32;
+  static constexpr int QA = BM * 8 / BS, QB = BN * 8 / BS;     // loads of a lane: codes
+  static constexpr int QS = (BM + BN) / 32 / NW;               // ... scales, 32 rows and two steps each
+  static constexpr int kB = BM * 8, kS = (BM + BN) * 8;        // first granule of b, of the scales
+  static constexpr int kGran = kS + (BM + BN) / 2;             // granules of a stage
+  static_assert(BM * 8 % BS == 0 && BN * 8 % BS == 0 && (BM + BN) / 32 % NW == 0, "whole loads");
   static_assert(NJ == 4, "four neighbouring results a lane");
 };
 
-// WHOLE: the steps are a multiple of four, so that no stage is skipped and the
-// reads and the matrix instructions of a half step are one run of code.
+// WHOLE: the steps are a multiple of four, so that no part of a stage is
+// skipped and the reads and the matrix instructions of a half step are one run
+// of code.
 template <int DT, int WM, int WN, int MI, int NJ, bool WHOLE>
 __device__ __forceinline__ void mx_gemm_body(const MxGemmArgs& g, uint32_t tiles_m, uint32_t tiles) {
   using T = MxTile<WM, WN, MI, NJ>;
   // distinct arrays, so that the compiler can tell the stage being read from
-  // those being filled
-  __shared__ __align__(16) uint4 s0[T::kGran], s1[T::kGran], s2[T::kGran], s3[T::kGran];
+  // the one being filled
+  __shared__ __align__(16) uint4 s0[T::kGran], s1[T::kGran];
   // workgroup b runs on XCD b % 8: each XCD takes a run of tiles, the row
   // tiles of a column tile one after the other, so that its L2 holds what
   // they share
@@ -268,17 +267,18 @@ __device__ __forceinline__ void mx_gemm_body(const MxGemmArgs& g, uint32_t tiles
   const uint32_t end = static_cast<uint32_t>(static_cast<uint64_t>(tiles) * (xcd + 1) / kXcds);
   const uint32_t tile0 = static_cast<uint32_t>(static_cast<uint64_t>(tiles) * xcd / kXcds) + blockIdx.x / kXcds;
   if (tile0 >= end) return;
-  // a tile takes a multiple of four stages, so that each starts at the same
-  // one; those past its last step are not multiplied
-  const uint32_t slots = WHOLE ? g.steps : (g.steps + 3) / 4 * 4;
+  // a tile takes an even number of stages, so that each starts at the same
+  // one; what is past its last step is not multiplied
+  const uint32_t stages = WHOLE ? g.steps / 2 : (g.steps + 3) / 4 * 2;
   const uint32_t tid = threadIdx.x, lane = tid & (kWave - 1);
   const uint32_t w = __builtin_amdgcn_readfirstlane(tid / kWave);
   const uint32_t c = lane & 31, h = lane >> 5, wm = w / WN, wn = w % WN;
   const uint32_t cb = g.steps * 64;
 
   auto col_of = [](uint32_t r) { return r / (NJ * 32) * (NJ * 32) + r % 32 * NJ + r % (NJ * 32) / 32; };
-  // The step to load next: a lane's offsets from the first row of its tile
-  // (within 256 rows of at most 2^19 bytes), to which a step adds.
+  // The stage to load next: a lane's offsets from the first row of its tile
+  // (within 256 rows of at most 2^19 bytes), to which a stage adds.
+  auto gran = [&](uint32_t q) { return (lane & 7) ^ ((q * 8 + lane / 8) >> 1 & 7); };   // granule of load q
   const uint8_t *base_a, *base_b, *base_s[T::QS];
   uint32_t oa[T::QA], ob[T::QB], os[T::QS];
   auto start = [&](uint32_t tile) {
@@ -288,49 +288,48 @@ __device__ __forceinline__ void mx_gemm_body(const MxGemmArgs& g, uint32_t tiles
     base_b = g.b + static_cast<size_t>(n0) * cb;
 #pragma unroll
     for (int q = 0; q < T::QA; ++q) {
-      const uint32_t p = (w * T::QA + q) * kWave + lane, r = p / 4, gr = (p & 3) ^ (r >> 2 & 3);
-      oa[q] = min(r, last_m) * cb + gr * 16;
+      oa[q] = min((w * T::QA + q) * 8 + lane / 8, last_m) * cb + gran(w * T::QA + q) * 16;
     }
 #pragma unroll
     for (int q = 0; q < T::QB; ++q) {
-      const uint32_t p = (w * T::QB + q) * kWave + lane, r = p / 4, gr = (p & 3) ^ (r >> 2 & 3);
-      ob[q] = min(col_of(r), last_n) * cb + gr * 16;
+      ob[q] = min(col_of((w * T::QB + q) * 8 + lane / 8), last_n) * cb + gran(w * T::QB + q) * 16;
     }
-    // (a wave's scale loads are all of a or all of b; rows past the last group
-    // read the last one)
+    // (groups past the last one read the last one)
 #pragma unroll
     for (int q = 0; q < T::QS; ++q) {
-      const uint32_t r0 = (w * T::QS + q) * kWave, r = r0 + lane;
-      const bool of_a = r0 < T::BM;
-      base_s[q] = of_a ? g.as + static_cast<size_t>(m0) * (cb / 16) : g.bs + static_cast<size_t>(n0) * (cb / 16);
-      const uint32_t row = of_a ? r : col_of(r - T::BM), last = of_a ? last_m : last_n;
-      os[q] = (min(row / 32, last / 32) * g.steps * 32 + row % 32) * 4;
+      const uint32_t gr = w * T::QS + q;
+      const bool of_a = gr < T::BM / 32;
+      const uint32_t first = of_a ? m0 / 32 + min(gr, last_m / 32) : n0 / 32 + min(gr - T::BM / 32, last_n / 32);
+      base_s[q] = (of_a ? g.as : g.bs) + static_cast<size_t>(first) * g.steps * 128;
+      os[q] = lane * 4;
     }
   };
   uint32_t next_k = 0, next_tile = tile0;
-  // (past a tile's last step, and the last tile: the last again; a tile's
-  // stages end with the fourth)
-  auto issue = [&](uint4* st, auto fourth) {
+  // (past a tile's last stage, and the last tile: the last again; a tile's
+  // stages end with the second)
+  auto issue = [&](uint4* st, auto second) {
+    // the last of an odd number of steps: its granules and scales twice
+    const bool half = !WHOLE && 2 * next_k + 1 >= g.steps;
 #pragma unroll
     for (int q = 0; q < T::QA; ++q)
-      __builtin_amdgcn_global_load_lds(reinterpret_cast<const uint32_t*>(base_a + oa[q]), st + (w * T::QA + q) * kWave,
-                                       16, 0, 0);
+      __builtin_amdgcn_global_load_lds(reinterpret_cast<const uint32_t*>(base_a + oa[q] - (half ? (gran(w * T::QA + q) & 4) * 16 : 0u)),
+                                       st + (w * T::QA + q) * kWave, 16, 0, 0);
 #pragma unroll
     for (int q = 0; q < T::QB; ++q)
-      __builtin_amdgcn_global_load_lds(reinterpret_cast<const uint32_t*>(base_b + ob[q]),
+      __builtin_amdgcn_global_load_lds(reinterpret_cast<const uint32_t*>(base_b + ob[q] - (half ? (gran(w * T::QB + q) & 4) * 16 : 0u)),
                                        st + T::kB + (w * T::QB + q) * kWave, 16, 0, 0);
 #pragma unroll
     for (int q = 0; q < T::QS; ++q)
-      __builtin_amdgcn_global_load_lds(reinterpret_cast<const uint32_t*>(base_s[q] + os[q]),
+      __builtin_amdgcn_global_load_lds(reinterpret_cast<const uint32_t*>(base_s[q] + (half ? os[q] & 127u : os[q])),
                                        st + T::kS + (w * T::QS + q) * (kWave / 4), 4, 0, 0);
     ++next_k;
-    if (next_k < g.steps) {
-      base_a += 64;
-      base_b += 64;
+    if (2 * next_k < g.steps) {
+      base_a += 128;
+      base_b += 128;
 #pragma unroll
-      for (int q = 0; q < T::QS; ++q) base_s[q] += 128;
+      for (int q = 0; q < T::QS; ++q) base_s[q] += 256;
     }
-    if (decltype(fourth)::value && next_k == slots && next_tile + per_xcd < end) {
+    if (decltype(second)::value && next_k == stages && next_tile + per_xcd < end) {
       next_k = 0;
       next_tile += per_xcd;
       start(next_tile);
@@ -343,24 +342,28 @@ __device__ __forceinline__ void mx_gemm_body(const MxGemmArgs& g, uint32_t tiles
     int a[MI], b[NJ];
   };
   // byte offsets of a lane's fragments and scales in a stage; taken anew at
-  // each read, or the compiler keeps one for each stage
-  uint32_t la = (wm * MI * 32 + c) * 64 + (h ^ (c >> 2 & 3)) * 16, lb = T::kB * 16 + (wn * NJ * 32 + c) * 64 + (h ^ (c >> 2 & 3)) * 16;
-  uint32_t lsa = T::kS * 16 + (wm * MI * 32 + c) * 4, lsb = T::kS * 16 + (T::BM + wn * NJ * 32 + c) * 4;
-  auto rd = [&](const uint4* st, uint32_t ks, Frag& f) {
+  // each read, or the compiler keeps one for each
+  const uint32_t sw = (h ^ (c >> 1 & 7)) * 16;
+  uint32_t la = (wm * MI * 32 + c) * 128 + sw, lb = T::kB * 16 + (wn * NJ * 32 + c) * 128 + sw;
+  uint32_t lsa = T::kS * 16 + (wm * MI * 64 + c) * 4;
+  uint32_t lsb = T::kS * 16 + (T::BM * 2 + (wn * NJ + c / 8) * 64 + (NJ * c & 31)) * 4;
+  auto rd = [&](const uint4* st, uint32_t q, Frag& f) {   // half step q of a stage
     asm volatile("" : "+v"(la), "+v"(lb));
     const uint8_t* const p = reinterpret_cast<const uint8_t*>(st);
 #pragma unroll
-    for (int i = 0; i < MI; ++i) f.a[i] = *reinterpret_cast<const u32x4*>(p + (la ^ (ks * 32)) + i * 2048);
+    for (int i = 0; i < MI; ++i) f.a[i] = *reinterpret_cast<const u32x4*>(p + (la ^ (q * 32)) + i * 4096);
 #pragma unroll
-    for (int j = 0; j < NJ; ++j) f.b[j] = *reinterpret_cast<const u32x4*>(p + (lb ^ (ks * 32)) + j * 2048);
+    for (int j = 0; j < NJ; ++j) f.b[j] = *reinterpret_cast<const u32x4*>(p + (lb ^ (q * 32)) + j * 4096);
   };
-  auto rd_scale = [&](const uint4* st, Scale& sc) {
+  auto rd_scale = [&](const uint4* st, uint32_t t, Scale& sc) {   // step t of a stage
     asm volatile("" : "+v"(lsa), "+v"(lsb));
-    const uint8_t* const p = reinterpret_cast<const uint8_t*>(st);
+    const uint8_t* const p = reinterpret_cast<const uint8_t*>(st) + t * 128;
 #pragma unroll
-    for (int i = 0; i < MI; ++i) sc.a[i] = *reinterpret_cast<const int*>(p + lsa + i * 128);
+    for (int i = 0; i < MI; ++i) sc.a[i] = *reinterpret_cast<const int*>(p + lsa + i * 256);
+    // (b's scales are in the order of its rows: a lane's are neighbours)
+    const u32x4 b = *reinterpret_cast<const u32x4*>(p + lsb);
 #pragma unroll
-    for (int j = 0; j < NJ; ++j) sc.b[j] = *reinterpret_cast<const int*>(p + lsb + j * 128);
+    for (int j = 0; j < NJ; ++j) sc.b[j] = static_cast<int>(b[j]);
   };
   // the scales that this half of the wave takes, to bytes 0 and 2
   auto own_scale = [&](const Scale& raw, Scale& sc) {
@@ -385,8 +388,22 @@ __device__ __forceinline__ void mx_gemm_body(const MxGemmArgs& g, uint32_t tiles
 #pragma unroll
       for (int j = 0; j < NJ; ++j) asm volatile("" : "+v"(acc[i][j]));
   };
+  // LDS reads between the matrix instructions of a half step, from the second
+  // on: the first one waits for the reads before
+  auto weave = [&](auto reads) {
+    constexpr int R = decltype(reads)::value, M = MI * NJ, per = (R + M - 2) / (M - 1);
+    pin();
+#pragma unroll
+    for (int i = 0; i < M; ++i) {
+      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(0x100, per, 0);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+  };
   using I0 = std::integral_constant<int, 0>;
   using I1 = std::integral_constant<int, 1>;
+  using Reads = std::integral_constant<int, MI + NJ>;
+  using ReadsScale = std::integral_constant<int, 2 * MI + NJ + 1>;
   auto clear = [&]() {
 #pragma unroll
     for (int i = 0; i < MI; ++i)
@@ -424,53 +441,45 @@ __device__ __forceinline__ void mx_gemm_body(const MxGemmArgs& g, uint32_t tiles
   };
   start(tile0);
   issue(s0, std::false_type{});
-  issue(s1, std::false_type{});
-  issue(s2, std::false_type{});
-  issue(s3, std::true_type{});
+  issue(s1, std::true_type{});
   Frag f0, f1;
   Scale sc, raw;
-  wait_loads_lds<3 * T::kLoads>();
+  wait_loads_lds<T::QA + T::QB + T::QS>();
   bare_barrier();
-  rd_scale(s0, raw);
+  rd_scale(s0, 0, raw);
   rd(s0, 0, f0);
-  // LDS reads between the matrix instructions of a half step, from the second
-  // on: the first one waits for the reads before
-  auto weave = [&](auto reads) {
-    constexpr int R = decltype(reads)::value, M = MI * NJ, per = (R + M - 2) / (M - 1);
-#pragma unroll
-    for (int i = 0; i < M; ++i) {
-      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-      __builtin_amdgcn_sched_group_barrier(0x100, per, 0);
-    }
-  };
-  // One step; its first half's fragments are in f0.
-  auto step = [&](uint4* cur, uint4* nxt, bool real, auto fourth) {
+  // One stage; its first half step's fragments are in f0, its first step's
+  // scales in raw.
+  auto stage = [&](uint4* cur, uint4* nxt, uint32_t k, auto second) {
+    const bool one = WHOLE || 2 * k < g.steps, two = WHOLE || 2 * k + 1 < g.steps;
     __builtin_amdgcn_sched_barrier(0);
     own_scale(raw, sc);
     rd(cur, 1, f1);
-    if (real) mma(I0{}, f0, sc);
-    pin();
-    weave(std::integral_constant<int, MI + NJ>{});
-    __builtin_amdgcn_sched_barrier(0);
-    // this wave has read its stage and its loads of the next have arrived;
-    // by the barrier, so have the others
-    wait_loads_lds<2 * T::kLoads>();
+    if (one) mma(I0{}, f0, sc);
+    weave(Reads{});
+    rd_scale(cur, 1, raw);
+    rd(cur, 2, f0);
+    if (one) mma(I1{}, f1, sc);
+    weave(ReadsScale{});
+    own_scale(raw, sc);
+    rd(cur, 3, f1);
+    if (two) mma(I0{}, f0, sc);
+    weave(Reads{});
+    // this wave has read its stage and its loads of the next have arrived; by
+    // the barrier, so have the others
+    wait_loads_lds<0>();
     bare_barrier();
-    issue(cur, fourth);
-    rd_scale(nxt, raw);
+    issue(cur, second);
+    rd_scale(nxt, 0, raw);
     rd(nxt, 0, f0);
-    if (real) mma(I1{}, f1, sc);
-    pin();
-    weave(std::integral_constant<int, 2 * (MI + NJ)>{});
-    __builtin_amdgcn_sched_barrier(0);
+    if (two) mma(I1{}, f1, sc);
+    weave(ReadsScale{});
   };
   for (uint32_t tile = tile0; tile < end; tile += per_xcd) {
     clear();
-    for (uint32_t k = 0; k < slots; k += 4) {
-      step(s0, s1, true, std::false_type{});
-      step(s1, s2, WHOLE || k + 1 < g.steps, std::false_type{});
-      step(s2, s3, WHOLE || k + 2 < g.steps, std::false_type{});
-      step(s3, s0, WHOLE || k + 3 < g.steps, std::true_type{});
+    for (uint32_t k = 0; k < stages; k += 2) {
+      stage(s0, s1, k, std::false_type{});
+      stage(s1, s0, k + 1, std::true_type{});
     }
     store(tile);
   }
