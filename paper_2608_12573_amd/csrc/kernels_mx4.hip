@@ -305,19 +305,27 @@ __device__ __forceinline__ void mx_gemm_body(const MxGemmArgs& g, uint32_t tiles
     }
   };
   uint32_t next_k = 0, next_tile = tile0;
-  // (past a tile's last stage, and the last tile: the last again; a tile's
-  // stages end with the second)
-  auto issue = [&](uint4* st, auto second) {
+  // (past a tile's last stage, and the last tile: the last again; the stages of
+  // a tile end with an odd one)
+  auto issue_a = [&](uint4* st) {
     // the last of an odd number of steps: its granules and scales twice
     const bool half = !WHOLE && 2 * next_k + 1 >= g.steps;
 #pragma unroll
     for (int q = 0; q < T::QA; ++q)
-      __builtin_amdgcn_global_load_lds(reinterpret_cast<const uint32_t*>(base_a + oa[q] - (half ? (gran(w * T::QA + q) & 4) * 16 : 0u)),
-                                       st + (w * T::QA + q) * kWave, 16, 0, 0);
+      __builtin_amdgcn_global_load_lds(
+          reinterpret_cast<const uint32_t*>(base_a + oa[q] - (half ? (gran(w * T::QA + q) & 4) * 16 : 0u)),
+          st + (w * T::QA + q) * kWave, 16, 0, 0);
+  };
+  auto issue_b = [&](uint4* st) {
+    const bool half = !WHOLE && 2 * next_k + 1 >= g.steps;
 #pragma unroll
     for (int q = 0; q < T::QB; ++q)
-      __builtin_amdgcn_global_load_lds(reinterpret_cast<const uint32_t*>(base_b + ob[q] - (half ? (gran(w * T::QB + q) & 4) * 16 : 0u)),
-                                       st + T::kB + (w * T::QB + q) * kWave, 16, 0, 0);
+      __builtin_amdgcn_global_load_lds(
+          reinterpret_cast<const uint32_t*>(base_b + ob[q] - (half ? (gran(w * T::QB + q) & 4) * 16 : 0u)),
+          st + T::kB + (w * T::QB + q) * kWave, 16, 0, 0);
+  };
+  auto issue_s = [&](uint4* st, auto odd) {
+    const bool half = !WHOLE && 2 * next_k + 1 >= g.steps;
 #pragma unroll
     for (int q = 0; q < T::QS; ++q)
       __builtin_amdgcn_global_load_lds(reinterpret_cast<const uint32_t*>(base_s[q] + (half ? os[q] & 127u : os[q])),
@@ -329,7 +337,7 @@ __device__ __forceinline__ void mx_gemm_body(const MxGemmArgs& g, uint32_t tiles
 #pragma unroll
       for (int q = 0; q < T::QS; ++q) base_s[q] += 256;
     }
-    if (decltype(second)::value && next_k == stages && next_tile + per_xcd < end) {
+    if (decltype(odd)::value && next_k == stages && next_tile + per_xcd < end) {
       next_k = 0;
       next_tile += per_xcd;
       start(next_tile);
@@ -388,8 +396,9 @@ __device__ __forceinline__ void mx_gemm_body(const MxGemmArgs& g, uint32_t tiles
 #pragma unroll
       for (int j = 0; j < NJ; ++j) asm volatile("" : "+v"(acc[i][j]));
   };
-  // LDS reads between the matrix instructions of a half step, from the second
-  // on: the first one waits for the reads before
+  // LDS reads and loads between the matrix instructions of a half step: the
+  // first one waits for the reads before, and loads issued one after the other
+  // keep the wave from its matrix instructions while they are taken
   auto weave = [&](auto reads) {
     constexpr int R = decltype(reads)::value, M = MI * NJ, per = (R + M - 2) / (M - 1);
     pin();
@@ -397,6 +406,7 @@ __device__ __forceinline__ void mx_gemm_body(const MxGemmArgs& g, uint32_t tiles
     for (int i = 0; i < M; ++i) {
       __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
       __builtin_amdgcn_sched_group_barrier(0x100, per, 0);
+      __builtin_amdgcn_sched_group_barrier(0x010, 1, 0);
     }
     __builtin_amdgcn_sched_barrier(0);
   };
@@ -440,23 +450,27 @@ __device__ __forceinline__ void mx_gemm_body(const MxGemmArgs& g, uint32_t tiles
     }
   };
   start(tile0);
-  issue(s0, std::false_type{});
-  issue(s1, std::true_type{});
+  issue_a(s0);
+  issue_b(s0);
+  issue_s(s0, std::false_type{});
+  issue_a(s1);
   Frag f0, f1;
   Scale sc, raw;
-  wait_loads_lds<T::QA + T::QB + T::QS>();
+  wait_loads_lds<T::QA>();
   bare_barrier();
   rd_scale(s0, 0, raw);
   rd(s0, 0, f0);
   // One stage; its first half step's fragments are in f0, its first step's
-  // scales in raw.
-  auto stage = [&](uint4* cur, uint4* nxt, uint32_t k, auto second) {
+  // scales in raw, and the loads of a for the next have been issued.
+  auto stage = [&](uint4* cur, uint4* nxt, uint32_t k, auto last) {
     const bool one = WHOLE || 2 * k < g.steps, two = WHOLE || 2 * k + 1 < g.steps;
     __builtin_amdgcn_sched_barrier(0);
     own_scale(raw, sc);
+    issue_b(nxt);
     rd(cur, 1, f1);
     if (one) mma(I0{}, f0, sc);
     weave(Reads{});
+    issue_s(nxt, last);
     rd_scale(cur, 1, raw);
     rd(cur, 2, f0);
     if (one) mma(I1{}, f1, sc);
@@ -469,7 +483,7 @@ __device__ __forceinline__ void mx_gemm_body(const MxGemmArgs& g, uint32_t tiles
     // the barrier, so have the others
     wait_loads_lds<0>();
     bare_barrier();
-    issue(cur, second);
+    issue_a(cur);
     rd_scale(nxt, 0, raw);
     rd(nxt, 0, f0);
     if (two) mma(I1{}, f1, sc);
@@ -478,8 +492,8 @@ __device__ __forceinline__ void mx_gemm_body(const MxGemmArgs& g, uint32_t tiles
   for (uint32_t tile = tile0; tile < end; tile += per_xcd) {
     clear();
     for (uint32_t k = 0; k < stages; k += 2) {
-      stage(s0, s1, k, std::false_type{});
-      stage(s1, s0, k + 1, std::true_type{});
+      stage(s0, s1, k, std::true_type{});     // (loads the tile's next odd stage)
+      stage(s1, s0, k + 1, std::false_type{});
     }
     store(tile);
   }
