@@ -305,8 +305,7 @@ __device__ __forceinline__ void mx_gemm_body(const MxGemmArgs& g, uint32_t tiles
     }
   };
   uint32_t next_k = 0, next_tile = tile0;
-  // (past a tile's last stage, and the last tile: the last again; the stages of
-  // a tile end with an odd one)
+  // (past a tile's last step, and the last tile: the last again)
   auto issue_a = [&](uint4* st) {
     // the last of an odd number of steps: its granules and scales twice
     const bool half = !WHOLE && 2 * next_k + 1 >= g.steps;
@@ -324,7 +323,7 @@ __device__ __forceinline__ void mx_gemm_body(const MxGemmArgs& g, uint32_t tiles
           reinterpret_cast<const uint32_t*>(base_b + ob[q] - (half ? (gran(w * T::QB + q) & 4) * 16 : 0u)),
           st + T::kB + (w * T::QB + q) * kWave, 16, 0, 0);
   };
-  auto issue_s = [&](uint4* st, auto odd) {
+  auto issue_s = [&](uint4* st) {
     const bool half = !WHOLE && 2 * next_k + 1 >= g.steps;
 #pragma unroll
     for (int q = 0; q < T::QS; ++q)
@@ -337,7 +336,10 @@ __device__ __forceinline__ void mx_gemm_body(const MxGemmArgs& g, uint32_t tiles
 #pragma unroll
       for (int q = 0; q < T::QS; ++q) base_s[q] += 256;
     }
-    if (decltype(odd)::value && next_k == stages && next_tile + per_xcd < end) {
+  };
+  // after a tile's last stage
+  auto turn = [&]() {
+    if (next_k == stages && next_tile + per_xcd < end) {
       next_k = 0;
       next_tile += per_xcd;
       start(next_tile);
@@ -452,7 +454,7 @@ __device__ __forceinline__ void mx_gemm_body(const MxGemmArgs& g, uint32_t tiles
   start(tile0);
   issue_a(s0);
   issue_b(s0);
-  issue_s(s0, std::false_type{});
+  issue_s(s0);
   issue_a(s1);
   Frag f0, f1;
   Scale sc, raw;
@@ -470,11 +472,12 @@ __device__ __forceinline__ void mx_gemm_body(const MxGemmArgs& g, uint32_t tiles
     rd(cur, 1, f1);
     if (one) mma(I0{}, f0, sc);
     weave(Reads{});
-    issue_s(nxt, last);
+    issue_s(nxt);
     rd_scale(cur, 1, raw);
     rd(cur, 2, f0);
     if (one) mma(I1{}, f1, sc);
     weave(ReadsScale{});
+    if (decltype(last)::value) turn();
     own_scale(raw, sc);
     rd(cur, 3, f1);
     if (two) mma(I0{}, f0, sc);
