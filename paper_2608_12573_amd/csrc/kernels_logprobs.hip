@@ -7,23 +7,26 @@
 //   alternatives: the n largest x_j as (x_j - lse, j), in the total order of
 //   the library's other selections (larger key first, then smaller index).
 //
-// k_lp reads a row once.  A lane keeps c, s = sum 2^(x L - c) and
-// q = sum 2^t t over t = x L - c, L = log2(e) in fp32, so that
+// k_lp reads a row once.  A lane keeps s = sum 2^t and q = sum 2^t t over
+// t = x L - c, L = log2(e) in fp32, with c of its wave, so that
 //   log2 sum = c + log2 s  and  H = ln 2 (log2 s - q / s).
-// c is a whole number near the lane's largest x L, changed only when a logit
+// c is a whole number near the wave's largest x L, changed only when a logit
 // passes it by 16 powers of two; fp32 holds it exactly, so t is rounded once
 // (one fma), and dividing the final c + log2 s by the same L leaves of L's own
 // rounding (a relative 1.3e-8, as if the row had another temperature) no more
 // than 1.3e-8 H in lse.
 //
-// Alternatives need no second pass.  The n-th best of the lanes' maxima of
-// the first step bounds the row's n-th best from below, so that only logits
-// at or above it are appended to a list in LDS; after 2, 4, 8... steps the
-// list is cut to its best n, which raises the bound.  The steps take the row
+// Alternatives need no second pass.  Of each of the NW waves the n / NW-th best
+// of its lanes' maxima of the first step is taken; the least of them bounds the
+// row's n-th best from below, so that only logits at or above it are appended
+// to a list in LDS; after 2, 4, 8... steps the list is cut to its best n, which
+// raises the bound.  The steps take the row
 // in pieces spread over all of it, so that the first is like the others where
 // logits depend on their place (a range of forbidden tokens).  A list that
 // overflows all the same (rows sorted by value) is replaced by n sweeps that
 // take the row's best of what is left.
+#include <type_traits>
+
 #include "device_common.h"
 #include "launch.h"
 
@@ -43,6 +46,7 @@ constexpr float kLpLarge = 1e6f;
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 
 // IEEE 754-2019 maximum: NaN if either is.
@@ -81,15 +85,27 @@ __device__ __forceinline__ float cand_value(uint64_t c) {
   return __uint_as_float(bits_from_key_f32(static_cast<uint32_t>(c >> 32)));
 }
 
+// Wave-wide reductions with a uniform result: DPP exchanges inside each
+// 16-lane row (quad swaps, half-row and row mirrors), then the four rows'.
+template <int CTRL> __device__ __forceinline__ float dpp_f(float x) {
+  return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), CTRL, 0xF, 0xF, false));
+}
+__device__ __forceinline__ float lane_f(float x, int lane) {
+  return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), lane));
+}
 __device__ __forceinline__ float wave_max_f(float x) {
-#pragma unroll
-  for (int o = kWave / 2; o > 0; o >>= 1) x = fmaxf(x, __shfl_xor(x, o, kWave));
-  return x;
+  x = fmaxf(x, dpp_f<0xB1>(x));
+  x = fmaxf(x, dpp_f<0x4E>(x));
+  x = fmaxf(x, dpp_f<0x141>(x));
+  x = fmaxf(x, dpp_f<0x140>(x));
+  return fmaxf(fmaxf(lane_f(x, 0), lane_f(x, 16)), fmaxf(lane_f(x, 32), lane_f(x, 48)));
 }
 __device__ __forceinline__ float wave_sum_f(float x) {
-#pragma unroll
-  for (int o = kWave / 2; o > 0; o >>= 1) x += __shfl_xor(x, o, kWave);
-  return x;
+  x += dpp_f<0xB1>(x);
+  x += dpp_f<0x4E>(x);
+  x += dpp_f<0x141>(x);
+  x += dpp_f<0x140>(x);
+  return (lane_f(x, 0) + lane_f(x, 16)) + (lane_f(x, 32) + lane_f(x, 48));
 }
 __device__ __forceinline__ uint64_t wave_max_u64(uint64_t x) {
 #pragma unroll
@@ -118,13 +134,11 @@ template <int BS> struct LpReduce {
   uint32_t odd[BS / kWave];
 };
 
-// The block's statistics, in every thread.
-template <int BS> __device__ __forceinline__ Stats block_stats(Stats a, LpReduce<BS>& r) {
+// The block's statistics, in every thread; a wave's lanes have one c.
+template <int BS> __device__ __forceinline__ Stats block_stats(const Stats& a, LpReduce<BS>& r) {
   constexpr int NW = BS / kWave;
   const uint32_t lane = threadIdx.x & (kWave - 1), w = threadIdx.x / kWave;
-  const float c = wave_max_f(a.c);
-  shift(a.s, a.q, a.c - c);
-  Stats t{c, wave_sum_f(a.s), wave_sum_f(a.q), __ballot(a.odd != 0) != 0 ? 1u : 0u};
+  Stats t{a.c, wave_sum_f(a.s), wave_sum_f(a.q), __ballot(a.odd != 0) != 0 ? 1u : 0u};
   if (NW == 1) return t;
   if (lane == 0) {
     r.c[w] = t.c;
@@ -150,18 +164,36 @@ template <int BS> __device__ __forceinline__ Stats block_stats(Stats a, LpReduce
   return t;
 }
 
+// Where c is near the largest x L, the sum is at least 2^-0.5.
+__device__ __forceinline__ bool needs_care(const Stats& t) { return t.odd || !(t.s >= 0.5f); }
+
 // What a row's outputs need, in 64 bits: lse = m + ls (log p = (x - m) - ls:
 // beside an m of the lowest value the sum would lose ls) and H.
 struct RowStats {
-  double m, ls, h;
+  double m, ls;
+  float h;
   __device__ __forceinline__ float logp(float x) const {
     return m == -__builtin_inf() ? kNegInf : static_cast<float>((static_cast<double>(x) - m) - ls);
   }
 };
+// log2 of a positive s: the exponent exactly, and the logarithm of a
+// significand in [0.75, 1.5), which is off by 2^-24 or so.
+__device__ __forceinline__ double log2_of(float s) {
+  int e;
+  float f = frexpf(s, &e);
+  if (f < 0.75f) {
+    f *= 2.0f;
+    --e;
+  }
+  return static_cast<double>(e) + static_cast<double>(__builtin_amdgcn_logf(f));
+}
+__device__ __forceinline__ float entropy_of(double l2, float q, float s) {
+  return static_cast<float>(kLn2 * (l2 - static_cast<double>(q / s)));
+}
 __device__ __forceinline__ RowStats row_stats(const Stats& t) {
-  const double l2 = log2(static_cast<double>(t.s));
-  return {static_cast<double>(t.c) / static_cast<double>(kL2E), l2 / static_cast<double>(kL2E),
-          kLn2 * (l2 - static_cast<double>(t.q) / static_cast<double>(t.s))};
+  constexpr double kInv = 1.0 / static_cast<double>(kL2E);
+  const double l2 = log2_of(t.s);
+  return {static_cast<double>(t.c) * kInv, l2 * kInv, entropy_of(l2, t.q, t.s)};
 }
 
 // The careful path: two sweeps of the row, x - m formed before the scale.
@@ -191,8 +223,8 @@ __device__ __forceinline__ RowStats careful_stats(const char* row, uint32_t V, L
     bad |= r.odd[i];
   }
   __syncthreads();
-  if (bad) return {__builtin_nan(""), __builtin_nan(""), __builtin_nan("")};
-  if (m == kNegInf) return {-__builtin_inf(), 0.0, 0.0};   // nothing is allowed
+  if (bad) return {__builtin_nan(""), __builtin_nan(""), __builtin_nanf("")};
+  if (m == kNegInf) return {-__builtin_inf(), 0.0, 0.0f};   // nothing is allowed
   float s = 0.0f, q = 0.0f;
   for (uint32_t i = threadIdx.x; i < V; i += BS) {
     const float t = fmaxf((E::load(row, i) - m) * kL2E, kLpFloor);
@@ -214,8 +246,8 @@ __device__ __forceinline__ RowStats careful_stats(const char* row, uint32_t V, L
     q += r.q[i];
   }
   __syncthreads();
-  const double l2 = log2(static_cast<double>(s));
-  return {static_cast<double>(m), kLn2 * l2, kLn2 * (l2 - static_cast<double>(q) / static_cast<double>(s))};
+  const double l2 = log2_of(s);
+  return {static_cast<double>(m), kLn2 * l2, entropy_of(l2, q, s)};
 }
 
 // The n best of elements [0, V) of a row, by n sweeps, into list (sorted,
@@ -245,33 +277,61 @@ __device__ __forceinline__ void sweep_top(const char* row, uint32_t V, uint32_t 
 }
 
 // The list's best n, sorted, in its first entries; returns how many there
-// are.  cnt <= CAP entries, all different.
+// are.  cnt <= CAP entries, all different; the list has room for four more.
 template <int BS, int CAP>
 __device__ __forceinline__ uint32_t cut_list(uint64_t* list, uint32_t cnt, uint32_t n) {
   constexpr int P = CAP / BS;
-  uint64_t mine[P];
-  uint32_t rank[P];
-#pragma unroll
-  for (int p = 0; p < P; ++p) {
-    const uint32_t i = p * BS + threadIdx.x;
-    mine[p] = i < cnt ? list[i] : 0ull;
-    rank[p] = 0;
-  }
-  if (cnt <= static_cast<uint32_t>(BS)) {
-    for (uint32_t j = 0; j < cnt; ++j) rank[0] += list[j] > mine[0];
-  } else {
-    for (uint32_t j = 0; j < cnt; ++j) {
-      const uint64_t o = list[j];
-#pragma unroll
-      for (int p = 0; p < P; ++p) rank[p] += o > mine[p];
-    }
-  }
+  if (threadIdx.x < 4) list[cnt + threadIdx.x] = 0;   // (read with the last ones, above none)
   __syncthreads();
+  auto rank_of = [&](auto turns) {
+    constexpr int Q = decltype(turns)::value;
+    uint64_t mine[Q];
+    uint32_t rank[Q];
 #pragma unroll
-  for (int p = 0; p < P; ++p)
-    if (mine[p] && rank[p] < n) list[rank[p]] = mine[p];
+    for (int p = 0; p < Q; ++p) {
+      const uint32_t i = p * BS + threadIdx.x;
+      mine[p] = i < cnt ? list[i] : 0ull;
+      rank[p] = 0;
+    }
+    for (uint32_t j = 0; j < cnt; j += 4) {
+      uint64_t o[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) o[k] = list[j + k];
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+#pragma unroll
+        for (int p = 0; p < Q; ++p) rank[p] += o[k] > mine[p];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int p = 0; p < Q; ++p)
+      if (mine[p] && rank[p] < n) list[rank[p]] = mine[p];
+  };
+  if (cnt <= static_cast<uint32_t>(BS)) rank_of(std::integral_constant<int, 1>{});
+  else rank_of(std::integral_constant<int, P>{});
   __syncthreads();
   return cnt < n ? cnt : n;
+}
+
+// A lower bound of the n-th best of the candidates that the block's lanes have
+// the best ones of (0: none): of each wave the n / NW-th best, and the least
+// of those.  list: BS entries; it is free again after the call.
+template <int BS> __device__ __forceinline__ uint64_t bound_of(uint64_t best, uint32_t n, uint64_t* list, uint64_t* red) {
+  constexpr int NW = BS / kWave;
+  const uint32_t lane = threadIdx.x & (kWave - 1), w = threadIdx.x / kWave;
+  uint64_t* const mine = list + w * kWave;
+  mine[lane] = best;
+  if (lane == 0) red[w] = kCandMin;
+  __syncthreads();
+  uint32_t above = 0;
+#pragma unroll 8
+  for (int i = 0; i < kWave; ++i) above += mine[i] > best;
+  if (best && above == (n + NW - 1) / NW - 1) red[w] = best;
+  __syncthreads();
+  uint64_t bound = red[0];
+#pragma unroll
+  for (int i = 1; i < NW; ++i) bound = red[i] < bound ? red[i] : bound;
+  return bound;
 }
 
 // Outputs of a row, by the whole block; list holds its n best, sorted.
@@ -279,7 +339,7 @@ __device__ __forceinline__ void write_row(const LpArgs& a, uint32_t r, const Row
                                           uint32_t found, float xy, int64_t y) {
   if (threadIdx.x == 0) {
     a.lse[r] = static_cast<float>(t.m + t.ls);
-    a.entropy[r] = static_cast<float>(t.h);
+    a.entropy[r] = t.h;
     float lp = 0.0f;                                              // no token
     if (y >= static_cast<int64_t>(a.V)) lp = __builtin_nanf("");  // not a token
     else if (y >= 0) lp = t.logp(xy);
@@ -305,19 +365,18 @@ __global__ __launch_bounds__(BS) void k_lp(LpArgs a) {
   using E = LpElem<DT>;
   constexpr int ES = E::ES, EPV = E::EPV, NW = BS / kWave;
   constexpr int CAP = TOP ? (BS == kWave ? 512 : 1024) : BS;
-  __shared__ __align__(16) uint64_t s_list[CAP];
-  __shared__ uint64_t s_bound, s_red[NW];
+  __shared__ __align__(16) uint64_t s_list[CAP + 4];
+  __shared__ uint64_t s_red[NW];
   __shared__ uint32_t s_cnt;
   __shared__ LpReduce<BS> s_stats;
-  const uint32_t tid = threadIdx.x, lane = tid & (kWave - 1), w = tid / kWave;
+  const uint32_t tid = threadIdx.x, lane = tid & (kWave - 1);
+  const uint32_t w = __builtin_amdgcn_readfirstlane(tid / kWave);
   const uint32_t r = a.row + (SPLIT ? blockIdx.x / a.G : blockIdx.x);
   const uint32_t g = SPLIT ? blockIdx.x % a.G : 0u;
   const char* const row = static_cast<const char*>(a.x) + static_cast<size_t>(r) * a.stride * ES;
   const uint32_t base = g * a.chunk;                                 // first element of this block
   const uint32_t D = SPLIT ? min(a.chunk, a.V - base) : a.V;
   const char* const x = row + static_cast<size_t>(base) * ES;
-  const int64_t y = SPLIT ? -1 : a.tokens[r];
-  const float xy = SPLIT ? 0.0f : token_logit<DT>(row, a.V, y);
 
   uint32_t head = static_cast<uint32_t>(((16 - (reinterpret_cast<uintptr_t>(x) & 15)) & 15) / ES);
   if (head > D) head = D;
@@ -325,33 +384,63 @@ __global__ __launch_bounds__(BS) void k_lp(LpArgs a) {
   const u32x4* const vec = reinterpret_cast<const u32x4*>(x + static_cast<size_t>(head) * ES);
   const uint32_t pieces = (nvec + kWave - 1) / kWave;                // of 64 vectors
   const uint32_t steps = (pieces + NW * U - 1) / (NW * U);
+  // piece u of step `step` of this wave
+  auto piece_of = [&](uint32_t step, int u) { return (u * NW + w) * steps + step; };
+  u32x4 v[U];
+  auto load = [&](uint32_t step) {
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      v[u] = __builtin_nontemporal_load(vec + min(piece_of(step, u) * kWave + lane, nvec - 1));
+  };
+  // vectors past the end hold nothing
+  auto blank = [&](uint32_t step) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const uint32_t first = piece_of(step, u) * kWave;
+      if (first + kWave > nvec && first + lane >= nvec)
+        v[u] = u32x4{E::kNegInfWord, E::kNegInfWord, E::kNegInfWord, E::kNegInfWord};
+    }
+  };
+  auto vec_max = [&](int u) {
+    float m = E::get(v[u], 0);
+#pragma unroll
+    for (int e = 1; e < EPV; ++e) m = max_nan(m, E::get(v[u], e));
+    return m;
+  };
+  if (steps) load(0);
+  const int64_t y = SPLIT ? -1 : a.tokens[r];
+  const float xy = SPLIT ? 0.0f : token_logit<DT>(row, a.V, y);
+  // elements before the first and after the last whole vector, one a lane
+  const uint32_t tail0 = head + nvec * EPV, ns = head + (D - tail0);
+  const uint32_t own_i = tid < head ? tid : tail0 + (tid - head);
+  const float own = tid < ns ? E::load(x, own_i) : kNegInf;
 
-  Stats st{-kLpLarge * kL2E, 0.0f, 0.0f, 0u};
-  // lim: the largest logit that the current c takes
-  float lim = -kLpLarge;
-  auto rebase = [&](float m) {       // m passed lim, or is NaN
-    if (!(m <= kLpLarge)) {
+  Stats st{-kLpLarge * kL2E, 0.0f, 0.0f, 0u};   // c: the wave's
+  float lim = -kLpLarge;                        // the largest logit that c takes
+  // some lane's m passed lim, or is NaN; the whole wave calls it
+  auto rebase = [&](float m) {
+    if (__ballot(!(m <= kLpLarge))) {
       st.odd = 1;
       return;
     }
+    m = wave_max_f(m);
     const float c = rintf(fmaxf(m, -kLpLarge) * kL2E);
     shift(st.s, st.q, st.c - c);
     st.c = c;
     lim = m + kLpSlack / kL2E;
   };
-  auto term = [&](float v) {
-    const float t = fmaxf(fmaf(v, kL2E, -st.c), kLpFloor);
+  auto term = [&](float z) {
+    const float t = fmaxf(fmaf(z, kL2E, -st.c), kLpFloor);
     const float e = exp2_fast(t);
     st.s += e;
     st.q = fmaf(e, t, st.q);
   };
-  uint64_t bound = kCandMin;         // candidates are at or above it
-  float boundf = kNegInf;
-  uint32_t cnt_now = 0;
+  uint64_t bound = kCandMin;                    // candidates are at or above it
+  float boundf = cand_value(kCandMin);
   bool over = false;
-  auto offer = [&](float v, uint32_t i) {
-    if (!(v < boundf)) {
-      const uint64_t c = cand(v, i);
+  auto offer = [&](float z, uint32_t i) {
+    if (!(z < boundf)) {
+      const uint64_t c = cand(z, i);
       if (c >= bound) {
         const uint32_t slot = atomicAdd(&s_cnt, 1u);
         if (slot < static_cast<uint32_t>(CAP)) s_list[slot] = c;
@@ -359,72 +448,71 @@ __global__ __launch_bounds__(BS) void k_lp(LpArgs a) {
     }
   };
 
-  if (TOP) {
-    if (tid == 0) s_cnt = 0;
-    __syncthreads();
+  if (TOP && tid == 0) s_cnt = 0;
+  {
+    // the first step's maxima: c, and the bound
+    float bm = own;
+    uint64_t best = 0;
+    if (steps) {
+      blank(0);
+      float vm[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        vm[u] = vec_max(u);
+        bm = max_nan(bm, vm[u]);
+      }
+      if (TOP) {
+        // a lane's maximum at an index no smaller than its own (the last of its
+        // vector); a maximum of 0 may be either zero, so it counts as -0
+        float top = vm[0];
+        uint32_t at = piece_of(0, 0);
+#pragma unroll
+        for (int u = 1; u < U; ++u)
+          if (vm[u] > top) {
+            top = vm[u];
+            at = piece_of(0, u);
+          }
+        if (top > kNegInf)
+          best = cand(top == 0.0f ? -0.0f : top, base + head + (at * kWave + lane) * EPV + EPV - 1);
+      }
+    }
+    if (__ballot(!(bm <= lim))) rebase(bm);
+    if (TOP && steps) {
+      bound = bound_of<BS>(best, a.n, s_list, s_red);
+      boundf = cand_value(bound);
+    } else if (TOP) {
+      __syncthreads();
+    }
   }
   for (uint32_t step = 0; step < steps; ++step) {
-    u32x4 v[U];
-    uint32_t vi[U];
+    if (step) {
+      load(step);
+      blank(step);
+    }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      vi[u] = ((u * NW + w) * steps + step) * kWave + lane;
-      v[u] = __builtin_nontemporal_load(vec + min(vi[u], nvec - 1));
-    }
+      if (step || TOP) {
+        // one compare for both: past c's range, or a candidate
+        const float m = vec_max(u);
+        if (__ballot(!(m < (TOP ? fminf(lim, boundf) : lim)))) {
+          if (__ballot(!(m <= lim))) rebase(m);
+          if (TOP && !over && !(m < boundf)) {
 #pragma unroll
-    for (int u = 0; u < U; ++u)
-      if (vi[u] >= nvec) v[u] = u32x4{E::kNegInfWord, E::kNegInfWord, E::kNegInfWord, E::kNegInfWord};
-    float vm[U];
-    float bm = kNegInf;
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      vm[u] = E::get(v[u], 0);
-#pragma unroll
-      for (int e = 1; e < EPV; ++e) vm[u] = max_nan(vm[u], E::get(v[u], e));
-      bm = max_nan(bm, vm[u]);
-    }
-    if (!(bm <= lim)) rebase(bm);
-    if (TOP && step == 0) {
-      // the lanes' maxima, each at an index no smaller than its own (the last
-      // of its vector); a maximum of 0 may be either zero, so it counts as -0
-      uint64_t best = 0;
-      if (bm > kNegInf) {
-        uint32_t at = 0;
-#pragma unroll
-        for (int u = U - 1; u >= 0; --u)
-          if (vm[u] == bm) at = vi[u];
-        best = cand(bm == 0.0f ? -0.0f : bm, base + head + at * EPV + EPV - 1);
-      }
-      s_list[tid] = best;
-      if (tid == 0) s_bound = kCandMin;
-      __syncthreads();
-      uint32_t above = 0;
-#pragma unroll 8
-      for (int i = 0; i < BS; ++i) above += s_list[i] > best;
-      if (best && above == a.n - 1) s_bound = best;
-      __syncthreads();
-      bound = s_bound;
-      boundf = cand_value(bound);
-    }
-    if (TOP && !over) {
-#pragma unroll
-      for (int u = 0; u < U; ++u)
-        if (!(vm[u] < boundf)) {
-#pragma unroll
-          for (int e = 0; e < EPV; ++e) offer(E::get(v[u], e), base + head + vi[u] * EPV + e);
+            for (int e = 0; e < EPV; ++e)
+              offer(E::get(v[u], e), base + head + (piece_of(step, u) * kWave + lane) * EPV + e);
+          }
         }
-    }
-#pragma unroll
-    for (int u = 0; u < U; ++u)
+      }
 #pragma unroll
       for (int e = 0; e < EPV; ++e) term(E::get(v[u], e));
+    }
     // the list is cut after 2, 4, 8... steps
     if (TOP && step > 0 && (step & (step + 1)) == 0 && step + 1 < steps) {
       __syncthreads();
-      cnt_now = s_cnt;
-      over = cnt_now > static_cast<uint32_t>(CAP);
-      if (!over && cnt_now > a.n) {
-        cut_list<BS, CAP>(s_list, cnt_now, a.n);
+      const uint32_t cnt = s_cnt;
+      over = cnt > static_cast<uint32_t>(CAP);
+      if (!over && cnt > a.n) {
+        cut_list<BS, CAP>(s_list, cnt, a.n);
         bound = s_list[a.n - 1];
         boundf = cand_value(bound);
         if (tid == 0) s_cnt = a.n;
@@ -432,22 +520,14 @@ __global__ __launch_bounds__(BS) void k_lp(LpArgs a) {
       __syncthreads();
     }
   }
-  // elements before the first and after the last whole vector
-  {
-    const uint32_t tail0 = head + nvec * EPV, ns = head + (D - tail0);
-    if (tid < ns) {
-      const uint32_t i = tid < head ? tid : tail0 + (tid - head);
-      const float v = E::load(x, i);
-      if (!(v <= lim)) rebase(v);
-      term(v);
-      if (TOP && !over) offer(v, base + i);
-    }
+  if (tid < ns) {
+    term(own);
+    if (TOP && !over) offer(own, base + own_i);
   }
   uint32_t found = 0;
   if (TOP) {
     __syncthreads();
     const uint32_t cnt = s_cnt;
-    __syncthreads();
     if (cnt > static_cast<uint32_t>(CAP)) {
       sweep_top<DT, BS>(x, D, base, a.n, s_list, s_red);
       found = a.n;
@@ -470,61 +550,59 @@ __global__ __launch_bounds__(BS) void k_lp(LpArgs a) {
     return;
   }
   RowStats rs;
-  if (t.odd || !(t.s > 0.0f)) rs = careful_stats<DT, BS>(row, a.V, s_stats);
+  if (needs_care(t)) rs = careful_stats<DT, BS>(row, a.V, s_stats);
   else rs = row_stats(t);
   write_row(a, r, rs, s_list, found, xy, y);
 }
 
-// Joins a row's G chunks.  A chunk's n-th best bounds the row's n-th best
-// from below, and so does the n-th best of the chunks' first.
+// Joins a row's G chunks, of whose candidates the best n are selected as k_lp
+// selects them from a step's.
 template <int DT, bool TOP> __global__ __launch_bounds__(kLpJoinBS) void k_lp_join(LpArgs a) {
-  constexpr int BS = kLpJoinBS, CAP = TOP ? 1024 : BS;
-  __shared__ __align__(16) uint64_t s_list[CAP];
+  constexpr int BS = kLpJoinBS, CAP = TOP ? 1024 : BS, U = 8;
+  __shared__ __align__(16) uint64_t s_list[CAP + 4];
   __shared__ uint64_t s_red[BS / kWave];
   __shared__ uint32_t s_cnt;
   __shared__ LpReduce<BS> s_stats;
   const uint32_t tid = threadIdx.x, r = a.row + blockIdx.x;
   const char* const row = static_cast<const char*>(a.x) + static_cast<size_t>(r) * a.stride * LpElem<DT>::ES;
-  const int64_t y = a.tokens[r];
-  const float xy = token_logit<DT>(row, a.V, y);
   const size_t first = static_cast<size_t>(blockIdx.x) * a.G;
   Stats st{-kLpLarge * kL2E, 0.0f, 0.0f, 0u};
   static_assert(kLpMaxChunks <= BS, "one chunk a thread");
   if (tid < a.G) {
-    const float* const p = a.part + (first + tid) * kLpPart;
+    const f32x4 p = *reinterpret_cast<const f32x4*>(a.part + (first + tid) * kLpPart);
     st = Stats{p[0], p[1], p[2], p[3] != 0.0f ? 1u : 0u};
   }
+  const uint64_t* const top = a.part_top + first * a.n;
+  const uint32_t total = TOP ? a.G * a.n : 0u;
+  // the first BS * U candidates stay in registers, the others are read twice
+  uint64_t mine[U];
+  uint64_t best = 0;
+  if (TOP) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const uint32_t i = u * BS + tid;
+      mine[u] = i < total ? top[i] : 0ull;
+    }
+  }
+  const int64_t y = a.tokens[r];
+  const float xy = token_logit<DT>(row, a.V, y);
   uint32_t found = 0;
   if (TOP) {
-    const uint64_t* const top = a.part_top + first * a.n;
-    // the largest of the chunks' n-th best
-    uint64_t bound = tid < a.G ? top[static_cast<size_t>(tid) * a.n + a.n - 1] : 0ull;
-    bound = wave_max_u64(bound);
-    if ((tid & (kWave - 1)) == 0) s_red[tid / kWave] = bound;
-    s_list[tid] = tid < a.G ? top[static_cast<size_t>(tid) * a.n] : 0ull;
-    if (tid == 0) s_cnt = 0;
-    __syncthreads();
 #pragma unroll
-    for (int i = 0; i < BS / kWave; ++i) bound = s_red[i] > bound ? s_red[i] : bound;
-    const uint64_t mine = s_list[tid];
-    uint32_t above = 0;
-    for (uint32_t i = 0; i < a.G; ++i) above += s_list[i] > mine;
-    __syncthreads();
-    if (tid == 0) s_red[0] = bound;
-    __syncthreads();
-    if (mine && above == a.n - 1 && mine > s_red[0]) s_red[0] = mine;
-    __syncthreads();
-    bound = s_red[0] > kCandMin ? s_red[0] : kCandMin;
-    for (uint32_t i = tid; i < a.G * a.n; i += BS) {
-      const uint64_t c = top[i];
-      if (c >= bound) {
-        const uint32_t slot = atomicAdd(&s_cnt, 1u);
-        if (slot < static_cast<uint32_t>(CAP)) s_list[slot] = c;
-      }
-    }
+    for (int u = 0; u < U; ++u) best = mine[u] > best ? mine[u] : best;
+    for (uint32_t i = U * BS + tid; i < total; i += BS) best = top[i] > best ? top[i] : best;
+    if (tid == 0) s_cnt = 0;
+    const uint64_t bound = bound_of<BS>(best, a.n, s_list, s_red);
+    auto offer = [&](uint64_t c) {
+      if (c < bound) return;
+      const uint32_t slot = atomicAdd(&s_cnt, 1u);
+      if (slot < static_cast<uint32_t>(CAP)) s_list[slot] = c;
+    };
+#pragma unroll
+    for (int u = 0; u < U; ++u) offer(mine[u]);
+    for (uint32_t i = U * BS + tid; i < total; i += BS) offer(top[i]);
     __syncthreads();
     const uint32_t cnt = s_cnt;
-    __syncthreads();
     if (cnt > static_cast<uint32_t>(CAP)) {
       sweep_top<DT, BS>(row, a.V, 0, a.n, s_list, s_red);
       found = a.n;
@@ -532,9 +610,13 @@ template <int DT, bool TOP> __global__ __launch_bounds__(kLpJoinBS) void k_lp_jo
       found = cut_list<BS, CAP>(s_list, cnt, a.n);
     }
   }
+  // the lanes of a wave to one c
+  const float c = wave_max_f(st.c);
+  shift(st.s, st.q, st.c - c);
+  st.c = c;
   const Stats t = block_stats<BS>(st, s_stats);
   RowStats rs;
-  if (t.odd || !(t.s > 0.0f)) rs = careful_stats<DT, BS>(row, a.V, s_stats);
+  if (needs_care(t)) rs = careful_stats<DT, BS>(row, a.V, s_stats);
   else rs = row_stats(t);
   write_row(a, r, rs, s_list, found, xy, y);
 }
@@ -675,8 +757,11 @@ void launch_lp(const LpArgs& a, uint32_t rows, hipStream_t s) {
   }
 }
 
-template <int DT> void launch_lp_dt(const LpArgs& a, int threads, uint32_t rows, hipStream_t s) {
-  if (threads == kWave) launch_lp<DT, kWave, 8>(a, rows, s);
+template <int DT> void launch_lp_dt(const LpArgs& a, uint32_t rows, hipStream_t s) {
+  const uint64_t bytes = static_cast<uint64_t>(a.G > 1 ? a.chunk : a.V) * LpElem<DT>::ES;
+  if (bytes <= 2 * kWave * 16) launch_lp<DT, kWave, 2>(a, rows, s);
+  else if (bytes <= static_cast<uint64_t>(kLpWaveBytes)) launch_lp<DT, kWave, 8>(a, rows, s);
+  else if (bytes <= 2 * kLpWaveBytes) launch_lp<DT, 256, 4>(a, rows, s);
   else launch_lp<DT, 256, 8>(a, rows, s);
   if (a.G > 1) {
     if (a.n) k_lp_join<DT, true><<<rows, kLpJoinBS, 0, s>>>(a);
@@ -713,15 +798,13 @@ hipError_t launch_logprobs(LpCall c) {
   a.chunk = L.chunk;
   a.part = reinterpret_cast<float*>(c.ws);
   a.part_top = reinterpret_cast<uint64_t*>(c.ws + L.off_top);
-  const uint64_t bytes = static_cast<uint64_t>(L.G > 1 ? L.chunk : a.V) * (c.dtype == PROFK_F32 ? 4 : 2);
-  const int threads = bytes <= static_cast<uint64_t>(kLpWaveBytes) ? kWave : 256;
   const int64_t step = rows_per_launch(256) / L.G;
   (void)hipGetLastError();
   for (int64_t r = 0; r < c.T; r += step) {
     const uint32_t rows = static_cast<uint32_t>(c.T - r < step ? c.T - r : step);
     a.row = static_cast<uint32_t>(r);
-    if (c.dtype == PROFK_F32) launch_lp_dt<PROFK_F32>(a, threads, rows, c.stream);
-    else launch_lp_dt<PROFK_BF16>(a, threads, rows, c.stream);
+    if (c.dtype == PROFK_F32) launch_lp_dt<PROFK_F32>(a, rows, c.stream);
+    else launch_lp_dt<PROFK_BF16>(a, rows, c.stream);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }

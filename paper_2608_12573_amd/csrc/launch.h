@@ -306,7 +306,7 @@ hipError_t launch_sae_decode(const SaeDecodeCall& c);
 // their gradient (kernels_logprobs.hip).
 constexpr int64_t kLpMaxTop = 64;             // most alternatives of a row
 constexpr int kLpWaveBytes = 8192;            // longest row (or chunk) that one wave takes
-constexpr int64_t kLpMinChunk = 4096;         // shortest chunk of a row split over workgroups
+constexpr int64_t kLpMinChunk = 2048;         // shortest chunk of a row split over workgroups
 constexpr int64_t kLpMaxChunks = 256;
 constexpr int kLpJoinBS = 256;
 constexpr int kLpPart = 4;                    // words of a chunk's statistics

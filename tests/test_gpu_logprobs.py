@@ -125,6 +125,10 @@ def _masked(kind, T, V, seed):
         x[0] *= 1e37
         x[1] = 3e38
         x[2] *= 1e30
+    elif kind == "low":          # at the lower end of the fast path's range
+        x -= 1e6
+        x[1] -= 90.0
+        x[2] -= 3000.0
     elif kind == "rising":
         x.sort(axis=1)
     elif kind == "falling":
@@ -144,7 +148,7 @@ def _masked(kind, T, V, seed):
     return x
 
 
-KINDS = ["half", "few", "none", "lowest", "range", "late", "nan", "large", "rising", "falling", "equal", "steps", "zeros",
+KINDS = ["half", "few", "none", "lowest", "range", "late", "nan", "large", "low", "rising", "falling", "equal", "steps", "zeros",
          "far", "one_lane"]
 
 
@@ -261,7 +265,7 @@ def test_gradient_strides(pad, offset, dtype):
     _check_grad(_x(2, 9001, 1), _tokens(2, 9001, 1), dtype, 0, pad, offset)
 
 
-@pytest.mark.parametrize("kind", ["half", "few", "none", "lowest", "nan", "large", "equal", "far"])
+@pytest.mark.parametrize("kind", ["half", "few", "none", "lowest", "nan", "large", "low", "equal", "far"])
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_gradient_masks(kind, dtype):
     _check_grad(_masked(kind, 5, 3001, 3), np.array([0, 5, 7, -1, 4000], dtype=np.int64), dtype, 8)
