@@ -43,6 +43,7 @@ constexpr float kLpFloor = -300.0f;  // least exponent: 2^-300 is 0 in fp32, and
 // path, as are rows of nothing above its negative: x L must not overflow, and
 // c / L is exact enough for x - lse only while c is small.
 constexpr float kLpLarge = 1e6f;
+constexpr float kLpHuge = 1e38f;     // above its negative, x L - c is finite
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
@@ -51,6 +52,7 @@ typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 
 // IEEE 754-2019 maximum: NaN if either is.
 __device__ __forceinline__ float max_nan(float a, float b) { return __builtin_elementwise_maximum(a, b); }
+__device__ __forceinline__ float min_nan(float a, float b) { return __builtin_elementwise_minimum(a, b); }
 __device__ __forceinline__ float exp2_fast(float t) { return __builtin_amdgcn_exp2f(t); }
 
 template <int DT> struct LpElem;
@@ -384,21 +386,27 @@ __global__ __launch_bounds__(BS) void k_lp(LpArgs a) {
   const u32x4* const vec = reinterpret_cast<const u32x4*>(x + static_cast<size_t>(head) * ES);
   const uint32_t pieces = (nvec + kWave - 1) / kWave;                // of 64 vectors
   const uint32_t steps = (pieces + NW * U - 1) / (NW * U);
-  // piece u of step `step` of this wave
-  auto piece_of = [&](uint32_t step, int u) { return (u * NW + w) * steps + step; };
+  // Piece u of step `step` of this wave starts at vector `first`; a lane reads
+  // vector `at` + lane: a piece that ends past the last vector is read as the
+  // row's last 64, and blanked where it is not those (a row of fewer vectors:
+  // past the last).  All of it is scalar, and the lane's offset is the same
+  // for every load.
+  auto first_of = [&](uint32_t step, int u) { return ((u * NW + w) * steps + step) * kWave; };
+  const uint32_t last_at = nvec > static_cast<uint32_t>(kWave) ? nvec - kWave : 0u;
+  const uint32_t lane_off = min(lane, nvec - 1);
+  auto at_of = [&](uint32_t step, int u) { return min(first_of(step, u), last_at); };
   u32x4 v[U];
   auto load = [&](uint32_t step) {
 #pragma unroll
-    for (int u = 0; u < U; ++u)
-      v[u] = __builtin_nontemporal_load(vec + min(piece_of(step, u) * kWave + lane, nvec - 1));
+    for (int u = 0; u < U; ++u) v[u] = __builtin_nontemporal_load(vec + at_of(step, u) + lane_off);
   };
-  // vectors past the end hold nothing
   auto blank = [&](uint32_t step) {
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const uint32_t first = piece_of(step, u) * kWave;
-      if (first + kWave > nvec && first + lane >= nvec)
-        v[u] = u32x4{E::kNegInfWord, E::kNegInfWord, E::kNegInfWord, E::kNegInfWord};
+      const uint32_t first = first_of(step, u), i = at_of(step, u) + lane;
+      if (__builtin_expect(first + kWave > nvec, 0)) {
+        if (i < first || i >= nvec) v[u] = u32x4{E::kNegInfWord, E::kNegInfWord, E::kNegInfWord, E::kNegInfWord};
+      }
     }
   };
   auto vec_max = [&](int u) {
@@ -424,13 +432,15 @@ __global__ __launch_bounds__(BS) void k_lp(LpArgs a) {
       return;
     }
     m = wave_max_f(m);
-    const float c = rintf(fmaxf(m, -kLpLarge) * kL2E);
+    const float c = lane_f(rintf(fmaxf(m, -kLpLarge) * kL2E), 0);
     shift(st.s, st.q, st.c - c);
     st.c = c;
-    lim = m + kLpSlack / kL2E;
+    lim = lane_f(m + kLpSlack / kL2E, 0);
   };
-  auto term = [&](float z) {
-    const float t = fmaxf(fmaf(z, kL2E, -st.c), kLpFloor);
+  // z's term; FLOOR: z may be -inf, or as low as makes t -inf
+  auto term = [&](float z, auto floor) {
+    float t = fmaf(z, kL2E, -st.c);
+    if (decltype(floor)::value) t = fmaxf(t, kLpFloor);
     const float e = exp2_fast(t);
     st.s += e;
     st.q = fmaf(e, t, st.q);
@@ -465,15 +475,14 @@ __global__ __launch_bounds__(BS) void k_lp(LpArgs a) {
         // a lane's maximum at an index no smaller than its own (the last of its
         // vector); a maximum of 0 may be either zero, so it counts as -0
         float top = vm[0];
-        uint32_t at = piece_of(0, 0);
+        uint32_t at = at_of(0, 0);
 #pragma unroll
         for (int u = 1; u < U; ++u)
           if (vm[u] > top) {
             top = vm[u];
-            at = piece_of(0, u);
+            at = at_of(0, u);
           }
-        if (top > kNegInf)
-          best = cand(top == 0.0f ? -0.0f : top, base + head + (at * kWave + lane) * EPV + EPV - 1);
+        if (top > kNegInf) best = cand(top == 0.0f ? -0.0f : top, base + head + (at + lane) * EPV + EPV - 1);
       }
     }
     if (__ballot(!(bm <= lim))) rebase(bm);
@@ -491,20 +500,32 @@ __global__ __launch_bounds__(BS) void k_lp(LpArgs a) {
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      if (step || TOP) {
-        // one compare for both: past c's range, or a candidate
-        const float m = vec_max(u);
-        if (__ballot(!(m < (TOP ? fminf(lim, boundf) : lim)))) {
-          if (__ballot(!(m <= lim))) rebase(m);
-          if (TOP && !over && !(m < boundf)) {
+      // one compare for both: past c's range, or a candidate
+      const float m = vec_max(u);
+      if (__ballot(!(m < (TOP ? fminf(lim, boundf) : lim)))) {
+        if (__ballot(!(m <= lim))) rebase(m);
+        if (TOP && !over && !(m < boundf)) {
 #pragma unroll
-            for (int e = 0; e < EPV; ++e)
-              offer(E::get(v[u], e), base + head + (piece_of(step, u) * kWave + lane) * EPV + e);
-          }
+          for (int e = 0; e < EPV; ++e)
+            offer(E::get(v[u], e), base + head + (at_of(step, u) + lane) * EPV + e);
         }
       }
+      // 16-bit rows are bound by the instructions of a term, of which the floor
+      // is one: half a one for the least logit decides whether it is needed
+      bool low = true;
+      if (DT == PROFK_BF16) {
+        float mn = E::get(v[u], 0);
 #pragma unroll
-      for (int e = 0; e < EPV; ++e) term(E::get(v[u], e));
+        for (int e = 1; e < EPV; ++e) mn = min_nan(mn, E::get(v[u], e));
+        low = __ballot(!(mn > -kLpHuge)) != 0;
+      }
+      if (low) {
+#pragma unroll
+        for (int e = 0; e < EPV; ++e) term(E::get(v[u], e), std::true_type{});
+      } else {
+#pragma unroll
+        for (int e = 0; e < EPV; ++e) term(E::get(v[u], e), std::false_type{});
+      }
     }
     // the list is cut after 2, 4, 8... steps
     if (TOP && step > 0 && (step & (step + 1)) == 0 && step + 1 < steps) {
@@ -521,7 +542,7 @@ __global__ __launch_bounds__(BS) void k_lp(LpArgs a) {
     }
   }
   if (tid < ns) {
-    term(own);
+    term(own, std::true_type{});
     if (TOP && !over) offer(own, base + own_i);
   }
   uint32_t found = 0;
