@@ -395,12 +395,12 @@ __global__ __launch_bounds__(BS) void k_lp(LpArgs a) {
   const uint32_t last_at = nvec > static_cast<uint32_t>(kWave) ? nvec - kWave : 0u;
   const uint32_t lane_off = min(lane, nvec - 1);
   auto at_of = [&](uint32_t step, int u) { return min(first_of(step, u), last_at); };
-  u32x4 v[U];
-  auto load = [&](uint32_t step) {
+  using Vecs = u32x4[U];
+  auto load = [&](uint32_t step, Vecs& v) {
 #pragma unroll
     for (int u = 0; u < U; ++u) v[u] = __builtin_nontemporal_load(vec + at_of(step, u) + lane_off);
   };
-  auto blank = [&](uint32_t step) {
+  auto blank = [&](uint32_t step, Vecs& v) {
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const uint32_t first = first_of(step, u), i = at_of(step, u) + lane;
@@ -409,13 +409,14 @@ __global__ __launch_bounds__(BS) void k_lp(LpArgs a) {
       }
     }
   };
-  auto vec_max = [&](int u) {
-    float m = E::get(v[u], 0);
+  auto vec_max = [](const u32x4& v) {
+    float m = E::get(v, 0);
 #pragma unroll
-    for (int e = 1; e < EPV; ++e) m = max_nan(m, E::get(v[u], e));
+    for (int e = 1; e < EPV; ++e) m = max_nan(m, E::get(v, e));
     return m;
   };
-  if (steps) load(0);
+  Vecs v0, v1;     // a step, and the next one, loaded meanwhile
+  if (steps) load(0, v0);
   const int64_t y = SPLIT ? -1 : a.tokens[r];
   const float xy = SPLIT ? 0.0f : token_logit<DT>(row, a.V, y);
   // elements before the first and after the last whole vector, one a lane
@@ -464,11 +465,11 @@ __global__ __launch_bounds__(BS) void k_lp(LpArgs a) {
     float bm = own;
     uint64_t best = 0;
     if (steps) {
-      blank(0);
+      blank(0, v0);
       float vm[U];
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        vm[u] = vec_max(u);
+        vm[u] = vec_max(v0[u]);
         bm = max_nan(bm, vm[u]);
       }
       if (TOP) {
@@ -493,15 +494,13 @@ __global__ __launch_bounds__(BS) void k_lp(LpArgs a) {
       __syncthreads();
     }
   }
-  for (uint32_t step = 0; step < steps; ++step) {
-    if (step) {
-      load(step);
-      blank(step);
-    }
+  auto take = [&](uint32_t step, Vecs& v, Vecs& next) {
+    if (step + 1 < steps) load(step + 1, next);
+    if (step) blank(step, v);
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       // one compare for both: past c's range, or a candidate
-      const float m = vec_max(u);
+      const float m = vec_max(v[u]);
       if (__ballot(!(m < (TOP ? fminf(lim, boundf) : lim)))) {
         if (__ballot(!(m <= lim))) rebase(m);
         if (TOP && !over && !(m < boundf)) {
@@ -540,6 +539,10 @@ __global__ __launch_bounds__(BS) void k_lp(LpArgs a) {
       }
       __syncthreads();
     }
+  };
+  for (uint32_t step = 0; step < steps; step += 2) {
+    take(step, v0, v1);
+    if (step + 1 < steps) take(step + 1, v1, v0);
   }
   if (tid < ns) {
     term(own, std::true_type{});
@@ -782,8 +785,7 @@ template <int DT> void launch_lp_dt(const LpArgs& a, uint32_t rows, hipStream_t 
   const uint64_t bytes = static_cast<uint64_t>(a.G > 1 ? a.chunk : a.V) * LpElem<DT>::ES;
   if (bytes <= 2 * kWave * 16) launch_lp<DT, kWave, 2>(a, rows, s);
   else if (bytes <= static_cast<uint64_t>(kLpWaveBytes)) launch_lp<DT, kWave, 8>(a, rows, s);
-  else if (bytes <= 2 * kLpWaveBytes) launch_lp<DT, 256, 4>(a, rows, s);
-  else launch_lp<DT, 256, 8>(a, rows, s);
+  else launch_lp<DT, 256, 4>(a, rows, s);
   if (a.G > 1) {
     if (a.n) k_lp_join<DT, true><<<rows, kLpJoinBS, 0, s>>>(a);
     else k_lp_join<DT, false><<<rows, kLpJoinBS, 0, s>>>(a);
