@@ -295,7 +295,9 @@ __device__ __forceinline__ uint32_t cut_list(uint64_t* list, uint32_t cnt, uint3
       mine[p] = i < cnt ? list[i] : 0ull;
       rank[p] = 0;
     }
-    for (uint32_t j = 0; j < cnt; j += 4) {
+    // (a wave without an entry has nothing to rank)
+    const uint32_t end = __ballot(mine[0] != 0) ? cnt : 0u;
+    for (uint32_t j = 0; j < end; j += 4) {
       uint64_t o[4];
 #pragma unroll
       for (int k = 0; k < 4; ++k) o[k] = list[j + k];
@@ -495,8 +497,8 @@ __global__ __launch_bounds__(BS) void k_lp(LpArgs a) {
     }
   }
   auto take = [&](uint32_t step, Vecs& v, Vecs& next) {
-    if (step + 1 < steps) load(step + 1, next);
-    if (step) blank(step, v);
+    if (BS > kWave && step + 1 < steps) load(step + 1, next);
+    if (BS > kWave && step) blank(step, v);
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       // one compare for both: past c's range, or a candidate
@@ -527,7 +529,7 @@ __global__ __launch_bounds__(BS) void k_lp(LpArgs a) {
       }
     }
     // the list is cut after 2, 4, 8... steps
-    if (TOP && step > 0 && (step & (step + 1)) == 0 && step + 1 < steps) {
+    if (BS > kWave && TOP && step > 0 && (step & (step + 1)) == 0 && step + 1 < steps) {
       __syncthreads();
       const uint32_t cnt = s_cnt;
       over = cnt > static_cast<uint32_t>(CAP);
@@ -540,9 +542,13 @@ __global__ __launch_bounds__(BS) void k_lp(LpArgs a) {
       __syncthreads();
     }
   };
-  for (uint32_t step = 0; step < steps; step += 2) {
-    take(step, v0, v1);
-    if (step + 1 < steps) take(step + 1, v1, v0);
+  if constexpr (BS == kWave) {
+    if (steps) take(0, v0, v0);      // (a wave's rows and chunks are one step)
+  } else {
+    for (uint32_t step = 0; step < steps; step += 2) {
+      take(step, v0, v1);
+      if (step + 1 < steps) take(step + 1, v1, v0);
+    }
   }
   if (tid < ns) {
     term(own, std::true_type{});
