@@ -213,8 +213,8 @@ def _dtype_code(t):
 def _stream():
     """The current stream's handle (torch.cuda.current_stream() builds a Stream
     object around it)."""
-    torch = _torch()
-    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+    C = _torch()._C
+    return C._cuda_getCurrentRawStream(C._cuda_getDevice())
 
 
 def _ptr(t):
@@ -554,20 +554,40 @@ MAX_TOP = 64                       # most alternatives of a row
 
 
 def _vector(t, name, dtype, shape, device):
-    """A contiguous input of exactly this dtype and shape, on `device`."""
+    """A contiguous tensor of exactly this dtype and shape, on `device` (any
+    GPU: None).  These calls check up to ten tensors each, so what is in order
+    passes on one condition."""
+    try:
+        if t.dtype is dtype and t.shape == shape and t.is_contiguous() and t.is_cuda and \
+                (device is None or t.device == device):
+            return
+    except AttributeError:
+        pass
     torch = _torch()
     if not isinstance(t, torch.Tensor):
         raise ProfkError(f"{name} must be a torch tensor")
     if t.dtype != dtype or tuple(t.shape) != shape or not t.is_contiguous():
-        raise ProfkError(f"{name} must be contiguous {dtype} of shape {shape}, got {t.dtype} {tuple(t.shape)}")
+        raise ProfkError(f"{name} must be contiguous {dtype} of shape {shape}, got {t.dtype} {tuple(t.shape)} "
+                         f"with strides {tuple(t.stride())}")
     _on_device(t, name, device)
 
 
-def _logits(x):
-    """Checks logits [T, V] (rows may be strided): dtype code, T, V, stride."""
-    dt = _input(x, "logits", 2, layout="rows")
-    T, V = x.shape
-    return dt, T, V, max(x.stride(0), V) if T > 1 else V
+def _rows(x, name):
+    """Checks a matrix whose rows may be strided: (dtype code, rows, columns,
+    elements from row to row)."""
+    torch = _torch()
+    if not isinstance(x, torch.Tensor) or x.dim() != 2 or not x.is_cuda:
+        _input(x, name, 2, layout="rows")
+    dt = F32 if x.dtype is torch.float32 else BF16 if x.dtype is torch.bfloat16 else _dtype_code(x)
+    R, C = x.shape
+    s0, s1 = x.stride()
+    if s1 != 1 or s0 < C:
+        if R <= 1 and (s1 == 1 or C <= 1):
+            s0 = C
+        else:
+            _input(x, name, 2, layout="rows")
+            s0 = max(s0, C)
+    return dt, R, C, s0
 
 
 def token_logprobs_workspace(T, V, n_top=0, device="cuda"):
@@ -596,24 +616,29 @@ def token_logprobs(logits, tokens, n_top=0, ws=None, out=None):
     Alternatives are most probable first, equal ones by smaller index; logits
     of -inf are never among them ((-inf, -1) where too few are left)."""
     torch = _torch()
-    dt, T, V, stride = _logits(logits)
-    _vector(tokens, "tokens", torch.int64, (T,), logits.device)
+    dt, T, V, stride = _rows(logits, "logits")
+    dev = logits.device
+    _vector(tokens, "tokens", torch.int64, (T,), dev)
     if not 0 <= n_top <= MAX_TOP:
         raise ProfkError(f"n_top must be from 0 to {MAX_TOP}, got {n_top}")
-    n = int(lib().profk_token_logprobs_workspace_size(T, V, n_top))
-    if ws is None:
-        ws = torch.empty(n, dtype=torch.uint8, device=logits.device)
-    else:
-        _bytes_buffer(ws, "ws", n, logits.device)
+    L = lib()
+    n = L.profk_token_logprobs_workspace_size(T, V, n_top)
+    if ws is not None:
+        _bytes_buffer(ws, "ws", n, dev)
+    elif n:
+        ws = torch.empty(n, dtype=torch.uint8, device=dev)
     if out is None:
-        out = token_logprobs_outputs(T, n_top, logits.device)
+        out = token_logprobs_outputs(T, n_top, dev)
     else:
-        for i, t in enumerate(out):
-            _vector(t, f"out[{i}]", torch.int64 if i == 4 else torch.float32, (T,) if i < 3 else (T, n_top),
-                    logits.device)
-    lp, h, lse, top, idx = out
-    _check(lib().profk_token_logprobs(dt, _ptr(logits), T, V, stride, _ptr(tokens), n_top, _ptr(lp), _ptr(h),
-                                      _ptr(lse), _ptr(top), _ptr(idx), _ptr(ws) if n else None, n, _stream()))
+        one, f32 = (T,), torch.float32
+        _vector(out[0], "out[0]", f32, one, dev)
+        _vector(out[1], "out[1]", f32, one, dev)
+        _vector(out[2], "out[2]", f32, one, dev)
+        _vector(out[3], "out[3]", f32, (T, n_top), dev)
+        _vector(out[4], "out[4]", torch.int64, (T, n_top), dev)
+    _check(L.profk_token_logprobs(dt, logits.data_ptr(), T, V, stride, tokens.data_ptr(), n_top, out[0].data_ptr(),
+                                  out[1].data_ptr(), out[2].data_ptr(), out[3].data_ptr(), out[4].data_ptr(),
+                                  ws.data_ptr() if n else None, n, _stream()))
     return out
 
 
@@ -624,30 +649,35 @@ def token_logprobs_grad(logits, tokens, lse, entropy, g_logprob, g_entropy=None,
     token_logprobs'.  out: the logits' dtype and shape, rows may be strided;
     it must not overlap the logits."""
     torch = _torch()
-    dt, T, V, stride = _logits(logits)
-    dev = logits.device
-    _vector(tokens, "tokens", torch.int64, (T,), dev)
-    for t, name in ((lse, "lse"), (entropy, "entropy"), (g_logprob, "g_logprob"), (g_entropy, "g_entropy")):
-        if t is not None or name == "lse":
-            _vector(t, name, torch.float32, (T,), dev)
-    if g_entropy is not None and entropy is None:
-        raise ProfkError("g_entropy needs the rows' entropy")
+    dt, T, V, stride = _rows(logits, "logits")
+    dev, f32, one = logits.device, torch.float32, (T,)
+    _vector(tokens, "tokens", torch.int64, one, dev)
+    _vector(lse, "lse", f32, one, dev)
+    if entropy is not None:
+        _vector(entropy, "entropy", f32, one, dev)
+    if g_logprob is not None:
+        _vector(g_logprob, "g_logprob", f32, one, dev)
+    if g_entropy is not None:
+        _vector(g_entropy, "g_entropy", f32, one, dev)
+        if entropy is None:
+            raise ProfkError("g_entropy needs the rows' entropy")
     n = 0
     if g_top is not None:
         if not isinstance(top_idx, torch.Tensor) or top_idx.dim() != 2 or top_idx.shape[1] > MAX_TOP:
             raise ProfkError(f"top_idx must be [T, n] with n at most {MAX_TOP}")
         n = top_idx.shape[1]
         _vector(top_idx, "top_idx", torch.int64, (T, n), dev)
-        _vector(g_top, "g_top", torch.float32, (T, n), dev)
+        _vector(g_top, "g_top", f32, (T, n), dev)
     if out is None:
         out = torch.empty((T, V), dtype=logits.dtype, device=dev)
-    ot, oT, oV, ostride = _logits(out)
-    if (ot, oT, oV) != (dt, T, V):
+    ot, oT, oV, ostride = _rows(out, "out")
+    if ot != dt or oT != T or oV != V:
         raise ProfkError("out must have the logits' dtype and shape")
     _on_device(out, "out", dev)
-    _check(lib().profk_token_logprobs_grad(dt, _ptr(logits), T, V, stride, _ptr(tokens), _ptr(lse), _ptr(entropy),
-                                           _ptr(g_logprob), _ptr(g_entropy), n, _ptr(top_idx), _ptr(g_top),
-                                           _ptr(out), ostride, _stream()))
+    _check(lib().profk_token_logprobs_grad(dt, logits.data_ptr(), T, V, stride, tokens.data_ptr(), lse.data_ptr(),
+                                           _ptr(entropy), _ptr(g_logprob), _ptr(g_entropy), n,
+                                           top_idx.data_ptr() if n else None, g_top.data_ptr() if n else None,
+                                           out.data_ptr(), ostride, _stream()))
     return out
 
 
@@ -688,41 +718,35 @@ def mx4_quantize(x, out=None):
     power-of-two scale per 32: (codes uint8 [R, Kp/2], scales uint8
     [R/32, Kp/128, 32, 4]), K rounded up to a multiple of 128 and, in the
     scales, R to one of 32."""
-    dt = _input(x, "x", 2, layout="rows")
-    R, K = x.shape
+    dt, R, K, stride = _rows(x, "x")
     if out is None:
         out = mx4_outputs(R, K, x.device)
-    elif _mx4(*out, "out", K, x.device) != R:
+    elif _mx4(out[0], out[1], "out", K, x.device) != R:
         raise ProfkError(f"out must have {R} rows")
-    _check(lib().profk_mx4_quantize(dt, _ptr(x), R, K, max(x.stride(0), K) if R > 1 else K, _ptr(out[0]), _ptr(out[1]),
-                                    _stream()))
+    _check(lib().profk_mx4_quantize(dt, x.data_ptr(), R, K, stride, out[0].data_ptr(), out[1].data_ptr(), _stream()))
     return out
+
+
+def _dense_out(shape, dtype, default, out, device):
+    """A contiguous fp32 or bf16 output of `shape`, given or new: (out, code)."""
+    torch = _torch()
+    if out is None:
+        out = torch.empty(shape, dtype=dtype or default, device=device)
+    elif dtype is not None and out.dtype != dtype:
+        raise ProfkError(f"out is {out.dtype}, not {dtype}")
+    elif not isinstance(out, torch.Tensor):
+        raise ProfkError("out must be a torch tensor")
+    _vector(out, "out", out.dtype, shape, device)
+    return out, _dtype_code(out)
 
 
 def mx4_dequantize(codes, scales, K, dtype=None, out=None):
     """The values [R, K] that codes and scales stand for, in fp32 or bf16
     (the default; every value is exact in it), or into `out`."""
-    torch = _torch()
     R = _mx4(codes, scales, "the", K)
-    if out is None:
-        out = torch.empty((R, K), dtype=dtype or torch.bfloat16, device=codes.device)
-    elif dtype is not None and out.dtype != dtype:
-        raise ProfkError(f"out is {out.dtype}, not {dtype}")
-    dt = _input(out, "out", 2)
-    _vector(out, "out", out.dtype, (R, K), codes.device)
-    _check(lib().profk_mx4_dequantize(dt, _ptr(codes), _ptr(scales), R, K, _ptr(out), _stream()))
+    out, dt = _dense_out((R, K), dtype, _torch().bfloat16, out, codes.device)
+    _check(lib().profk_mx4_dequantize(dt, codes.data_ptr(), scales.data_ptr(), R, K, out.data_ptr(), _stream()))
     return out
-
-
-def _mx4_out(M, N, dtype, out, device):
-    torch = _torch()
-    if out is None:
-        out = torch.empty((M, N), dtype=dtype or torch.float32, device=device)
-    elif dtype is not None and out.dtype != dtype:
-        raise ProfkError(f"out is {out.dtype}, not {dtype}")
-    dt = _input(out, "out", 2)
-    _vector(out, "out", out.dtype, (M, N), device)
-    return out, dt
 
 
 def mx4_matmul(a_codes, a_scales, b_codes, b_scales, K, dtype=None, out=None):
@@ -730,14 +754,14 @@ def mx4_matmul(a_codes, a_scales, b_codes, b_scales, K, dtype=None, out=None):
     [M, N], fp32 sums."""
     M = _mx4(a_codes, a_scales, "a's", K)
     N = _mx4(b_codes, b_scales, "b's", K, a_codes.device)
-    out, dt = _mx4_out(M, N, dtype, out, a_codes.device)
-    _check(lib().profk_mx4_matmul(_ptr(a_codes), _ptr(a_scales), M, _ptr(b_codes), _ptr(b_scales), N, K, dt, _ptr(out),
-                                  _stream()))
+    out, dt = _dense_out((M, N), dtype, _torch().float32, out, a_codes.device)
+    _check(lib().profk_mx4_matmul(a_codes.data_ptr(), a_scales.data_ptr(), M, b_codes.data_ptr(), b_scales.data_ptr(),
+                                  N, K, dt, out.data_ptr(), _stream()))
     return out
 
 
 def mx4_linear_workspace(M, K, N, device="cuda"):
-    """A workspace for mx4_linear."""
+    """A workspace for mx4_linear (may be empty)."""
     torch = _torch()
     return torch.empty(int(lib().profk_mx4_linear_workspace_size(M, K, N)), dtype=torch.uint8, device=device)
 
@@ -745,15 +769,17 @@ def mx4_linear_workspace(M, K, N, device="cuda"):
 def mx4_linear(x, w_codes, w_scales, dtype=None, ws=None, out=None):
     """x W^T: fp32 or bf16 x [M, K] (rows may be strided), quantised in the
     call, and W [N, K] from mx4_quantize; fp32 (the default) or bf16 [M, N]."""
-    dt = _input(x, "x", 2, layout="rows")
-    M, K = x.shape
-    N = _mx4(w_codes, w_scales, "the weights'", K, x.device)
-    out, odt = _mx4_out(M, N, dtype, out, x.device)
-    n = int(lib().profk_mx4_linear_workspace_size(M, K, N))
-    if ws is None:
-        ws = mx4_linear_workspace(M, K, N, x.device)
-    else:
-        _bytes_buffer(ws, "ws", n, x.device)
-    _check(lib().profk_mx4_linear(dt, _ptr(x), M, K, max(x.stride(0), K) if M > 1 else K, _ptr(w_codes), _ptr(w_scales),
-                                  N, odt, _ptr(out), _ptr(ws), n, _stream()))
+    torch = _torch()
+    dt, M, K, stride = _rows(x, "x")
+    dev = x.device
+    N = _mx4(w_codes, w_scales, "the weights'", K, dev)
+    out, odt = _dense_out((M, N), dtype, torch.float32, out, dev)
+    L = lib()
+    n = L.profk_mx4_linear_workspace_size(M, K, N)
+    if ws is not None:
+        _bytes_buffer(ws, "ws", n, dev)
+    elif n:
+        ws = torch.empty(n, dtype=torch.uint8, device=dev)
+    _check(L.profk_mx4_linear(dt, x.data_ptr(), M, K, stride, w_codes.data_ptr(), w_scales.data_ptr(), N, odt,
+                              out.data_ptr(), ws.data_ptr() if n else None, n, _stream()))
     return out
