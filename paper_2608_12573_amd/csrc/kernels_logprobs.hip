@@ -317,22 +317,43 @@ __device__ __forceinline__ uint32_t cut_list(uint64_t* list, uint32_t cnt, uint3
   return cnt < n ? cnt : n;
 }
 
+__device__ __forceinline__ uint32_t wave_min_u32(uint32_t x) { return ~wave_max_u32(~x); }
+
+// The r-th largest x of the wave's lanes with `in` (0 if they are fewer); left:
+// how many are at least as large.  Found from its highest bit, a ballot a bit,
+// until a prefix is reached by r lanes alone, of which it is the least.
+// (Ranking 64 lanes by comparing all with all goes through LDS 64 times.)
+__device__ __forceinline__ uint32_t wave_kth(uint32_t x, bool in, uint32_t r, uint32_t& left) {
+  uint32_t p = 0;
+  left = static_cast<uint32_t>(__popcll(__ballot(in)));
+  if (left < r) return 0;
+  for (uint32_t bit = 0x80000000u; bit != 0 && left != r; bit >>= 1) {
+    const uint32_t n = static_cast<uint32_t>(__popcll(__ballot(in && x >= (p | bit))));
+    if (n >= r) {
+      p |= bit;
+      left = n;
+    }
+  }
+  return left == r ? wave_min_u32(in && x >= p ? x : 0xFFFFFFFFu) : p;
+}
+
 // A lower bound of the n-th best of the candidates that the block's lanes have
 // the best ones of (0: none): of each wave the n / NW-th best, and the least
-// of those.  list: BS entries; it is free again after the call.
-template <int BS> __device__ __forceinline__ uint64_t bound_of(uint64_t best, uint32_t n, uint64_t* list, uint64_t* red) {
+// of those.
+template <int BS> __device__ __forceinline__ uint64_t bound_of(uint64_t best, uint32_t n, uint64_t* red) {
   constexpr int NW = BS / kWave;
-  const uint32_t lane = threadIdx.x & (kWave - 1), w = threadIdx.x / kWave;
-  uint64_t* const mine = list + w * kWave;
-  mine[lane] = best;
-  if (lane == 0) red[w] = kCandMin;
+  const uint32_t r = (n + NW - 1) / NW;
+  const uint32_t key = static_cast<uint32_t>(best >> 32), low = static_cast<uint32_t>(best);
+  uint32_t left;
+  const uint32_t k = wave_kth(key, best != 0, r, left);
+  uint64_t bound = static_cast<uint64_t>(k) << 32;
+  // those that have the r-th key itself: by index
+  if (k) bound |= wave_kth(low, key == k, r - static_cast<uint32_t>(__popcll(__ballot(key > k))), left);
+  if (bound < kCandMin) bound = kCandMin;
+  if (NW == 1) return bound;
+  if ((threadIdx.x & (kWave - 1)) == 0) red[threadIdx.x / kWave] = bound;
   __syncthreads();
-  uint32_t above = 0;
-#pragma unroll 8
-  for (int i = 0; i < kWave; ++i) above += mine[i] > best;
-  if (best && above == (n + NW - 1) / NW - 1) red[w] = best;
-  __syncthreads();
-  uint64_t bound = red[0];
+  bound = red[0];
 #pragma unroll
   for (int i = 1; i < NW; ++i) bound = red[i] < bound ? red[i] : bound;
   return bound;
@@ -490,11 +511,10 @@ __global__ __launch_bounds__(BS) void k_lp(LpArgs a) {
     }
     if (__ballot(!(bm <= lim))) rebase(bm);
     if (TOP && steps) {
-      bound = bound_of<BS>(best, a.n, s_list, s_red);
+      bound = bound_of<BS>(best, a.n, s_red);
       boundf = cand_value(bound);
-    } else if (TOP) {
-      __syncthreads();
     }
+    if (TOP && (NW == 1 || !steps)) __syncthreads();   // (s_cnt)
   }
   auto take = [&](uint32_t step, Vecs& v, Vecs& next) {
     if (BS > kWave && step + 1 < steps) load(step + 1, next);
@@ -622,7 +642,7 @@ template <int DT, bool TOP> __global__ __launch_bounds__(kLpJoinBS) void k_lp_jo
     for (int u = 0; u < U; ++u) best = mine[u] > best ? mine[u] : best;
     for (uint32_t i = U * BS + tid; i < total; i += BS) best = top[i] > best ? top[i] : best;
     if (tid == 0) s_cnt = 0;
-    const uint64_t bound = bound_of<BS>(best, a.n, s_list, s_red);
+    const uint64_t bound = bound_of<BS>(best, a.n, s_red);
     auto offer = [&](uint64_t c) {
       if (c < bound) return;
       const uint32_t slot = atomicAdd(&s_cnt, 1u);
