@@ -714,6 +714,15 @@ template <int DT> __global__ __launch_bounds__(kGradBS) void k_lp_grad(LpGradArg
   const uint32_t body = head + piece * kPiece;
   const uint32_t hi = piece + 1 == a.pieces || a.V - body < kPiece ? a.V : body + kPiece;
   if (lo >= a.V) return;
+  // the piece's logits first: what follows waits for loads of its own
+  const uint32_t nvec = hi > body ? (hi - body) / EPV : 0u;
+  u32x4 v[kGradU];
+#pragma unroll
+  for (int u = 0; u < kGradU; ++u) {
+    const uint32_t i = u * BS + tid;
+    v[u] = u32x4{};
+    if (i < nvec) v[u] = *reinterpret_cast<const u32x4u*>(x + (static_cast<size_t>(body) + i * EPV) * ES);
+  }
 
   const float h = a.g_entropy ? a.g_entropy[r] : 0.0f;
   const int64_t y = a.tokens ? a.tokens[r] : -1;
@@ -755,13 +764,6 @@ template <int DT> __global__ __launch_bounds__(kGradBS) void k_lp_grad(LpGradArg
     }
   }
 
-  const uint32_t nvec = hi > body ? (hi - body) / EPV : 0u;
-  u32x4 v[kGradU];
-#pragma unroll
-  for (int u = 0; u < kGradU; ++u) {
-    const uint32_t i = u * BS + tid;
-    if (i < nvec) v[u] = *reinterpret_cast<const u32x4u*>(x + (static_cast<size_t>(body) + i * EPV) * ES);
-  }
 #pragma unroll
   for (int u = 0; u < kGradU; ++u) {
     const uint32_t i = u * BS + tid;
