@@ -422,33 +422,46 @@ __device__ __forceinline__ void mx_gemm_body(const MxGemmArgs& g, uint32_t tiles
 #pragma unroll
       for (int j = 0; j < NJ; ++j) acc[i][j] = f32x16{};
   };
+  // (the stores address the output itself: through a pointer of no known
+  // address space each would wait for the loads to LDS and for the store before)
   auto store = [&](uint32_t tile) {
     using O = std::conditional_t<DT == PROFK_F32, float, __bf16>;
-    const uint32_t m = tile % tiles_m * T::BM + wm * MI * 32 + 4 * h, n = tile / tiles_m * T::BN + wn * NJ * 32 + NJ * c;
-    if (n >= g.N) return;
-    O* p = static_cast<O*>(g.out) + static_cast<size_t>(m) * g.N + n;
-    const bool whole = n + NJ <= g.N;
+    const uint32_t mw = tile % tiles_m * T::BM + wm * MI * 32, nw = tile / tiles_m * T::BN + wn * NJ * 32;
+    const uint32_t m = mw + 4 * h, n = nw + NJ * c;
+    size_t at = static_cast<size_t>(m) * g.N + n;
+    O* const out = static_cast<O*>(g.out);
+    auto put4 = [&](size_t o, int i, int v) {
+      if constexpr (DT == PROFK_F32)
+        *reinterpret_cast<f32x4u*>(out + o) = f32x4{acc[i][0][v], acc[i][1][v], acc[i][2][v], acc[i][3][v]};
+      else
+        *reinterpret_cast<u32x2u*>(out + o) = u32x2u{pack_bf16(acc[i][0][v], acc[i][1][v]), pack_bf16(acc[i][2][v], acc[i][3][v])};
+    };
+    auto rows = [&](auto put) {
 #pragma unroll
-    for (int i = 0; i < MI; ++i) {
-      // (no row's address or mask is kept through the steps)
-      asm volatile("" : "+v"(p));
-      __builtin_amdgcn_sched_barrier(0);
+      for (int i = 0; i < MI; ++i) {
+        // (no row's address or mask is kept through the steps)
+        asm volatile("" : "+v"(at));
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-      for (int v = 0; v < 16; ++v) {
-        const uint32_t r = i * 32 + 8 * (v / 4) + (v % 4);
-        if (m + r >= g.M) continue;
-        O* const o = p + static_cast<size_t>(r) * g.N;
-        if (whole) {
-          if constexpr (DT == PROFK_F32)
-            *reinterpret_cast<f32x4u*>(o) = f32x4{acc[i][0][v], acc[i][1][v], acc[i][2][v], acc[i][3][v]};
-          else
-            *reinterpret_cast<u32x2u*>(o) = u32x2u{pack_bf16(acc[i][0][v], acc[i][1][v]), pack_bf16(acc[i][2][v], acc[i][3][v])};
-        } else {
-          o[0] = static_cast<O>(acc[i][0][v]);
-          if (n + 1 < g.N) o[1] = static_cast<O>(acc[i][1][v]);
-          if (n + 2 < g.N) o[2] = static_cast<O>(acc[i][2][v]);
+        for (int v = 0; v < 16; ++v) {
+          const uint32_t r = i * 32 + 8 * (v / 4) + (v % 4);
+          put(at + static_cast<size_t>(r) * g.N, r, i, v);
         }
       }
+    };
+    if (mw + MI * 32 <= g.M && nw + NJ * 32 <= g.N) {
+      rows([&](size_t o, uint32_t, int i, int v) { put4(o, i, v); });
+    } else {
+      rows([&](size_t o, uint32_t r, int i, int v) {
+        if (m + r >= g.M || n >= g.N) return;
+        if (n + NJ <= g.N) {
+          put4(o, i, v);
+        } else {
+          out[o] = static_cast<O>(acc[i][0][v]);
+          if (n + 1 < g.N) out[o + 1] = static_cast<O>(acc[i][1][v]);
+          if (n + 2 < g.N) out[o + 2] = static_cast<O>(acc[i][2][v]);
+        }
+      });
     }
   };
   start(tile0);
