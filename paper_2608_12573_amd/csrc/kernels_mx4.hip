@@ -42,6 +42,9 @@ __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
 }
 
 // ------------------------------------------------------------- quantise ---
+// Bound by memory: 131072 x 2048 fp32 to codes 248 us (4.9 TB/s read and
+// written), codes to bf16 121 us (5.6 TB/s); a copy of 1 GiB reaches 5.2.
+//
 // A lane takes 8 values, four lanes a block.  The convert instruction divides
 // by its scale and rounds; small blocks are scaled up by 2^64 first, so that
 // neither the values nor the scale are subnormal.
@@ -241,6 +244,16 @@ __device__ __forceinline__ void bare_barrier() {
 // neighbours and are stored together.
 //
 // Rows past M or N are read as the last one and not stored.
+//
+// 256 x 256 tiles on eight waves of 64 x 128: a stage moves 68 KB for 32 matrix
+// instructions a wave, of 32 cycles, two waves a SIMD.  Measured: 4096 x 4096 x
+// 65536 to bf16 566 us (3.9 PFLOP/s), 4096 x 2048 x 131072 665 us (3.3), 4096 x
+// 512 x 12288 to fp32 39 us (5.2 TB/s of output, a copy's rate).  The same
+// instructions on random codes in registers alone reach 6.3 PFLOP/s, the clock
+// falling to about 1.6 GHz (8.8 on zeros); the library's bf16 product of 8192^3
+// 1.2.  Bound by the matrix cores at that clock and, of short K, by the stores.
+// Four waves of 128 x 128 read a third less from LDS and were slower (631 us at
+// 4096 x 4096 x 65536: one wave a SIMD hides no wait).
 template <int WM, int WN, int MI, int NJ> struct MxTile {
   static constexpr int NW = WM * WN, BS = NW * kWave, BM = WM * MI * 32, BN = WN * NJ * 32;
   static constexpr int QA = BM * 8 / BS, QB = BN * 8 / BS;     // loads of a lane: codes
@@ -529,16 +542,20 @@ __global__ __launch_bounds__(WM * WN * 64, WAVES) void k_mx_gemm(MxGemmArgs g, u
 // sits in LDS, its rows 16 bytes apart from a whole number of banks.
 // KSPLIT: the workgroup's waves each take a part of the steps of the same
 // groups, and their sums are added in wave order.
+// Measured: 1 x 4096 x 131072 45 us (6.4 TB/s; a plain read reaches 7).  Loads
+// straight to registers, 32 rows of 32 bytes each, took 81 us, and 114 past
+// the caches.
 constexpr int kMxFewBS = 256;
 constexpr int kMxCodes = -1;                          // a's type where it is quantised already
 constexpr uint32_t kMxFewStage = 32 * 128 + 32 * 8;   // bytes of a wave's stage: codes, then scales
 constexpr int kMxFewLoads = 5;                        // loads of a stage
-// LDS for a: two workgroups a CU, or one.
-constexpr uint32_t kMxFewLdsSmall = 10 * 1024, kMxFewLds = 72 * 1024;
+// LDS for a: beside another workgroup on the CU, or alone.
+constexpr uint32_t kMxFewLdsSmall = 10 * 1024, kMxFewLds = 64 * 1024;
 __host__ __device__ constexpr uint32_t mx_few_row(uint32_t steps) { return steps * 64 + 16; }   // LDS bytes of a row of a
 __host__ __device__ constexpr uint32_t mx_few_lds(uint32_t M, uint32_t steps) { return M * (mx_few_row(steps) + steps * 4); }
-constexpr bool mx_few(uint64_t M, uint64_t steps) {
-  return M <= 32 && steps <= kMxFewLds / 64 && mx_few_lds(static_cast<uint32_t>(M), static_cast<uint32_t>(steps)) <= kMxFewLds;
+// a fits `lds` bytes.
+constexpr bool mx_few(uint64_t M, uint64_t steps, uint32_t lds) {
+  return M <= 32 && steps <= lds / 64 && mx_few_lds(static_cast<uint32_t>(M), static_cast<uint32_t>(steps)) <= lds;
 }
 
 template <int DT, int XDT, bool KSPLIT, int LDS> __device__ __forceinline__ void mx_few_body(const MxGemmArgs& g) {
@@ -690,27 +707,41 @@ template <int DT, int WM, int WN, int MI, int NJ, int PER> void launch_gemm(cons
   else k_mx_gemm<DT, WM, WN, MI, NJ, kWaves, false><<<grid, T::BS, 0, s>>>(g, tm, tiles);
 }
 
-template <int DT, int XDT, int LDS> void launch_few(const MxGemmArgs& g, uint32_t cus, uint32_t per_cu, hipStream_t s) {
-  // few groups: the waves of a workgroup share one
-  const uint32_t groups = (g.N + 31) / 32, most = per_cu * cus;
-  if (groups < 4 * cus && g.steps >= 8) k_mx_few<DT, XDT, true, LDS><<<groups < most ? groups : most, kMxFewBS, 0, s>>>(g);
-  else k_mx_few<DT, XDT, false, LDS><<<(groups + 3) / 4 < most ? (groups + 3) / 4 : most, kMxFewBS, 0, s>>>(g);
-}
-
-template <int DT, int XDT> void launch_few_any(const MxGemmArgs& g, uint32_t cus, hipStream_t s) {
-  if (mx_few_lds(g.M, g.steps) <= kMxFewLdsSmall) launch_few<DT, XDT, kMxFewLdsSmall>(g, cus, 2, s);
-  else if constexpr (XDT == kMxCodes) launch_few<DT, XDT, kMxFewLds>(g, cus, 1, s);
+// The kernel of few rows, true, or none (false: the tiled product's case).
+// Where a fits beside a second workgroup's stages it is the faster one, and it
+// quantises a itself (K = 4096, N = 131072, with the quantisation: M = 1 50 us).
+// With a larger a it is so where the waves of a workgroup share the steps of a
+// group, as they do where the groups are few (M = 8, K = 4096, N = 8192: 9
+// against 13 us); without sharing it is not (M = 16 and 32, N = 131072: 61 and
+// 71 against 57 and 62 us).
+template <int DT, int XDT> bool launch_few(const MxGemmArgs& g, uint32_t cus, hipStream_t s) {
+  const uint32_t groups = (g.N + 31) / 32;
+  const bool share = groups < 4 * cus && g.steps >= 8;
+  if (mx_few(g.M, g.steps, kMxFewLdsSmall)) {
+    const uint32_t most = 2 * cus;
+    if (share) k_mx_few<DT, XDT, true, kMxFewLdsSmall><<<groups < most ? groups : most, kMxFewBS, 0, s>>>(g);
+    else k_mx_few<DT, XDT, false, kMxFewLdsSmall><<<(groups + 3) / 4 < most ? (groups + 3) / 4 : most, kMxFewBS, 0, s>>>(g);
+    return true;
+  }
+  if constexpr (XDT == kMxCodes) {
+    if (share && mx_few(g.M, g.steps, kMxFewLds)) {
+      k_mx_few<DT, XDT, true, kMxFewLds><<<groups < cus ? groups : cus, kMxFewBS, 0, s>>>(g);
+      return true;
+    }
+  }
+  return false;
 }
 
 template <int DT> void launch_product(const MxGemmArgs& g, int x_dtype, uint32_t cus, hipStream_t s) {
-  if (mx_few(g.M, g.steps)) {
-    if (!g.x) launch_few_any<DT, kMxCodes>(g, cus, s);
-    else if (x_dtype == PROFK_F32) launch_few_any<DT, PROFK_F32>(g, cus, s);
-    else launch_few_any<DT, PROFK_BF16>(g, cus, s);
+  if (!g.x ? launch_few<DT, kMxCodes>(g, cus, s)
+           : x_dtype == PROFK_F32 ? launch_few<DT, PROFK_F32>(g, cus, s) : launch_few<DT, PROFK_BF16>(g, cus, s))
     return;
-  }
-  const uint64_t big = static_cast<uint64_t>((g.M + 255) / 256) * ((g.N + 255) / 256);
-  if (g.M > 128 && big >= 128) launch_gemm<DT, 4, 2, 2, 4, 1>(g, cus, s);
+  // Tiles of 256 x 256 where every CU has one, else two workgroups a CU of 128 x
+  // 128 (M x K x N, us with the larger and the smaller: 2048 x 4096 x 4096, 128
+  // large tiles, 29 and 23; 2048 x 4096 x 8192, 256 of them, 36 and 42; 512 x 2048
+  // x 50000, 392, 33 and 35; 128 x 4096 x 131072, half of each empty, 91 and 70).
+  const uint64_t large = static_cast<uint64_t>((g.M + 255) / 256) * ((g.N + 255) / 256);
+  if (g.M > 128 && large >= cus) launch_gemm<DT, 4, 2, 2, 4, 1>(g, cus, s);
   else launch_gemm<DT, 4, 1, 1, 4, 2>(g, cus, s);
 }
 
@@ -760,9 +791,7 @@ hipError_t launch_mx_dequantize(int dtype, const uint8_t* codes, const uint8_t* 
 // is larger, that every workgroup does so costs more (K = 4096, N = 131072:
 // M = 4 59.2 us against 55.2 and the launch, M = 16 77.9 against 63.7 and it).
 bool mx_quantizes_x(int64_t M, int64_t K) {
-  const uint64_t steps = mx_steps(K);
-  return mx_few(static_cast<uint64_t>(M), steps) &&
-         mx_few_lds(static_cast<uint32_t>(M), static_cast<uint32_t>(steps)) <= kMxFewLdsSmall;
+  return mx_few(static_cast<uint64_t>(M), mx_steps(K), kMxFewLdsSmall);
 }
 
 hipError_t launch_mx_matmul(const MxMatmulCall& c) {
