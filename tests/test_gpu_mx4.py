@@ -115,7 +115,8 @@ def _pair(M, N, K, seed):
 
 SIZES = [(1, 1, 1), (1, 7, 33), (2, 64, 32), (3, 129, 128), (1, 1000, 4096), (17, 255, 257), (31, 33, 512), (33, 513, 640),
          (64, 64, 1000), (77, 501, 1000), (127, 130, 384), (128, 128, 128), (129, 257, 129), (255, 511, 896),
-         (256, 256, 256), (300, 700, 2048), (513, 1025, 768), (1000, 37, 1500), (5, 70001, 300)]
+         (256, 256, 256), (300, 700, 2048), (513, 1025, 768), (1000, 37, 1500), (5, 70001, 300),
+         (20, 300, 2048), (32, 1001, 3001), (3, 40000, 1000), (1, 140001, 130), (600, 30000, 512), (1025, 33001, 300)]
 
 
 @pytest.mark.parametrize("M,N,K", SIZES)
