@@ -6,6 +6,8 @@
 #include <mutex>
 
 #include "launch.h"
+#include "logprobs.h"
+#include "mx4.h"
 #include "plan_internal.h"
 #include "profk.h"
 

@@ -27,15 +27,16 @@
 // take the row's best of what is left.
 //
 // Measured: 4096 x 131072 bf16 with 20 alternatives 194 us (5.5 TB/s), without
-// 178 (6.0): about 7 instructions a logit, one of them the exponential at a
-// quarter of the others' rate, keep the SIMDs 80 % busy beside the loads, so
-// that 16-bit rows are bound by both; 32-bit rows by memory.  16384 x 512 fp32
+// 178 (6.0): 9 and 7 vector instructions a logit keep the SIMDs busy for 77 and
+// 68 % of the time beside the loads, so that 16-bit rows are bound by both;
+// 32-bit rows by memory.  16384 x 512 fp32
 // with 8 alternatives 18 us, without 10: the selection's instructions.  64 x
 // 100003 fp32 14 us and 5 for the join, 1 x 131072 8 and 5: latency.
 #include <type_traits>
 
 #include "device_common.h"
 #include "launch.h"
+#include "logprobs.h"
 
 namespace profk {
 

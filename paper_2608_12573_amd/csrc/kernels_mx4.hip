@@ -22,6 +22,7 @@
 
 #include "device_common.h"
 #include "launch.h"
+#include "mx4.h"
 
 namespace profk {
 

@@ -302,85 +302,6 @@ size_t sae_decode_workspace(uint32_t B, uint32_t K);
 uint32_t sae_decode_max_dict();
 hipError_t launch_sae_decode(const SaeDecodeCall& c);
 
-// Token log probabilities, entropy and alternatives of rows of logits, and
-// their gradient (kernels_logprobs.hip).
-constexpr int64_t kLpMaxTop = 64;             // most alternatives of a row
-constexpr int kLpWaveBytes = 8192;            // longest row (or chunk) that one wave takes
-constexpr int64_t kLpMinChunk = 2048;         // shortest chunk of a row split over workgroups
-constexpr int64_t kLpMaxChunks = 256;
-constexpr int kLpJoinBS = 256;
-constexpr int kLpPart = 4;                    // words of a chunk's statistics
-
-struct LpArgs {
-  const void* x;
-  uint64_t stride;      // elements between row starts
-  uint32_t V, n;        // n: alternatives (0: none)
-  const int64_t* tokens;
-  float *logprob, *entropy, *lse, *top;
-  int64_t* top_idx;
-  uint32_t row;         // first row of this launch
-  uint32_t G, chunk;    // chunks of a row, and their elements
-  float* part;          // G > 1: the chunks' statistics
-  uint64_t* part_top;   // ... and their n best
-};
-
-struct LpLayout {
-  uint32_t G = 1, chunk = 0;
-  size_t off_top = 0, bytes = 0;              // workspace (0: none)
-};
-
-LpLayout lp_layout(int64_t T, int64_t V, int64_t n, int num_cus);
-
-struct LpCall {
-  int dtype;
-  int64_t T;
-  LpArgs a;
-  LpLayout L;
-  uint8_t* ws;
-  hipStream_t stream;
-};
-
-hipError_t launch_logprobs(LpCall c);
-
-struct LpGradArgs {
-  const void* x;
-  uint64_t stride;
-  uint32_t V, n;
-  const int64_t* tokens;                      // null: no token has a gradient
-  const float *lse, *entropy, *g_logprob, *g_entropy, *g_top;
-  const int64_t* top_idx;
-  void* out;
-  uint64_t out_stride;
-  uint32_t row, pieces;                       // first row of this launch; workgroups of a row
-};
-
-hipError_t launch_logprobs_grad(LpGradArgs a, int dtype, int64_t T, hipStream_t s);
-
-// Microscaled 4-bit values (kernels_mx4.hip): K padded to whole steps of 128,
-// 64 bytes of codes and 4 of scales each (of rows padded to groups of 32).
-uint64_t mx_steps(int64_t K);
-constexpr int64_t kMxMaxK = 1 << 20;
-hipError_t launch_mx_quantize(int dtype, const void* x, uint64_t stride, int64_t R, int64_t K, uint8_t* codes,
-                              uint8_t* scales, hipStream_t s);
-hipError_t launch_mx_dequantize(int dtype, const uint8_t* codes, const uint8_t* scales, int64_t R, int64_t K,
-                                void* out, hipStream_t s);
-
-struct MxMatmulCall {
-  const uint8_t *a, *as;      // codes and scales [M, ..]
-  const uint8_t *b, *bs;      // ... [N, ..]
-  int64_t M, N, K;
-  int out_dtype;
-  void* out;                  // [M, N]
-  hipStream_t stream;
-  const void* x;              // set: a is not quantised yet (mx_quantizes_x)
-  uint64_t x_stride;
-  int x_dtype;
-};
-
-// The product's kernel for this shape quantises a itself.
-bool mx_quantizes_x(int64_t M, int64_t K);
-hipError_t launch_mx_matmul(const MxMatmulCall& c);
-
 // Inspection helpers.
 hipError_t launch_sample_indices(uint64_t seed, uint64_t row, uint32_t S, uint64_t N,
                                  int64_t* out, hipStream_t s);
