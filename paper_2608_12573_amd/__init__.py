@@ -547,7 +547,6 @@ def debug_sae_sample(x, w_enc, b_enc, p, seed=0, ws=None):
     return keys.to(torch.int64) & 0xFFFFFFFF
 
 
-
 # ------------------------------------------- rows of logits: probabilities ---
 
 MAX_TOP = 64                       # most alternatives of a row
@@ -732,10 +731,10 @@ def _dense_out(shape, dtype, default, out, device):
     torch = _torch()
     if out is None:
         out = torch.empty(shape, dtype=dtype or default, device=device)
-    elif dtype is not None and out.dtype != dtype:
-        raise ProfkError(f"out is {out.dtype}, not {dtype}")
     elif not isinstance(out, torch.Tensor):
         raise ProfkError("out must be a torch tensor")
+    elif dtype is not None and out.dtype != dtype:
+        raise ProfkError(f"out is {out.dtype}, not {dtype}")
     _vector(out, "out", out.dtype, shape, device)
     return out, _dtype_code(out)
 

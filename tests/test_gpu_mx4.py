@@ -273,3 +273,21 @@ def test_refusals_on_the_device():
     for call in bad:
         with pytest.raises(pk.ProfkError):
             call()
+
+
+def test_output_refusals():
+    t = torch()
+    x = t.ones(4, 100, device="cuda")
+    q = pk.mx4_quantize(x)
+    for out, dtype, match in (([0.0], t.float32, "torch tensor"), ([0.0], None, "torch tensor"),
+                              (t.empty(4, 4, device="cuda"), t.bfloat16, "not torch.bfloat16"),
+                              (t.empty(4, 5, device="cuda"), None, "shape"),
+                              (t.empty(4, 4), None, "CUDA tensor"),
+                              (t.empty(4, 4, device="cuda").half(), None, "unsupported dtype")):
+        print(match, dtype, flush=True)
+        for call in (lambda: pk.mx4_matmul(*q, *q, 100, dtype=dtype, out=out),
+                     lambda: pk.mx4_linear(x, *q, dtype=dtype, out=out)):
+            with pytest.raises(pk.ProfkError, match=match):
+                call()
+    with pytest.raises(pk.ProfkError, match="4 rows"):
+        pk.mx4_quantize(x, out=pk.mx4_outputs(5, 100, "cuda"))
