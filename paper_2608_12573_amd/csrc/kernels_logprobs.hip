@@ -10,11 +10,12 @@
 // k_lp reads a row once.  A lane keeps s = sum 2^t and q = sum 2^t t over
 // t = x L - c, L = log2(e) in fp32, with c of its wave, so that
 //   log2 sum = c + log2 s  and  H = ln 2 (log2 s - q / s).
-// c is a whole number near the wave's largest x L, changed only when a logit
-// passes it by 16 powers of two; fp32 holds it exactly, so t is rounded once
-// (one fma), and dividing the final c + log2 s by the same L leaves of L's own
-// rounding (a relative 1.3e-8, as if the row had another temperature) no more
-// than 1.3e-8 H in lse.
+// c is the whole number nearest to the wave's largest x L so far; fp32 holds it
+// exactly, so t is rounded once (one fma), and dividing the final c + log2 s by
+// the same L leaves of L's own rounding (a relative 1.3e-8, as if the row had
+// another temperature) no more than 1.3e-8 H in lse.  No t passes 1/2: where c
+// is left behind, log2 s and q / s grow by as much as it is behind, and their
+// difference loses what they were rounded by (16 powers of two: 2e-6 of H).
 //
 // Alternatives need no second pass.  Of each of the NW waves the n / NW-th best
 // of its lanes' maxima of the first step is taken; the least of them bounds the
@@ -45,7 +46,6 @@ namespace {
 constexpr float kL2E = 1.44269504088896340736f;   // log2(e), rounded to fp32
 constexpr double kLn2 = 0.69314718055994530942;
 constexpr float kNegInf = -__builtin_inff();
-constexpr float kLpSlack = 16.0f;    // powers of two a term may pass c by
 constexpr float kLpFloor = -300.0f;  // least exponent: 2^-300 is 0 in fp32, and 0 * -300 is no NaN
 // Rows with a logit past this (or +inf, or NaN) are summed by the careful
 // path, as are rows of nothing above its negative: x L must not overflow, and
@@ -197,8 +197,10 @@ __device__ __forceinline__ double log2_of(float s) {
   }
   return static_cast<double>(e) + static_cast<double>(__builtin_amdgcn_logf(f));
 }
+// (the roundings of q and s may leave a row of one logit just below 0)
 __device__ __forceinline__ float entropy_of(double l2, float q, float s) {
-  return static_cast<float>(kLn2 * (l2 - static_cast<double>(q / s)));
+  const float h = static_cast<float>(kLn2 * (l2 - static_cast<double>(q / s)));
+  return h < 0.0f ? 0.0f : h;
 }
 __device__ __forceinline__ RowStats row_stats(const Stats& t) {
   constexpr double kInv = 1.0 / static_cast<double>(kL2E);
@@ -456,7 +458,7 @@ __global__ __launch_bounds__(BS) void k_lp(LpArgs a) {
   const float own = tid < ns ? E::load(x, own_i) : kNegInf;
 
   Stats st{-kLpLarge * kL2E, 0.0f, 0.0f, 0u};   // c: the wave's
-  float lim = -kLpLarge;                        // the largest logit that c takes
+  float lim = -kLpLarge;                        // the largest logit that c has been set for
   // some lane's m passed lim, or is NaN; the whole wave calls it
   auto rebase = [&](float m) {
     if (__ballot(!(m <= kLpLarge))) {
@@ -467,7 +469,7 @@ __global__ __launch_bounds__(BS) void k_lp(LpArgs a) {
     const float c = lane_f(rintf(fmaxf(m, -kLpLarge) * kL2E), 0);
     shift(st.s, st.q, st.c - c);
     st.c = c;
-    lim = lane_f(m + kLpSlack / kL2E, 0);
+    lim = lane_f(m, 0);
   };
   // z's term; FLOOR: z may be -inf, or as low as makes t -inf
   auto term = [&](float z, auto floor) {
@@ -529,7 +531,7 @@ __global__ __launch_bounds__(BS) void k_lp(LpArgs a) {
     if (BS > kWave && step) blank(step, v);
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      // one compare for both: past c's range, or a candidate
+      // one compare for both: a larger logit than c is set for, or a candidate
       const float m = vec_max(v[u]);
       if (__ballot(!(m < (TOP ? fminf(lim, boundf) : lim)))) {
         if (__ballot(!(m <= lim))) rebase(m);
