@@ -42,13 +42,14 @@ def train(w, x, y, steps, lr, entropy_weight):
     g_h = given * (-entropy_weight / given.sum())
     out = pk.token_logprobs_outputs(x.shape[0], 0, x.device)
     ws = pk.token_logprobs_workspace(x.shape[0], w.shape[0], 0, x.device)
+    low = torch.empty(x.shape[0], device=x.device)
     d = torch.empty((x.shape[0], w.shape[0]), device=x.device)
     xf, m, history = x.float(), torch.zeros_like(w), []
     for _ in range(steps):
         logits = xf @ w.t()
-        lp, h, lse, _, _ = pk.token_logprobs(logits, y, ws=ws, out=out)
+        lp, h, lse, _, _ = pk.token_logprobs(logits, y, ws=ws, out=out, lse_low=low)
         history.append((lp.sum() / given.sum()).item())
-        pk.token_logprobs_grad(logits, y, lse, h, g_lp, g_h, out=d)
+        pk.token_logprobs_grad(logits, y, lse, h, g_lp, g_h, out=d, lse_low=low)
         m.mul_(0.9).add_(d.t() @ xf)
         w.sub_(m, alpha=lr)
     return history

@@ -314,7 +314,8 @@ int profk_debug_sae_sample(const profk_plan_t* plan, const void* x, const void* 
  *   logprob = x_y - lse
  *   entropy = -sum_j p_j log p_j  (terms with p_j = 0 are 0)
  *   alternatives: the n_top largest x_j in the total order, as (x_j - lse, j).
- * All sums are fp32; a row's last step is taken in 64 bits.
+ * All sums are fp32; a row's last step is taken in 64 bits and rounded once.
+ * entropy is never below 0.
  *
  *   logits   fp32 or bf16 [T, V], rows row_stride elements apart.  T = 0 is
  *            accepted and does nothing; 1 <= V <= 2^31 - 1.
@@ -340,12 +341,22 @@ int profk_token_logprobs(int32_t dtype, const void* logits, int64_t T, int64_t V
                          float* out_lse, float* out_top_logprob, int64_t* out_top_idx, void* ws,
                          size_t ws_bytes, void* stream);
 
+/* The same, and out_lse_low fp32 [T]: what the rounding of lse to fp32 leaves,
+ * so that lse + lse_low is the log-sum-exp as the row's sums give it (0 where
+ * lse is not finite).  NULL: profk_token_logprobs. */
+int profk_token_logprobs_ex(int32_t dtype, const void* logits, int64_t T, int64_t V, int64_t row_stride,
+                            const int64_t* tokens, int64_t n_top, float* out_logprob, float* out_entropy,
+                            float* out_lse, float* out_lse_low, float* out_top_logprob, int64_t* out_top_idx,
+                            void* ws, size_t ws_bytes, void* stream);
+
 /* The gradient of sum_r g_logprob[r] logprob[r] + g_entropy[r] entropy[r] +
  * sum_i g_top[r, i] top_logprob[r, i] with respect to the logits:
  *   out_j = g ([j = y] - p_j) - h p_j (log p_j + H) + sum_i t_i ([j = a_i] - p_j)
- * rounded once to the logits' dtype.  lse and entropy are the forward call's;
- * where an lse is 16384 or more in size, too coarse in fp32 for p, it is taken
- * from the row again (slowly).
+ * computed in fp32 and rounded once to the logits' dtype.  lse and entropy are
+ * the forward call's.  From an lse that is rounded to fp32, all p_j of its row
+ * are off by one common factor, up to 2^-24 |lse| from 1: 6e-6 at 100, 6e-5 at
+ * 1000.  Where |lse| is 16384 or more it is taken from the row again (slowly: by
+ * each workgroup of the row).  profk_token_logprobs_grad_ex has neither.
  * top_idx may be the call's alternatives or any other indices.  g_logprob (with
  * tokens), g_entropy (with entropy) and the alternatives (n_top = 0) may each
  * be left out as NULL.  top_idx entries that are negative or V and more take
@@ -357,6 +368,15 @@ int profk_token_logprobs_grad(int32_t dtype, const void* logits, int64_t T, int6
                               const float* g_logprob, const float* g_entropy, int64_t n_top,
                               const int64_t* top_idx, const float* g_top, void* out, int64_t out_stride,
                               void* stream);
+
+/* The same from the forward call's lse and lse_low, p_j = exp((x_j - lse) -
+ * lse_low): no less exact for a large lse, and no row is read again.  lse_low =
+ * NULL: profk_token_logprobs_grad. */
+int profk_token_logprobs_grad_ex(int32_t dtype, const void* logits, int64_t T, int64_t V, int64_t row_stride,
+                                 const int64_t* tokens, const float* lse, const float* lse_low,
+                                 const float* entropy, const float* g_logprob, const float* g_entropy,
+                                 int64_t n_top, const int64_t* top_idx, const float* g_top, void* out,
+                                 int64_t out_stride, void* stream);
 
 /* ---- Microscaled 4-bit floating point (MXFP4) ----
  *

@@ -97,6 +97,26 @@ def grad_row(x, y, lse, h, g_lp, g_h, top_idx, g_top):
     return d
 
 
+def grad_of_logits(x, y, g_lp, g_h, top_idx, g_top):
+    """The gradient of grad_row's sum from the logits alone: the gradients of
+    the log probabilities l, then through l = x - lse (dl_i/dx_j = [i = j] -
+    p_j); H = -sum p l adds -p (l + 1) to the former.  A row with a value of
+    its own (finite lse), y below V."""
+    x = np.asarray(x, dtype=np.float64)
+    l = log_softmax(x)
+    p = np.exp(l)
+    u = np.zeros(x.size)
+    if g_lp is not None and y >= 0:
+        u[y] += g_lp
+    for j, t in zip(top_idx, g_top):
+        if 0 <= j < x.size:
+            u[j] += t
+    if g_h is not None:
+        on = p > 0
+        u[on] -= g_h * p[on] * (l[on] + 1.0)
+    return u - p * u.sum()
+
+
 def grad_scale(x, y, lse, h, g_lp, g_h, top_idx, g_top):
     """The magnitude that a rounded gradient's error is proportional to: the
     sum of the terms' magnitudes, each p's error growing with |x - lse|."""

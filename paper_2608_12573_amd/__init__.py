@@ -117,7 +117,9 @@ def lib():
         L.profk_token_logprobs_workspace_size.argtypes = [i64, i64, i64]
         L.profk_token_logprobs_workspace_size.restype = sz
         L.profk_token_logprobs.argtypes = [i32, vp, i64, i64, i64, vp, i64, vp, vp, vp, vp, vp, vp, sz, vp]
+        L.profk_token_logprobs_ex.argtypes = [i32, vp, i64, i64, i64, vp, i64, vp, vp, vp, vp, vp, vp, vp, sz, vp]
         L.profk_token_logprobs_grad.argtypes = [i32, vp, i64, i64, i64, vp, vp, vp, vp, vp, i64, vp, vp, vp, i64, vp]
+        L.profk_token_logprobs_grad_ex.argtypes = [i32, vp, i64, i64, i64, vp, vp, vp, vp, vp, vp, i64, vp, vp, vp, i64, vp]
         for f in (L.profk_mx4_codes_size, L.profk_mx4_scales_size):
             f.argtypes, f.restype = [i64, i64], sz
         L.profk_mx4_linear_workspace_size.argtypes = [i64, i64, i64]
@@ -604,7 +606,7 @@ def token_logprobs_outputs(T, n_top=0, device="cuda"):
             torch.empty((T, n_top), dtype=torch.int64, device=device))
 
 
-def token_logprobs(logits, tokens, n_top=0, ws=None, out=None):
+def token_logprobs(logits, tokens, n_top=0, ws=None, out=None, lse_low=None):
     """Log probabilities of the given tokens under softmax(logits), with each
     row's entropy, log-sum-exp and n_top most probable alternatives:
     (logprob [T], entropy [T], lse [T], top_logprob [T, n_top],
@@ -613,13 +615,17 @@ def token_logprobs(logits, tokens, n_top=0, ws=None, out=None):
     logits: fp32 or bf16 [T, V], rows may be strided.  tokens: int64 [T];
     negative for rows without a token (logprob 0), NaN results from V up.
     Alternatives are most probable first, equal ones by smaller index; logits
-    of -inf are never among them ((-inf, -1) where too few are left)."""
+    of -inf are never among them ((-inf, -1) where too few are left).
+    lse_low: fp32 [T] that takes what rounding lse to fp32 leaves, for
+    token_logprobs_grad."""
     torch = _torch()
     dt, T, V, stride = _rows(logits, "logits")
     dev = logits.device
     _vector(tokens, "tokens", torch.int64, (T,), dev)
     if not 0 <= n_top <= MAX_TOP:
         raise ProfkError(f"n_top must be from 0 to {MAX_TOP}, got {n_top}")
+    if lse_low is not None:
+        _vector(lse_low, "lse_low", torch.float32, (T,), dev)
     L = lib()
     n = L.profk_token_logprobs_workspace_size(T, V, n_top)
     if ws is not None:
@@ -635,23 +641,28 @@ def token_logprobs(logits, tokens, n_top=0, ws=None, out=None):
         _vector(out[2], "out[2]", f32, one, dev)
         _vector(out[3], "out[3]", f32, (T, n_top), dev)
         _vector(out[4], "out[4]", torch.int64, (T, n_top), dev)
-    _check(L.profk_token_logprobs(dt, logits.data_ptr(), T, V, stride, tokens.data_ptr(), n_top, out[0].data_ptr(),
-                                  out[1].data_ptr(), out[2].data_ptr(), out[3].data_ptr(), out[4].data_ptr(),
-                                  ws.data_ptr() if n else None, n, _stream()))
+    _check(L.profk_token_logprobs_ex(dt, logits.data_ptr(), T, V, stride, tokens.data_ptr(), n_top, out[0].data_ptr(),
+                                     out[1].data_ptr(), out[2].data_ptr(), _ptr(lse_low), out[3].data_ptr(),
+                                     out[4].data_ptr(), ws.data_ptr() if n else None, n, _stream()))
     return out
 
 
-def token_logprobs_grad(logits, tokens, lse, entropy, g_logprob, g_entropy=None, top_idx=None, g_top=None, out=None):
+def token_logprobs_grad(logits, tokens, lse, entropy, g_logprob, g_entropy=None, top_idx=None, g_top=None, out=None,
+                        lse_low=None):
     """The gradient with respect to the logits of token_logprobs' outputs,
     given theirs: g_logprob [T], g_entropy [T] or None, and g_top [T, n] for
     the alternatives at top_idx [T, n] or None.  lse and entropy are
-    token_logprobs'.  out: the logits' dtype and shape, rows may be strided;
-    it must not overlap the logits."""
+    token_logprobs', and so is lse_low: without it the row's probabilities are
+    those of an lse rounded to fp32, all off by up to 2^-24 |lse| of
+    themselves.  out: the logits' dtype and shape, rows may be strided; it must
+    not overlap the logits."""
     torch = _torch()
     dt, T, V, stride = _rows(logits, "logits")
     dev, f32, one = logits.device, torch.float32, (T,)
     _vector(tokens, "tokens", torch.int64, one, dev)
     _vector(lse, "lse", f32, one, dev)
+    if lse_low is not None:
+        _vector(lse_low, "lse_low", f32, one, dev)
     if entropy is not None:
         _vector(entropy, "entropy", f32, one, dev)
     if g_logprob is not None:
@@ -673,10 +684,10 @@ def token_logprobs_grad(logits, tokens, lse, entropy, g_logprob, g_entropy=None,
     if ot != dt or oT != T or oV != V:
         raise ProfkError("out must have the logits' dtype and shape")
     _on_device(out, "out", dev)
-    _check(lib().profk_token_logprobs_grad(dt, logits.data_ptr(), T, V, stride, tokens.data_ptr(), lse.data_ptr(),
-                                           _ptr(entropy), _ptr(g_logprob), _ptr(g_entropy), n,
-                                           top_idx.data_ptr() if n else None, g_top.data_ptr() if n else None,
-                                           out.data_ptr(), ostride, _stream()))
+    _check(lib().profk_token_logprobs_grad_ex(dt, logits.data_ptr(), T, V, stride, tokens.data_ptr(), lse.data_ptr(),
+                                              _ptr(lse_low), _ptr(entropy), _ptr(g_logprob), _ptr(g_entropy), n,
+                                              top_idx.data_ptr() if n else None, g_top.data_ptr() if n else None,
+                                              out.data_ptr(), ostride, _stream()))
     return out
 
 

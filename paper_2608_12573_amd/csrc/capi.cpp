@@ -334,6 +334,14 @@ int profk_token_logprobs(int32_t dtype, const void* logits, int64_t T, int64_t V
                          const int64_t* tokens, int64_t n_top, float* out_logprob, float* out_entropy,
                          float* out_lse, float* out_top_logprob, int64_t* out_top_idx, void* ws, size_t ws_bytes,
                          void* stream) {
+  return profk_token_logprobs_ex(dtype, logits, T, V, row_stride, tokens, n_top, out_logprob, out_entropy, out_lse,
+                                 nullptr, out_top_logprob, out_top_idx, ws, ws_bytes, stream);
+}
+
+int profk_token_logprobs_ex(int32_t dtype, const void* logits, int64_t T, int64_t V, int64_t row_stride,
+                            const int64_t* tokens, int64_t n_top, float* out_logprob, float* out_entropy,
+                            float* out_lse, float* out_lse_low, float* out_top_logprob, int64_t* out_top_idx,
+                            void* ws, size_t ws_bytes, void* stream) {
   const int rc = check_logits(dtype, T, V, row_stride, n_top);
   if (rc != PROFK_OK || T == 0) return rc;
   if (!logits || !tokens || !out_logprob || !out_entropy || !out_lse) return PROFK_ENULL;
@@ -353,6 +361,7 @@ int profk_token_logprobs(int32_t dtype, const void* logits, int64_t T, int64_t V
   c.a.logprob = out_logprob;
   c.a.entropy = out_entropy;
   c.a.lse = out_lse;
+  c.a.lse_low = out_lse_low;
   c.a.top = out_top_logprob;
   c.a.top_idx = out_top_idx;
   c.L = L;
@@ -367,6 +376,15 @@ int profk_token_logprobs_grad(int32_t dtype, const void* logits, int64_t T, int6
                               const float* g_logprob, const float* g_entropy, int64_t n_top,
                               const int64_t* top_idx, const float* g_top, void* out, int64_t out_stride,
                               void* stream) {
+  return profk_token_logprobs_grad_ex(dtype, logits, T, V, row_stride, tokens, lse, nullptr, entropy, g_logprob,
+                                      g_entropy, n_top, top_idx, g_top, out, out_stride, stream);
+}
+
+int profk_token_logprobs_grad_ex(int32_t dtype, const void* logits, int64_t T, int64_t V, int64_t row_stride,
+                                 const int64_t* tokens, const float* lse, const float* lse_low, const float* entropy,
+                                 const float* g_logprob, const float* g_entropy, int64_t n_top,
+                                 const int64_t* top_idx, const float* g_top, void* out, int64_t out_stride,
+                                 void* stream) {
   const int rc = check_logits(dtype, T, V, row_stride, n_top);
   if (rc != PROFK_OK) return rc;
   if (check_logits(dtype, T, V, out_stride, n_top) != PROFK_OK) return PROFK_EINVAL;
@@ -386,6 +404,7 @@ int profk_token_logprobs_grad(int32_t dtype, const void* logits, int64_t T, int6
   a.n = static_cast<uint32_t>(n_top);
   a.tokens = g_logprob ? tokens : nullptr;
   a.lse = lse;
+  a.lse_low = lse_low;
   a.entropy = entropy;
   a.g_logprob = g_logprob;
   a.g_entropy = g_entropy;

@@ -373,7 +373,13 @@ template <int BS> __device__ __forceinline__ uint64_t bound_of(uint64_t best, ui
 __device__ __forceinline__ void write_row(const LpArgs& a, uint32_t r, const RowStats& t, const uint64_t* list,
                                           uint32_t found, float xy, int64_t y) {
   if (threadIdx.x == 0) {
-    a.lse[r] = static_cast<float>(t.m + t.ls);
+    const float lse = static_cast<float>(t.m + t.ls);
+    a.lse[r] = lse;
+    // (from m first: beside an m of the lowest value the sum has lost ls)
+    if (a.lse_low) {
+      const bool finite = fabsf(lse) < __builtin_inff();
+      a.lse_low[r] = finite ? static_cast<float>((t.m - static_cast<double>(lse)) + t.ls) : 0.0f;
+    }
     a.entropy[r] = t.h;
     float lp = 0.0f;                                              // no token
     if (y >= static_cast<int64_t>(a.V)) lp = __builtin_nanf("");  // not a token
@@ -693,9 +699,11 @@ constexpr int kGradU = 4;
 
 typedef uint32_t u32x4u __attribute__((ext_vector_type(4), aligned(2)));   // at any element's address
 
-// From this size on an fp32 lse is too coarse for p (2^-10 of it off, and
-// useless beside a row of the lowest value), and the row's statistics are
-// taken from its logits again.
+// An lse rounded to fp32 alone leaves all of a row's p off by half a unit in its
+// last place, 2^-24 of |lse| at most; with what the rounding left (lse_low) they
+// are as exact as x - lse is.  Without it, from this size on lse is too coarse
+// (2^-10 of p off, and useless beside a row of the lowest value), and the row's
+// statistics are taken from its logits again, by each of its workgroups.
 constexpr float kCoarseLse = 16384.0f;
 
 struct GradRow {
@@ -736,6 +744,9 @@ template <int DT> __global__ __launch_bounds__(kGradBS) void k_lp_grad(LpGradArg
     if (i < nvec) v[u] = *reinterpret_cast<const u32x4u*>(x + (static_cast<size_t>(body) + i * EPV) * ES);
   }
 
+  GradRow g;
+  g.m = a.lse[r];
+  g.ls = a.lse_low ? a.lse_low[r] : 0.0f;
   const float h = a.g_entropy ? a.g_entropy[r] : 0.0f;
   const int64_t y = a.tokens ? a.tokens[r] : -1;
   float gy = a.g_logprob && y >= 0 ? a.g_logprob[r] : 0.0f;
@@ -745,11 +756,8 @@ template <int DT> __global__ __launch_bounds__(kGradBS) void k_lp_grad(LpGradArg
   const int64_t* const at = a.n ? a.top_idx + r * a.n : nullptr;
   for (uint32_t i = 0; i < a.n; ++i)
     if (at[i] >= 0 && at[i] < static_cast<int64_t>(a.V)) G += gt[i];
-  GradRow g;
-  g.m = a.lse[r];
-  g.ls = 0.0f;
   g.empty = g.m == kNegInf;
-  if (fabsf(g.m) >= kCoarseLse && fabsf(g.m) < __builtin_inff()) {
+  if (!a.lse_low && fabsf(g.m) >= kCoarseLse && fabsf(g.m) < __builtin_inff()) {
     const RowStats t = careful_stats<DT, BS>(x, a.V, s_stats);
     g.m = static_cast<float>(t.m);
     g.ls = static_cast<float>(t.ls);
@@ -759,7 +767,7 @@ template <int DT> __global__ __launch_bounds__(kGradBS) void k_lp_grad(LpGradArg
   if (a.g_entropy) g.a = -fmaf(h, a.entropy[r], G);
   if (!(g.m == g.m)) g.a = __builtin_nanf("");
   if (g.empty) {
-    g.m = 0.0f;
+    g.m = g.ls = 0.0f;
     g.a = g.b = 0.0f;
   }
   // the elements of this piece that take a gradient of their own

@@ -21,7 +21,7 @@ struct LpArgs {
   uint64_t stride;      // elements between row starts
   uint32_t V, n;        // n: alternatives (0: none)
   const int64_t* tokens;
-  float *logprob, *entropy, *lse, *top;
+  float *logprob, *entropy, *lse, *lse_low, *top;   // lse_low: null, or what lse's rounding leaves
   int64_t* top_idx;
   uint32_t row;         // first row of this launch
   uint32_t G, chunk;    // chunks of a row, and their elements
@@ -52,7 +52,7 @@ struct LpGradArgs {
   uint64_t stride;
   uint32_t V, n;
   const int64_t* tokens;                      // null: no token has a gradient
-  const float *lse, *entropy, *g_logprob, *g_entropy, *g_top;
+  const float *lse, *lse_low, *entropy, *g_logprob, *g_entropy, *g_top;   // lse_low: may be null
   const int64_t* top_idx;
   void* out;
   uint64_t out_stride;
