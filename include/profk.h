@@ -370,13 +370,14 @@ int profk_token_logprobs_grad(int32_t dtype, const void* logits, int64_t T, int6
                               void* stream);
 
 /* The same from the forward call's lse and lse_low, p_j = exp((x_j - lse) -
- * lse_low): no less exact for a large lse, and no row is read again.  lse_low =
- * NULL: profk_token_logprobs_grad. */
+ * lse_low): no less exact for a large lse, and no row is read again; and with
+ * g_lse[r] lse[r] in the sum, which adds g_lse p_j.  Either may be NULL; both:
+ * profk_token_logprobs_grad. */
 int profk_token_logprobs_grad_ex(int32_t dtype, const void* logits, int64_t T, int64_t V, int64_t row_stride,
                                  const int64_t* tokens, const float* lse, const float* lse_low,
                                  const float* entropy, const float* g_logprob, const float* g_entropy,
-                                 int64_t n_top, const int64_t* top_idx, const float* g_top, void* out,
-                                 int64_t out_stride, void* stream);
+                                 const float* g_lse, int64_t n_top, const int64_t* top_idx, const float* g_top,
+                                 void* out, int64_t out_stride, void* stream);
 
 /* ---- Microscaled 4-bit floating point (MXFP4) ----
  *

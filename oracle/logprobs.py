@@ -97,11 +97,12 @@ def grad_row(x, y, lse, h, g_lp, g_h, top_idx, g_top):
     return d
 
 
-def grad_of_logits(x, y, g_lp, g_h, top_idx, g_top):
-    """The gradient of grad_row's sum from the logits alone: the gradients of
-    the log probabilities l, then through l = x - lse (dl_i/dx_j = [i = j] -
-    p_j); H = -sum p l adds -p (l + 1) to the former.  A row with a value of
-    its own (finite lse), y below V."""
+def grad_of_logits(x, y, g_lp, g_h, top_idx, g_top, g_lse=0.0):
+    """The gradient of grad_row's sum and g_lse lse, from the logits alone: the
+    gradients of the log probabilities l, then through l = x - lse
+    (dl_i/dx_j = [i = j] - p_j); H = -sum p l adds -p (l + 1) to the former, and
+    lse has the gradient p.  A row with a value of its own (finite lse), y below
+    V."""
     x = np.asarray(x, dtype=np.float64)
     l = log_softmax(x)
     p = np.exp(l)
@@ -114,7 +115,7 @@ def grad_of_logits(x, y, g_lp, g_h, top_idx, g_top):
     if g_h is not None:
         on = p > 0
         u[on] -= g_h * p[on] * (l[on] + 1.0)
-    return u - p * u.sum()
+    return u + p * (g_lse - u.sum())
 
 
 def grad_scale(x, y, lse, h, g_lp, g_h, top_idx, g_top):

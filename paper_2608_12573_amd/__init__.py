@@ -119,7 +119,8 @@ def lib():
         L.profk_token_logprobs.argtypes = [i32, vp, i64, i64, i64, vp, i64, vp, vp, vp, vp, vp, vp, sz, vp]
         L.profk_token_logprobs_ex.argtypes = [i32, vp, i64, i64, i64, vp, i64, vp, vp, vp, vp, vp, vp, vp, sz, vp]
         L.profk_token_logprobs_grad.argtypes = [i32, vp, i64, i64, i64, vp, vp, vp, vp, vp, i64, vp, vp, vp, i64, vp]
-        L.profk_token_logprobs_grad_ex.argtypes = [i32, vp, i64, i64, i64, vp, vp, vp, vp, vp, vp, i64, vp, vp, vp, i64, vp]
+        L.profk_token_logprobs_grad_ex.argtypes = [i32, vp, i64, i64, i64, vp, vp, vp, vp, vp, vp, vp, i64, vp, vp, vp, i64,
+                                                   vp]
         for f in (L.profk_mx4_codes_size, L.profk_mx4_scales_size):
             f.argtypes, f.restype = [i64, i64], sz
         L.profk_mx4_linear_workspace_size.argtypes = [i64, i64, i64]
@@ -617,10 +618,16 @@ def token_logprobs(logits, tokens, n_top=0, ws=None, out=None, lse_low=None):
     Alternatives are most probable first, equal ones by smaller index; logits
     of -inf are never among them ((-inf, -1) where too few are left).
     lse_low: fp32 [T] that takes what rounding lse to fp32 leaves, for
-    token_logprobs_grad."""
+    token_logprobs_grad.
+
+    Where logits require a gradient, the new outputs are differentiable with
+    respect to them (the logits are kept for it).  Into a given `out` nothing is
+    recorded: the caller takes the gradient with token_logprobs_grad."""
     torch = _torch()
     dt, T, V, stride = _rows(logits, "logits")
     dev = logits.device
+    if logits.requires_grad and out is None and torch.is_grad_enabled():
+        return _differentiable_logprobs().apply(logits, tokens, n_top, ws, lse_low)
     _vector(tokens, "tokens", torch.int64, (T,), dev)
     if not 0 <= n_top <= MAX_TOP:
         raise ProfkError(f"n_top must be from 0 to {MAX_TOP}, got {n_top}")
@@ -648,10 +655,10 @@ def token_logprobs(logits, tokens, n_top=0, ws=None, out=None, lse_low=None):
 
 
 def token_logprobs_grad(logits, tokens, lse, entropy, g_logprob, g_entropy=None, top_idx=None, g_top=None, out=None,
-                        lse_low=None):
+                        lse_low=None, g_lse=None):
     """The gradient with respect to the logits of token_logprobs' outputs,
-    given theirs: g_logprob [T], g_entropy [T] or None, and g_top [T, n] for
-    the alternatives at top_idx [T, n] or None.  lse and entropy are
+    given theirs: g_logprob [T], g_entropy [T] and g_lse [T] or None, and g_top
+    [T, n] for the alternatives at top_idx [T, n] or None.  lse and entropy are
     token_logprobs', and so is lse_low: without it the row's probabilities are
     those of an lse rounded to fp32, all off by up to 2^-24 |lse| of
     themselves.  out: the logits' dtype and shape, rows may be strided; it must
@@ -671,6 +678,8 @@ def token_logprobs_grad(logits, tokens, lse, entropy, g_logprob, g_entropy=None,
         _vector(g_entropy, "g_entropy", f32, one, dev)
         if entropy is None:
             raise ProfkError("g_entropy needs the rows' entropy")
+    if g_lse is not None:
+        _vector(g_lse, "g_lse", f32, one, dev)
     n = 0
     if g_top is not None:
         if not isinstance(top_idx, torch.Tensor) or top_idx.dim() != 2 or top_idx.shape[1] > MAX_TOP:
@@ -685,10 +694,48 @@ def token_logprobs_grad(logits, tokens, lse, entropy, g_logprob, g_entropy=None,
         raise ProfkError("out must have the logits' dtype and shape")
     _on_device(out, "out", dev)
     _check(lib().profk_token_logprobs_grad_ex(dt, logits.data_ptr(), T, V, stride, tokens.data_ptr(), lse.data_ptr(),
-                                              _ptr(lse_low), _ptr(entropy), _ptr(g_logprob), _ptr(g_entropy), n,
+                                              _ptr(lse_low), _ptr(entropy), _ptr(g_logprob), _ptr(g_entropy), _ptr(g_lse), n,
                                               top_idx.data_ptr() if n else None, g_top.data_ptr() if n else None,
                                               out.data_ptr(), ostride, _stream()))
     return out
+
+
+_logprobs_function = None
+
+
+def _differentiable_logprobs():
+    """token_logprobs and its gradient as one autograd function (made on first
+    use: torch is imported late)."""
+    global _logprobs_function
+    if _logprobs_function is None:
+        torch = _torch()
+
+        class TokenLogprobs(torch.autograd.Function):
+            @staticmethod
+            def forward(ctx, logits, tokens, n_top, ws, lse_low):
+                low = torch.empty(logits.shape[0], dtype=torch.float32, device=logits.device)
+                out = token_logprobs(logits, tokens, n_top, ws=ws, lse_low=low)
+                if lse_low is not None:
+                    _vector(lse_low, "lse_low", low.dtype, tuple(low.shape), low.device)
+                    lse_low.copy_(low)
+                ctx.save_for_backward(logits, tokens, out[2], low, out[1], out[4])
+                ctx.set_materialize_grads(False)
+                ctx.mark_non_differentiable(out[4])
+                return out
+
+            @staticmethod
+            @torch.autograd.function.once_differentiable
+            def backward(ctx, g_logprob, g_entropy, g_lse, g_top, _):
+                logits, tokens, lse, low, entropy, top_idx = ctx.saved_tensors
+                # (of a sum, autograd gives one number spread over the rows)
+                g_logprob, g_entropy, g_lse, g_top = (g if g is None else g.contiguous()
+                                                      for g in (g_logprob, g_entropy, g_lse, g_top))
+                d = token_logprobs_grad(logits, tokens, lse, entropy, g_logprob, g_entropy, top_idx, g_top,
+                                        lse_low=low, g_lse=g_lse)
+                return d, None, None, None, None
+
+        _logprobs_function = TokenLogprobs
+    return _logprobs_function
 
 
 # ------------------------------------------------- microscaled 4-bit values ---
@@ -727,7 +774,7 @@ def mx4_quantize(x, out=None):
     """fp32 or bf16 x [R, K] (rows may be strided) in 4 bits a value with one
     power-of-two scale per 32: (codes uint8 [R, Kp/2], scales uint8
     [R/32, Kp/128, 32, 4]), K rounded up to a multiple of 128 and, in the
-    scales, R to one of 32."""
+    scales, R to one of 32.  A rounding: no gradient passes."""
     dt, R, K, stride = _rows(x, "x")
     if out is None:
         out = mx4_outputs(R, K, x.device)
@@ -778,7 +825,8 @@ def mx4_linear_workspace(M, K, N, device="cuda"):
 
 def mx4_linear(x, w_codes, w_scales, dtype=None, ws=None, out=None):
     """x W^T: fp32 or bf16 x [M, K] (rows may be strided), quantised in the
-    call, and W [N, K] from mx4_quantize; fp32 (the default) or bf16 [M, N]."""
+    call, and W [N, K] from mx4_quantize; fp32 (the default) or bf16 [M, N].
+    For serving: nothing is recorded for a gradient of x."""
     torch = _torch()
     dt, M, K, stride = _rows(x, "x")
     dev = x.device

@@ -377,12 +377,12 @@ int profk_token_logprobs_grad(int32_t dtype, const void* logits, int64_t T, int6
                               const int64_t* top_idx, const float* g_top, void* out, int64_t out_stride,
                               void* stream) {
   return profk_token_logprobs_grad_ex(dtype, logits, T, V, row_stride, tokens, lse, nullptr, entropy, g_logprob,
-                                      g_entropy, n_top, top_idx, g_top, out, out_stride, stream);
+                                      g_entropy, nullptr, n_top, top_idx, g_top, out, out_stride, stream);
 }
 
 int profk_token_logprobs_grad_ex(int32_t dtype, const void* logits, int64_t T, int64_t V, int64_t row_stride,
                                  const int64_t* tokens, const float* lse, const float* lse_low, const float* entropy,
-                                 const float* g_logprob, const float* g_entropy, int64_t n_top,
+                                 const float* g_logprob, const float* g_entropy, const float* g_lse, int64_t n_top,
                                  const int64_t* top_idx, const float* g_top, void* out, int64_t out_stride,
                                  void* stream) {
   const int rc = check_logits(dtype, T, V, row_stride, n_top);
@@ -408,6 +408,7 @@ int profk_token_logprobs_grad_ex(int32_t dtype, const void* logits, int64_t T, i
   a.entropy = entropy;
   a.g_logprob = g_logprob;
   a.g_entropy = g_entropy;
+  a.g_lse = g_lse;
   a.g_top = g_top;
   a.top_idx = top_idx;
   a.out = out;

@@ -688,7 +688,8 @@ template <int DT, bool TOP> __global__ __launch_bounds__(kLpJoinBS) void k_lp_jo
 }
 
 // ------------------------------------------------------------ gradient ----
-// With p = exp(x - lse), G = g + sum_i t_i (g only where y is a token):
+// With p = exp(x - lse), G = g + sum_i t_i - l (g only where y is a token; l of
+// lse itself, whose gradient is p):
 //   dx_j = -p_j (G + h (log p_j + H))  +  g [j = y] + sum_i t_i [j = a_i].
 // One workgroup per piece of a row: the first term for all of it, then the
 // few elements that take the second are written again, behind a barrier.
@@ -751,7 +752,7 @@ template <int DT> __global__ __launch_bounds__(kGradBS) void k_lp_grad(LpGradArg
   const int64_t y = a.tokens ? a.tokens[r] : -1;
   float gy = a.g_logprob && y >= 0 ? a.g_logprob[r] : 0.0f;
   if (y >= static_cast<int64_t>(a.V)) gy = __builtin_nanf("");
-  float G = gy;
+  float G = a.g_lse ? gy - a.g_lse[r] : gy;
   const float* const gt = a.n ? a.g_top + r * a.n : nullptr;
   const int64_t* const at = a.n ? a.top_idx + r * a.n : nullptr;
   for (uint32_t i = 0; i < a.n; ++i)

@@ -52,7 +52,7 @@ struct LpGradArgs {
   uint64_t stride;
   uint32_t V, n;
   const int64_t* tokens;                      // null: no token has a gradient
-  const float *lse, *lse_low, *entropy, *g_logprob, *g_entropy, *g_top;   // lse_low: may be null
+  const float *lse, *lse_low, *entropy, *g_logprob, *g_entropy, *g_lse, *g_top;   // lse_low, g_..: may be null
   const int64_t* top_idx;
   void* out;
   uint64_t out_stride;

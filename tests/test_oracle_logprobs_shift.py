@@ -17,6 +17,7 @@ def test_gradient_of_logits_equals_differences(y, top):
         return g_lp * lp + g_h * h + sum(t * (z[j] - lse) for j, t in zip(top, g_top) if 0 <= j < z.size)
 
     d = olp.grad_of_logits(x, y, g_lp, g_h, top, g_top)
+    assert np.abs(olp.grad_of_logits(x, y, g_lp, g_h, top, g_top, 0.3) - d - 0.3 * np.exp(olp.log_softmax(x))).max() < 1e-12
     e = 1e-5
     num = np.array([(f(x + e * np.eye(9)[j]) - f(x - e * np.eye(9)[j])) / (2 * e) for j in range(9)])
     assert np.abs(d - num).max() < 1e-9
