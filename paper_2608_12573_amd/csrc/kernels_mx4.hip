@@ -550,8 +550,17 @@ constexpr int kMxFewBS = 256;
 constexpr int kMxCodes = -1;                          // a's type where it is quantised already
 constexpr uint32_t kMxFewStage = 32 * 128 + 32 * 8;   // bytes of a wave's stage: codes, then scales
 constexpr int kMxFewLoads = 5;                        // loads of a stage
-// LDS for a: beside another workgroup on the CU, or alone.
+// LDS for a.  With the smaller one, two workgroups fit a CU where each wave
+// takes its own groups; the sums of waves that share them take their place.
 constexpr uint32_t kMxFewLdsSmall = 10 * 1024, kMxFewLds = 64 * 1024;
+constexpr uint32_t kCuLds = 160 * 1024;
+// Workgroups of a kernel that a CU holds, by their LDS: a, the waves' four
+// stages, and the sums of all waves but one.
+constexpr uint32_t mx_few_per_cu(bool ksplit, uint32_t lds) {
+  return kCuLds / (lds + kMxFewBS / kWave * 4 * kMxFewStage + (ksplit ? (kMxFewBS / kWave - 1) * 16 * kWave * 4 : 4));
+}
+static_assert(mx_few_per_cu(false, kMxFewLdsSmall) == 2 && mx_few_per_cu(true, kMxFewLdsSmall) == 1 &&
+              mx_few_per_cu(true, kMxFewLds) == 1, "LDS of the kernel of few rows");
 __host__ __device__ constexpr uint32_t mx_few_row(uint32_t steps) { return steps * 64 + 16; }   // LDS bytes of a row of a
 __host__ __device__ constexpr uint32_t mx_few_lds(uint32_t M, uint32_t steps) { return M * (mx_few_row(steps) + steps * 4); }
 // a fits `lds` bytes.
@@ -714,14 +723,21 @@ template <int DT, int WM, int WN, int MI, int NJ, int PER> void launch_gemm(cons
 // With a larger a it is so where the waves of a workgroup share the steps of a
 // group, as they do where the groups are few (M = 8, K = 4096, N = 8192: 9
 // against 13 us); without sharing it is not (M = 16 and 32, N = 131072: 61 and
-// 71 against 57 and 62 us).
+// 71 against 57 and 62 us).  The grid is what the CUs hold at once: workgroups
+// past that fill their stages and quantise a again when the first ones end (K =
+// 4096, M = 4, one and two a CU where one fits: N = 10000 12.9 and 17.1 us, 16384
+// 14.1 and 18.1, 32000 21.9 and 25.4).
 template <int DT, int XDT> bool launch_few(const MxGemmArgs& g, uint32_t cus, hipStream_t s) {
   const uint32_t groups = (g.N + 31) / 32;
   const bool share = groups < 4 * cus && g.steps >= 8;
   if (mx_few(g.M, g.steps, kMxFewLdsSmall)) {
-    const uint32_t most = 2 * cus;
-    if (share) k_mx_few<DT, XDT, true, kMxFewLdsSmall><<<groups < most ? groups : most, kMxFewBS, 0, s>>>(g);
-    else k_mx_few<DT, XDT, false, kMxFewLdsSmall><<<(groups + 3) / 4 < most ? (groups + 3) / 4 : most, kMxFewBS, 0, s>>>(g);
+    if (share) {
+      const uint32_t most = mx_few_per_cu(true, kMxFewLdsSmall) * cus;
+      k_mx_few<DT, XDT, true, kMxFewLdsSmall><<<groups < most ? groups : most, kMxFewBS, 0, s>>>(g);
+    } else {
+      const uint32_t quads = (groups + 3) / 4, most = mx_few_per_cu(false, kMxFewLdsSmall) * cus;
+      k_mx_few<DT, XDT, false, kMxFewLdsSmall><<<quads < most ? quads : most, kMxFewBS, 0, s>>>(g);
+    }
     return true;
   }
   if constexpr (XDT == kMxCodes) {
