@@ -330,6 +330,10 @@ int profk_debug_sae_sample(const profk_plan_t* plan, const void* x, const void* 
  *            order; -NaN is never one), and a NaN gradient.
  *   outputs  logprob, entropy, lse fp32 [T]; alternatives fp32 and int64
  *            [T, n_top], 0 <= n_top <= 64 (NULL for n_top = 0).
+ *   time     one read of the logits; rows with a logit past 1e6, or none above
+ *            -1e6, are read twice more, and rows whose alternatives stand out
+ *            late or not at all (equal or sorted logits, a few allowed ones
+ *            under a finite mask, a small range of them) n_top times more.
  *   ws       profk_token_logprobs_workspace_size(T, V, n_top) bytes, 16-byte
  *            aligned, for few rows, which are split over several workgroups;
  *            0 (and NULL) otherwise.

@@ -248,11 +248,16 @@ __device__ __forceinline__ void bare_barrier() {
 //
 // 256 x 256 tiles on eight waves of 64 x 128: a stage moves 68 KB for 32 matrix
 // instructions a wave, of 32 cycles, two waves a SIMD.  Measured: 4096 x 4096 x
-// 65536 to bf16 566 us (3.9 PFLOP/s), 4096 x 2048 x 131072 665 us (3.3), 4096 x
-// 512 x 12288 to fp32 39 us (5.2 TB/s of output, a copy's rate).  The same
-// instructions on random codes in registers alone reach 6.3 PFLOP/s, the clock
-// falling to about 1.6 GHz (8.8 on zeros); the library's bf16 product of 8192^3
-// 1.2.  Bound by the matrix cores at that clock and, of short K, by the stores.
+// 65536 to bf16 566 us (3.9 PFLOP/s), 4096 x 2048 x 131072 636 to 665 us (3.5 to
+// 3.3, as the clock falls), 4096 x 512 x 12288 to fp32 41 us (4.9 TB/s of output,
+// near a copy's rate).  The same instructions on random codes in registers alone
+// reach 6.3 PFLOP/s, at about 1.6 GHz (8.8 on zeros); the library's bf16 product
+// of 8192^3 1.2.  Of short K it is bound by the stores.  Of long K by no unit
+// alone: at 4096 x 4096 x 65536 the matrix cores are busy for 54 % of the cycles,
+// and waves wait for 40 % of theirs, at each stage's barrier and for its loads;
+// a tile's first stage waits for the stores of the tile before as well, which
+// are counted with the loads (the same operations with twice the outputs, 4096 x
+// 2048 x 131072, take about 90 us more).
 // Four waves of 128 x 128 read a third less from LDS and were slower (631 us at
 // 4096 x 4096 x 65536: one wave a SIMD hides no wait).
 template <int WM, int WN, int MI, int NJ> struct MxTile {
@@ -757,6 +762,9 @@ template <int DT> void launch_product(const MxGemmArgs& g, int x_dtype, uint32_t
   // 128 (M x K x N, us with the larger and the smaller: 2048 x 4096 x 4096, 128
   // large tiles, 29 and 23; 2048 x 4096 x 8192, 256 of them, 36 and 42; 512 x 2048
   // x 50000, 392, 33 and 35; 128 x 4096 x 131072, half of each empty, 91 and 70).
+  // The rule does not see a second round of large tiles that is nearly empty: from
+  // 257 to about 320 of them the smaller ones would be faster (2304 x 4096 x 7680,
+  // 270, 54 and 51; 4096 x 512 x 4352, 272, 16 and 12; at 376, 57 and 62).
   const uint64_t large = static_cast<uint64_t>((g.M + 255) / 256) * ((g.N + 255) / 256);
   if (g.M > 128 && large >= cus) launch_gemm<DT, 4, 2, 2, 4, 1>(g, cus, s);
   else launch_gemm<DT, 4, 1, 1, 4, 2>(g, cus, s);
