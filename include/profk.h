@@ -429,6 +429,115 @@ int profk_mx4_linear(int32_t dtype, const void* x, int64_t M, int64_t K, int64_t
                      const uint8_t* w_codes, const uint8_t* w_scales, int64_t N, int32_t out_dtype, void* out,
                      void* ws, size_t ws_bytes, void* stream);
 
+/* ---- Layer norm ----
+ *
+ * Of one row x of D values, m = mean x, r = 1 / sqrt(mean (x - m)^2 + eps):
+ *   out = (x - m) r weight + bias
+ * and with n = (x - m) r and g = dy weight, for gradients dy of out,
+ *   dx = r (g - mean g - n mean(g n)),  dweight = sum over the rows dy n,
+ *   dbias = sum over the rows dy.
+ * All in fp32; every output is rounded once.  The sums over the rows are taken
+ * in an order that depends on T, D and the GPU alone.
+ *
+ *   x, dx     fp32 or bf16 (`dtype`) [T, D], rows x_stride and dx_stride
+ *             elements apart, at any element's alignment; 1 <= D <= 2^20.
+ *             T = 0 writes nothing but zeros to dweight and dbias.
+ *   out, dy   fp32 or bf16 [T, D], of a type of their own.
+ *   weight, bias, dweight, dbias  [D], of one type, `param_dtype`.  weight NULL:
+ *             1; bias NULL: 0.
+ *   mean, rstd  fp32 [T]: m and r (outputs that may be NULL; the gradient's
+ *             inputs).
+ *   eps       finite, above 0 (a row of equal values has no direction without).
+ *   NaN, inf  a row with either is NaN.
+ * out may be x itself, of the same type and stride; else the memory from an
+ * output's first element to its last must not overlap x's or dy's
+ * (PROFK_EINVAL).  Any of dx, dweight and dbias may be NULL.  ws:
+ * profk_layer_norm_grad_workspace_size(T, D) bytes, 16-byte aligned; NULL is
+ * accepted without dweight and dbias. */
+int profk_layer_norm(int32_t dtype, const void* x, int64_t T, int64_t D, int64_t x_stride, int32_t param_dtype,
+                     const void* weight, const void* bias, float eps, int32_t out_dtype, void* out,
+                     int64_t out_stride, float* mean, float* rstd, void* stream);
+size_t profk_layer_norm_grad_workspace_size(int64_t T, int64_t D);
+int profk_layer_norm_grad(int32_t dtype, const void* x, int64_t T, int64_t D, int64_t x_stride, int32_t dy_dtype,
+                          const void* dy, int64_t dy_stride, int32_t param_dtype, const void* weight,
+                          const float* mean, const float* rstd, void* dx, int64_t dx_stride, void* dweight,
+                          void* dbias, void* ws, size_t ws_bytes, void* stream);
+
+/* ---- Dense product with bias, activation and residual ----
+ *
+ *   z = x W^T + bias,  out = act(z) + residual
+ *   dz = dy act'(z),  dx = dz W,  dW = dz^T x,  dbias = sum over the rows dz
+ * (the residual's gradient is dy).  x bf16 [M, K] and W bf16 [N, K], rows at any
+ * stride and alignment; products are exact, sums fp32; bias fp32 [N].
+ *
+ *   activation  PROFK_ACT_*: gelu is z/2 (1 + erf(z / sqrt 2)), silu z / (1 +
+ *             e^-z).  An infinite z gives their limits; relu has slope 0 at 0.
+ *   out, pre, residual, dy  fp32 or bf16 (`out_dtype`, `dtype`) [M, N]; out and
+ *             pre contiguous.  pre, where it is not NULL, takes z, rounded, for
+ *             the gradient (needed there but for PROFK_ACT_NONE).  residual may
+ *             be out itself (of stride N).
+ *   dx, dW    contiguous bf16 [M, K], [N, K], from dz rounded to bf16; dbias
+ *             fp32 [N].  Any of them may be NULL.
+ *   sizes     1 <= K <= 2^20, 0 <= M, N <= 2^31 - 1.  M = 0 sets dW and dbias to
+ *             zero, N = 0 dx.
+ *   ws        profk_linear_workspace_size(M, K, N) and
+ *             profk_linear_grad_workspace_size(M, K, N) bytes, 16-byte aligned
+ *             (NULL for 0).
+ * Outputs must not overlap inputs otherwise (PROFK_EINVAL). */
+enum { PROFK_ACT_NONE = 0, PROFK_ACT_RELU = 1, PROFK_ACT_GELU = 2, PROFK_ACT_SILU = 3 };
+size_t profk_linear_workspace_size(int64_t M, int64_t K, int64_t N);
+int profk_linear(const void* x, int64_t M, int64_t K, int64_t x_stride, const void* w, int64_t N, int64_t w_stride,
+                 const float* bias, int32_t activation, int32_t out_dtype, const void* residual,
+                 int64_t residual_stride, void* out, void* pre, void* ws, size_t ws_bytes, void* stream);
+size_t profk_linear_grad_workspace_size(int64_t M, int64_t K, int64_t N);
+int profk_linear_grad(int32_t dtype, const void* dy, int64_t dy_stride, const void* pre, int32_t activation,
+                      const void* x, int64_t M, int64_t K, int64_t x_stride, const void* w, int64_t N,
+                      int64_t w_stride, void* dx, void* dw, float* dbias, void* ws, size_t ws_bytes, void* stream);
+
+/* ---- Penalties, biases and masks on rows of logits ----
+ *
+ * Of one row x of V logits with a history of tokens, the first n_prompt of them
+ * a prompt, and c_v the occurrences of v after the prompt:
+ *   u_v = x_v / repetition if x_v > 0, x_v repetition otherwise, where v is in
+ *         the history; x_v where it is not
+ *   out_v = u_v - [c_v > 0] presence - c_v frequency + bias_v, or -inf where the
+ *         row's mask forbids v
+ * in fp32, rounded once to the logits' dtype.
+ *
+ *   logits, out  fp32 or bf16 [T, V], rows x_stride and out_stride elements
+ *             apart; out may be the logits (same stride), and must not overlap
+ *             them otherwise (PROFK_EINVAL).  T = 0 is accepted, 1 <= V <= 2^31 - 1.
+ *   tokens    int64 [n_tokens], row r's history at token_offsets[r] up to
+ *             token_offsets[r + 1] (int64 [T + 1]); NULL: no history.  Tokens
+ *             outside 0 .. V - 1 (padding) count nowhere.  n_prompt int64 [T] or
+ *             NULL (0).  repetition, presence, frequency fp32 [T] or NULL (1, 0, 0).
+ *   bias_ids  int64 [n_bias], bias_values fp32 [n_bias], row r's at
+ *             bias_offsets[r] .. (int64 [T + 1]); NULL: none.  Of the same token
+ *             twice in a row the last entry stands.  Both lists hold fewer than
+ *             2^31 entries; offsets past a list's end are taken as its end.
+ *   allowed   32 tokens a word, the lowest bit first, [n_masks] masks of
+ *             allowed_stride >= ceil(V / 32) words; NULL: all are allowed.  mask
+ *             int64 [T]: the row's mask, negative for none; a mask from n_masks up
+ *             makes the row NaN.  mask NULL: row r has mask r, or all the only
+ *             one (n_masks must be T or 1).
+ *   NaN, inf  stay where they are allowed; where they are forbidden -inf.  A row
+ *             that allows nothing is all -inf.
+ *
+ * profk_adjust_logits_grad: the gradient with respect to the logits, that of out
+ * times 1 / repetition, repetition or 1 as above, and 0 where the mask forbids.
+ * out may be d_out (same stride); it must not overlap the logits. */
+int profk_adjust_logits(int32_t dtype, const void* logits, int64_t T, int64_t V, int64_t x_stride,
+                        const int64_t* tokens, const int64_t* token_offsets, int64_t n_tokens,
+                        const int64_t* n_prompt, const float* repetition, const float* presence,
+                        const float* frequency, const int64_t* bias_ids, const float* bias_values,
+                        const int64_t* bias_offsets, int64_t n_bias, const uint32_t* allowed, int64_t n_masks,
+                        int64_t allowed_stride, const int64_t* mask, void* out, int64_t out_stride, void* stream);
+int profk_adjust_logits_grad(int32_t dtype, const void* d_out, int64_t d_stride, const void* logits, int64_t T,
+                             int64_t V, int64_t x_stride, const int64_t* tokens, const int64_t* token_offsets,
+                             int64_t n_tokens, const float* repetition, const uint32_t* allowed, int64_t n_masks,
+                             int64_t allowed_stride, const int64_t* mask, void* out, int64_t out_stride,
+                             void* stream);
+
 /* profk_topk with stages 1-2 replaced by a caller-given threshold key, to
  * drive the underflow and overflow paths on purpose.  A key alone names no
  * threshold pair, so this entry point filters with key >= tau_key also for

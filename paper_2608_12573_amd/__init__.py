@@ -12,6 +12,9 @@ built, every call raises instead of computing anything on the CPU.
     d_logits = token_logprobs_grad(logits, tokens, lse, entropy, g_logprob)
     codes, scales = mx4_quantize(w)               # 4-bit microscaled weights
     logits = mx4_linear(x, codes, scales)         # x w^T
+    y, mean, rstd = layer_norm(x, weight, bias)
+    z = linear(x, w, bias, activation="gelu")     # with gradients, as layer_norm
+    logits = adjust_logits(logits, tokens, offsets, repetition=r, allowed=masks)
 """
 
 import ctypes
@@ -129,6 +132,19 @@ def lib():
         L.profk_mx4_dequantize.argtypes = [i32, vp, vp, i64, i64, vp, vp]
         L.profk_mx4_matmul.argtypes = [vp, vp, i64, vp, vp, i64, i64, i32, vp, vp]
         L.profk_mx4_linear.argtypes = [i32, vp, i64, i64, i64, vp, vp, i64, i32, vp, vp, sz, vp]
+        L.profk_layer_norm.argtypes = [i32, vp, i64, i64, i64, i32, vp, vp, ctypes.c_float, i32, vp, i64, vp, vp, vp]
+        L.profk_layer_norm_grad_workspace_size.argtypes = [i64, i64]
+        L.profk_layer_norm_grad_workspace_size.restype = sz
+        L.profk_layer_norm_grad.argtypes = [i32, vp, i64, i64, i64, i32, vp, i64, i32, vp, vp, vp, vp, i64, vp, vp, vp, sz,
+                                            vp]
+        for f in (L.profk_linear_workspace_size, L.profk_linear_grad_workspace_size):
+            f.argtypes, f.restype = [i64, i64, i64], sz
+        L.profk_linear.argtypes = [vp, i64, i64, i64, vp, i64, i64, vp, i32, i32, vp, i64, vp, vp, vp, sz, vp]
+        L.profk_linear_grad.argtypes = [i32, vp, i64, vp, i32, vp, i64, i64, i64, vp, i64, i64, vp, vp, vp, vp, sz, vp]
+        L.profk_adjust_logits.argtypes = [i32, vp, i64, i64, i64, vp, vp, i64, vp, vp, vp, vp, vp, vp, vp, i64, vp, i64,
+                                          i64, vp, vp, i64, vp]
+        L.profk_adjust_logits_grad.argtypes = [i32, vp, i64, vp, i64, i64, i64, vp, vp, i64, vp, vp, i64, i64, vp, vp, i64,
+                                               vp]
         L.profk_debug_sae_sample.argtypes = [P(Plan), vp, vp, vp, i64, i64, i64, u64, vp, vp, sz, vp]
         _lib = L
     return _lib
@@ -841,3 +857,413 @@ def mx4_linear(x, w_codes, w_scales, dtype=None, ws=None, out=None):
     _check(L.profk_mx4_linear(dt, x.data_ptr(), M, K, stride, w_codes.data_ptr(), w_scales.data_ptr(), N, odt,
                               out.data_ptr(), ws.data_ptr() if n else None, n, _stream()))
     return out
+
+
+# ------------------------------------------------------------- layer norm ---
+
+def _here(device):
+    """The calls below go to the current device's stream: a tensor of another
+    GPU is refused."""
+    if device.index != _torch()._C._cuda_getDevice():
+        raise ProfkError(f"the tensors are on {device}, which is not the current device")
+
+
+def _out_rows(out, name, R, C, dtype, device):
+    """Checks an output matrix whose rows may be strided: its row stride."""
+    dt, oR, oC, stride = _rows(out, name)
+    if oR != R or oC != C or (dtype is not None and out.dtype != dtype):
+        raise ProfkError(f"{name} must be {dtype or out.dtype} of shape {(R, C)}, got {out.dtype} {(oR, oC)}")
+    _on_device(out, name, device)
+    return stride
+
+
+def _params(weight, bias, D, device):
+    """Checks a scale and shift of one type (either may be None): its code."""
+    torch = _torch()
+    one = weight if weight is not None else bias
+    if one is None:
+        return F32
+    dt = _dtype_code(one) if isinstance(one, torch.Tensor) else F32
+    if weight is not None:
+        _vector(weight, "weight", one.dtype if isinstance(one, torch.Tensor) else None, (D,), device)
+    if bias is not None:
+        _vector(bias, "bias", one.dtype if isinstance(one, torch.Tensor) else None, (D,), device)
+    return dt
+
+
+def layer_norm_outputs(T, D, dtype=None, device="cuda"):
+    """New outputs of layer_norm: (out [T, D] of dtype, bf16 by default, mean
+    fp32 [T], rstd fp32 [T])."""
+    torch = _torch()
+    return (torch.empty((T, D), dtype=dtype or torch.bfloat16, device=device),
+            torch.empty(T, dtype=torch.float32, device=device), torch.empty(T, dtype=torch.float32, device=device))
+
+
+def layer_norm(x, weight=None, bias=None, eps=1e-5, dtype=None, out=None):
+    """Rows normalised to mean 0 and variance 1, times weight, plus bias:
+    (out [T, D], mean [T], rstd [T]), rstd = 1 / sqrt(variance + eps).
+
+    x: fp32 or bf16 [T, D], rows may be strided.  weight and bias: fp32 or bf16
+    [D], of one type, or None.  out: fp32 or bf16 (x's type by default), rows may
+    be strided; it may be x itself.  Sums and statistics are fp32.
+
+    Where x, weight or bias require a gradient, the new outputs are
+    differentiable with respect to them (mean and rstd are not).  Into a given
+    `out` nothing is recorded: the caller takes layer_norm_grad."""
+    torch = _torch()
+    dt, T, D, stride = _rows(x, "x")
+    dev = x.device
+    if out is None and torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in (x, weight, bias)):
+        return _differentiable("layer_norm").apply(x, weight, bias, eps, dtype)
+    pdt = _params(weight, bias, D, dev)
+    _here(dev)
+    if out is None:
+        out = layer_norm_outputs(T, D, dtype or x.dtype, dev)
+    ostride = _out_rows(out[0], "out[0]", T, D, dtype, dev)
+    _vector(out[1], "out[1]", torch.float32, (T,), dev)
+    _vector(out[2], "out[2]", torch.float32, (T,), dev)
+    _check(lib().profk_layer_norm(dt, x.data_ptr(), T, D, stride, pdt, _ptr(weight), _ptr(bias), eps,
+                                  _dtype_code(out[0]), out[0].data_ptr(), ostride, out[1].data_ptr(), out[2].data_ptr(),
+                                  _stream()))
+    return out
+
+
+def layer_norm_grad_workspace(T, D, device="cuda"):
+    """A workspace for layer_norm_grad."""
+    torch = _torch()
+    return torch.empty(int(lib().profk_layer_norm_grad_workspace_size(T, D)), dtype=torch.uint8, device=device)
+
+
+def layer_norm_grad(dy, x, weight, mean, rstd, ws=None, out=None, need=(True, True, True)):
+    """The gradients of layer_norm's rows, weight and bias for dy [T, D] (fp32 or
+    bf16, rows may be strided), given its inputs and statistics: (dx of x's type,
+    dweight, dbias, of weight's type or fp32).  out: the three, given; a None
+    among them, and what `need` (of new ones) leaves out, is not computed."""
+    torch = _torch()
+    dt, T, D, stride = _rows(x, "x")
+    dev, f32 = x.device, torch.float32
+    ddt, dT, dD, dstride = _rows(dy, "dy")
+    if (dT, dD) != (T, D):
+        raise ProfkError(f"dy must have x's shape {(T, D)}, got {(dT, dD)}")
+    _on_device(dy, "dy", dev)
+    pdt = _params(weight, None, D, dev)
+    _vector(mean, "mean", f32, (T,), dev)
+    _vector(rstd, "rstd", f32, (T,), dev)
+    _here(dev)
+    ptype = weight.dtype if weight is not None else f32
+    if out is None:
+        out = (torch.empty((T, D), dtype=x.dtype, device=dev) if need[0] else None,
+               torch.empty(D, dtype=ptype, device=dev) if need[1] else None,
+               torch.empty(D, dtype=ptype, device=dev) if need[2] else None)
+    ostride = _out_rows(out[0], "out[0]", T, D, x.dtype, dev) if out[0] is not None else D
+    for i in (1, 2):
+        if out[i] is not None:
+            _vector(out[i], f"out[{i}]", ptype, (D,), dev)
+    L = lib()
+    n = L.profk_layer_norm_grad_workspace_size(T, D) if out[1] is not None or out[2] is not None else 0
+    if ws is not None:
+        _bytes_buffer(ws, "ws", n, dev)
+    elif n:
+        ws = torch.empty(n, dtype=torch.uint8, device=dev)
+    _check(L.profk_layer_norm_grad(dt, x.data_ptr(), T, D, stride, ddt, dy.data_ptr(), dstride, pdt, _ptr(weight),
+                                   mean.data_ptr(), rstd.data_ptr(), _ptr(out[0]), ostride, _ptr(out[1]), _ptr(out[2]),
+                                   ws.data_ptr() if n else None, n, _stream()))
+    return out
+
+
+# ----------------------------------------------------------- dense product ---
+
+ACTIVATIONS = {None: 0, "relu": 1, "gelu": 2, "silu": 3}
+
+
+def _activation(name):
+    code = ACTIVATIONS.get(name)
+    if code is None:
+        raise ProfkError(f"activation must be one of {', '.join(str(a) for a in ACTIVATIONS)}, got {name!r}")
+    return code
+
+
+def _product(x, w):
+    """Checks the operands of a product: (M, K, N and the two row strides)."""
+    dt, M, K, xs = _rows(x, "x")
+    wt, N, wK, wstride = _rows(w, "w")
+    if dt != BF16 or wt != BF16:
+        raise ProfkError("x and w must be bfloat16")
+    if wK != K:
+        raise ProfkError(f"w must have x's {K} columns, got {wK}")
+    _on_device(w, "w", x.device)
+    return M, K, N, xs, wstride
+
+
+def linear_workspace(M, K, N, device="cuda"):
+    """A workspace for linear (may be empty)."""
+    torch = _torch()
+    return torch.empty(int(lib().profk_linear_workspace_size(M, K, N)), dtype=torch.uint8, device=device)
+
+
+def linear(x, w, bias=None, activation=None, residual=None, dtype=None, ws=None, out=None, pre=None):
+    """act(x W^T + bias) + residual: bf16 x [M, K] and W [N, K] (rows of either
+    may be strided), fp32 bias [N]; fp32 (the default) or bf16 [M, N], fp32 sums,
+    rounded once.
+
+    activation: None, "relu", "gelu" (by erf) or "silu".  residual: of the
+    output's type, rows may be strided; it may be `out` itself.  pre: takes
+    x W^T + bias, of the output's type, for linear_grad.
+
+    Where an input requires a gradient, a new output is differentiable with
+    respect to x, w, bias and residual.  Into a given `out` nothing is recorded:
+    the caller takes linear_grad."""
+    torch = _torch()
+    M, K, N, xs, wstride = _product(x, w)
+    dev = x.device
+    act = _activation(activation)
+    if out is None and torch.is_grad_enabled() and \
+            any(t is not None and t.requires_grad for t in (x, w, bias, residual)):
+        if pre is not None:
+            raise ProfkError("pre is kept by the recorded call itself")
+        return _differentiable("linear").apply(x, w, bias, residual, activation, dtype, ws)
+    if bias is not None:
+        _vector(bias, "bias", torch.float32, (N,), dev)
+    _here(dev)
+    out, odt = _dense_out((M, N), dtype, torch.float32, out, dev)
+    if pre is not None:
+        _vector(pre, "pre", out.dtype, (M, N), dev)
+    rs = _out_rows(residual, "residual", M, N, out.dtype, dev) if residual is not None else N
+    L = lib()
+    n = L.profk_linear_workspace_size(M, K, N)
+    if ws is not None:
+        _bytes_buffer(ws, "ws", n, dev)
+    elif n:
+        ws = torch.empty(n, dtype=torch.uint8, device=dev)
+    _check(L.profk_linear(x.data_ptr(), M, K, xs, w.data_ptr(), N, wstride, _ptr(bias), act, odt, _ptr(residual), rs,
+                          out.data_ptr(), _ptr(pre), ws.data_ptr() if n else None, n, _stream()))
+    return out
+
+
+def linear_grad_workspace(M, K, N, device="cuda"):
+    """A workspace for linear_grad."""
+    torch = _torch()
+    return torch.empty(int(lib().profk_linear_grad_workspace_size(M, K, N)), dtype=torch.uint8, device=device)
+
+
+def linear_grad(dy, x, w, pre=None, activation=None, ws=None, out=None, need=(True, True, True)):
+    """The gradients of linear's x, W and bias for dy [M, N] (fp32 or bf16, rows
+    may be strided): (dx bf16 [M, K], dW bf16 [N, K], dbias fp32 [N]); the
+    residual's is dy.  pre: linear's, of dy's type (not needed without an
+    activation).  out: the three, given; a None among them, and what `need` (of
+    new ones) leaves out, is not computed."""
+    torch = _torch()
+    M, K, N, xs, wstride = _product(x, w)
+    dev = x.device
+    act = _activation(activation)
+    ddt, dM, dN, dstride = _rows(dy, "dy")
+    if (dM, dN) != (M, N):
+        raise ProfkError(f"dy must be of shape {(M, N)}, got {(dM, dN)}")
+    _on_device(dy, "dy", dev)
+    if act:
+        _vector(pre, "pre", dy.dtype, (M, N), dev)
+    else:
+        pre = None
+    _here(dev)
+    bf16 = torch.bfloat16
+    if out is None:
+        out = (torch.empty((M, K), dtype=bf16, device=dev) if need[0] else None,
+               torch.empty((N, K), dtype=bf16, device=dev) if need[1] else None,
+               torch.empty(N, dtype=torch.float32, device=dev) if need[2] else None)
+    for i, (t, shape) in enumerate(((bf16, (M, K)), (bf16, (N, K)), (torch.float32, (N,)))):
+        if out[i] is not None:
+            _vector(out[i], f"out[{i}]", t, shape, dev)
+    L = lib()
+    n = L.profk_linear_grad_workspace_size(M, K, N)
+    if ws is not None:
+        _bytes_buffer(ws, "ws", n, dev)
+    elif n:
+        ws = torch.empty(n, dtype=torch.uint8, device=dev)
+    _check(L.profk_linear_grad(ddt, dy.data_ptr(), dstride, _ptr(pre), act, x.data_ptr(), M, K, xs, w.data_ptr(), N,
+                               wstride, _ptr(out[0]), _ptr(out[1]), _ptr(out[2]), ws.data_ptr() if n else None, n,
+                               _stream()))
+    return out
+
+
+# ------------------------------------- penalties, biases and masks on logits ---
+
+def _list(t, name, dtype, device):
+    """A contiguous vector of any length: its length."""
+    torch = _torch()
+    if not isinstance(t, torch.Tensor) or t.dim() != 1:
+        raise ProfkError(f"{name} must be a 1-dimensional torch tensor")
+    _vector(t, name, dtype, tuple(t.shape), device)
+    return t.shape[0]
+
+
+def _history(T, V, tokens, offsets, repetition, allowed, mask, dev):
+    """Checks what adjust_logits and its gradient share: (tokens, masks, words
+    from mask to mask)."""
+    torch = _torch()
+    i64, n_tokens, n_masks, words = torch.int64, 0, 0, 0
+    if (tokens is None) != (offsets is None):
+        raise ProfkError("tokens and offsets are given together")
+    if tokens is not None:
+        n_tokens = _list(tokens, "tokens", i64, dev)
+        _vector(offsets, "offsets", i64, (T + 1,), dev)
+    if repetition is not None:
+        _vector(repetition, "repetition", torch.float32, (T,), dev)
+    if allowed is not None:
+        if not isinstance(allowed, torch.Tensor) or allowed.dim() != 2 or allowed.shape[1] != -(-V // 32) or \
+                allowed.shape[0] < 1:
+            raise ProfkError(f"allowed must be [masks, {-(-V // 32)}]")
+        n_masks, words = allowed.shape
+        _vector(allowed, "allowed", torch.int32, (n_masks, words), dev)
+        if mask is None and n_masks not in (1, T):
+            raise ProfkError(f"mask must say which of {n_masks} masks each of the {T} rows has")
+    if mask is not None:
+        if allowed is None:
+            raise ProfkError("mask names rows of allowed, which is not given")
+        _vector(mask, "mask", i64, (T,), dev)
+    return n_tokens, n_masks, words
+
+
+def adjust_logits(logits, tokens=None, offsets=None, n_prompt=None, repetition=None, presence=None, frequency=None,
+                  bias=None, allowed=None, mask=None, out=None):
+    """Penalties for repeated tokens, biases and masks of allowed tokens on rows
+    of logits (fp32 or bf16 [T, V], rows may be strided): a new tensor of their
+    type, or into `out`, which may be the logits.
+
+    tokens int64, offsets int64 [T + 1]: row r's history is
+    tokens[offsets[r]:offsets[r + 1]], the first n_prompt[r] (int64 [T]) of it a
+    prompt.  repetition, presence and frequency: fp32 [T], or None.  A token of
+    the history has its logit divided by repetition where it is positive and
+    multiplied where it is not; one that occurs c > 0 times after the prompt loses
+    presence + c frequency.  Tokens outside 0 .. V - 1 count nowhere.
+    bias: (ids int64, values fp32, offsets int64 [T + 1]), added; of an id twice in
+    a row the last stands.  allowed: int32 [masks, ceil(V / 32)], bit v % 32 of
+    word v // 32 set where v is allowed; forbidden logits become -inf.  mask: int64
+    [T], the row's mask, negative for none (None: row r has mask r, or all the
+    only one); a row that names a mask that is not there is NaN.
+
+    Where logits require a gradient, the new tensor is differentiable with
+    respect to them.  Into a given `out` nothing is recorded: the caller takes
+    adjust_logits_grad."""
+    torch = _torch()
+    dt, T, V, stride = _rows(logits, "logits")
+    dev, f32 = logits.device, torch.float32
+    if out is None and logits.requires_grad and torch.is_grad_enabled():
+        return _differentiable("adjust_logits").apply(logits, tokens, offsets, n_prompt, repetition, presence, frequency,
+                                                      bias, allowed, mask)
+    n_tokens, n_masks, words = _history(T, V, tokens, offsets, repetition, allowed, mask, dev)
+    if n_prompt is not None:
+        _vector(n_prompt, "n_prompt", torch.int64, (T,), dev)
+    if presence is not None:
+        _vector(presence, "presence", f32, (T,), dev)
+    if frequency is not None:
+        _vector(frequency, "frequency", f32, (T,), dev)
+    ids = values = at = None
+    n_bias = 0
+    if bias is not None:
+        ids, values, at = bias
+        n_bias = _list(ids, "bias[0]", torch.int64, dev)
+        _vector(values, "bias[1]", f32, (n_bias,), dev)
+        _vector(at, "bias[2]", torch.int64, (T + 1,), dev)
+    _here(dev)
+    if out is None:
+        out = torch.empty((T, V), dtype=logits.dtype, device=dev)
+    ostride = _out_rows(out, "out", T, V, logits.dtype, dev)
+    _check(lib().profk_adjust_logits(dt, logits.data_ptr(), T, V, stride, _ptr(tokens), _ptr(offsets), n_tokens,
+                                     _ptr(n_prompt), _ptr(repetition), _ptr(presence), _ptr(frequency), _ptr(ids),
+                                     _ptr(values), _ptr(at), n_bias, _ptr(allowed), n_masks, words, _ptr(mask),
+                                     out.data_ptr(), ostride, _stream()))
+    return out
+
+
+def adjust_logits_grad(d_out, logits, tokens=None, offsets=None, n_prompt=None, repetition=None, allowed=None,
+                       mask=None, out=None):
+    """The gradient of adjust_logits with respect to the logits, for d_out of
+    their type and shape (rows may be strided), given what adjust_logits was given
+    (n_prompt, presences, frequencies and biases have no part in it).  out may be
+    d_out."""
+    torch = _torch()
+    dt, T, V, stride = _rows(logits, "logits")
+    dev = logits.device
+    dstride = _out_rows(d_out, "d_out", T, V, logits.dtype, dev)
+    n_tokens, n_masks, words = _history(T, V, tokens, offsets, repetition, allowed, mask, dev)
+    if n_prompt is not None:
+        _vector(n_prompt, "n_prompt", torch.int64, (T,), dev)
+    _here(dev)
+    if out is None:
+        out = torch.empty((T, V), dtype=logits.dtype, device=dev)
+    ostride = _out_rows(out, "out", T, V, logits.dtype, dev)
+    _check(lib().profk_adjust_logits_grad(dt, d_out.data_ptr(), dstride, logits.data_ptr(), T, V, stride, _ptr(tokens),
+                                          _ptr(offsets), n_tokens, _ptr(repetition), _ptr(allowed), n_masks, words,
+                                          _ptr(mask), out.data_ptr(), ostride, _stream()))
+    return out
+
+
+_functions = {}
+
+
+def _differentiable(name):
+    """layer_norm, linear or adjust_logits and its gradient as one autograd
+    function (made on first use: torch is imported late)."""
+    if _functions:
+        return _functions[name]
+    torch = _torch()
+    once = torch.autograd.function.once_differentiable
+
+    def rows(g):
+        # (of a sum, autograd gives one number spread over the rows)
+        return g if g.dim() == 2 and (g.stride(1) == 1 and g.stride(0) >= g.shape[1]) else g.contiguous()
+
+    class LayerNorm(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, x, weight, bias, eps, dtype):
+            out = layer_norm(x, weight, bias, eps, dtype)
+            ctx.save_for_backward(x, weight, out[1], out[2])
+            ctx.bias_dtype = None if bias is None else bias.dtype
+            ctx.mark_non_differentiable(out[1], out[2])
+            return out
+
+        @staticmethod
+        @once
+        def backward(ctx, dy, _m, _r):
+            x, weight, mean, rstd = ctx.saved_tensors
+            dx, dw, db = layer_norm_grad(rows(dy), x, weight, mean, rstd, need=ctx.needs_input_grad[:3])
+            # (without a weight the shift's gradient is fp32)
+            return dx, dw, db if db is None else db.to(ctx.bias_dtype), None, None
+
+    class Linear(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, x, w, bias, residual, activation, dtype, ws):
+            pre = None
+            if activation is not None and any(ctx.needs_input_grad[:3]):
+                pre = torch.empty((x.shape[0], w.shape[0]), dtype=dtype or torch.float32, device=x.device)
+            out = linear(x, w, bias, activation, residual, dtype, ws=ws, pre=pre)
+            ctx.save_for_backward(x, w, pre)
+            ctx.activation = activation
+            return out
+
+        @staticmethod
+        @once
+        def backward(ctx, dy):
+            x, w, pre = ctx.saved_tensors
+            need = ctx.needs_input_grad
+            d = (None, None, None)
+            if any(need[:3]):
+                d = linear_grad(rows(dy), x, w, pre, ctx.activation, need=need[:3])
+            return d + (dy if need[3] else None, None, None, None)
+
+    class AdjustLogits(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, logits, tokens, offsets, n_prompt, repetition, presence, frequency, bias, allowed, mask):
+            out = adjust_logits(logits, tokens, offsets, n_prompt, repetition, presence, frequency, bias, allowed, mask)
+            ctx.save_for_backward(logits, tokens, offsets, repetition, allowed, mask)
+            return out
+
+        @staticmethod
+        @once
+        def backward(ctx, d_out):
+            logits, tokens, offsets, repetition, allowed, mask = ctx.saved_tensors
+            d = adjust_logits_grad(rows(d_out), logits, tokens, offsets, None, repetition, allowed, mask)
+            return (d,) + (None,) * 9
+
+    _functions.update(layer_norm=LayerNorm, linear=Linear, adjust_logits=AdjustLogits)
+    return _functions[name]

@@ -2,12 +2,16 @@
 // carving and launches.  Declarations and contracts are in include/profk.h.
 #include <hip/hip_runtime.h>
 
+#include <cmath>
 #include <cstdint>
 #include <mutex>
 
+#include "adjust.h"
 #include "launch.h"
+#include "linear.h"
 #include "logprobs.h"
 #include "mx4.h"
+#include "norm.h"
 #include "plan_internal.h"
 #include "profk.h"
 
@@ -505,6 +509,250 @@ int profk_mx4_linear(int32_t dtype, const void* x, int64_t M, int64_t K, int64_t
   const int rc = profk_mx4_quantize(dtype, x, M, K, row_stride, codes, scales, stream);
   if (rc != PROFK_OK) return rc;
   return profk_mx4_matmul(codes, scales, M, w_codes, w_scales, N, K, out_dtype, out, stream);
+}
+
+// ---- Layer norm ----
+
+namespace {
+
+// Rows of C elements, row_stride apart, whose byte offsets fit 63 bits.
+bool rows_ok(int64_t R, int64_t C, int64_t stride) {
+  return R >= 0 && R <= static_cast<int64_t>(INT32_MAX) && C >= 0 && stride >= C &&
+         stride <= INT64_MAX / 8 / (R > 0 ? R : 1);
+}
+
+// A matrix in memory, from its first element to its last.
+struct Span {
+  uintptr_t at, bytes;
+  Span(const void* p, int64_t R, int64_t C, int64_t stride, int32_t dtype)
+      : at(reinterpret_cast<uintptr_t>(p)),
+        bytes(p && R > 0 && C > 0 ? static_cast<uintptr_t>((R - 1) * stride + C) * elem_size(dtype) : 0) {}
+};
+bool overlap(const Span& a, const Span& b) {
+  return a.bytes && b.bytes && a.at < b.at + b.bytes && b.at < a.at + a.bytes;
+}
+
+bool norm_ok(int64_t T, int64_t D) { return T >= 0 && T <= static_cast<int64_t>(INT32_MAX) && D >= 1 && D <= profk::kNormMaxD; }
+
+}  // namespace
+
+int profk_layer_norm(int32_t dtype, const void* x, int64_t T, int64_t D, int64_t x_stride, int32_t param_dtype,
+                     const void* weight, const void* bias, float eps, int32_t out_dtype, void* out,
+                     int64_t out_stride, float* mean, float* rstd, void* stream) {
+  if (!dtype_ok(dtype) || !dtype_ok(param_dtype) || !dtype_ok(out_dtype)) return PROFK_EDTYPE;
+  if (!norm_ok(T, D) || !rows_ok(T, D, x_stride) || !rows_ok(T, D, out_stride)) return PROFK_EINVAL;
+  if (!(eps > 0.0f) || std::isinf(eps)) return PROFK_EINVAL;
+  if (T == 0) return PROFK_OK;
+  if (!x || !out) return PROFK_ENULL;
+  if (!aligned(x, elem_size(dtype)) || !aligned(out, elem_size(out_dtype)) || !aligned(mean, 4) || !aligned(rstd, 4) ||
+      !aligned(weight, elem_size(param_dtype)) || !aligned(bias, elem_size(param_dtype)))
+    return PROFK_EINVAL;
+  const bool same = x == out && dtype == out_dtype && (x_stride == out_stride || T == 1);
+  if (!same && overlap(Span(x, T, D, x_stride, dtype), Span(out, T, D, out_stride, out_dtype))) return PROFK_EINVAL;
+  const profk::NormArgs a{x, static_cast<uint64_t>(x_stride), static_cast<uint64_t>(out_stride),
+                          static_cast<uint32_t>(T), static_cast<uint32_t>(D), weight, bias, param_dtype, eps, out,
+                          mean, rstd};
+  const hipError_t e = profk::launch_norm(a, dtype, out_dtype, static_cast<hipStream_t>(stream));
+  return e == hipSuccess ? PROFK_OK : hip_fail(e);
+}
+
+size_t profk_layer_norm_grad_workspace_size(int64_t T, int64_t D) {
+  if (!norm_ok(T, D)) return 0;
+  return align256(static_cast<size_t>(profk::norm_grad_parts(T, D, profk::device_cu_count())) * 2 * static_cast<size_t>(D) * 4);
+}
+
+int profk_layer_norm_grad(int32_t dtype, const void* x, int64_t T, int64_t D, int64_t x_stride, int32_t dy_dtype,
+                          const void* dy, int64_t dy_stride, int32_t param_dtype, const void* weight,
+                          const float* mean, const float* rstd, void* dx, int64_t dx_stride, void* dweight,
+                          void* dbias, void* ws, size_t ws_bytes, void* stream) {
+  if (!dtype_ok(dtype) || !dtype_ok(param_dtype) || !dtype_ok(dy_dtype)) return PROFK_EDTYPE;
+  if (!norm_ok(T, D) || !rows_ok(T, D, x_stride) || !rows_ok(T, D, dy_stride) || !rows_ok(T, D, dx_stride))
+    return PROFK_EINVAL;
+  const bool sums = dweight || dbias;
+  if ((T == 0 && !sums) || (!sums && !dx)) return PROFK_OK;
+  if ((T > 0 && (!x || !dy || !mean || !rstd)) || (sums && !ws)) return PROFK_ENULL;
+  if (!aligned(x, elem_size(dtype)) || !aligned(dx, elem_size(dtype)) || !aligned(dy, elem_size(dy_dtype)) ||
+      !aligned(mean, 4) || !aligned(rstd, 4) || !aligned(weight, elem_size(param_dtype)) ||
+      !aligned(dweight, elem_size(param_dtype)) || !aligned(dbias, elem_size(param_dtype)) || !aligned(ws, 16))
+    return PROFK_EINVAL;
+  const Span out(dx, T, D, dx_stride, dtype);
+  if (overlap(out, Span(x, T, D, x_stride, dtype)) || overlap(out, Span(dy, T, D, dy_stride, dy_dtype)))
+    return PROFK_EINVAL;
+  if (sums && ws_bytes < profk_layer_norm_grad_workspace_size(T, D)) return PROFK_EWORKSPACE;
+  const profk::NormGradArgs a{x, dy, static_cast<uint64_t>(x_stride), static_cast<uint64_t>(dy_stride),
+                              static_cast<uint64_t>(dx_stride), static_cast<uint32_t>(T), static_cast<uint32_t>(D),
+                              weight, param_dtype, mean, rstd, dx, dweight, dbias,
+                              sums ? static_cast<float*>(ws) : nullptr,
+                              profk::norm_grad_parts(T, D, profk::device_cu_count())};
+  const hipError_t e = profk::launch_norm_grad(a, dtype, dy_dtype, static_cast<hipStream_t>(stream));
+  return e == hipSuccess ? PROFK_OK : hip_fail(e);
+}
+
+// ---- Dense product ----
+
+namespace {
+
+int check_linear(int64_t M, int64_t K, int64_t x_stride, int64_t N, int64_t w_stride, int32_t act) {
+  if (K < 1 || K > profk::kLinMaxK || !rows_ok(M, K, x_stride) || !rows_ok(N, K, w_stride)) return PROFK_EINVAL;
+  if (act < PROFK_ACT_NONE || act > PROFK_ACT_SILU) return PROFK_EINVAL;
+  return PROFK_OK;
+}
+
+}  // namespace
+
+size_t profk_linear_workspace_size(int64_t M, int64_t K, int64_t N) {
+  if (check_linear(M, K, K, N, K, PROFK_ACT_NONE) != PROFK_OK || M == 0 || N == 0) return 0;
+  return profk::lin_workspace(M, N, K, profk::device_cu_count());
+}
+
+int profk_linear(const void* x, int64_t M, int64_t K, int64_t x_stride, const void* w, int64_t N, int64_t w_stride,
+                 const float* bias, int32_t activation, int32_t out_dtype, const void* residual,
+                 int64_t residual_stride, void* out, void* pre, void* ws, size_t ws_bytes, void* stream) {
+  if (!dtype_ok(out_dtype)) return PROFK_EDTYPE;
+  if (check_linear(M, K, x_stride, N, w_stride, activation) != PROFK_OK) return PROFK_EINVAL;
+  if (residual && !rows_ok(M, N, residual_stride)) return PROFK_EINVAL;
+  if (M == 0 || N == 0) return PROFK_OK;
+  const size_t need = profk_linear_workspace_size(M, K, N);
+  if (!x || !w || !out || (need && !ws)) return PROFK_ENULL;
+  const size_t es = elem_size(out_dtype);
+  if (!aligned(x, 2) || !aligned(w, 2) || !aligned(bias, 4) || !aligned(residual, es) || !aligned(out, es) ||
+      !aligned(pre, es) || !aligned(ws, 16))
+    return PROFK_EINVAL;
+  const Span sx(x, M, K, x_stride, PROFK_BF16), sw(w, N, K, w_stride, PROFK_BF16), so(out, M, N, N, out_dtype),
+      sp(pre, M, N, N, out_dtype), sr(residual, M, N, residual_stride, out_dtype), sb(bias, 1, N, N, PROFK_F32);
+  const bool same = residual == out && (residual_stride == N || M == 1);
+  for (const Span& o : {so, sp})
+    if (overlap(o, sx) || overlap(o, sw) || overlap(o, sb)) return PROFK_EINVAL;
+  if (overlap(so, sp) || overlap(sp, sr) || (!same && overlap(so, sr))) return PROFK_EINVAL;
+  if (ws_bytes < need) return PROFK_EWORKSPACE;
+  const profk::LinCall c{x, w, static_cast<uint64_t>(x_stride), static_cast<uint64_t>(w_stride), M, N, K, bias,
+                         activation, out_dtype, residual, static_cast<uint64_t>(residual_stride), out, pre, ws};
+  const hipError_t e = profk::launch_linear(c, static_cast<hipStream_t>(stream));
+  return e == hipSuccess ? PROFK_OK : hip_fail(e);
+}
+
+size_t profk_linear_grad_workspace_size(int64_t M, int64_t K, int64_t N) {
+  if (check_linear(M, K, K, N, K, PROFK_ACT_NONE) != PROFK_OK) return 0;
+  return profk::lin_grad_workspace(M, N, K, profk::device_cu_count());
+}
+
+int profk_linear_grad(int32_t dtype, const void* dy, int64_t dy_stride, const void* pre, int32_t activation,
+                      const void* x, int64_t M, int64_t K, int64_t x_stride, const void* w, int64_t N,
+                      int64_t w_stride, void* dx, void* dw, float* dbias, void* ws, size_t ws_bytes, void* stream) {
+  if (!dtype_ok(dtype)) return PROFK_EDTYPE;
+  if (check_linear(M, K, x_stride, N, w_stride, activation) != PROFK_OK || !rows_ok(M, N, dy_stride)) return PROFK_EINVAL;
+  if ((!dx || M == 0) && ((!dw && !dbias) || N == 0)) return PROFK_OK;
+  if (M > 0 && N > 0 && (!dy || (activation != PROFK_ACT_NONE && !pre) || (dw && !x) || (dx && !w))) return PROFK_ENULL;
+  const size_t need = profk_linear_grad_workspace_size(M, K, N);
+  if (need && !ws) return PROFK_ENULL;
+  if (!aligned(x, 2) || !aligned(w, 2) || !aligned(dy, elem_size(dtype)) || !aligned(pre, elem_size(dtype)) ||
+      !aligned(dx, 2) || !aligned(dw, 2) || !aligned(dbias, 4) || !aligned(ws, 16))
+    return PROFK_EINVAL;
+  const Span sx(x, M, K, x_stride, PROFK_BF16), sw(w, N, K, w_stride, PROFK_BF16), sd(dy, M, N, dy_stride, dtype),
+      sp(pre, M, N, N, dtype), s1(dx, M, K, K, PROFK_BF16), s2(dw, N, K, K, PROFK_BF16), s3(dbias, 1, N, N, PROFK_F32);
+  for (const Span& o : {s1, s2, s3})
+    if (overlap(o, sx) || overlap(o, sw) || overlap(o, sd) || overlap(o, sp)) return PROFK_EINVAL;
+  if (overlap(s1, s2) || overlap(s1, s3) || overlap(s2, s3)) return PROFK_EINVAL;
+  if (ws_bytes < need) return PROFK_EWORKSPACE;
+  const profk::LinGradCall c{dy, pre, static_cast<uint64_t>(dy_stride), dtype, activation, x, w,
+                             static_cast<uint64_t>(x_stride), static_cast<uint64_t>(w_stride), M, N, K, dx, dw, dbias,
+                             ws};
+  const hipError_t e = profk::launch_linear_grad(c, static_cast<hipStream_t>(stream));
+  return e == hipSuccess ? PROFK_OK : hip_fail(e);
+}
+
+// ---- Penalties, biases and masks ----
+
+namespace {
+
+// The parts that both calls have; returns PROFK_OK for a call with rows.
+int check_adjust(int32_t dtype, const void* logits, int64_t T, int64_t V, int64_t x_stride, const int64_t* tokens,
+                 const int64_t* token_offsets, int64_t n_tokens, const float* repetition, const uint32_t* allowed,
+                 int64_t n_masks, int64_t allowed_stride, const int64_t* mask, const void* out, int64_t out_stride,
+                 profk::AdjustArgs* a) {
+  if (!dtype_ok(dtype)) return PROFK_EDTYPE;
+  if (V < 1 || V > static_cast<int64_t>(INT32_MAX) || !rows_ok(T, V, x_stride) || !rows_ok(T, V, out_stride))
+    return PROFK_EINVAL;
+  if (tokens && (n_tokens < 0 || n_tokens > static_cast<int64_t>(INT32_MAX))) return PROFK_EINVAL;
+  if (allowed) {
+    if (n_masks < 1 || allowed_stride < (V + 31) / 32 || allowed_stride > INT64_MAX / 8 / n_masks) return PROFK_EINVAL;
+    if (!mask && n_masks != 1 && n_masks != T) return PROFK_EINVAL;
+  }
+  if (T == 0) return PROFK_OK;
+  if (!logits || !out || (tokens && !token_offsets)) return PROFK_ENULL;
+  if (!aligned(logits, elem_size(dtype)) || !aligned(out, elem_size(dtype)) || !aligned(tokens, 8) ||
+      !aligned(token_offsets, 8) || !aligned(repetition, 4) || !aligned(allowed, 4) || !aligned(mask, 8))
+    return PROFK_EINVAL;
+  a->x = logits;
+  a->out = const_cast<void*>(out);
+  a->stride = static_cast<uint64_t>(x_stride);
+  a->out_stride = static_cast<uint64_t>(out_stride);
+  a->V = static_cast<uint32_t>(V);
+  a->tokens = tokens;
+  a->offsets = token_offsets;
+  a->n_tokens = n_tokens;
+  a->repetition = repetition;
+  a->allowed = allowed;
+  a->allowed_stride = static_cast<uint64_t>(allowed_stride);
+  a->n_masks = n_masks;
+  a->mask = mask;
+  return PROFK_OK;
+}
+
+}  // namespace
+
+int profk_adjust_logits(int32_t dtype, const void* logits, int64_t T, int64_t V, int64_t x_stride,
+                        const int64_t* tokens, const int64_t* token_offsets, int64_t n_tokens,
+                        const int64_t* n_prompt, const float* repetition, const float* presence,
+                        const float* frequency, const int64_t* bias_ids, const float* bias_values,
+                        const int64_t* bias_offsets, int64_t n_bias, const uint32_t* allowed, int64_t n_masks,
+                        int64_t allowed_stride, const int64_t* mask, void* out, int64_t out_stride, void* stream) {
+  profk::AdjustArgs a{};
+  const int rc = check_adjust(dtype, logits, T, V, x_stride, tokens, token_offsets, n_tokens, repetition, allowed,
+                              n_masks, allowed_stride, mask, out, out_stride, &a);
+  if (rc != PROFK_OK) return rc;
+  if (bias_ids && (n_bias < 0 || n_bias > static_cast<int64_t>(INT32_MAX))) return PROFK_EINVAL;
+  if (T == 0) return PROFK_OK;
+  if (bias_ids && (!bias_values || !bias_offsets)) return PROFK_ENULL;
+  if (!aligned(n_prompt, 8) || !aligned(presence, 4) || !aligned(frequency, 4) || !aligned(bias_ids, 8) ||
+      !aligned(bias_values, 4) || !aligned(bias_offsets, 8))
+    return PROFK_EINVAL;
+  const bool same = logits == out && (x_stride == out_stride || T == 1);
+  if (!same && overlap(Span(logits, T, V, x_stride, dtype), Span(out, T, V, out_stride, dtype))) return PROFK_EINVAL;
+  a.n_prompt = n_prompt;
+  a.presence = presence;
+  a.frequency = frequency;
+  a.bias_ids = bias_ids;
+  a.bias_values = bias_values;
+  a.bias_offsets = bias_offsets;
+  a.n_bias = n_bias;
+  const hipError_t e = profk::launch_adjust(a, dtype, T, static_cast<hipStream_t>(stream));
+  return e == hipSuccess ? PROFK_OK : hip_fail(e);
+}
+
+int profk_adjust_logits_grad(int32_t dtype, const void* d_out, int64_t d_stride, const void* logits, int64_t T,
+                             int64_t V, int64_t x_stride, const int64_t* tokens, const int64_t* token_offsets,
+                             int64_t n_tokens, const float* repetition, const uint32_t* allowed, int64_t n_masks,
+                             int64_t allowed_stride, const int64_t* mask, void* out, int64_t out_stride,
+                             void* stream) {
+  profk::AdjustArgs a{};
+  const int rc = check_adjust(dtype, logits, T, V, x_stride, tokens, token_offsets, n_tokens, repetition, allowed,
+                              n_masks, allowed_stride, mask, out, out_stride, &a);
+  if (rc != PROFK_OK) return rc;
+  if (!rows_ok(T, V, d_stride)) return PROFK_EINVAL;
+  if (T == 0) return PROFK_OK;
+  if (!d_out) return PROFK_ENULL;
+  if (!aligned(d_out, elem_size(dtype))) return PROFK_EINVAL;
+  const Span so(out, T, V, out_stride, dtype);
+  const bool same = d_out == out && (d_stride == out_stride || T == 1);
+  if (overlap(so, Span(logits, T, V, x_stride, dtype)) || (!same && overlap(so, Span(d_out, T, V, d_stride, dtype))))
+    return PROFK_EINVAL;
+  // (without a repetition penalty the history has no part in the gradient)
+  if (!repetition) a.tokens = nullptr;
+  a.dy = d_out;
+  a.dy_stride = static_cast<uint64_t>(d_stride);
+  const hipError_t e = profk::launch_adjust(a, dtype, T, static_cast<hipStream_t>(stream));
+  return e == hipSuccess ? PROFK_OK : hip_fail(e);
 }
 
 int profk_debug_sample_indices(uint64_t seed, int64_t row, int64_t S, int64_t N, int64_t* out_dev,

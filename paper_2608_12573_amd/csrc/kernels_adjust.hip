@@ -1,0 +1,147 @@
+// Penalties for repeated tokens, biases and masks of allowed tokens on rows of
+// logits, and the gradient with respect to the logits.
+//
+// Of a row x with its history (the first n_prompt tokens of it a prompt), c_v
+// the occurrences of v after the prompt:
+//   u_v = x_v / repetition if x_v > 0, x_v repetition otherwise, where v is in
+//         the history, else x_v
+//   y_v = u_v - [c_v > 0] presence - c_v frequency + bias_v, or -inf where the
+//         row's mask forbids v
+//   dx_v = dy_v (1 / repetition, repetition or 1), or 0 where it is forbidden.
+//
+// A workgroup takes a piece of a row.  It counts the history's tokens that fall
+// into its piece in LDS, a word a token (integer atomics: their order changes
+// nothing), notes the last bias of each token beside it, and streams the piece
+// once.  Every piece reads the whole history again, from the caches.
+#include "adjust.h"
+#include "elem8.h"
+#include "launch.h"
+
+namespace profk {
+
+namespace {
+
+constexpr uint32_t kAdjPrompt = 0x80000000u;   // of a token's word: it is in the prompt; the rest counts it after
+constexpr uint32_t kAdjMaxPiece = 8192;        // elements (LDS: a word each, two with biases)
+
+__device__ __forceinline__ int64_t clamp64(int64_t x, int64_t lo, int64_t hi) { return x < lo ? lo : x > hi ? hi : x; }
+
+template <int DT, bool GRAD> __global__ __launch_bounds__(512) void k_adjust(AdjustArgs a) {
+  extern __shared__ __align__(16) uint32_t s_word[];     // [piece], then the biases' [piece]
+  const uint32_t row = a.row + blockIdx.x / a.pieces, p = blockIdx.x % a.pieces;
+  const uint32_t v0 = p * a.piece, n = min(a.piece, a.V - v0);
+  constexpr uint32_t ES = DT == PROFK_F32 ? 4 : 2;
+  const uint32_t tid = threadIdx.x, BS = blockDim.x;
+  // (a list's offsets may be anything: none reaches past the list)
+  int64_t h0 = 0, h1 = 0, b0 = 0, b1 = 0;
+  if (a.tokens) {
+    h0 = clamp64(a.offsets[row], 0, a.n_tokens);
+    h1 = clamp64(a.offsets[row + 1], h0, a.n_tokens);
+  }
+  if (!GRAD && a.bias_ids) {
+    b0 = clamp64(a.bias_offsets[row], 0, a.n_bias);
+    b1 = clamp64(a.bias_offsets[row + 1], b0, a.n_bias);
+  }
+  const bool hist = h1 > h0, bias = b1 > b0;
+  uint32_t* const s_bias = s_word + (a.tokens ? a.piece : 0);
+  if (hist || bias) {
+    for (uint32_t i = tid; i < a.piece; i += BS) {
+      if (hist) s_word[i] = 0;
+      if (bias) s_bias[i] = 0;
+    }
+    __syncthreads();
+    const int64_t made = h0 + (a.n_prompt && hist ? clamp64(a.n_prompt[row], 0, h1 - h0) : 0);
+    for (int64_t i = h0 + tid; i < h1; i += BS) {
+      const uint64_t v = static_cast<uint64_t>(a.tokens[i]) - v0;
+      if (v < n) {
+        if (i < made) atomicOr(s_word + v, kAdjPrompt);
+        else atomicAdd(s_word + v, 1u);
+      }
+    }
+    for (int64_t i = b0 + tid; i < b1; i += BS) {
+      const uint64_t v = static_cast<uint64_t>(a.bias_ids[i]) - v0;
+      if (v < n) atomicMax(s_bias + v, static_cast<uint32_t>(i - b0) + 1);
+    }
+    __syncthreads();
+  }
+  const uint32_t* words = nullptr;
+  bool lost = false;                 // the row names a mask that is not there
+  if (a.allowed) {
+    const int64_t k = a.mask ? a.mask[row] : a.n_masks == 1 ? 0 : row;
+    lost = k >= a.n_masks;
+    if (k >= 0 && !lost) words = a.allowed + static_cast<uint64_t>(k) * a.allowed_stride;
+  }
+  const float rep = a.repetition ? a.repetition[row] : 1.0f;
+  const float pres = !GRAD && a.presence ? a.presence[row] : 0.0f;
+  const float freq = !GRAD && a.frequency ? a.frequency[row] : 0.0f;
+  const float nan = __builtin_nanf("");
+  const char* const x = static_cast<const char*>(a.x) + (row * a.stride + v0) * ES;
+  const char* const src = GRAD ? static_cast<const char*>(a.dy) + (row * a.dy_stride + v0) * ES : x;
+  char* const out = static_cast<char*>(a.out) + (row * a.out_stride + v0) * ES;
+  for (uint32_t i = tid * 8; i < n; i += BS * 8) {
+    float y[8];
+    load8<DT>(src, i, n, y);
+    // (a piece starts at a multiple of 32 tokens)
+    const uint32_t ok = words ? words[(v0 + i) / 32] >> (i % 32) : 0xFFu;
+    // (the words past the row's end stay 0)
+    u32x4 c4[2] = {}, k4[2] = {};
+    if (hist) {
+      c4[0] = *reinterpret_cast<const u32x4*>(s_word + i);
+      c4[1] = *reinterpret_cast<const u32x4*>(s_word + i + 4);
+    }
+    if (bias) {
+      k4[0] = *reinterpret_cast<const u32x4*>(s_bias + i);
+      k4[1] = *reinterpret_cast<const u32x4*>(s_bias + i + 4);
+    }
+#pragma unroll
+    for (uint32_t e = 0; e < 8; ++e) {
+      const uint32_t c = c4[e / 4][e % 4], k = k4[e / 4][e % 4];
+      if (c) {
+        if constexpr (GRAD) {
+          if (a.repetition) y[e] = load1(x, i + e, DT) > 0.0f ? y[e] / rep : y[e] * rep;
+        } else {
+          if (a.repetition) y[e] = y[e] > 0.0f ? y[e] / rep : y[e] * rep;
+          const uint32_t m = c & ~kAdjPrompt;
+          if (m) y[e] -= fmaf(static_cast<float>(m), freq, pres);
+        }
+      }
+      if (k) y[e] += a.bias_values[b0 + k - 1];
+      if (!(ok >> e & 1)) y[e] = GRAD ? 0.0f : -__builtin_inff();
+      if (lost) y[e] = nan;
+    }
+    store8<DT>(out, i, n, y);
+  }
+}
+
+}  // namespace
+
+hipError_t launch_adjust(AdjustArgs a, int dtype, int64_t T, hipStream_t s) {
+  const uint32_t cus = static_cast<uint32_t>(device_cu_count());
+  // pieces of whole words of the mask; more of them where the rows are few
+  uint32_t piece = kAdjMaxPiece;
+  while (piece > 1024 && static_cast<uint64_t>(T) * ((a.V + piece - 1) / piece) < 2 * cus) piece /= 2;
+  if (a.V < piece) piece = (a.V + 31) / 32 * 32;
+  a.piece = piece;
+  a.pieces = (a.V + piece - 1) / piece;
+  uint32_t bs = 512;
+  while (bs > 64 && bs * 8 >= 2 * piece) bs /= 2;
+  const uint32_t lds = ((a.tokens ? piece : 0) + (!a.dy && a.bias_ids ? piece : 0)) * 4;
+  const int64_t step = ((int64_t{1} << 31) - 1) / bs / a.pieces < 1 ? 1 : ((int64_t{1} << 31) - 1) / bs / a.pieces;
+  (void)hipGetLastError();
+  for (int64_t r = 0; r < T; r += step) {
+    a.row = static_cast<uint32_t>(r);
+    const uint32_t grid = static_cast<uint32_t>(T - r < step ? T - r : step) * a.pieces;
+    if (dtype == PROFK_F32) {
+      if (a.dy) k_adjust<PROFK_F32, true><<<grid, bs, lds, s>>>(a);
+      else k_adjust<PROFK_F32, false><<<grid, bs, lds, s>>>(a);
+    } else {
+      if (a.dy) k_adjust<PROFK_BF16, true><<<grid, bs, lds, s>>>(a);
+      else k_adjust<PROFK_BF16, false><<<grid, bs, lds, s>>>(a);
+    }
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
+
+}  // namespace profk

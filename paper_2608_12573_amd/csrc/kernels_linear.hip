@@ -1,0 +1,296 @@
+// The dense product of bf16 matrices with bias, activation and residual in its
+// epilogue, and its gradients.
+//
+//   z = x W^T + b,  y = act(z) + residual,  dz = dy act'(z)
+//   dx = dz W,  dW = dz^T x,  db = sum over the rows of dz.
+// Products are exact in fp32 and summed in it on the matrix cores; bias,
+// activation and residual are fp32, and y (and z, where it is kept) is rounded
+// once.  dz is rounded to bf16 for the matrix cores: within 2^-8 of each term,
+// which the two products average over their sums.  db is summed from dz before
+// that.
+//
+// All three products are P[i, j] = sum_k A(i, k) B(j, k) with either operand's k
+// neighbouring in memory ("along") or a whole row apart ("across").
+#include <type_traits>
+
+#include "elem8.h"
+#include "launch.h"
+#include "linear.h"
+
+namespace profk {
+
+namespace {
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+
+// ------------------------------------------------------------ activations ---
+// An infinite z gives the limit, NaN stays NaN.
+__device__ __forceinline__ float act_of(float z, int act) {
+  if (act == PROFK_ACT_RELU) return z < 0.0f ? 0.0f : z;
+  if (act == PROFK_ACT_GELU) return 0.5f * (z < -40.0f ? -40.0f : z) * erfcf(z * -0.70710678118654752f);
+  if (act == PROFK_ACT_SILU) return (z < -126.0f ? -126.0f : z) / (1.0f + __expf(-z));
+  return z;
+}
+__device__ __forceinline__ float slope_of(float z, int act) {
+  if (act == PROFK_ACT_RELU) return z > 0.0f ? 1.0f : 0.0f;
+  if (act == PROFK_ACT_GELU) {
+    const float c = z < -40.0f ? -40.0f : z > 40.0f ? 40.0f : z;
+    return 0.5f * erfcf(c * -0.70710678118654752f) + c * __expf(-0.5f * c * c) * 0.39894228040143268f;
+  }
+  if (act == PROFK_ACT_SILU) {
+    const float c = z < -126.0f ? -126.0f : z > 126.0f ? 126.0f : z;   // (e^126 is infinite: p = 0)
+    const float p = 1.0f / (1.0f + __expf(-c));
+    return p * (1.0f + c * (1.0f - p));
+  }
+  return 1.0f;
+}
+
+// ---------------------------------------------------------------- product ---
+struct ProdArgs {
+  const __bf16 *a, *b;
+  uint64_t as, bs;                  // elements from row to row (along: of i or j, across: of k)
+  uint32_t I, J, K;
+  const float* bias;                // [J]
+  int act, out_dtype;
+  const void* residual;
+  uint64_t residual_stride;
+  void *out, *pre;                  // [I, J]
+  uint32_t i0, j0;                  // first row and column of this launch
+};
+
+__device__ __forceinline__ void put(const ProdArgs& g, uint32_t i, uint32_t j, float z) {
+  const size_t at = static_cast<size_t>(i) * g.J + j;
+  if (g.bias) z += g.bias[j];
+  float y = act_of(z, g.act);
+  if (g.residual) {
+    const size_t r = i * g.residual_stride + j;
+    y += g.out_dtype == PROFK_F32 ? static_cast<const float*>(g.residual)[r]
+                                  : static_cast<float>(static_cast<const __bf16*>(g.residual)[r]);
+  }
+  if (g.out_dtype == PROFK_F32) {
+    static_cast<float*>(g.out)[at] = y;
+    if (g.pre) static_cast<float*>(g.pre)[at] = z;
+  } else {
+    static_cast<__bf16*>(g.out)[at] = static_cast<__bf16>(y);
+    if (g.pre) static_cast<__bf16*>(g.pre)[at] = static_cast<__bf16>(z);
+  }
+}
+
+// Any sizes, strides and alignments: tiles of 128 x 128 on four waves of 64 x 64,
+// 32 of k at a time through registers to LDS, its rows 80 bytes apart.
+constexpr uint32_t kAnyB = 128, kAnyK = 32, kAnyRow = 40;
+
+// 8 neighbours in memory, those from `left` on 0.
+__device__ __forceinline__ u32x4 load_part8(const __bf16* p, uint32_t left) {
+  return load_raw8<PROFK_BF16>(p, 0, left).q[0];
+}
+
+template <bool ACROSS> struct AnyTile {
+  u32x4 v[2];
+  // rows r0 .. r0 + 127 of R, k0 .. k0 + 31 of K
+  __device__ __forceinline__ void load(const __bf16* p, uint64_t stride, uint32_t r0, uint32_t R, uint32_t k0, uint32_t K) {
+#pragma unroll
+    for (uint32_t q = 0; q < 2; ++q) {
+      const uint32_t t = threadIdx.x + q * 256;
+      const uint32_t r = r0 + (ACROSS ? t % 16 * 8 : t / 4), k = k0 + (ACROSS ? t / 16 : t % 4 * 8);
+      v[q] = u32x4{};
+      if (r < R && k < K) v[q] = ACROSS ? load_part8(p + k * stride + r, R - r) : load_part8(p + r * stride + k, K - k);
+    }
+  }
+  __device__ __forceinline__ void store(uint16_t* s) const {
+#pragma unroll
+    for (uint32_t q = 0; q < 2; ++q) {
+      const uint32_t t = threadIdx.x + q * 256;
+      if constexpr (ACROSS) {
+#pragma unroll
+        for (uint32_t e = 0; e < 8; ++e)
+          s[(t % 16 * 8 + e) * kAnyRow + t / 16] = static_cast<uint16_t>(v[q][e / 2] >> (16 * (e % 2)));
+      } else {
+        *reinterpret_cast<u32x4*>(s + t / 4 * kAnyRow + t % 4 * 8) = v[q];
+      }
+    }
+  }
+};
+
+template <bool TA, bool TB> __global__ __launch_bounds__(256) void k_prod_any(ProdArgs g, uint32_t tiles_i) {
+  __shared__ __align__(16) uint16_t sa[kAnyB * kAnyRow], sb[kAnyB * kAnyRow];
+  const uint32_t i0 = g.i0 + blockIdx.x % tiles_i * kAnyB, j0 = g.j0 + blockIdx.x / tiles_i * kAnyB;
+  const uint32_t lane = threadIdx.x & (kWave - 1), w = threadIdx.x / kWave;
+  const uint32_t c = lane & 31, h = lane >> 5, wi = w / 2 * 64, wj = w % 2 * 64;
+  AnyTile<TA> ta;
+  AnyTile<TB> tb;
+  f32x16 acc[2][2] = {};
+  ta.load(g.a, g.as, i0, g.I, 0, g.K);
+  tb.load(g.b, g.bs, j0, g.J, 0, g.K);
+  for (uint32_t k0 = 0; k0 < g.K; k0 += kAnyK) {
+    __syncthreads();
+    ta.store(sa);
+    tb.store(sb);
+    __syncthreads();
+    if (k0 + kAnyK < g.K) {
+      ta.load(g.a, g.as, i0, g.I, k0 + kAnyK, g.K);
+      tb.load(g.b, g.bs, j0, g.J, k0 + kAnyK, g.K);
+    }
+#pragma unroll
+    for (uint32_t q = 0; q < 2; ++q) {
+      bf16x8 fa[2], fb[2];
+#pragma unroll
+      for (uint32_t u = 0; u < 2; ++u) {
+        fa[u] = *reinterpret_cast<const bf16x8*>(sa + (wi + u * 32 + c) * kAnyRow + q * 16 + h * 8);
+        fb[u] = *reinterpret_cast<const bf16x8*>(sb + (wj + u * 32 + c) * kAnyRow + q * 16 + h * 8);
+      }
+#pragma unroll
+      for (uint32_t u = 0; u < 2; ++u)
+#pragma unroll
+        for (uint32_t v = 0; v < 2; ++v)
+          acc[u][v] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa[u], fb[v], acc[u][v], 0, 0, 0);
+    }
+  }
+#pragma unroll
+  for (uint32_t u = 0; u < 2; ++u)
+#pragma unroll
+    for (uint32_t v = 0; v < 2; ++v)
+#pragma unroll
+      for (uint32_t e = 0; e < 16; ++e) {
+        const uint32_t i = i0 + wi + u * 32 + 8 * (e / 4) + 4 * h + e % 4, j = j0 + wj + v * 32 + c;
+        if (i < g.I && j < g.J) put(g, i, j, acc[u][v][e]);
+      }
+}
+
+template <bool TA, bool TB> hipError_t launch_product(ProdArgs g, hipStream_t s) {
+  const uint64_t ti = (g.I + kAnyB - 1) / kAnyB, tj = (g.J + kAnyB - 1) / kAnyB;
+  (void)hipGetLastError();
+  constexpr uint64_t kMost = 2048;   // tiles a side of a launch (fewer than 2^32 threads)
+  for (uint64_t j = 0; j < tj; j += kMost) {
+    for (uint64_t i = 0; i < ti; i += kMost) {
+      g.i0 = static_cast<uint32_t>(i * kAnyB);
+      g.j0 = static_cast<uint32_t>(j * kAnyB);
+      const uint32_t ni = static_cast<uint32_t>(ti - i < kMost ? ti - i : kMost);
+      const uint32_t nj = static_cast<uint32_t>(tj - j < kMost ? tj - j : kMost);
+      k_prod_any<TA, TB><<<ni * nj, 256, 0, s>>>(g, ni);
+      const hipError_t e = hipGetLastError();
+      if (e != hipSuccess) return e;
+    }
+  }
+  return hipSuccess;
+}
+
+// --------------------------------------------------------------------- dz ---
+// dz = dy act'(z) to bf16, and the sums of its columns over a part of the rows.
+struct DzArgs {
+  const void *dy, *pre;
+  uint64_t dy_stride;
+  uint32_t M, N, parts;
+  int act;
+  __bf16* dz;                       // rows dz_stride apart; null: only the sums
+  uint64_t dz_stride;
+  float* part;                      // [parts, N], or null
+};
+
+template <int DT> __global__ __launch_bounds__(256) void k_dz(DzArgs a) {
+  const uint32_t j = (blockIdx.x * 256 + threadIdx.x) * 8, p = blockIdx.y;
+  if (j >= a.N) return;
+  constexpr uint32_t ES = DT == PROFK_F32 ? 4 : 2;
+  const uint32_t r0 = static_cast<uint32_t>(static_cast<uint64_t>(a.M) * p / a.parts);
+  const uint32_t r1 = static_cast<uint32_t>(static_cast<uint64_t>(a.M) * (p + 1) / a.parts);
+  float sum[8] = {}, d[8], z[8];
+  for (uint32_t r = r0; r < r1; ++r) {
+    load8<DT>(static_cast<const char*>(a.dy) + r * a.dy_stride * ES, j, a.N, d);
+    if (a.pre) {
+      load8<DT>(static_cast<const char*>(a.pre) + static_cast<uint64_t>(r) * a.N * ES, j, a.N, z);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) d[e] *= slope_of(z[e], a.act);
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) sum[e] += d[e];
+    if (a.dz) store8<PROFK_BF16>(a.dz + r * a.dz_stride, j, a.N, d);
+  }
+  if (a.part) store8<PROFK_F32>(a.part + static_cast<size_t>(p) * a.N, j, a.N, sum);
+}
+
+constexpr uint32_t kJoinCols = 64, kJoinRows = 16;
+
+__global__ __launch_bounds__(kJoinCols * kJoinRows) void k_db_join(const float* part, uint32_t parts, uint32_t N, float* db) {
+  __shared__ float s[kJoinRows][kJoinCols];
+  const uint32_t c = threadIdx.x % kJoinCols, k = threadIdx.x / kJoinCols, j = blockIdx.x * kJoinCols + c;
+  float sum = 0.0f;
+  if (j < N)
+    for (uint32_t p = k; p < parts; p += kJoinRows) sum += part[static_cast<size_t>(p) * N + j];
+  s[k][c] = sum;
+  __syncthreads();
+  if (k != 0 || j >= N) return;
+#pragma unroll
+  for (uint32_t q = 1; q < kJoinRows; ++q) sum += s[q][c];
+  db[j] = sum;
+}
+
+uint32_t dz_parts(int64_t M, int64_t N, int num_cus) {
+  const int64_t slabs = N > 0 ? (N + 2047) / 2048 : 1, most = (static_cast<int64_t>(num_cus) * 8 + slabs - 1) / slabs;
+  const int64_t parts = M < most ? M : most;
+  return parts < 1 ? 1u : static_cast<uint32_t>(parts);
+}
+
+size_t align256(size_t n) { return (n + 255) / 256 * 256; }
+
+struct GradLayout {
+  size_t dz, part, bytes;           // offsets
+  uint64_t dz_stride;
+  uint32_t parts;
+};
+GradLayout grad_layout(int64_t M, int64_t N, int64_t K, int num_cus) {
+  GradLayout L{};
+  L.dz_stride = (static_cast<uint64_t>(N) + 7) / 8 * 8;
+  L.parts = dz_parts(M, N, num_cus);
+  L.part = align256(static_cast<size_t>(M) * L.dz_stride * 2);
+  L.bytes = L.part + align256(static_cast<size_t>(L.parts) * N * 4);
+  return L;
+}
+
+}  // namespace
+
+size_t lin_workspace(int64_t, int64_t, int64_t, int) { return 0; }
+
+size_t lin_grad_workspace(int64_t M, int64_t N, int64_t K, int num_cus) { return grad_layout(M, N, K, num_cus).bytes; }
+
+hipError_t launch_linear(const LinCall& c, hipStream_t s) {
+  const ProdArgs g{static_cast<const __bf16*>(c.x), static_cast<const __bf16*>(c.w), c.x_stride, c.w_stride,
+                   static_cast<uint32_t>(c.M), static_cast<uint32_t>(c.N), static_cast<uint32_t>(c.K), c.bias, c.act,
+                   c.out_dtype, c.residual, c.residual_stride, c.out, c.pre, 0, 0};
+  return launch_product<false, false>(g, s);
+}
+
+hipError_t launch_linear_grad(const LinGradCall& c, hipStream_t s) {
+  const GradLayout L = grad_layout(c.M, c.N, c.K, device_cu_count());
+  uint8_t* const ws = static_cast<uint8_t*>(c.ws);
+  const uint32_t M = static_cast<uint32_t>(c.M), N = static_cast<uint32_t>(c.N), K = static_cast<uint32_t>(c.K);
+  __bf16* const dz = reinterpret_cast<__bf16*>(ws + L.dz);
+  float* const part = reinterpret_cast<float*>(ws + L.part);
+  const DzArgs d{c.dy, c.act == PROFK_ACT_NONE ? nullptr : c.pre, c.dy_stride, M, N, L.parts, c.act,
+                 c.dx || c.dw ? dz : nullptr, L.dz_stride, c.db ? part : nullptr};
+  (void)hipGetLastError();
+  const dim3 grid((N + 2047) / 2048, L.parts);
+  hipError_t e = hipSuccess;
+  if (N) {
+    if (c.dtype == PROFK_F32) k_dz<PROFK_F32><<<grid, 256, 0, s>>>(d);
+    else k_dz<PROFK_BF16><<<grid, 256, 0, s>>>(d);
+    e = hipGetLastError();
+  }
+  if (e == hipSuccess && c.db && N) {
+    k_db_join<<<(N + kJoinCols - 1) / kJoinCols, kJoinCols * kJoinRows, 0, s>>>(part, L.parts, N, c.db);
+    e = hipGetLastError();
+  }
+  if (e == hipSuccess && c.dx && M) {
+    const ProdArgs g{dz, static_cast<const __bf16*>(c.w), L.dz_stride, c.w_stride, M, K, N, nullptr, PROFK_ACT_NONE,
+                     PROFK_BF16, nullptr, 0, c.dx, nullptr, 0, 0};
+    e = launch_product<false, true>(g, s);
+  }
+  if (e == hipSuccess && c.dw && N) {
+    const ProdArgs g{dz, static_cast<const __bf16*>(c.x), L.dz_stride, c.x_stride, N, K, M, nullptr, PROFK_ACT_NONE,
+                     PROFK_BF16, nullptr, 0, c.dw, nullptr, 0, 0};
+    e = launch_product<true, true>(g, s);
+  }
+  return e;
+}
+
+}  // namespace profk
