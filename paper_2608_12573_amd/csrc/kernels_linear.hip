@@ -13,9 +13,9 @@
 // neighbouring in memory ("along") or a whole row apart ("across").
 #include <type_traits>
 
-#include "elem8.h"
 #include "launch.h"
 #include "linear.h"
+#include "product.h"
 
 namespace profk {
 
@@ -24,45 +24,18 @@ namespace {
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
-// ------------------------------------------------------------ activations ---
-// An infinite z gives the limit, NaN stays NaN.
-__device__ __forceinline__ float act_of(float z, int act) {
-  if (act == PROFK_ACT_RELU) return z < 0.0f ? 0.0f : z;
-  if (act == PROFK_ACT_GELU) return 0.5f * (z < -40.0f ? -40.0f : z) * erfcf(z * -0.70710678118654752f);
-  if (act == PROFK_ACT_SILU) return (z < -126.0f ? -126.0f : z) / (1.0f + __expf(-z));
+// ------------------------------------------------- product of any operands ---
+__device__ __forceinline__ float act_any(float z, int act) {
+  if (act == PROFK_ACT_RELU) return act_of<PROFK_ACT_RELU>(z);
+  if (act == PROFK_ACT_GELU) return act_of<PROFK_ACT_GELU>(z);
+  if (act == PROFK_ACT_SILU) return act_of<PROFK_ACT_SILU>(z);
   return z;
 }
-__device__ __forceinline__ float slope_of(float z, int act) {
-  if (act == PROFK_ACT_RELU) return z > 0.0f ? 1.0f : 0.0f;
-  if (act == PROFK_ACT_GELU) {
-    const float c = z < -40.0f ? -40.0f : z > 40.0f ? 40.0f : z;
-    return 0.5f * erfcf(c * -0.70710678118654752f) + c * __expf(-0.5f * c * c) * 0.39894228040143268f;
-  }
-  if (act == PROFK_ACT_SILU) {
-    const float c = z < -126.0f ? -126.0f : z > 126.0f ? 126.0f : z;   // (e^126 is infinite: p = 0)
-    const float p = 1.0f / (1.0f + __expf(-c));
-    return p * (1.0f + c * (1.0f - p));
-  }
-  return 1.0f;
-}
-
-// ---------------------------------------------------------------- product ---
-struct ProdArgs {
-  const __bf16 *a, *b;
-  uint64_t as, bs;                  // elements from row to row (along: of i or j, across: of k)
-  uint32_t I, J, K;
-  const float* bias;                // [J]
-  int act, out_dtype;
-  const void* residual;
-  uint64_t residual_stride;
-  void *out, *pre;                  // [I, J]
-  uint32_t i0, j0;                  // first row and column of this launch
-};
 
 __device__ __forceinline__ void put(const ProdArgs& g, uint32_t i, uint32_t j, float z) {
   const size_t at = static_cast<size_t>(i) * g.J + j;
   if (g.bias) z += g.bias[j];
-  float y = act_of(z, g.act);
+  float y = act_any(z, g.act);
   if (g.residual) {
     const size_t r = i * g.residual_stride + j;
     y += g.out_dtype == PROFK_F32 ? static_cast<const float*>(g.residual)[r]
@@ -158,7 +131,7 @@ template <bool TA, bool TB> __global__ __launch_bounds__(256) void k_prod_any(Pr
       }
 }
 
-template <bool TA, bool TB> hipError_t launch_product(ProdArgs g, hipStream_t s) {
+template <bool TA, bool TB> hipError_t launch_any(ProdArgs g, hipStream_t s) {
   const uint64_t ti = (g.I + kAnyB - 1) / kAnyB, tj = (g.J + kAnyB - 1) / kAnyB;
   (void)hipGetLastError();
   constexpr uint64_t kMost = 2048;   // tiles a side of a launch (fewer than 2^32 threads)
@@ -182,13 +155,12 @@ struct DzArgs {
   const void *dy, *pre;
   uint64_t dy_stride;
   uint32_t M, N, parts;
-  int act;
   __bf16* dz;                       // rows dz_stride apart; null: only the sums
   uint64_t dz_stride;
   float* part;                      // [parts, N], or null
 };
 
-template <int DT> __global__ __launch_bounds__(256) void k_dz(DzArgs a) {
+template <int DT, int ACT> __global__ __launch_bounds__(256) void k_dz(DzArgs a) {
   const uint32_t j = (blockIdx.x * 256 + threadIdx.x) * 8, p = blockIdx.y;
   if (j >= a.N) return;
   constexpr uint32_t ES = DT == PROFK_F32 ? 4 : 2;
@@ -197,10 +169,10 @@ template <int DT> __global__ __launch_bounds__(256) void k_dz(DzArgs a) {
   float sum[8] = {}, d[8], z[8];
   for (uint32_t r = r0; r < r1; ++r) {
     load8<DT>(static_cast<const char*>(a.dy) + r * a.dy_stride * ES, j, a.N, d);
-    if (a.pre) {
+    if constexpr (ACT != PROFK_ACT_NONE) {
       load8<DT>(static_cast<const char*>(a.pre) + static_cast<uint64_t>(r) * a.N * ES, j, a.N, z);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) d[e] *= slope_of(z[e], a.act);
+      for (int e = 0; e < 8; ++e) d[e] *= slope_of<ACT>(z[e]);
     }
 #pragma unroll
     for (int e = 0; e < 8; ++e) sum[e] += d[e];
@@ -257,7 +229,9 @@ hipError_t launch_linear(const LinCall& c, hipStream_t s) {
   const ProdArgs g{static_cast<const __bf16*>(c.x), static_cast<const __bf16*>(c.w), c.x_stride, c.w_stride,
                    static_cast<uint32_t>(c.M), static_cast<uint32_t>(c.N), static_cast<uint32_t>(c.K), c.bias, c.act,
                    c.out_dtype, c.residual, c.residual_stride, c.out, c.pre, 0, 0};
-  return launch_product<false, false>(g, s);
+  (void)hipGetLastError();
+  if (launch_product_along(g, static_cast<uint32_t>(device_cu_count()), s)) return hipGetLastError();
+  return launch_any<false, false>(g, s);
 }
 
 hipError_t launch_linear_grad(const LinGradCall& c, hipStream_t s) {
@@ -266,14 +240,21 @@ hipError_t launch_linear_grad(const LinGradCall& c, hipStream_t s) {
   const uint32_t M = static_cast<uint32_t>(c.M), N = static_cast<uint32_t>(c.N), K = static_cast<uint32_t>(c.K);
   __bf16* const dz = reinterpret_cast<__bf16*>(ws + L.dz);
   float* const part = reinterpret_cast<float*>(ws + L.part);
-  const DzArgs d{c.dy, c.act == PROFK_ACT_NONE ? nullptr : c.pre, c.dy_stride, M, N, L.parts, c.act,
-                 c.dx || c.dw ? dz : nullptr, L.dz_stride, c.db ? part : nullptr};
+  // (without an activation, dy in bf16 is dz)
+  const bool given = c.act == PROFK_ACT_NONE && c.dtype == PROFK_BF16;
+  const DzArgs d{c.dy, c.pre, c.dy_stride, M, N, L.parts, (c.dx || c.dw) && !given ? dz : nullptr, L.dz_stride,
+                 c.db ? part : nullptr};
+  const __bf16* const z = given ? static_cast<const __bf16*>(c.dy) : dz;
+  const uint64_t z_stride = given ? c.dy_stride : L.dz_stride;
+  const uint32_t cus = static_cast<uint32_t>(device_cu_count());
   (void)hipGetLastError();
   const dim3 grid((N + 2047) / 2048, L.parts);
   hipError_t e = hipSuccess;
-  if (N) {
-    if (c.dtype == PROFK_F32) k_dz<PROFK_F32><<<grid, 256, 0, s>>>(d);
-    else k_dz<PROFK_BF16><<<grid, 256, 0, s>>>(d);
+  if (N && (d.dz || d.part)) {
+    with_act(c.act, [&](auto act) {
+      if (c.dtype == PROFK_F32) k_dz<PROFK_F32, decltype(act)::value><<<grid, 256, 0, s>>>(d);
+      else k_dz<PROFK_BF16, decltype(act)::value><<<grid, 256, 0, s>>>(d);
+    });
     e = hipGetLastError();
   }
   if (e == hipSuccess && c.db && N) {
@@ -281,14 +262,14 @@ hipError_t launch_linear_grad(const LinGradCall& c, hipStream_t s) {
     e = hipGetLastError();
   }
   if (e == hipSuccess && c.dx && M) {
-    const ProdArgs g{dz, static_cast<const __bf16*>(c.w), L.dz_stride, c.w_stride, M, K, N, nullptr, PROFK_ACT_NONE,
+    const ProdArgs g{z, static_cast<const __bf16*>(c.w), z_stride, c.w_stride, M, K, N, nullptr, PROFK_ACT_NONE,
                      PROFK_BF16, nullptr, 0, c.dx, nullptr, 0, 0};
-    e = launch_product<false, true>(g, s);
+    e = launch_product_grad(g, false, cus, s) ? hipGetLastError() : launch_any<false, true>(g, s);
   }
   if (e == hipSuccess && c.dw && N) {
-    const ProdArgs g{dz, static_cast<const __bf16*>(c.x), L.dz_stride, c.x_stride, N, K, M, nullptr, PROFK_ACT_NONE,
+    const ProdArgs g{z, static_cast<const __bf16*>(c.x), z_stride, c.x_stride, N, K, M, nullptr, PROFK_ACT_NONE,
                      PROFK_BF16, nullptr, 0, c.dw, nullptr, 0, 0};
-    e = launch_product<true, true>(g, s);
+    e = launch_product_grad(g, true, cus, s) ? hipGetLastError() : launch_any<true, true>(g, s);
   }
   return e;
 }

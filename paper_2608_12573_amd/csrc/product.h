@@ -1,0 +1,86 @@
+// The dense product P[i, j] = sum_k A(i, k) B(j, k) of bf16 operands: its
+// arguments, epilogue and launches (kernels_product.hip, kernels_product_grad.hip,
+// kernels_linear.hip).
+#pragma once
+
+#include "elem8.h"
+
+namespace profk {
+
+// An operand lies "along" k, a row of K neighbours for each i (or j), or
+// "across" it, a row of neighbouring i for each k.
+struct ProdArgs {
+  const __bf16 *a, *b;
+  uint64_t as, bs;                  // elements from row to row
+  uint32_t I, J, K;
+  const float* bias;                // [J]
+  int act, out_dtype;
+  const void* residual;             // [I, J] of out_dtype
+  uint64_t residual_stride;
+  void *out, *pre;                  // [I, J]
+  uint32_t i0, j0;                  // kernel of any sizes: first row and column of this launch
+};
+
+// ------------------------------------------------------------ activations ---
+// An infinite z gives the limit, NaN stays NaN.
+//
+// gelu's normal distribution function: with t = 1 / (1 + p |z| / sqrt 2),
+//   Phi(-|z|) = (a1 t + .. + a5 t^5) e^(-z^2 / 2) / 2,
+// formula 7.1.26 of Abramowitz and Stegun, within 7.5e-8 of it.  The library's
+// erf has two branches and many more instructions a value.
+struct Normal {
+  float cdf, density;               // density: e^(-z^2 / 2)
+};
+__device__ __forceinline__ Normal normal_of(float z) {
+  const float t = __builtin_amdgcn_rcpf(fmaf(0.3275911f * 0.70710678118654752f, fabsf(z), 1.0f));
+  const float e = __builtin_amdgcn_exp2f(z * z * -0.72134752044448170f);
+  float q = fmaf(t, 0.5f * 1.061405429f, 0.5f * -1.453152027f);
+  q = fmaf(t, q, 0.5f * 1.421413741f);
+  q = fmaf(t, q, 0.5f * -0.284496736f);
+  q = fmaf(t, q, 0.5f * 0.254829592f);
+  q *= t * e;
+  return {z < 0.0f ? q : 1.0f - q, e};
+}
+__device__ __forceinline__ float sigmoid_of(float z) {
+  return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(z * -1.4426950408889634f));
+}
+template <int ACT> __device__ __forceinline__ float act_of(float z) {
+  if constexpr (ACT == PROFK_ACT_RELU) return z < 0.0f ? 0.0f : z;
+  if constexpr (ACT == PROFK_ACT_GELU) return (z < -40.0f ? -40.0f : z) * normal_of(z).cdf;
+  if constexpr (ACT == PROFK_ACT_SILU) return (z < -200.0f ? -200.0f : z) * sigmoid_of(z);   // (2^288 is infinite)
+  return z;
+}
+template <int ACT> __device__ __forceinline__ float slope_of(float z) {
+  if constexpr (ACT == PROFK_ACT_RELU) return z > 0.0f ? 1.0f : 0.0f;
+  if constexpr (ACT == PROFK_ACT_GELU) {
+    const float c = z < -40.0f ? -40.0f : z > 40.0f ? 40.0f : z;
+    const Normal n = normal_of(c);
+    return fmaf(c * n.density, 0.39894228040143268f, n.cdf);
+  }
+  if constexpr (ACT == PROFK_ACT_SILU) {
+    const float c = z < -200.0f ? -200.0f : z > 200.0f ? 200.0f : z;
+    const float p = sigmoid_of(c);
+    return p * fmaf(c, 1.0f - p, 1.0f);
+  }
+  return 1.0f;
+}
+
+// f(std::integral_constant<int, ACT>) for an activation known at run time.
+template <class F> void with_act(int act, F f) {
+  if (act == PROFK_ACT_RELU) f(std::integral_constant<int, PROFK_ACT_RELU>{});
+  else if (act == PROFK_ACT_GELU) f(std::integral_constant<int, PROFK_ACT_GELU>{});
+  else if (act == PROFK_ACT_SILU) f(std::integral_constant<int, PROFK_ACT_SILU>{});
+  else f(std::integral_constant<int, PROFK_ACT_NONE>{});
+}
+
+// The tiled product; false: these operands are not aligned as it needs them.
+bool launch_product_along(const ProdArgs& g, uint32_t cus, hipStream_t s);              // A and B along k
+bool launch_product_grad(const ProdArgs& g, bool a_across, uint32_t cus, hipStream_t s); // B across k, A as said
+
+// Operands that the tiled product takes: rows of whole 16-byte granules.  `len`
+// is the length of a row.
+inline bool granules(const void* p, uint64_t stride, uint32_t len) {
+  return reinterpret_cast<uintptr_t>(p) % 16 == 0 && stride % 8 == 0 && len % 8 == 0 && stride <= (1u << 21);
+}
+
+}  // namespace profk

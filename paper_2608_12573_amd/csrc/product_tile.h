@@ -1,0 +1,404 @@
+// The tiled product on the matrix cores (kernels_product.hip,
+// kernels_product_grad.hip).
+//
+// A workgroup of WM x WN waves computes tiles of BM x BN outputs, a wave MI x NJ
+// accumulators of 32 x 32 with the 32x32x16 instruction.  A stage is 64 of k of
+// both operands, loaded straight to LDS in granules of 16 bytes; there are two,
+// and one is filled, on into the workgroup's next tile, while the other is
+// multiplied.  Fragments are read a quarter of a stage (16 of k, one instruction
+// for each accumulator) ahead, under the matrix instructions of the one before.
+//
+// An operand along k is 128 bytes a row in a stage, whole lines; granule g of row
+// r is at position g ^ (r / 2 % 8) of its eight, so that a fragment's read of
+// sixteen rows covers all 64 banks once.  One across k is BM (or BN) neighbours
+// for each of the 64 k; a fragment is two transposing reads, in which sixteen
+// lanes take 4 k of 16 neighbours.  Granule g of row k is at position g ^ (4 (k %
+// 4)): the four rows of a read then cover all banks once.
+//
+// Rows past I or J are read as the last and not stored; granules past K are read
+// from zeros, of both operands (a product of what lies there may be NaN).
+//
+// Output column n of a wave's slab is in fragment n % NJ, lane n / NJ, where B is
+// along k (its rows are in LDS in that order), so that a lane's NJ results of a
+// row are neighbours; where it is across, in fragment n / 32, lane n % 32.
+#pragma once
+
+#include <type_traits>
+
+#include "launch.h"
+#include "product.h"
+
+namespace profk {
+
+namespace {
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x4u __attribute__((ext_vector_type(4), aligned(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x2u __attribute__((ext_vector_type(2), aligned(2)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+
+constexpr uint32_t kProdXcds = 8;
+constexpr uint32_t kStageK = 64;
+
+__device__ const uint4 g_zero_granule = {0, 0, 0, 0};
+
+// s_waitcnt vmcnt(N) lgkmcnt(0) (gfx9 encoding: vmcnt in bits 3:0 and 15:14,
+// expcnt in 6:4, lgkmcnt in 11:8): all but this wave's N newest loads are done,
+// and so are its LDS reads.
+template <int N> __device__ __forceinline__ void prod_wait() {
+  static_assert(N >= 0 && N < 64, "vmcnt");
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt((N & 0xF) | ((N >> 4) << 14) | (0x7 << 4));
+  asm volatile("" ::: "memory");
+}
+// A workgroup barrier that waits for nothing else, across which the compiler
+// moves no memory access.
+__device__ __forceinline__ void prod_barrier() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+
+template <int WM, int WN, int MI, int NJ> struct ProdTile {
+  static constexpr int NW = WM * WN, BS = NW * kWave, BM = WM * MI * 32, BN = WN * NJ * 32;
+  static constexpr int QA = BM * 8 / BS, QB = BN * 8 / BS;   // loads of a lane
+  static constexpr int kB = BM * 8, kGran = (BM + BN) * 8;   // first granule of b; granules of a stage
+  static_assert(BM * 8 % BS == 0 && BN * 8 % BS == 0 && NJ == 4, "whole loads, four neighbouring results a lane");
+};
+
+// One operand's part of a stage: what a lane loads, and where it reads.  BW
+// neighbours (BM or BN), Q loads a lane, F fragments a wave, PERM: its rows are in
+// LDS in the order of the outputs.
+template <bool ACROSS, int BW, int Q, int F, bool PERM, bool WHOLE> struct ProdSide {
+  static_assert(!(ACROSS && PERM), "granules of neighbours stay together");
+  const uint8_t* base;
+  uint32_t off[Q], w, lane;
+  uint32_t K, adv;                  // k of a stage's row, and bytes from stage to stage
+  uint64_t row_bytes;
+  uint32_t rd0;
+  __device__ __forceinline__ static uint32_t order(uint32_t r) {
+    return PERM ? r / (F * 32) * (F * 32) + r % 32 * F + r % (F * 32) / 32 : r;
+  }
+  // wave, its first fragment's rows and its lane
+  __device__ __forceinline__ void init(uint32_t wave, uint32_t l, uint32_t first, uint64_t stride, uint32_t k) {
+    w = wave;
+    lane = l;
+    K = k;
+    row_bytes = stride * 2;
+    adv = ACROSS ? static_cast<uint32_t>(row_bytes) * kStageK : kStageK * 2;
+    if constexpr (ACROSS) {
+      const uint32_t t = lane & 15, b = lane >> 4 & 1, h = lane >> 5;
+      rd0 = (8 * h + t / 4) * (BW * 2) + ((first / 32 ^ t / 4) * 4 + b * 2 + t % 4 / 2) * 16 + t % 2 * 8;
+    } else {
+      const uint32_t c = lane & 31, h = lane >> 5;
+      rd0 = (first + c) * 128 + (h ^ (c >> 1 & 7)) * 16;
+    }
+  }
+  // granule of load q: its k (across) or its first k (along)
+  __device__ __forceinline__ uint32_t k_of(int q) const {
+    const uint32_t p = (w * Q + q) * kWave + lane;
+    if constexpr (ACROSS) return p / (BW / 8);
+    else return ((p & 7) ^ (p >> 4 & 7)) * 8;
+  }
+  __device__ __forceinline__ void start(const __bf16* p, uint32_t r0, uint32_t R) {
+    if constexpr (ACROSS) {
+      base = reinterpret_cast<const uint8_t*>(p + r0);
+#pragma unroll
+      for (int q = 0; q < Q; ++q) {
+        const uint32_t at = (w * Q + q) * kWave + lane, k = at / (BW / 8), g = at % (BW / 8) ^ (k & 3) * 4;
+        off[q] = k * static_cast<uint32_t>(row_bytes) + min(g, (R - r0) / 8 - 1) * 16;
+      }
+    } else {
+      base = reinterpret_cast<const uint8_t*>(p) + r0 * row_bytes;
+#pragma unroll
+      for (int q = 0; q < Q; ++q) {
+        const uint32_t r = order((w * Q + q) * 8 + lane / 8);
+        off[q] = min(r, R - 1 - r0) * static_cast<uint32_t>(row_bytes) + k_of(q) * 2;
+      }
+    }
+  }
+  // stage `next` of the tile to LDS
+  __device__ __forceinline__ void issue(uint4* st, uint32_t next) const {
+#pragma unroll
+    for (int q = 0; q < Q; ++q) {
+      const uint8_t* p = base + off[q];
+      if constexpr (!WHOLE) p = next * kStageK + k_of(q) < K ? p : reinterpret_cast<const uint8_t*>(&g_zero_granule);
+      __builtin_amdgcn_global_load_lds(reinterpret_cast<const uint32_t*>(p), st + (w * Q + q) * kWave, 16, 0, 0);
+    }
+  }
+  // fragments of quarter q of a stage
+  __device__ __forceinline__ void read(const uint4* st, uint32_t q, u32x4 (&f)[F]) {
+    // (taken anew, or the compiler keeps an address for each read)
+    asm volatile("" : "+v"(rd0));
+    if constexpr (ACROSS) {
+      typedef __attribute__((address_space(3))) s16x4* lds4;
+      typedef const __attribute__((address_space(3))) uint8_t* lds8;
+      const lds8 p = (lds8)reinterpret_cast<const uint8_t*>(st);
+#pragma unroll
+      for (int u = 0; u < F; ++u) {
+        const uint32_t at = (rd0 ^ (u * 64)) + q * (16 * BW * 2);
+        const u32x2 lo = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(p + at)));
+        const u32x2 hi = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(p + at + 4 * BW * 2)));
+        f[u] = u32x4{lo[0], lo[1], hi[0], hi[1]};
+      }
+    } else {
+      const uint8_t* const p = reinterpret_cast<const uint8_t*>(st);
+#pragma unroll
+      for (int u = 0; u < F; ++u) f[u] = *reinterpret_cast<const u32x4*>(p + (rd0 ^ (q * 32)) + u * 4096);
+    }
+  }
+};
+
+// WHOLE: K is a multiple of two stages.
+template <bool TA, bool TB, int ACT, int DT, int WM, int WN, int MI, int NJ, bool WHOLE>
+__device__ __forceinline__ void prod_body(const ProdArgs& g, uint32_t tiles_i, uint32_t tiles) {
+  using T = ProdTile<WM, WN, MI, NJ>;
+  // distinct arrays, so that the compiler can tell the stage being read from
+  // the one being filled
+  __shared__ __align__(16) uint4 s0[T::kGran], s1[T::kGran];
+  // workgroup b runs on XCD b % 8: each XCD takes a run of tiles, the row
+  // tiles of a column tile one after the other, so that its L2 holds what
+  // they share
+  const uint32_t xcd = blockIdx.x % kProdXcds, per_xcd = gridDim.x / kProdXcds;   // (the grid is a multiple of 8)
+  const uint32_t end = static_cast<uint32_t>(static_cast<uint64_t>(tiles) * (xcd + 1) / kProdXcds);
+  const uint32_t tile0 = static_cast<uint32_t>(static_cast<uint64_t>(tiles) * xcd / kProdXcds) + blockIdx.x / kProdXcds;
+  if (tile0 >= end) return;
+  // a tile takes an even number of stages, so that each starts at the same one
+  const uint32_t stages = (g.K + 2 * kStageK - 1) / (2 * kStageK) * 2;
+  const uint32_t tid = threadIdx.x, lane = tid & (kWave - 1);
+  const uint32_t w = __builtin_amdgcn_readfirstlane(tid / kWave);
+  const uint32_t c = lane & 31, h = lane >> 5, wm = w / WN, wn = w % WN;
+
+  ProdSide<TA, T::BM, T::QA, MI, false, WHOLE> sa;
+  ProdSide<TB, T::BN, T::QB, NJ, !TB, WHOLE> sb;
+  sa.init(w, lane, wm * MI * 32, g.as, g.K);
+  sb.init(w, lane, wn * NJ * 32, g.bs, g.K);
+  auto start = [&](uint32_t tile) {
+    sa.start(g.a, tile % tiles_i * T::BM, g.I);
+    sb.start(g.b, tile / tiles_i * T::BN, g.J);
+  };
+  uint32_t next_k = 0, next_tile = tile0;
+  // (past the last tile: its last stage again)
+  auto issue_a = [&](uint4* st) { sa.issue(st, next_k); };
+  auto issue_b = [&](uint4* st) {
+    sb.issue(st + T::kB, next_k);
+    ++next_k;
+    if (WHOLE ? next_k < stages : next_k * kStageK < g.K) {
+      sa.base += sa.adv;
+      sb.base += sb.adv;
+    }
+  };
+  // after a tile's last stage
+  auto turn = [&]() {
+    if (next_k == stages) {
+      if (next_tile + per_xcd < end) {
+        next_k = 0;
+        next_tile += per_xcd;
+        start(next_tile);
+      } else {
+        next_k = stages - 1;
+      }
+    }
+  };
+  struct Frag {
+    u32x4 a[MI], b[NJ];
+  };
+  auto rd = [&](const uint4* st, uint32_t q, Frag& f) {
+    sa.read(st, q, f.a);
+    sb.read(st + T::kB, q, f.b);
+  };
+  f32x16 acc[MI][NJ];
+  auto mma = [&](const Frag& f) {
+#pragma unroll
+    for (int i = 0; i < MI; ++i)
+#pragma unroll
+      for (int j = 0; j < NJ; ++j)
+        acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, f.a[i]),
+                                                            __builtin_bit_cast(bf16x8, f.b[j]), acc[i][j], 0, 0, 0);
+  };
+  // The accumulators exist here: a quarter's instructions, which touch no
+  // memory, would else be moved past the barriers to where they are stored.
+  auto pin = [&]() {
+#pragma unroll
+    for (int i = 0; i < MI; ++i)
+#pragma unroll
+      for (int j = 0; j < NJ; ++j) asm volatile("" : "+v"(acc[i][j]));
+  };
+  // LDS reads and loads between the matrix instructions of a quarter: the first
+  // one waits for the reads before, and loads issued one after the other keep
+  // the wave from its matrix instructions while they are taken
+  constexpr int kReads = MI * (TA ? 2 : 1) + NJ * (TB ? 2 : 1);
+  auto weave = [&]() {
+    constexpr int M = MI * NJ, per = (kReads + M - 2) / (M - 1);
+    pin();
+#pragma unroll
+    for (int i = 0; i < M; ++i) {
+      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(0x100, per, 0);
+      __builtin_amdgcn_sched_group_barrier(0x010, 1, 0);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  auto clear = [&]() {
+#pragma unroll
+    for (int i = 0; i < MI; ++i)
+#pragma unroll
+      for (int j = 0; j < NJ; ++j) acc[i][j] = f32x16{};
+  };
+  using O = std::conditional_t<DT == PROFK_F32, float, __bf16>;
+  auto store = [&](uint32_t tile) {
+    const uint32_t mw = tile % tiles_i * T::BM + wm * MI * 32, nw = tile / tiles_i * T::BN + wn * NJ * 32;
+    const uint32_t m = mw + 4 * h, n = nw + (TB ? c : NJ * c);
+    O* const out = static_cast<O*>(g.out);
+    if constexpr (TB) {
+      // (no epilogue: a gradient) neighbouring lanes hold neighbouring columns
+#pragma unroll
+      for (int i = 0; i < MI; ++i) {
+        uint32_t first = m + i * 32;
+        asm volatile("" : "+v"(first));
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int v = 0; v < 16; ++v) {
+          const uint32_t r = first + 8 * (v / 4) + v % 4;
+          O* const p = out + static_cast<size_t>(r) * g.J + n;
+          if (r < g.I) {
+#pragma unroll
+            for (int j = 0; j < NJ; ++j)
+              if (n + j * 32 < g.J) p[j * 32] = static_cast<O>(acc[i][j][v]);
+          }
+        }
+      }
+    } else {
+      f32x4 bias = {};
+      if (g.bias) {
+#pragma unroll
+        for (uint32_t j = 0; j < 4; ++j) bias[j] = n + j < g.J ? g.bias[n + j] : 0.0f;
+      }
+      const bool whole = n + NJ <= g.J;
+      auto put4 = [&](O* p, const f32x4& y) {
+        if (whole) {
+          if constexpr (DT == PROFK_F32) *reinterpret_cast<f32x4u*>(p) = y;
+          else *reinterpret_cast<u32x2u*>(p) = u32x2u{pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3])};
+        } else {
+          p[0] = static_cast<O>(y[0]);
+          if (n + 1 < g.J) p[1] = static_cast<O>(y[1]);
+          if (n + 2 < g.J) p[2] = static_cast<O>(y[2]);
+        }
+      };
+      if (n < g.J) {
+#pragma unroll
+        for (int i = 0; i < MI; ++i) {
+          uint32_t first = m + i * 32;
+          // (no row's address or mask is kept through the steps)
+          asm volatile("" : "+v"(first));
+          __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+          for (int v = 0; v < 16; ++v) {
+            const uint32_t r = first + 8 * (v / 4) + v % 4;
+            if (r < g.I) {
+              const size_t at = static_cast<size_t>(r) * g.J + n;
+              f32x4 z = f32x4{acc[i][0][v], acc[i][1][v], acc[i][2][v], acc[i][3][v]} + bias;
+              if (g.pre) put4(static_cast<O*>(g.pre) + at, z);
+#pragma unroll
+              for (int j = 0; j < 4; ++j) z[j] = act_of<ACT>(z[j]);
+              if (g.residual) {
+                const O* const q = static_cast<const O*>(g.residual) + r * g.residual_stride + n;
+                if (whole) {
+                  if constexpr (DT == PROFK_F32) {
+                    z += *reinterpret_cast<const f32x4u*>(q);
+                  } else {
+                    const u32x2u u = *reinterpret_cast<const u32x2u*>(q);
+                    z += f32x4{__uint_as_float(u[0] << 16), __uint_as_float(u[0] & 0xFFFF0000u),
+                               __uint_as_float(u[1] << 16), __uint_as_float(u[1] & 0xFFFF0000u)};
+                  }
+                } else {
+                  z[0] += static_cast<float>(q[0]);
+                  if (n + 1 < g.J) z[1] += static_cast<float>(q[1]);
+                  if (n + 2 < g.J) z[2] += static_cast<float>(q[2]);
+                }
+              }
+              put4(out + at, z);
+            }
+          }
+        }
+      }
+    }
+  };
+  start(tile0);
+  issue_a(s0);
+  issue_b(s0);
+  issue_a(s1);
+  Frag f0, f1;
+  prod_wait<T::QA>();
+  prod_barrier();
+  rd(s0, 0, f0);
+  // One stage; its first quarter's fragments are in f0, and the loads of a for
+  // the next have been issued.
+  auto stage = [&](uint4* cur, uint4* nxt, auto last) {
+    __builtin_amdgcn_sched_barrier(0);
+    issue_b(nxt);
+    rd(cur, 1, f1);
+    mma(f0);
+    weave();
+    rd(cur, 2, f0);
+    mma(f1);
+    weave();
+    if (decltype(last)::value) turn();
+    rd(cur, 3, f1);
+    mma(f0);
+    weave();
+    // this wave has read its stage and its loads of the next have arrived; by
+    // the barrier, so have the others
+    prod_wait<0>();
+    prod_barrier();
+    issue_a(cur);
+    rd(nxt, 0, f0);
+    mma(f1);
+    weave();
+  };
+  for (uint32_t tile = tile0; tile < end; tile += per_xcd) {
+    clear();
+    for (uint32_t k = 0; k < stages; k += 2) {
+      stage(s0, s1, std::true_type{});     // (loads the tile's next odd stage)
+      stage(s1, s0, std::false_type{});
+    }
+    store(tile);
+  }
+  prod_wait<0>();   // (no load may reach LDS after the workgroup's end)
+}
+
+template <bool TA, bool TB, int ACT, int DT, int WM, int WN, int MI, int NJ, int WAVES, bool WHOLE>
+__global__ __launch_bounds__(WM * WN * 64, WAVES) void k_prod(ProdArgs g, uint32_t tiles_i, uint32_t tiles) {
+  prod_body<TA, TB, ACT, DT, WM, WN, MI, NJ, WHOLE>(g, tiles_i, tiles);
+}
+
+// PER: workgroups a CU holds.
+template <bool TA, bool TB, int ACT, int DT, int WM, int WN, int MI, int NJ, int PER>
+void launch_tiles(const ProdArgs& g, uint32_t cus, hipStream_t s) {
+  using T = ProdTile<WM, WN, MI, NJ>;
+  const uint32_t ti = (g.I + T::BM - 1) / T::BM, tj = (g.J + T::BN - 1) / T::BN, tiles = ti * tj;
+  uint32_t grid = (tiles + kProdXcds - 1) / kProdXcds * kProdXcds;
+  if (grid > PER * cus) grid = PER * cus / kProdXcds * kProdXcds;
+  constexpr int kWaves = PER * WM * WN / 4;
+  if (g.K % (2 * kStageK) == 0) k_prod<TA, TB, ACT, DT, WM, WN, MI, NJ, kWaves, true><<<grid, T::BS, 0, s>>>(g, ti, tiles);
+  else k_prod<TA, TB, ACT, DT, WM, WN, MI, NJ, kWaves, false><<<grid, T::BS, 0, s>>>(g, ti, tiles);
+}
+
+// Tiles of 256 x 256 where every CU has one, else two workgroups a CU of 128 x 128.
+template <bool TA, bool TB, int ACT, int DT> void launch_shape(const ProdArgs& g, uint32_t cus, hipStream_t s) {
+  const uint64_t large = static_cast<uint64_t>((g.I + 255) / 256) * ((g.J + 255) / 256);
+  if (g.I > 128 && large >= cus) launch_tiles<TA, TB, ACT, DT, 4, 2, 2, 4, 1>(g, cus, s);
+  else launch_tiles<TA, TB, ACT, DT, 4, 1, 1, 4, 2>(g, cus, s);
+}
+
+// Tiles are counted in 32 bits.
+inline bool tiles_fit(const ProdArgs& g) {
+  return static_cast<uint64_t>((g.I + 127) / 128) * ((g.J + 127) / 128) < (uint64_t{1} << 31);
+}
+
+}  // namespace
+
+}  // namespace profk
