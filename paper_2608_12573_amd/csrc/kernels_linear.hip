@@ -16,6 +16,7 @@
 #include "launch.h"
 #include "linear.h"
 #include "product.h"
+#include "product_put.h"
 
 namespace profk {
 
@@ -25,31 +26,6 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
 // ------------------------------------------------- product of any operands ---
-__device__ __forceinline__ float act_any(float z, int act) {
-  if (act == PROFK_ACT_RELU) return act_of<PROFK_ACT_RELU>(z);
-  if (act == PROFK_ACT_GELU) return act_of<PROFK_ACT_GELU>(z);
-  if (act == PROFK_ACT_SILU) return act_of<PROFK_ACT_SILU>(z);
-  return z;
-}
-
-__device__ __forceinline__ void put(const ProdArgs& g, uint32_t i, uint32_t j, float z) {
-  const size_t at = static_cast<size_t>(i) * g.J + j;
-  if (g.bias) z += g.bias[j];
-  float y = act_any(z, g.act);
-  if (g.residual) {
-    const size_t r = i * g.residual_stride + j;
-    y += g.out_dtype == PROFK_F32 ? static_cast<const float*>(g.residual)[r]
-                                  : static_cast<float>(static_cast<const __bf16*>(g.residual)[r]);
-  }
-  if (g.out_dtype == PROFK_F32) {
-    static_cast<float*>(g.out)[at] = y;
-    if (g.pre) static_cast<float*>(g.pre)[at] = z;
-  } else {
-    static_cast<__bf16*>(g.out)[at] = static_cast<__bf16>(y);
-    if (g.pre) static_cast<__bf16*>(g.pre)[at] = static_cast<__bf16>(z);
-  }
-}
-
 // Any sizes, strides and alignments: tiles of 128 x 128 on four waves of 64 x 64,
 // 32 of k at a time through registers to LDS, its rows 80 bytes apart.
 constexpr uint32_t kAnyB = 128, kAnyK = 32, kAnyRow = 40;
@@ -230,7 +206,9 @@ hipError_t launch_linear(const LinCall& c, hipStream_t s) {
                    static_cast<uint32_t>(c.M), static_cast<uint32_t>(c.N), static_cast<uint32_t>(c.K), c.bias, c.act,
                    c.out_dtype, c.residual, c.residual_stride, c.out, c.pre, 0, 0};
   (void)hipGetLastError();
-  if (launch_product_along(g, static_cast<uint32_t>(device_cu_count()), s)) return hipGetLastError();
+  const uint32_t cus = static_cast<uint32_t>(device_cu_count());
+  if (launch_product_few(g, cus, s)) return hipGetLastError();
+  if (launch_product_along(g, cus, s)) return hipGetLastError();
   return launch_any<false, false>(g, s);
 }
 

@@ -73,7 +73,8 @@ template <class F> void with_act(int act, F f) {
   else f(std::integral_constant<int, PROFK_ACT_NONE>{});
 }
 
-// The tiled product; false: these operands are not aligned as it needs them.
+// The product of few rows, and the tiled one; false: these operands are not aligned as they need them.
+bool launch_product_few(const ProdArgs& g, uint32_t cus, hipStream_t s);                // A and B along k, I <= 32
 bool launch_product_along(const ProdArgs& g, uint32_t cus, hipStream_t s);              // A and B along k
 bool launch_product_grad(const ProdArgs& g, bool a_across, uint32_t cus, hipStream_t s); // B across k, A as said
 

@@ -79,6 +79,18 @@ def test_forward(M, K, N, act, out, bias, residual):
     _linear(M, K, N, act, out, bias, residual, M + 3 * K + 7 * N)
 
 
+# few rows: more groups of columns than are at work at once, with K shared by the
+# waves of a workgroup or not; tiles of 256 x 256, and more than one a workgroup
+@pytest.mark.parametrize("M,K,N", [(1, 72, 70000), (3, 584, 50008), (8, 512, 33000), (9, 64, 33001), (16, 1024, 9000),
+                                   (17, 520, 33000), (32, 712, 5003), (1, 8192, 33), (5, 448, 140000), (31, 8, 100000),
+                                   (4096, 64, 4096), (4000, 72, 4200), (5000, 136, 5003), (300, 8, 65541),
+                                   (130, 200, 40000)])
+@pytest.mark.parametrize("act,out", [(None, "f32"), ("gelu", "bf16")])
+def test_many_groups_and_tiles(M, K, N, act, out):
+    note(f"linear {M}x{K}x{N} {act} {out}")
+    _linear(M, K, N, act, out, True, act is not None, M + K + N, pre=M < 1000)
+
+
 @pytest.mark.parametrize("M,K,N", [(1, 4096, 640), (2, 72, 40), (9, 264, 96), (40, 1000, 200), (200, 264, 300), (300, 64, 520)])
 @pytest.mark.parametrize("pad,off", [(1, 0), (0, 1), (3, 2), (8, 0), (8, 8), (4, 4)])
 def test_strides_and_alignment(M, K, N, pad, off):
@@ -108,6 +120,13 @@ def _grad(M, K, N, act, dt, seed, pad=0, off=0):
 def test_grad(M, K, N, act, dt):
     note(f"linear_grad {M}x{K}x{N} {act} {dt}")
     _grad(M, K, N, act, dt, M + K + N)
+
+
+@pytest.mark.parametrize("M,K,N", [(4096, 4096, 64), (72, 4200, 4104), (4200, 72, 4104), (4100, 4360, 40)])
+@pytest.mark.parametrize("act", [None, "gelu"])
+def test_grad_of_large_tiles(M, K, N, act):
+    note(f"linear_grad {M}x{K}x{N} {act}")
+    _grad(M, K, N, act, "bf16", M + K + N)
 
 
 @pytest.mark.parametrize("M,K,N", [(2, 72, 40), (64, 264, 96), (200, 264, 320), (300, 64, 520)])
