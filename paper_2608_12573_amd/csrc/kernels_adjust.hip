@@ -22,6 +22,7 @@ namespace profk {
 namespace {
 
 constexpr uint32_t kAdjPrompt = 0x80000000u;   // of a token's word: it is in the prompt; the rest counts it after
+constexpr uint32_t kAdjChunks = 2;             // of 8 elements, of a thread
 constexpr uint32_t kAdjMaxPiece = 8192;        // elements (LDS: a word each, two with biases)
 
 __device__ __forceinline__ int64_t clamp64(int64_t x, int64_t lo, int64_t hi) { return x < lo ? lo : x > hi ? hi : x; }
@@ -42,6 +43,13 @@ template <int DT, bool GRAD> __global__ __launch_bounds__(512) void k_adjust(Adj
     b0 = clamp64(a.bias_offsets[row], 0, a.n_bias);
     b1 = clamp64(a.bias_offsets[row + 1], b0, a.n_bias);
   }
+  const char* const x = static_cast<const char*>(a.x) + (row * a.stride + v0) * ES;
+  const char* const src = GRAD ? static_cast<const char*>(a.dy) + (row * a.dy_stride + v0) * ES : x;
+  char* const out = static_cast<char*>(a.out) + (row * a.out_stride + v0) * ES;
+  // the piece, loaded under the search of the lists
+  Raw8<DT> raw[kAdjChunks];
+#pragma unroll
+  for (uint32_t q = 0; q < kAdjChunks; ++q) raw[q] = load_raw8<DT>(src, (q * BS + tid) * 8, n);
   const bool hist = h1 > h0, bias = b1 > b0;
   uint32_t* const s_bias = s_word + (a.tokens ? a.piece : 0);
   if (hist || bias) {
@@ -51,11 +59,18 @@ template <int DT, bool GRAD> __global__ __launch_bounds__(512) void k_adjust(Adj
     }
     __syncthreads();
     const int64_t made = h0 + (a.n_prompt && hist ? clamp64(a.n_prompt[row], 0, h1 - h0) : 0);
-    for (int64_t i = h0 + tid; i < h1; i += BS) {
-      const uint64_t v = static_cast<uint64_t>(a.tokens[i]) - v0;
-      if (v < n) {
-        if (i < made) atomicOr(s_word + v, kAdjPrompt);
-        else atomicAdd(s_word + v, 1u);
+    // (four tokens at a time: a load waits for none before it)
+    for (int64_t i = h0 + tid; i < h1; i += 4 * BS) {
+      int64_t tok[4];
+#pragma unroll
+      for (uint32_t q = 0; q < 4; ++q) tok[q] = i + q * BS < h1 ? a.tokens[i + q * BS] : -1;
+#pragma unroll
+      for (uint32_t q = 0; q < 4; ++q) {
+        const uint64_t v = static_cast<uint64_t>(tok[q]) - v0;
+        if (tok[q] >= 0 && v < n) {
+          if (i + q * BS < made) atomicOr(s_word + v, kAdjPrompt);
+          else atomicAdd(s_word + v, 1u);
+        }
       }
     }
     for (int64_t i = b0 + tid; i < b1; i += BS) {
@@ -75,12 +90,12 @@ template <int DT, bool GRAD> __global__ __launch_bounds__(512) void k_adjust(Adj
   const float pres = !GRAD && a.presence ? a.presence[row] : 0.0f;
   const float freq = !GRAD && a.frequency ? a.frequency[row] : 0.0f;
   const float nan = __builtin_nanf("");
-  const char* const x = static_cast<const char*>(a.x) + (row * a.stride + v0) * ES;
-  const char* const src = GRAD ? static_cast<const char*>(a.dy) + (row * a.dy_stride + v0) * ES : x;
-  char* const out = static_cast<char*>(a.out) + (row * a.out_stride + v0) * ES;
-  for (uint32_t i = tid * 8; i < n; i += BS * 8) {
+#pragma unroll
+  for (uint32_t q = 0; q < kAdjChunks; ++q) {
+    const uint32_t i = (q * BS + tid) * 8;
+    if (i >= n) return;
     float y[8];
-    load8<DT>(src, i, n, y);
+    to_f32<DT>(raw[q], y);
     // (a piece starts at a multiple of 32 tokens)
     const uint32_t ok = words ? words[(v0 + i) / 32] >> (i % 32) : 0xFFu;
     // (the words past the row's end stay 0)
@@ -124,7 +139,7 @@ hipError_t launch_adjust(AdjustArgs a, int dtype, int64_t T, hipStream_t s) {
   a.piece = piece;
   a.pieces = (a.V + piece - 1) / piece;
   uint32_t bs = 512;
-  while (bs > 64 && bs * 8 >= 2 * piece) bs /= 2;
+  while (bs > 64 && bs * 8 * kAdjChunks >= 2 * piece) bs /= 2;
   const uint32_t lds = ((a.tokens ? piece : 0) + (!a.dy && a.bias_ids ? piece : 0)) * 4;
   const int64_t step = ((int64_t{1} << 31) - 1) / bs / a.pieces < 1 ? 1 : ((int64_t{1} << 31) - 1) / bs / a.pieces;
   (void)hipGetLastError();

@@ -13,6 +13,7 @@
 // neighbouring in memory ("along") or a whole row apart ("across").
 #include <type_traits>
 
+#include "join.h"
 #include "launch.h"
 #include "linear.h"
 #include "product.h"
@@ -157,20 +158,10 @@ template <int DT, int ACT> __global__ __launch_bounds__(256) void k_dz(DzArgs a)
   if (a.part) store8<PROFK_F32>(a.part + static_cast<size_t>(p) * a.N, j, a.N, sum);
 }
 
-constexpr uint32_t kJoinCols = 64, kJoinRows = 16;
-
-__global__ __launch_bounds__(kJoinCols * kJoinRows) void k_db_join(const float* part, uint32_t parts, uint32_t N, float* db) {
-  __shared__ float s[kJoinRows][kJoinCols];
-  const uint32_t c = threadIdx.x % kJoinCols, k = threadIdx.x / kJoinCols, j = blockIdx.x * kJoinCols + c;
-  float sum = 0.0f;
-  if (j < N)
-    for (uint32_t p = k; p < parts; p += kJoinRows) sum += part[static_cast<size_t>(p) * N + j];
-  s[k][c] = sum;
-  __syncthreads();
-  if (k != 0 || j >= N) return;
-#pragma unroll
-  for (uint32_t q = 1; q < kJoinRows; ++q) sum += s[q][c];
-  db[j] = sum;
+__global__ __launch_bounds__(kJoinBS) void k_db_join(const float* part, uint32_t parts, uint32_t N, float* db) {
+  const float sum = join_parts(part, parts, N);
+  const uint32_t j = blockIdx.x * kJoinCols + threadIdx.x;
+  if (threadIdx.x < kJoinCols && j < N) db[j] = sum;
 }
 
 uint32_t dz_parts(int64_t M, int64_t N, int num_cus) {
@@ -236,7 +227,7 @@ hipError_t launch_linear_grad(const LinGradCall& c, hipStream_t s) {
     e = hipGetLastError();
   }
   if (e == hipSuccess && c.db && N) {
-    k_db_join<<<(N + kJoinCols - 1) / kJoinCols, kJoinCols * kJoinRows, 0, s>>>(part, L.parts, N, c.db);
+    k_db_join<<<(N + kJoinCols - 1) / kJoinCols, kJoinBS, 0, s>>>(part, L.parts, N, c.db);
     e = hipGetLastError();
   }
   if (e == hipSuccess && c.dx && M) {

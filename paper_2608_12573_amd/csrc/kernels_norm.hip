@@ -14,6 +14,7 @@
 //   dw = sum dy n,  db = sum dy.
 // All in fp32; every output is rounded once.
 #include "elem8.h"
+#include "join.h"
 #include "launch.h"
 #include "norm.h"
 
@@ -21,25 +22,25 @@ namespace profk {
 
 namespace {
 
-constexpr uint32_t kJoinCols = 64, kJoinRows = 16;   // join: columns and rows of partial sums of a workgroup
-
-// Sums over the threads of a row: a wave's, or all BS.  `slot` alternates
-// between successive sums, so that one barrier each is enough.
-template <int BS, bool WAVE, int N> __device__ __forceinline__ void row_sum(float (&v)[N], float (*slot)[N]) {
+// Sums over the GS threads of a row, a wave or more, in every one of them.  Rows
+// of more than a wave: the workgroup's rows go together, and `slot` [waves of the
+// workgroup] alternates between successive sums, so that one barrier each is enough.
+template <int GS, int N> __device__ __forceinline__ void row_sum(float (&v)[N], float (*slot)[N]) {
 #pragma unroll
   for (int k = 0; k < N; ++k) v[k] = wave_sum(v[k]);
-  if constexpr (!WAVE) {
-    constexpr int NW = BS / kWave;
+  if constexpr (GS > kWave) {
+    constexpr uint32_t NW = GS / kWave;
+    const uint32_t w = threadIdx.x / kWave, first = w / NW * NW;
     if ((threadIdx.x & (kWave - 1)) == 0) {
 #pragma unroll
-      for (int k = 0; k < N; ++k) slot[threadIdx.x / kWave][k] = v[k];
+      for (int k = 0; k < N; ++k) slot[w][k] = v[k];
     }
     __syncthreads();
 #pragma unroll
     for (int k = 0; k < N; ++k) {
-      float s = slot[0][k];
+      float s = slot[first][k];
 #pragma unroll
-      for (int w = 1; w < NW; ++w) s += slot[w][k];
+      for (uint32_t q = 1; q < NW; ++q) s += slot[first + q][k];
       v[k] = s;
     }
   }
@@ -69,15 +70,16 @@ template <int DT> __device__ __forceinline__ void* row_at(void* x, uint64_t stri
   return static_cast<char*>(x) + r * stride * (DT == PROFK_F32 ? 4 : 2);
 }
 
-// A row in the registers of one wave or of a workgroup, C chunks of 8 elements
-// a thread; workgroups go through the rows, the scale and shift kept in
+// A row in the registers of GS threads, C chunks of 8 elements each, R rows a
+// workgroup; workgroups go through the rows, the scale and shift kept in
 // registers and the next row loaded under this one.
-template <int XDT, int YDT, int BS, int C, bool WAVE> __global__ __launch_bounds__(BS) void k_norm(NormArgs a) {
-  constexpr uint32_t GS = WAVE ? kWave : BS, R = BS / GS;
+template <int XDT, int YDT, int GS, int R, int C> __global__ __launch_bounds__(GS * R) void k_norm(NormArgs a) {
+  constexpr uint32_t BS = GS * R;
+  static_assert(GS == kWave || R == 1, "a row that is left out meets no barrier");
   __shared__ float s_red[BS / kWave][1], s_sq[BS / kWave][2];
-  const uint32_t t = WAVE ? threadIdx.x & (kWave - 1) : threadIdx.x;
+  const uint32_t t = threadIdx.x % GS;
   const uint32_t step = gridDim.x * R;
-  uint32_t row = blockIdx.x * R + (WAVE ? threadIdx.x / kWave : 0);
+  uint32_t row = blockIdx.x * R + threadIdx.x / GS;
   if (row >= a.T) return;      // (a whole wave, or the workgroup)
   float w[C][8], b[C][8];
   Raw8<XDT> next[C];
@@ -101,7 +103,7 @@ template <int XDT, int YDT, int BS, int C, bool WAVE> __global__ __launch_bounds
 #pragma unroll
       for (int c = 0; c < C; ++c) next[c] = load_raw8<XDT>(row_at<XDT>(a.x, a.stride, row + step), (c * GS + t) * 8, a.D);
     }
-    row_sum<BS, WAVE>(s, s_red);
+    row_sum<GS>(s, s_red);
     const float m = s[0] * inv;
     float q[2] = {0.0f, 0.0f};
 #pragma unroll
@@ -114,7 +116,7 @@ template <int XDT, int YDT, int BS, int C, bool WAVE> __global__ __launch_bounds
         q[1] = fmaf(v[c][e], v[c][e], q[1]);
       }
     }
-    row_sum<BS, WAVE>(q, s_sq);
+    row_sum<GS>(q, s_sq);
     const float d = q[0] * inv, r = row_rstd(q[1] * inv, d, a.eps);
     void* const out = row_at<YDT>(a.out, a.out_stride, row);
 #pragma unroll
@@ -145,7 +147,7 @@ template <int XDT, int YDT> __global__ __launch_bounds__(1024) void k_norm_long(
 #pragma unroll
       for (int e = 0; e < 8; ++e) s[0] += v[e];
     }
-    row_sum<BS, false>(s, s_red);
+    row_sum<BS>(s, s_red);
     const float m = s[0] * inv;
     float q[2] = {0.0f, 0.0f};
     for (uint32_t i = threadIdx.x * 8; i < a.D; i += BS * 8) {
@@ -157,7 +159,7 @@ template <int XDT, int YDT> __global__ __launch_bounds__(1024) void k_norm_long(
         q[1] = fmaf(c, c, q[1]);
       }
     }
-    row_sum<BS, false>(q, s_sq);
+    row_sum<BS>(q, s_sq);
     const float d = q[0] * inv, r = row_rstd(q[1] * inv, d, a.eps);
     void* const out = row_at<YDT>(a.out, a.out_stride, row);
     for (uint32_t i = threadIdx.x * 8; i < a.D; i += BS * 8) {
@@ -176,33 +178,38 @@ template <int XDT, int YDT> __global__ __launch_bounds__(1024) void k_norm_long(
   }
 }
 
-// The gradients of rows in registers: one sum of two numbers a row, and each
-// workgroup's sums of dy n and dy over its rows kept in registers until its end.
-template <int XDT, int YDT, int BS, int C, bool WAVE> __global__ __launch_bounds__(BS) void k_norm_grad(NormGradArgs a) {
-  constexpr uint32_t GS = WAVE ? kWave : BS, R = BS / GS;
+// The gradients of rows in registers: one sum of two numbers a row, and the sums
+// of dy n and dy over a thread's rows kept in registers until its end, when the
+// workgroup's R rows of threads are added.
+template <int XDT, int YDT, int GS, int R, int C> __global__ __launch_bounds__(GS * R) void k_norm_grad(NormGradArgs a) {
+  constexpr uint32_t BS = GS * R;
   __shared__ float s_red[2][BS / kWave][2];
-  const uint32_t t = WAVE ? threadIdx.x & (kWave - 1) : threadIdx.x;
+  __shared__ float s_sum[R > 1 ? 2 * GS * C * 8 : 1];
+  const uint32_t t = threadIdx.x % GS, sub = threadIdx.x / GS;
   const uint32_t step = gridDim.x * R;
-  uint32_t row = blockIdx.x * R + (WAVE ? threadIdx.x / kWave : 0);
   float w[C][8], dw[C][8] = {}, db[C][8] = {};
   Raw8<XDT> nx[C];
   Raw8<YDT> ny[C];
-  float nm = 0.0f, nr = 0.0f;
+  float nm, nr;
+  // (a row that is not there has a gradient of 0)
   auto load = [&](uint32_t r) {
+    const uint32_t D = r < a.T ? a.D : 0;
 #pragma unroll
     for (int c = 0; c < C; ++c) {
-      nx[c] = load_raw8<XDT>(row_at<XDT>(a.x, a.stride, r), (c * GS + t) * 8, a.D);
-      ny[c] = load_raw8<YDT>(row_at<YDT>(a.dy, a.dy_stride, r), (c * GS + t) * 8, a.D);
+      nx[c] = load_raw8<XDT>(row_at<XDT>(a.x, a.stride, r), (c * GS + t) * 8, D);
+      ny[c] = load_raw8<YDT>(row_at<YDT>(a.dy, a.dy_stride, r), (c * GS + t) * 8, D);
     }
-    nm = a.mean[r];
-    nr = a.rstd[r];
+    nm = D ? a.mean[r] : 0.0f;
+    nr = D ? a.rstd[r] : 0.0f;
   };
-  if (row < a.T) load(row);
+  uint32_t row0 = blockIdx.x * R;
+  load(row0 + sub);
 #pragma unroll
   for (int c = 0; c < C; ++c) load_param8(a.w, a.p_dtype, (c * GS + t) * 8, a.D, 1.0f, w[c]);
   const float inv = 1.0f / static_cast<float>(a.D);
   uint32_t slot = 0;
-  for (; row < a.T; row += step, slot ^= 1) {
+  for (; row0 < a.T; row0 += step, slot ^= 1) {
+    const uint32_t row = row0 + sub;
     float n[C][8], g[C][8], s[2] = {0.0f, 0.0f};
     const float m = nm, r = nr;
 #pragma unroll
@@ -220,51 +227,52 @@ template <int XDT, int YDT, int BS, int C, bool WAVE> __global__ __launch_bounds
         s[1] = fmaf(g[c][e], n[c][e], s[1]);
       }
     }
-    if (a.T - row > step) load(row + step);
+    if (a.T - row0 > step) load(row + step);
     if (a.dx) {       // (the same for all: the barrier is met by the whole workgroup)
-      row_sum<BS, WAVE>(s, s_red[slot]);
+      row_sum<GS>(s, s_red[slot]);
       s[0] *= inv;
       s[1] *= inv;
-      void* const out = row_at<XDT>(a.dx, a.dx_stride, row);
+      if (R == 1 || row < a.T) {
+        void* const out = row_at<XDT>(a.dx, a.dx_stride, row);
 #pragma unroll
-      for (int c = 0; c < C; ++c) {
+        for (int c = 0; c < C; ++c) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) g[c][e] = r * (g[c][e] - s[0] - n[c][e] * s[1]);
-        store8<XDT>(out, (c * GS + t) * 8, a.D, g[c]);
+          for (int e = 0; e < 8; ++e) g[c][e] = r * (g[c][e] - s[0] - n[c][e] * s[1]);
+          store8<XDT>(out, (c * GS + t) * 8, a.D, g[c]);
+        }
       }
     }
   }
   if (!a.part) return;
   float* const part = a.part + static_cast<size_t>(blockIdx.x) * 2 * a.D;
-  if constexpr (WAVE) {
-    // the waves' sums, in wave order
-    __shared__ float s_sum[2][C * kWave * 8];
-    for (uint32_t k = 0; k < R; ++k) {
-      if (threadIdx.x / kWave == k) {
+  if constexpr (R > 1) {
+#pragma unroll
+    for (uint32_t k = 1; k < R; ++k) {
+      if (sub == k) {
 #pragma unroll
         for (int c = 0; c < C; ++c)
 #pragma unroll
           for (int e = 0; e < 8; ++e) {
-            const uint32_t i = (c * 8 + e) * kWave + t;
-            s_sum[0][i] = k ? s_sum[0][i] + dw[c][e] : dw[c][e];
-            s_sum[1][i] = k ? s_sum[1][i] + db[c][e] : db[c][e];
+            const uint32_t i = (c * 8 + e) * GS + t;
+            s_sum[i] = k > 1 ? s_sum[i] + dw[c][e] : dw[c][e];
+            s_sum[GS * C * 8 + i] = k > 1 ? s_sum[GS * C * 8 + i] + db[c][e] : db[c][e];
           }
       }
       __syncthreads();
     }
-    for (uint32_t i = threadIdx.x; i < C * kWave * 8; i += BS) {
-      const uint32_t col = (i / (8 * kWave) * kWave + i % kWave) * 8 + i / kWave % 8;
-      if (col < a.D) {
-        part[col] = s_sum[0][i];
-        part[a.D + col] = s_sum[1][i];
-      }
-    }
-  } else {
+    if (sub != 0) return;
 #pragma unroll
-    for (int c = 0; c < C; ++c) {
-      store8<PROFK_F32>(part, (c * GS + t) * 8, a.D, dw[c]);
-      store8<PROFK_F32>(part + a.D, (c * GS + t) * 8, a.D, db[c]);
-    }
+    for (int c = 0; c < C; ++c)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        dw[c][e] += s_sum[(c * 8 + e) * GS + t];
+        db[c][e] += s_sum[GS * C * 8 + (c * 8 + e) * GS + t];
+      }
+  }
+#pragma unroll
+  for (int c = 0; c < C; ++c) {
+    store8<PROFK_F32>(part, (c * GS + t) * 8, a.D, dw[c]);
+    store8<PROFK_F32>(part + a.D, (c * GS + t) * 8, a.D, db[c]);
   }
 }
 
@@ -292,7 +300,7 @@ template <int XDT, int YDT> __global__ __launch_bounds__(1024) void k_norm_grad_
         s[1] = fmaf(q, (n[e] - m) * r, s[1]);
       }
     }
-    row_sum<BS, false>(s, s_red[slot]);
+    row_sum<BS>(s, s_red[slot]);
     s[0] *= inv;
     s[1] *= inv;
     for (uint32_t i = threadIdx.x * 8; i < a.D; i += BS * 8) {
@@ -328,19 +336,11 @@ template <int XDT, int YDT> __global__ __launch_bounds__(256) void k_norm_cols(N
   store8<PROFK_F32>(part + a.D, i, a.D, db);
 }
 
-// The parts' sums, in a fixed order, to dw and db.
-__global__ __launch_bounds__(kJoinCols * kJoinRows) void k_norm_join(NormGradArgs a) {
-  __shared__ float s[kJoinRows][kJoinCols];
-  const uint32_t c = threadIdx.x % kJoinCols, k = threadIdx.x / kJoinCols;
-  const uint32_t col = blockIdx.x * kJoinCols + c;     // of 2 D
-  float sum = 0.0f;
-  if (col < 2 * a.D)
-    for (uint32_t p = k; p < a.parts; p += kJoinRows) sum += a.part[static_cast<size_t>(p) * 2 * a.D + col];
-  s[k][c] = sum;
-  __syncthreads();
-  if (k != 0 || col >= 2 * a.D) return;
-#pragma unroll
-  for (uint32_t j = 1; j < kJoinRows; ++j) sum += s[j][c];
+// The parts' sums to dw and db.
+__global__ __launch_bounds__(kJoinBS) void k_norm_join(NormGradArgs a) {
+  const float sum = join_parts(a.part, a.parts, 2 * a.D);
+  const uint32_t col = blockIdx.x * kJoinCols + threadIdx.x;
+  if (threadIdx.x >= kJoinCols || col >= 2 * a.D) return;
   void* const out = col < a.D ? a.dw : a.db;
   const uint32_t i = col < a.D ? col : col - a.D;
   if (!out) return;
@@ -349,28 +349,25 @@ __global__ __launch_bounds__(kJoinCols * kJoinRows) void k_norm_join(NormGradArg
 }
 
 // Longest rows that are kept in registers.
-constexpr uint32_t kWaveD = 1024, kBlockD = 16384;
-// Workgroups a CU of the kernels that go through the rows.
-constexpr uint32_t kPerCu = 4;
+constexpr uint32_t kBlockD = 16384;
 
-// f(BS, C, WAVE) for rows of D <= kBlockD.
+// f(threads of a row, chunks of a thread) for rows of D <= kBlockD.
 template <class F> void with_shape(uint32_t D, F f) {
   using std::integral_constant;
-  auto shape = [&](auto bs, auto c, auto wave) { f(bs, c, wave); };
-  if (D <= 512) shape(integral_constant<int, 256>{}, integral_constant<int, 1>{}, std::true_type{});
-  else if (D <= 1024) shape(integral_constant<int, 256>{}, integral_constant<int, 2>{}, std::true_type{});
-  else if (D <= 2048) shape(integral_constant<int, 256>{}, integral_constant<int, 1>{}, std::false_type{});
-  else if (D <= 4096) shape(integral_constant<int, 256>{}, integral_constant<int, 2>{}, std::false_type{});
-  else if (D <= 8192) shape(integral_constant<int, 512>{}, integral_constant<int, 2>{}, std::false_type{});
-  else shape(integral_constant<int, 1024>{}, integral_constant<int, 2>{}, std::false_type{});
+  if (D <= 512) f(integral_constant<int, 64>{}, integral_constant<int, 1>{});
+  else if (D <= 1024) f(integral_constant<int, 64>{}, integral_constant<int, 2>{});
+  else if (D <= 2048) f(integral_constant<int, 256>{}, integral_constant<int, 1>{});
+  else if (D <= 4096) f(integral_constant<int, 256>{}, integral_constant<int, 2>{});
+  else if (D <= 8192) f(integral_constant<int, 512>{}, integral_constant<int, 2>{});
+  else f(integral_constant<int, 1024>{}, integral_constant<int, 2>{});
 }
 
-// Workgroups that go through T rows of D.
-uint32_t row_grid(uint32_t T, uint32_t D, uint32_t cus) {
-  const uint32_t rows = D <= kWaveD ? 4 : 1;
-  const uint32_t per_cu = D <= 4096 ? kPerCu : D <= 8192 ? kPerCu / 2 : 1;
-  const uint32_t need = (T + rows - 1) / rows;
-  return need < per_cu * cus ? need : per_cu * cus;
+// Rows of a workgroup of the two kernels, and its workgroups a CU.
+constexpr int norm_rows_of(int gs) { return gs == 64 ? 4 : 1; }
+constexpr int grad_rows_of(int gs) { return gs == 64 ? 8 : gs == 256 ? 2 : 1; }
+uint32_t row_grid(uint32_t T, uint32_t rows, uint32_t threads, uint32_t cus) {
+  const uint32_t need = (T + rows - 1) / rows, most = (threads <= 256 ? 4 : threads <= 512 ? 2 : 1) * cus;
+  return need < most ? need : most;
 }
 
 template <int XDT, int YDT> void norm_rows(const NormArgs& a, uint32_t cus, hipStream_t s) {
@@ -378,9 +375,9 @@ template <int XDT, int YDT> void norm_rows(const NormArgs& a, uint32_t cus, hipS
     k_norm_long<XDT, YDT><<<a.T < 2 * cus ? a.T : 2 * cus, 1024, 0, s>>>(a);
     return;
   }
-  with_shape(a.D, [&](auto bs, auto c, auto wave) {
-    k_norm<XDT, YDT, decltype(bs)::value, decltype(c)::value, decltype(wave)::value>
-        <<<row_grid(a.T, a.D, cus), decltype(bs)::value, 0, s>>>(a);
+  with_shape(a.D, [&](auto gs, auto c) {
+    constexpr int GS = decltype(gs)::value, R = norm_rows_of(GS);
+    k_norm<XDT, YDT, GS, R, decltype(c)::value><<<row_grid(a.T, R, GS * R, cus), GS * R, 0, s>>>(a);
   });
 }
 
@@ -390,9 +387,9 @@ template <int XDT, int YDT> void norm_grad_rows(const NormGradArgs& a, uint32_t 
     if (a.part) k_norm_cols<XDT, YDT><<<dim3((a.D + 2047) / 2048, a.parts), 256, 0, s>>>(a);
     return;
   }
-  with_shape(a.D, [&](auto bs, auto c, auto wave) {
-    k_norm_grad<XDT, YDT, decltype(bs)::value, decltype(c)::value, decltype(wave)::value>
-        <<<a.parts, decltype(bs)::value, 0, s>>>(a);
+  with_shape(a.D, [&](auto gs, auto c) {
+    constexpr int GS = decltype(gs)::value, R = grad_rows_of(GS);
+    k_norm_grad<XDT, YDT, GS, R, decltype(c)::value><<<a.parts, GS * R, 0, s>>>(a);
   });
 }
 
@@ -401,7 +398,14 @@ template <int XDT, int YDT> void norm_grad_rows(const NormGradArgs& a, uint32_t 
 uint32_t norm_grad_parts(int64_t T, int64_t D, int num_cus) {
   const uint32_t cus = static_cast<uint32_t>(num_cus);
   if (T <= 0) return 1;
-  if (D <= static_cast<int64_t>(kBlockD)) return row_grid(static_cast<uint32_t>(T), static_cast<uint32_t>(D), cus);
+  if (D <= static_cast<int64_t>(kBlockD)) {
+    uint32_t parts = 0;
+    with_shape(static_cast<uint32_t>(D), [&](auto gs, auto) {
+      constexpr int GS = decltype(gs)::value, R = grad_rows_of(GS);
+      parts = row_grid(static_cast<uint32_t>(T), R, GS * R, cus);
+    });
+    return parts;
+  }
   const uint32_t slabs = static_cast<uint32_t>((D + 2047) / 2048), most = (4 * cus + slabs - 1) / slabs;
   return static_cast<uint32_t>(T < most ? T : most);
 }
@@ -431,7 +435,7 @@ hipError_t launch_norm_grad(const NormGradArgs& a, int dtype, int dy_dtype, hipS
   }
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || !a.part) return e;
-  k_norm_join<<<(2 * a.D + kJoinCols - 1) / kJoinCols, kJoinCols * kJoinRows, 0, s>>>(a);
+  k_norm_join<<<(2 * a.D + kJoinCols - 1) / kJoinCols, kJoinBS, 0, s>>>(a);
   return hipGetLastError();
 }
 

@@ -32,11 +32,11 @@ namespace profk {
 
 namespace {
 
-typedef float f32x4 __attribute__((ext_vector_type(4)));
-typedef float f32x4u __attribute__((ext_vector_type(4), aligned(4)));
+typedef float f32x2u __attribute__((ext_vector_type(2), aligned(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x2u __attribute__((ext_vector_type(2), aligned(2)));
+typedef uint32_t __attribute__((aligned(2))) u32u;
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
@@ -66,7 +66,7 @@ template <int WM, int WN, int MI, int NJ> struct ProdTile {
   static constexpr int NW = WM * WN, BS = NW * kWave, BM = WM * MI * 32, BN = WN * NJ * 32;
   static constexpr int QA = BM * 8 / BS, QB = BN * 8 / BS;   // loads of a lane
   static constexpr int kB = BM * 8, kGran = (BM + BN) * 8;   // first granule of b; granules of a stage
-  static_assert(BM * 8 % BS == 0 && BN * 8 % BS == 0 && NJ == 4, "whole loads, four neighbouring results a lane");
+  static_assert(BM * 8 % BS == 0 && BN * 8 % BS == 0 && (NJ == 2 || NJ == 4), "whole loads, neighbouring results of a lane");
 };
 
 // One operand's part of a stage: what a lane loads, and where it reads.  BW
@@ -272,20 +272,24 @@ __device__ __forceinline__ void prod_body(const ProdArgs& g, uint32_t tiles_i, u
         }
       }
     } else {
-      f32x4 bias = {};
-      if (g.bias) {
+      float bias[NJ];
 #pragma unroll
-        for (uint32_t j = 0; j < 4; ++j) bias[j] = n + j < g.J ? g.bias[n + j] : 0.0f;
-      }
+      for (uint32_t j = 0; j < NJ; ++j) bias[j] = g.bias && n + j < g.J ? g.bias[n + j] : 0.0f;
       const bool whole = n + NJ <= g.J;
-      auto put4 = [&](O* p, const f32x4& y) {
+      auto put_all = [&](O* p, const float (&y)[NJ]) {
         if (whole) {
-          if constexpr (DT == PROFK_F32) *reinterpret_cast<f32x4u*>(p) = y;
-          else *reinterpret_cast<u32x2u*>(p) = u32x2u{pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3])};
+          if constexpr (DT == PROFK_F32) {
+#pragma unroll
+            for (int j = 0; j < NJ; j += 2) *reinterpret_cast<f32x2u*>(p + j) = f32x2u{y[j], y[j + 1]};
+          } else if constexpr (NJ == 4) {
+            *reinterpret_cast<u32x2u*>(p) = u32x2u{pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3])};
+          } else {
+            *reinterpret_cast<u32u*>(p) = pack_bf16(y[0], y[1]);
+          }
         } else {
-          p[0] = static_cast<O>(y[0]);
-          if (n + 1 < g.J) p[1] = static_cast<O>(y[1]);
-          if (n + 2 < g.J) p[2] = static_cast<O>(y[2]);
+#pragma unroll
+          for (uint32_t j = 0; j < NJ - 1; ++j)
+            if (n + j < g.J) p[j] = static_cast<O>(y[j]);
         }
       };
       if (n < g.J) {
@@ -300,27 +304,34 @@ __device__ __forceinline__ void prod_body(const ProdArgs& g, uint32_t tiles_i, u
             const uint32_t r = first + 8 * (v / 4) + v % 4;
             if (r < g.I) {
               const size_t at = static_cast<size_t>(r) * g.J + n;
-              f32x4 z = f32x4{acc[i][0][v], acc[i][1][v], acc[i][2][v], acc[i][3][v]} + bias;
-              if (g.pre) put4(static_cast<O*>(g.pre) + at, z);
+              float z[NJ];
 #pragma unroll
-              for (int j = 0; j < 4; ++j) z[j] = act_of<ACT>(z[j]);
+              for (int j = 0; j < NJ; ++j) z[j] = acc[i][j][v] + bias[j];
+              if (g.pre) put_all(static_cast<O*>(g.pre) + at, z);
+#pragma unroll
+              for (int j = 0; j < NJ; ++j) z[j] = act_of<ACT>(z[j]);
               if (g.residual) {
                 const O* const q = static_cast<const O*>(g.residual) + r * g.residual_stride + n;
                 if (whole) {
-                  if constexpr (DT == PROFK_F32) {
-                    z += *reinterpret_cast<const f32x4u*>(q);
-                  } else {
-                    const u32x2u u = *reinterpret_cast<const u32x2u*>(q);
-                    z += f32x4{__uint_as_float(u[0] << 16), __uint_as_float(u[0] & 0xFFFF0000u),
-                               __uint_as_float(u[1] << 16), __uint_as_float(u[1] & 0xFFFF0000u)};
+#pragma unroll
+                  for (int j = 0; j < NJ; j += 2) {
+                    if constexpr (DT == PROFK_F32) {
+                      const f32x2u u = *reinterpret_cast<const f32x2u*>(q + j);
+                      z[j] += u[0];
+                      z[j + 1] += u[1];
+                    } else {
+                      const uint32_t u = *reinterpret_cast<const u32u*>(q + j);
+                      z[j] += __uint_as_float(u << 16);
+                      z[j + 1] += __uint_as_float(u & 0xFFFF0000u);
+                    }
                   }
                 } else {
-                  z[0] += static_cast<float>(q[0]);
-                  if (n + 1 < g.J) z[1] += static_cast<float>(q[1]);
-                  if (n + 2 < g.J) z[2] += static_cast<float>(q[2]);
+#pragma unroll
+                  for (uint32_t j = 0; j < NJ - 1; ++j)
+                    if (n + j < g.J) z[j] += static_cast<float>(q[j]);
                 }
               }
-              put4(out + at, z);
+              put_all(out + at, z);
             }
           }
         }
@@ -391,7 +402,7 @@ void launch_tiles(const ProdArgs& g, uint32_t cus, hipStream_t s) {
 template <bool TA, bool TB, int ACT, int DT> void launch_shape(const ProdArgs& g, uint32_t cus, hipStream_t s) {
   const uint64_t large = static_cast<uint64_t>((g.I + 255) / 256) * ((g.J + 255) / 256);
   if (g.I > 128 && large >= cus) launch_tiles<TA, TB, ACT, DT, 4, 2, 2, 4, 1>(g, cus, s);
-  else launch_tiles<TA, TB, ACT, DT, 4, 1, 1, 4, 2>(g, cus, s);
+  else launch_tiles<TA, TB, ACT, DT, 2, 2, 2, 2, 2>(g, cus, s);
 }
 
 // Tiles are counted in 32 bits.
