@@ -514,7 +514,7 @@ int profk_linear_grad(int32_t dtype, const void* dy, int64_t dy_stride, const vo
  *   bias_ids  int64 [n_bias], bias_values fp32 [n_bias], row r's at
  *             bias_offsets[r] .. (int64 [T + 1]); NULL: none.  Of the same token
  *             twice in a row the last entry stands.  Both lists hold fewer than
- *             2^31 entries; offsets past a list's end are taken as its end.
+ *             2^30 entries; offsets past a list's end are taken as its end.
  *   allowed   32 tokens a word, the lowest bit first, [n_masks] masks of
  *             allowed_stride >= ceil(V / 32) words; NULL: all are allowed.  mask
  *             int64 [T]: the row's mask, negative for none; a mask from n_masks up

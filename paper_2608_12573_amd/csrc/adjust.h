@@ -9,6 +9,8 @@
 
 namespace profk {
 
+constexpr int64_t kAdjMaxList = (int64_t{1} << 30) - 1;   // entries of a list
+
 struct AdjustArgs {
   const void* x;                    // logits
   const void* dy;                   // gradient of the adjusted logits (null: the forward call)

@@ -673,7 +673,7 @@ int check_adjust(int32_t dtype, const void* logits, int64_t T, int64_t V, int64_
   if (!dtype_ok(dtype)) return PROFK_EDTYPE;
   if (V < 1 || V > static_cast<int64_t>(INT32_MAX) || !rows_ok(T, V, x_stride) || !rows_ok(T, V, out_stride))
     return PROFK_EINVAL;
-  if (tokens && (n_tokens < 0 || n_tokens > static_cast<int64_t>(INT32_MAX))) return PROFK_EINVAL;
+  if (tokens && (n_tokens < 0 || n_tokens > profk::kAdjMaxList)) return PROFK_EINVAL;
   if (allowed) {
     if (n_masks < 1 || allowed_stride < (V + 31) / 32 || allowed_stride > INT64_MAX / 8 / n_masks) return PROFK_EINVAL;
     if (!mask && n_masks != 1 && n_masks != T) return PROFK_EINVAL;
@@ -711,7 +711,7 @@ int profk_adjust_logits(int32_t dtype, const void* logits, int64_t T, int64_t V,
   const int rc = check_adjust(dtype, logits, T, V, x_stride, tokens, token_offsets, n_tokens, repetition, allowed,
                               n_masks, allowed_stride, mask, out, out_stride, &a);
   if (rc != PROFK_OK) return rc;
-  if (bias_ids && (n_bias < 0 || n_bias > static_cast<int64_t>(INT32_MAX))) return PROFK_EINVAL;
+  if (bias_ids && (n_bias < 0 || n_bias > profk::kAdjMaxList)) return PROFK_EINVAL;
   if (T == 0) return PROFK_OK;
   if (bias_ids && (!bias_values || !bias_offsets)) return PROFK_ENULL;
   if (!aligned(n_prompt, 8) || !aligned(presence, 4) || !aligned(frequency, 4) || !aligned(bias_ids, 8) ||

@@ -11,8 +11,7 @@
 //
 // A workgroup takes a piece of a row.  It counts the history's tokens that fall
 // into its piece in LDS, a word a token (integer atomics: their order changes
-// nothing), notes the last bias of each token beside it, and streams the piece
-// once.  Every piece reads the whole history again, from the caches.
+// nothing), lists the biases of its tokens, and streams the piece once.  Every piece reads the whole history again, from the caches.
 #include "adjust.h"
 #include "elem8.h"
 #include "launch.h"
@@ -21,14 +20,17 @@ namespace profk {
 
 namespace {
 
-constexpr uint32_t kAdjPrompt = 0x80000000u;   // of a token's word: it is in the prompt; the rest counts it after
+// Of a token's word: it is in the prompt, it has a bias; the rest counts it after
+// the prompt.
+constexpr uint32_t kAdjPrompt = 0x80000000u, kAdjBias = 0x40000000u;
+constexpr uint32_t kAdjList = 256;             // biases of a piece that are kept in LDS
 constexpr uint32_t kAdjChunks = 2;             // of 8 elements, of a thread
-constexpr uint32_t kAdjMaxPiece = 8192;        // elements (LDS: a word each, two with biases)
+constexpr uint32_t kAdjMaxPiece = 8192;        // elements (LDS: a word each)
 
 __device__ __forceinline__ int64_t clamp64(int64_t x, int64_t lo, int64_t hi) { return x < lo ? lo : x > hi ? hi : x; }
 
 template <int DT, bool GRAD> __global__ __launch_bounds__(512) void k_adjust(AdjustArgs a) {
-  extern __shared__ __align__(16) uint32_t s_word[];     // [piece], then the biases' [piece]
+  extern __shared__ __align__(16) uint32_t s_word[];     // [piece]
   const uint32_t row = a.row + blockIdx.x / a.pieces, p = blockIdx.x % a.pieces;
   const uint32_t v0 = p * a.piece, n = min(a.piece, a.V - v0);
   constexpr uint32_t ES = DT == PROFK_F32 ? 4 : 2;
@@ -51,12 +53,10 @@ template <int DT, bool GRAD> __global__ __launch_bounds__(512) void k_adjust(Adj
 #pragma unroll
   for (uint32_t q = 0; q < kAdjChunks; ++q) raw[q] = load_raw8<DT>(src, (q * BS + tid) * 8, n);
   const bool hist = h1 > h0, bias = b1 > b0;
-  uint32_t* const s_bias = s_word + (a.tokens ? a.piece : 0);
+  __shared__ uint32_t s_n, s_tok[kAdjList], s_at[kAdjList];
   if (hist || bias) {
-    for (uint32_t i = tid; i < a.piece; i += BS) {
-      if (hist) s_word[i] = 0;
-      if (bias) s_bias[i] = 0;
-    }
+    for (uint32_t i = tid * 4; i < a.piece; i += BS * 4) *reinterpret_cast<u32x4*>(s_word + i) = u32x4{};
+    if (tid == 0) s_n = 0;
     __syncthreads();
     const int64_t made = h0 + (a.n_prompt && hist ? clamp64(a.n_prompt[row], 0, h1 - h0) : 0);
     // (four tokens at a time: a load waits for none before it)
@@ -75,10 +75,29 @@ template <int DT, bool GRAD> __global__ __launch_bounds__(512) void k_adjust(Adj
     }
     for (int64_t i = b0 + tid; i < b1; i += BS) {
       const uint64_t v = static_cast<uint64_t>(a.bias_ids[i]) - v0;
-      if (v < n) atomicMax(s_bias + v, static_cast<uint32_t>(i - b0) + 1);
+      if (v < n) {
+        atomicOr(s_word + v, kAdjBias);
+        const uint32_t k = atomicAdd(&s_n, 1u);
+        if (k < kAdjList) {
+          s_tok[k] = static_cast<uint32_t>(v);
+          s_at[k] = static_cast<uint32_t>(i - b0);
+        }
+      }
     }
     __syncthreads();
   }
+  // the last bias of token v of the piece: from the list in LDS, whose order may
+  // be any, or, where that did not hold them all, from the row's
+  auto bias_of = [&](uint32_t v) {
+    int64_t at = -1;
+    if (s_n <= kAdjList) {
+      for (uint32_t k = 0; k < s_n; ++k)
+        if (s_tok[k] == v && static_cast<int64_t>(s_at[k]) > at) at = s_at[k];
+    } else {
+      for (at = b1 - b0 - 1; a.bias_ids[b0 + at] != static_cast<int64_t>(v0) + v;) --at;
+    }
+    return a.bias_values[b0 + at];
+  };
   const uint32_t* words = nullptr;
   bool lost = false;                 // the row names a mask that is not there
   if (a.allowed) {
@@ -99,28 +118,24 @@ template <int DT, bool GRAD> __global__ __launch_bounds__(512) void k_adjust(Adj
     // (a piece starts at a multiple of 32 tokens)
     const uint32_t ok = words ? words[(v0 + i) / 32] >> (i % 32) : 0xFFu;
     // (the words past the row's end stay 0)
-    u32x4 c4[2] = {}, k4[2] = {};
-    if (hist) {
+    u32x4 c4[2] = {};
+    if (hist || bias) {
       c4[0] = *reinterpret_cast<const u32x4*>(s_word + i);
       c4[1] = *reinterpret_cast<const u32x4*>(s_word + i + 4);
     }
-    if (bias) {
-      k4[0] = *reinterpret_cast<const u32x4*>(s_bias + i);
-      k4[1] = *reinterpret_cast<const u32x4*>(s_bias + i + 4);
-    }
 #pragma unroll
     for (uint32_t e = 0; e < 8; ++e) {
-      const uint32_t c = c4[e / 4][e % 4], k = k4[e / 4][e % 4];
-      if (c) {
+      const uint32_t c = c4[e / 4][e % 4];
+      if (c & ~kAdjBias) {
         if constexpr (GRAD) {
           if (a.repetition) y[e] = load1(x, i + e, DT) > 0.0f ? y[e] / rep : y[e] * rep;
         } else {
           if (a.repetition) y[e] = y[e] > 0.0f ? y[e] / rep : y[e] * rep;
-          const uint32_t m = c & ~kAdjPrompt;
+          const uint32_t m = c & ~(kAdjPrompt | kAdjBias);
           if (m) y[e] -= fmaf(static_cast<float>(m), freq, pres);
         }
       }
-      if (k) y[e] += a.bias_values[b0 + k - 1];
+      if (!GRAD && (c & kAdjBias)) y[e] += bias_of(i + e);
       if (!(ok >> e & 1)) y[e] = GRAD ? 0.0f : -__builtin_inff();
       if (lost) y[e] = nan;
     }
@@ -139,8 +154,9 @@ hipError_t launch_adjust(AdjustArgs a, int dtype, int64_t T, hipStream_t s) {
   a.piece = piece;
   a.pieces = (a.V + piece - 1) / piece;
   uint32_t bs = 512;
-  while (bs > 64 && bs * 8 * kAdjChunks >= 2 * piece) bs /= 2;
-  const uint32_t lds = ((a.tokens ? piece : 0) + (!a.dy && a.bias_ids ? piece : 0)) * 4;
+  // (no fewer threads than go through an average history in one step)
+  while (bs > 64 && bs * 8 * kAdjChunks >= 2 * piece && (!a.tokens || bs * 4 >= 2 * (a.n_tokens / T))) bs /= 2;
+  const uint32_t lds = a.tokens || (!a.dy && a.bias_ids) ? piece * 4 : 0;
   const int64_t step = ((int64_t{1} << 31) - 1) / bs / a.pieces < 1 ? 1 : ((int64_t{1} << 31) - 1) / bs / a.pieces;
   (void)hipGetLastError();
   for (int64_t r = 0; r < T; r += step) {

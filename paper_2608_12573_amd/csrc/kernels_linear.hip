@@ -153,7 +153,7 @@ template <int DT, int ACT> __global__ __launch_bounds__(256) void k_dz(DzArgs a)
     }
 #pragma unroll
     for (int e = 0; e < 8; ++e) sum[e] += d[e];
-    if (a.dz) store8<PROFK_BF16>(a.dz + r * a.dz_stride, j, a.N, d);
+    if (a.dz) store8<PROFK_BF16>(a.dz + r * a.dz_stride, j, static_cast<uint32_t>(a.dz_stride), d);   // (0 past N)
   }
   if (a.part) store8<PROFK_F32>(a.part + static_cast<size_t>(p) * a.N, j, a.N, sum);
 }
@@ -172,8 +172,32 @@ uint32_t dz_parts(int64_t M, int64_t N, int num_cus) {
 
 size_t align256(size_t n) { return (n + 255) / 256 * 256; }
 
+// Rows of any stride and alignment, to rows of whole 16-byte granules (Kp
+// elements, zeros past K).
+__global__ __launch_bounds__(256) void k_pad(const __bf16* x, uint64_t stride, uint32_t R, uint32_t K, __bf16* out) {
+  const uint32_t per = (K + 7) / 8;
+  const uint64_t n = static_cast<uint64_t>(R) * per;
+  for (uint64_t i = blockIdx.x * uint64_t{256} + threadIdx.x; i < n; i += gridDim.x * uint64_t{256}) {
+    const uint32_t r = static_cast<uint32_t>(i / per), k = static_cast<uint32_t>(i % per) * 8;
+    reinterpret_cast<u32x4*>(out)[i] = load_raw8<PROFK_BF16>(x + r * stride, k, K).q[0];
+  }
+}
+
+uint64_t padded(int64_t K) { return (static_cast<uint64_t>(K) + 7) / 8 * 8; }
+size_t pad_bytes(int64_t R, int64_t K) { return K % 8 ? align256(static_cast<size_t>(R) * padded(K) * 2) : 0; }
+
+// Operands whose rows are not whole granules (K % 8) are copied: a pass over
+// them, where the tiled product is that much faster than the one of any operands
+// (4096 x 4095 x 12288 .. us against ..).
+hipError_t pad(const void* x, uint64_t stride, int64_t R, int64_t K, void* out, hipStream_t s) {
+  const uint64_t blocks = (static_cast<uint64_t>(R) * (padded(K) / 8) + 255) / 256;
+  k_pad<<<blocks < 8192 ? static_cast<uint32_t>(blocks) : 8192, 256, 0, s>>>(
+      static_cast<const __bf16*>(x), stride, static_cast<uint32_t>(R), static_cast<uint32_t>(K), static_cast<__bf16*>(out));
+  return hipGetLastError();
+}
+
 struct GradLayout {
-  size_t dz, part, bytes;           // offsets
+  size_t dz, part, x, w, bytes;     // offsets
   uint64_t dz_stride;
   uint32_t parts;
 };
@@ -182,44 +206,57 @@ GradLayout grad_layout(int64_t M, int64_t N, int64_t K, int num_cus) {
   L.dz_stride = (static_cast<uint64_t>(N) + 7) / 8 * 8;
   L.parts = dz_parts(M, N, num_cus);
   L.part = align256(static_cast<size_t>(M) * L.dz_stride * 2);
-  L.bytes = L.part + align256(static_cast<size_t>(L.parts) * N * 4);
+  L.x = L.part + align256(static_cast<size_t>(L.parts) * N * 4);
+  L.w = L.x + pad_bytes(M, K);
+  L.bytes = L.w + pad_bytes(N, K);
   return L;
 }
 
 }  // namespace
 
-size_t lin_workspace(int64_t, int64_t, int64_t, int) { return 0; }
+size_t lin_workspace(int64_t M, int64_t N, int64_t K, int) { return pad_bytes(M, K) + pad_bytes(N, K); }
 
 size_t lin_grad_workspace(int64_t M, int64_t N, int64_t K, int num_cus) { return grad_layout(M, N, K, num_cus).bytes; }
 
 hipError_t launch_linear(const LinCall& c, hipStream_t s) {
-  const ProdArgs g{static_cast<const __bf16*>(c.x), static_cast<const __bf16*>(c.w), c.x_stride, c.w_stride,
-                   static_cast<uint32_t>(c.M), static_cast<uint32_t>(c.N), static_cast<uint32_t>(c.K), c.bias, c.act,
-                   c.out_dtype, c.residual, c.residual_stride, c.out, c.pre, 0, 0};
-  (void)hipGetLastError();
+  ProdArgs g{static_cast<const __bf16*>(c.x), static_cast<const __bf16*>(c.w), c.x_stride, c.w_stride,
+             static_cast<uint32_t>(c.M), static_cast<uint32_t>(c.N), static_cast<uint32_t>(c.K), c.bias, c.act,
+             c.out_dtype, c.residual, c.residual_stride, c.out, c.pre, 0, 0, false, false};
   const uint32_t cus = static_cast<uint32_t>(device_cu_count());
+  (void)hipGetLastError();
+  if (c.K % 8) {
+    uint8_t* const ws = static_cast<uint8_t*>(c.ws);
+    __bf16* const x = reinterpret_cast<__bf16*>(ws);
+    __bf16* const w = reinterpret_cast<__bf16*>(ws + pad_bytes(c.M, c.K));
+    hipError_t e = pad(c.x, c.x_stride, c.M, c.K, x, s);
+    if (e == hipSuccess) e = pad(c.w, c.w_stride, c.N, c.K, w, s);
+    if (e != hipSuccess) return e;
+    g.a = x;
+    g.b = w;
+    g.as = g.bs = padded(c.K);
+    g.a_padded = g.b_padded = true;
+  }
   if (launch_product_few(g, cus, s)) return hipGetLastError();
   if (launch_product_along(g, cus, s)) return hipGetLastError();
   return launch_any<false, false>(g, s);
 }
 
 hipError_t launch_linear_grad(const LinGradCall& c, hipStream_t s) {
-  const GradLayout L = grad_layout(c.M, c.N, c.K, device_cu_count());
+  const uint32_t cus = static_cast<uint32_t>(device_cu_count());
+  const GradLayout L = grad_layout(c.M, c.N, c.K, static_cast<int>(cus));
   uint8_t* const ws = static_cast<uint8_t*>(c.ws);
   const uint32_t M = static_cast<uint32_t>(c.M), N = static_cast<uint32_t>(c.N), K = static_cast<uint32_t>(c.K);
   __bf16* const dz = reinterpret_cast<__bf16*>(ws + L.dz);
   float* const part = reinterpret_cast<float*>(ws + L.part);
   // (without an activation, dy in bf16 is dz)
-  const bool given = c.act == PROFK_ACT_NONE && c.dtype == PROFK_BF16;
-  const DzArgs d{c.dy, c.pre, c.dy_stride, M, N, L.parts, (c.dx || c.dw) && !given ? dz : nullptr, L.dz_stride,
+  const bool given = c.act == PROFK_ACT_NONE && c.dtype == PROFK_BF16 && granules(c.dy, c.dy_stride, N, false);
+  const bool dx = c.dx && M, dw = c.dw && N;
+  const DzArgs d{c.dy, c.pre, c.dy_stride, M, N, L.parts, (dx || dw) && !given ? dz : nullptr, L.dz_stride,
                  c.db ? part : nullptr};
-  const __bf16* const z = given ? static_cast<const __bf16*>(c.dy) : dz;
-  const uint64_t z_stride = given ? c.dy_stride : L.dz_stride;
-  const uint32_t cus = static_cast<uint32_t>(device_cu_count());
   (void)hipGetLastError();
-  const dim3 grid((N + 2047) / 2048, L.parts);
   hipError_t e = hipSuccess;
   if (N && (d.dz || d.part)) {
+    const dim3 grid((N + 2047) / 2048, L.parts);
     with_act(c.act, [&](auto act) {
       if (c.dtype == PROFK_F32) k_dz<PROFK_F32, decltype(act)::value><<<grid, 256, 0, s>>>(d);
       else k_dz<PROFK_BF16, decltype(act)::value><<<grid, 256, 0, s>>>(d);
@@ -230,15 +267,37 @@ hipError_t launch_linear_grad(const LinGradCall& c, hipStream_t s) {
     k_db_join<<<(N + kJoinCols - 1) / kJoinCols, kJoinBS, 0, s>>>(part, L.parts, N, c.db);
     e = hipGetLastError();
   }
-  if (e == hipSuccess && c.dx && M) {
-    const ProdArgs g{z, static_cast<const __bf16*>(c.w), z_stride, c.w_stride, M, K, N, nullptr, PROFK_ACT_NONE,
-                     PROFK_BF16, nullptr, 0, c.dx, nullptr, 0, 0};
-    e = launch_product_grad(g, false, cus, s) ? hipGetLastError() : launch_any<false, true>(g, s);
+  ProdArgs g{};
+  g.a = given ? static_cast<const __bf16*>(c.dy) : dz;
+  g.as = given ? c.dy_stride : L.dz_stride;
+  g.a_padded = !given;
+  g.b_padded = K % 8 != 0;
+  g.J = K;
+  g.act = PROFK_ACT_NONE;
+  g.out_dtype = PROFK_BF16;
+  // b: W or x, copied where its rows are not whole granules
+  auto other = [&](const void* p, uint64_t stride, int64_t R, size_t at) {
+    g.b = static_cast<const __bf16*>(p);
+    g.bs = stride;
+    if (g.b_padded && R > 0) {
+      e = pad(p, stride, R, K, ws + at, s);
+      g.b = reinterpret_cast<const __bf16*>(ws + at);
+      g.bs = padded(K);
+    }
+  };
+  if (e == hipSuccess && dx) {
+    other(c.w, c.w_stride, N, L.w);
+    g.I = M;
+    g.K = N;
+    g.out = c.dx;
+    if (e == hipSuccess) e = launch_product_grad(g, false, cus, s) ? hipGetLastError() : launch_any<false, true>(g, s);
   }
-  if (e == hipSuccess && c.dw && N) {
-    const ProdArgs g{z, static_cast<const __bf16*>(c.x), z_stride, c.x_stride, N, K, M, nullptr, PROFK_ACT_NONE,
-                     PROFK_BF16, nullptr, 0, c.dw, nullptr, 0, 0};
-    e = launch_product_grad(g, true, cus, s) ? hipGetLastError() : launch_any<true, true>(g, s);
+  if (e == hipSuccess && dw) {
+    other(c.x, c.x_stride, M, L.x);
+    g.I = N;
+    g.K = M;
+    g.out = c.dw;
+    if (e == hipSuccess) e = launch_product_grad(g, true, cus, s) ? hipGetLastError() : launch_any<true, true>(g, s);
   }
   return e;
 }

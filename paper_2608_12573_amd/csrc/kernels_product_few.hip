@@ -181,7 +181,7 @@ template <int NG, int XL> void few_launch(const ProdArgs& g, uint32_t cus, hipSt
 }  // namespace
 
 bool launch_product_few(const ProdArgs& g, uint32_t cus, hipStream_t s) {
-  if (g.I > 32 || !granules(g.a, g.as, g.K) || !granules(g.b, g.bs, g.K)) return false;
+  if (g.I > 32 || !granules(g.a, g.as, g.K, g.a_padded) || !granules(g.b, g.bs, g.K, g.b_padded)) return false;
   const bool wide = g.J >= 32 * 4 * cus;
   if (g.I <= 8) wide ? few_launch<2, 1>(g, cus, s) : few_launch<1, 1>(g, cus, s);
   else if (g.I <= 16) wide ? few_launch<2, 2>(g, cus, s) : few_launch<1, 2>(g, cus, s);

@@ -5,7 +5,7 @@
 namespace profk {
 
 bool launch_product_grad(const ProdArgs& g, bool a_across, uint32_t cus, hipStream_t s) {
-  if (!granules(g.a, g.as, a_across ? g.I : g.K) || !granules(g.b, g.bs, g.J) || !tiles_fit(g) || g.K == 0) return false;
+  if (!granules(g.a, g.as, a_across ? g.I : g.K, g.a_padded) || !granules(g.b, g.bs, g.J, g.b_padded) || !tiles_fit(g) || g.K == 0) return false;
   if (a_across) launch_shape<true, true, PROFK_ACT_NONE, PROFK_BF16>(g, cus, s);
   else launch_shape<false, true, PROFK_ACT_NONE, PROFK_BF16>(g, cus, s);
   return true;

@@ -19,6 +19,7 @@ struct ProdArgs {
   uint64_t residual_stride;
   void *out, *pre;                  // [I, J]
   uint32_t i0, j0;                  // kernel of any sizes: first row and column of this launch
+  bool a_padded, b_padded;          // rows end in whole granules of 8, zeros past their end
 };
 
 // ------------------------------------------------------------ activations ---
@@ -80,8 +81,8 @@ bool launch_product_grad(const ProdArgs& g, bool a_across, uint32_t cus, hipStre
 
 // Operands that the tiled product takes: rows of whole 16-byte granules.  `len`
 // is the length of a row.
-inline bool granules(const void* p, uint64_t stride, uint32_t len) {
-  return reinterpret_cast<uintptr_t>(p) % 16 == 0 && stride % 8 == 0 && len % 8 == 0 && stride <= (1u << 21);
+inline bool granules(const void* p, uint64_t stride, uint32_t len, bool padded) {
+  return reinterpret_cast<uintptr_t>(p) % 16 == 0 && stride % 8 == 0 && (padded || len % 8 == 0) && stride <= (1u << 21);
 }
 
 }  // namespace profk

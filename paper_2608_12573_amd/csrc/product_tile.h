@@ -42,6 +42,7 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
 constexpr uint32_t kProdXcds = 8;
 constexpr uint32_t kStageK = 64;
+constexpr uint32_t kPanel = 8;      // column tiles of a panel
 
 __device__ const uint4 g_zero_granule = {0, 0, 0, 0};
 
@@ -109,7 +110,7 @@ template <bool ACROSS, int BW, int Q, int F, bool PERM, bool WHOLE> struct ProdS
 #pragma unroll
       for (int q = 0; q < Q; ++q) {
         const uint32_t at = (w * Q + q) * kWave + lane, k = at / (BW / 8), g = at % (BW / 8) ^ (k & 3) * 4;
-        off[q] = k * static_cast<uint32_t>(row_bytes) + min(g, (R - r0) / 8 - 1) * 16;
+        off[q] = k * static_cast<uint32_t>(row_bytes) + min(g, (R - r0 + 7) / 8 - 1) * 16;
       }
     } else {
       base = reinterpret_cast<const uint8_t*>(p) + r0 * row_bytes;
@@ -159,9 +160,9 @@ __device__ __forceinline__ void prod_body(const ProdArgs& g, uint32_t tiles_i, u
   // distinct arrays, so that the compiler can tell the stage being read from
   // the one being filled
   __shared__ __align__(16) uint4 s0[T::kGran], s1[T::kGran];
-  // workgroup b runs on XCD b % 8: each XCD takes a run of tiles, the row
-  // tiles of a column tile one after the other, so that its L2 holds what
-  // they share
+  // workgroup b runs on XCD b % 8: each XCD takes a run of tiles, and goes through
+  // panels of kPanel column tiles row by row, so that what it works on at a time
+  // is near a square, which shares most in its L2
   const uint32_t xcd = blockIdx.x % kProdXcds, per_xcd = gridDim.x / kProdXcds;   // (the grid is a multiple of 8)
   const uint32_t end = static_cast<uint32_t>(static_cast<uint64_t>(tiles) * (xcd + 1) / kProdXcds);
   const uint32_t tile0 = static_cast<uint32_t>(static_cast<uint64_t>(tiles) * xcd / kProdXcds) + blockIdx.x / kProdXcds;
@@ -176,9 +177,18 @@ __device__ __forceinline__ void prod_body(const ProdArgs& g, uint32_t tiles_i, u
   ProdSide<TB, T::BN, T::QB, NJ, !TB, WHOLE> sb;
   sa.init(w, lane, wm * MI * 32, g.as, g.K);
   sb.init(w, lane, wn * NJ * 32, g.bs, g.K);
+  const uint32_t tiles_j = (g.J + T::BN - 1) / T::BN;
+  auto place = [&](uint32_t tile, uint32_t& i, uint32_t& j) {
+    const uint32_t p = tile / (kPanel * tiles_i), rest = tile - p * (kPanel * tiles_i);
+    const uint32_t width = min(kPanel, tiles_j - p * kPanel);
+    i = rest / width * T::BM;
+    j = (p * kPanel + rest % width) * T::BN;
+  };
   auto start = [&](uint32_t tile) {
-    sa.start(g.a, tile % tiles_i * T::BM, g.I);
-    sb.start(g.b, tile / tiles_i * T::BN, g.J);
+    uint32_t i, j;
+    place(tile, i, j);
+    sa.start(g.a, i, g.I);
+    sb.start(g.b, j, g.J);
   };
   uint32_t next_k = 0, next_tile = tile0;
   // (past the last tile: its last stage again)
@@ -250,7 +260,9 @@ __device__ __forceinline__ void prod_body(const ProdArgs& g, uint32_t tiles_i, u
   };
   using O = std::conditional_t<DT == PROFK_F32, float, __bf16>;
   auto store = [&](uint32_t tile) {
-    const uint32_t mw = tile % tiles_i * T::BM + wm * MI * 32, nw = tile / tiles_i * T::BN + wn * NJ * 32;
+    uint32_t ti, tj;
+    place(tile, ti, tj);
+    const uint32_t mw = ti + wm * MI * 32, nw = tj + wn * NJ * 32;
     const uint32_t m = mw + 4 * h, n = nw + (TB ? c : NJ * c);
     O* const out = static_cast<O*>(g.out);
     if constexpr (TB) {

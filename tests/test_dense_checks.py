@@ -85,8 +85,8 @@ def test_linear_grad_refusals(kw, rc):
 
 @pytest.mark.parametrize("kw,rc", [
     (dict(dt=2), pk.EDTYPE), (dict(V=0), pk.EINVAL), (dict(V=2**31, st=2**31, ost=2**31), pk.EINVAL),
-    (dict(st=99), pk.EINVAL), (dict(ost=99), pk.EINVAL), (dict(nt=-1), pk.EINVAL), (dict(nt=2**31), pk.EINVAL),
-    (dict(nb=-1), pk.EINVAL), (dict(nm=0), pk.EINVAL), (dict(ast=3), pk.EINVAL), (dict(mask=None, nm=2), pk.EINVAL),
+    (dict(st=99), pk.EINVAL), (dict(ost=99), pk.EINVAL), (dict(nt=-1), pk.EINVAL), (dict(nt=2**30), pk.EINVAL),
+    (dict(nb=-1), pk.EINVAL), (dict(nb=2**30), pk.EINVAL), (dict(nm=0), pk.EINVAL), (dict(ast=3), pk.EINVAL), (dict(mask=None, nm=2), pk.EINVAL),
     (dict(x=None), pk.ENULL), (dict(off=None), pk.ENULL), (dict(out=None), pk.ENULL), (dict(bv=None), pk.ENULL),
     (dict(bo=None), pk.ENULL), (dict(tok=ctypes.c_void_p((2 << 32) + 4)), pk.EINVAL), (dict(al=ODD2), pk.EINVAL),
     (dict(x=ODD2), pk.EINVAL), (dict(out=A, ost=101), pk.EINVAL),

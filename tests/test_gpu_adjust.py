@@ -115,6 +115,16 @@ def test_histories(history, V):
     _check(pk.adjust_logits(x, **one), *_want(x, one), "f32")
 
 
+@pytest.mark.parametrize("V,n", [(40, 300), (3000, 900), (30000, 3000)])
+def test_many_biases(V, n):
+    note(f"adjust_logits {n} biases of {V}")
+    x, kw = _case(4, V, "f32", n, biases=n)
+    _check(pk.adjust_logits(x, **kw), *_want(x, kw), "f32")
+    # all of them on few tokens
+    few = dict(kw, bias=(kw["bias"][0] % 7,) + kw["bias"][1:])
+    _check(pk.adjust_logits(x, **few), *_want(x, few), "f32")
+
+
 @pytest.mark.parametrize("name", ["repetition", "presence", "frequency", "bias", "allowed", None])
 def test_each_alone(name):
     note(f"adjust_logits with {name} alone")
