@@ -196,8 +196,15 @@ hipError_t pad(const void* x, uint64_t stride, int64_t R, int64_t K, void* out, 
   return hipGetLastError();
 }
 
+// Bytes of the sums of K's parts of an I x J product.
+size_t sums_bytes(int64_t I, int64_t J, int64_t K, uint32_t cus) {
+  if (I < 1 || J < 1 || K < 1) return 0;
+  const ProdPlan p = plan_product(static_cast<uint64_t>(I), static_cast<uint64_t>(J), static_cast<uint64_t>(K), cus);
+  return p.parts == 1 ? 0 : align256(static_cast<size_t>(p.parts) * static_cast<size_t>(I) * static_cast<size_t>(J) * 4);
+}
+
 struct GradLayout {
-  size_t dz, part, x, w, bytes;     // offsets
+  size_t dz, part, x, w, sums, bytes;   // offsets
   uint64_t dz_stride;
   uint32_t parts;
 };
@@ -208,24 +215,56 @@ GradLayout grad_layout(int64_t M, int64_t N, int64_t K, int num_cus) {
   L.part = align256(static_cast<size_t>(M) * L.dz_stride * 2);
   L.x = L.part + align256(static_cast<size_t>(L.parts) * N * 4);
   L.w = L.x + pad_bytes(M, K);
-  L.bytes = L.w + pad_bytes(N, K);
+  L.sums = L.w + pad_bytes(N, K);
+  const uint32_t cus = static_cast<uint32_t>(num_cus);
+  const size_t dx = sums_bytes(M, K, N, cus), dw = sums_bytes(N, K, M, cus);   // (one after the other)
+  L.bytes = L.sums + (dx > dw ? dx : dw);
   return L;
 }
 
 }  // namespace
 
-size_t lin_workspace(int64_t M, int64_t N, int64_t K, int) { return pad_bytes(M, K) + pad_bytes(N, K); }
+// Each way to go about a product costs the stages of the tiles that a CU takes
+// one after the other, and the join that writes and reads the parts' sums; the
+// least is taken.  A stage is of 64 of k: 1.35 us for a tile of 256 x 256, 1.0 for
+// two of 128 x 128, 0.64 for one.
+ProdPlan plan_product(uint64_t I, uint64_t J, uint64_t K, uint32_t cus) {
+  ProdPlan best{false, 1, 0};
+  if (!I || !J || !K) return best;
+  double least = 0.0;
+  for (int large = 0; large < 2; ++large) {
+    if (large && (I <= 128 || J <= 128)) continue;
+    const uint64_t b = large ? 256 : 128, tiles = ((I + b - 1) / b) * ((J + b - 1) / b);
+    for (uint32_t parts = 1; parts <= 16; parts *= 2) {
+      const uint64_t part_k = ((K + parts - 1) / parts + 127) / 128 * 128, used = (K + part_k - 1) / part_k;
+      if (parts > 1 && (part_k < 256 || used != parts)) break;
+      const uint64_t items = tiles * parts, slots = (large ? 1 : 2) * uint64_t{cus};
+      const double stage = large ? 1.35 : items <= cus ? 0.64 : 1.0;
+      double us = static_cast<double>((items + slots - 1) / slots) * static_cast<double>(part_k / 64) * stage;
+      if (parts > 1) us += 4.0 + static_cast<double>(parts) * static_cast<double>(I) * static_cast<double>(J) * 8.0 / 6e6;
+      if ((!large && parts == 1) || us < least) {
+        least = us;
+        best = {large == 1, parts, static_cast<uint32_t>(part_k)};
+      }
+    }
+  }
+  return best;
+}
+
+size_t lin_workspace(int64_t M, int64_t N, int64_t K, int num_cus) {
+  return pad_bytes(M, K) + pad_bytes(N, K) + (M > 32 ? sums_bytes(M, N, K, static_cast<uint32_t>(num_cus)) : 0);
+}
 
 size_t lin_grad_workspace(int64_t M, int64_t N, int64_t K, int num_cus) { return grad_layout(M, N, K, num_cus).bytes; }
 
 hipError_t launch_linear(const LinCall& c, hipStream_t s) {
   ProdArgs g{static_cast<const __bf16*>(c.x), static_cast<const __bf16*>(c.w), c.x_stride, c.w_stride,
              static_cast<uint32_t>(c.M), static_cast<uint32_t>(c.N), static_cast<uint32_t>(c.K), c.bias, c.act,
-             c.out_dtype, c.residual, c.residual_stride, c.out, c.pre, 0, 0, false, false};
+             c.out_dtype, c.residual, c.residual_stride, c.out, c.pre, 0, 0, 1, 0, false, false};
   const uint32_t cus = static_cast<uint32_t>(device_cu_count());
   (void)hipGetLastError();
+  uint8_t* const ws = static_cast<uint8_t*>(c.ws);
   if (c.K % 8) {
-    uint8_t* const ws = static_cast<uint8_t*>(c.ws);
     __bf16* const x = reinterpret_cast<__bf16*>(ws);
     __bf16* const w = reinterpret_cast<__bf16*>(ws + pad_bytes(c.M, c.K));
     hipError_t e = pad(c.x, c.x_stride, c.M, c.K, x, s);
@@ -237,7 +276,8 @@ hipError_t launch_linear(const LinCall& c, hipStream_t s) {
     g.a_padded = g.b_padded = true;
   }
   if (launch_product_few(g, cus, s)) return hipGetLastError();
-  if (launch_product_along(g, cus, s)) return hipGetLastError();
+  float* const sums = reinterpret_cast<float*>(ws + pad_bytes(c.M, c.K) + pad_bytes(c.N, c.K));
+  if (launch_product_along(g, plan_product(g.I, g.J, g.K, cus), sums, cus, s)) return hipGetLastError();
   return launch_any<false, false>(g, s);
 }
 
@@ -267,7 +307,9 @@ hipError_t launch_linear_grad(const LinGradCall& c, hipStream_t s) {
     k_db_join<<<(N + kJoinCols - 1) / kJoinCols, kJoinBS, 0, s>>>(part, L.parts, N, c.db);
     e = hipGetLastError();
   }
+  float* const sums = reinterpret_cast<float*>(ws + L.sums);
   ProdArgs g{};
+  g.parts = 1;
   g.a = given ? static_cast<const __bf16*>(c.dy) : dz;
   g.as = given ? c.dy_stride : L.dz_stride;
   g.a_padded = !given;
@@ -290,14 +332,16 @@ hipError_t launch_linear_grad(const LinGradCall& c, hipStream_t s) {
     g.I = M;
     g.K = N;
     g.out = c.dx;
-    if (e == hipSuccess) e = launch_product_grad(g, false, cus, s) ? hipGetLastError() : launch_any<false, true>(g, s);
+    if (e == hipSuccess)
+      e = launch_product_grad(g, false, plan_product(M, K, N, cus), sums, cus, s) ? hipGetLastError() : launch_any<false, true>(g, s);
   }
   if (e == hipSuccess && dw) {
     other(c.x, c.x_stride, M, L.x);
     g.I = N;
     g.K = M;
     g.out = c.dw;
-    if (e == hipSuccess) e = launch_product_grad(g, true, cus, s) ? hipGetLastError() : launch_any<true, true>(g, s);
+    if (e == hipSuccess)
+      e = launch_product_grad(g, true, plan_product(N, K, M, cus), sums, cus, s) ? hipGetLastError() : launch_any<true, true>(g, s);
   }
   return e;
 }

@@ -19,6 +19,7 @@ struct ProdArgs {
   uint64_t residual_stride;
   void *out, *pre;                  // [I, J]
   uint32_t i0, j0;                  // kernel of any sizes: first row and column of this launch
+  uint32_t parts, part_k;           // tiled kernels: K in parts of part_k, their fp32 sums to out [parts, I, J]
   bool a_padded, b_padded;          // rows end in whole granules of 8, zeros past their end
 };
 
@@ -74,10 +75,20 @@ template <class F> void with_act(int act, F f) {
   else f(std::integral_constant<int, PROFK_ACT_NONE>{});
 }
 
-// The product of few rows, and the tiled one; false: these operands are not aligned as they need them.
+// How the tiled product goes about a size: tiles of 256 x 256 on a CU each, or
+// two of 128 x 128, and K in parts whose sums are joined by another kernel.
+struct ProdPlan {
+  bool large;
+  uint32_t parts, part_k;
+};
+ProdPlan plan_product(uint64_t I, uint64_t J, uint64_t K, uint32_t cus);
+
+// The product of few rows, and the tiled one; false: these operands are not
+// aligned as they need them.
 bool launch_product_few(const ProdArgs& g, uint32_t cus, hipStream_t s);                // A and B along k, I <= 32
-bool launch_product_along(const ProdArgs& g, uint32_t cus, hipStream_t s);              // A and B along k
-bool launch_product_grad(const ProdArgs& g, bool a_across, uint32_t cus, hipStream_t s); // B across k, A as said
+bool launch_product_along(ProdArgs g, const ProdPlan& p, float* sums, uint32_t cus, hipStream_t s);   // A and B along k
+bool launch_product_grad(ProdArgs g, bool a_across, const ProdPlan& p, float* sums, uint32_t cus,
+                         hipStream_t s);                                               // B across k, A as said
 
 // Operands that the tiled product takes: rows of whole 16-byte granules.  `len`
 // is the length of a row.

@@ -32,6 +32,7 @@ namespace profk {
 
 namespace {
 
+typedef float f32x4u __attribute__((ext_vector_type(4), aligned(4)));
 typedef float f32x2u __attribute__((ext_vector_type(2), aligned(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
@@ -121,6 +122,11 @@ template <bool ACROSS, int BW, int Q, int F, bool PERM, bool WHOLE> struct ProdS
       }
     }
   }
+  // on to a tile's first k, with `left` from there
+  __device__ __forceinline__ void skip(uint32_t k, uint32_t left) {
+    base += k * (ACROSS ? row_bytes : uint64_t{2});
+    K = left;
+  }
   // stage `next` of the tile to LDS
   __device__ __forceinline__ void issue(uint4* st, uint32_t next) const {
 #pragma unroll
@@ -153,9 +159,12 @@ template <bool ACROSS, int BW, int Q, int F, bool PERM, bool WHOLE> struct ProdS
   }
 };
 
-// WHOLE: K is a multiple of two stages.
-template <bool TA, bool TB, int ACT, int DT, int WM, int WN, int MI, int NJ, bool WHOLE>
+// WHOLE: K is a multiple of two stages.  SPLIT: K is taken in g.parts parts of
+// g.part_k, a whole number of two stages (the last may hold less), each a tile of
+// its own whose sums go to g.out [parts, I, J].
+template <bool TA, bool TB, int ACT, int DT, int WM, int WN, int MI, int NJ, bool WHOLE, bool SPLIT>
 __device__ __forceinline__ void prod_body(const ProdArgs& g, uint32_t tiles_i, uint32_t tiles) {
+  static_assert(!SPLIT || (!WHOLE && ACT == PROFK_ACT_NONE && DT == PROFK_F32), "sums of parts");
   using T = ProdTile<WM, WN, MI, NJ>;
   // distinct arrays, so that the compiler can tell the stage being read from
   // the one being filled
@@ -168,7 +177,8 @@ __device__ __forceinline__ void prod_body(const ProdArgs& g, uint32_t tiles_i, u
   const uint32_t tile0 = static_cast<uint32_t>(static_cast<uint64_t>(tiles) * xcd / kProdXcds) + blockIdx.x / kProdXcds;
   if (tile0 >= end) return;
   // a tile takes an even number of stages, so that each starts at the same one
-  const uint32_t stages = (g.K + 2 * kStageK - 1) / (2 * kStageK) * 2;
+  const uint32_t tile_k = SPLIT ? g.part_k : g.K, of_part = SPLIT ? tiles / g.parts : tiles;
+  const uint32_t stages = (tile_k + 2 * kStageK - 1) / (2 * kStageK) * 2;
   const uint32_t tid = threadIdx.x, lane = tid & (kWave - 1);
   const uint32_t w = __builtin_amdgcn_readfirstlane(tid / kWave);
   const uint32_t c = lane & 31, h = lane >> 5, wm = w / WN, wn = w % WN;
@@ -179,6 +189,7 @@ __device__ __forceinline__ void prod_body(const ProdArgs& g, uint32_t tiles_i, u
   sb.init(w, lane, wn * NJ * 32, g.bs, g.K);
   const uint32_t tiles_j = (g.J + T::BN - 1) / T::BN;
   auto place = [&](uint32_t tile, uint32_t& i, uint32_t& j) {
+    if (SPLIT) tile %= of_part;
     const uint32_t p = tile / (kPanel * tiles_i), rest = tile - p * (kPanel * tiles_i);
     const uint32_t width = min(kPanel, tiles_j - p * kPanel);
     i = rest / width * T::BM;
@@ -189,6 +200,11 @@ __device__ __forceinline__ void prod_body(const ProdArgs& g, uint32_t tiles_i, u
     place(tile, i, j);
     sa.start(g.a, i, g.I);
     sb.start(g.b, j, g.J);
+    if constexpr (SPLIT) {
+      const uint32_t k = tile / of_part * g.part_k;
+      sa.skip(k, g.K - k);
+      sb.skip(k, g.K - k);
+    }
   };
   uint32_t next_k = 0, next_tile = tile0;
   // (past the last tile: its last stage again)
@@ -196,7 +212,7 @@ __device__ __forceinline__ void prod_body(const ProdArgs& g, uint32_t tiles_i, u
   auto issue_b = [&](uint4* st) {
     sb.issue(st + T::kB, next_k);
     ++next_k;
-    if (WHOLE ? next_k < stages : next_k * kStageK < g.K) {
+    if (WHOLE ? next_k < stages : next_k < stages && next_k * kStageK < sa.K) {
       sa.base += sa.adv;
       sb.base += sb.adv;
     }
@@ -264,90 +280,105 @@ __device__ __forceinline__ void prod_body(const ProdArgs& g, uint32_t tiles_i, u
     place(tile, ti, tj);
     const uint32_t mw = ti + wm * MI * 32, nw = tj + wn * NJ * 32;
     const uint32_t m = mw + 4 * h, n = nw + (TB ? c : NJ * c);
-    O* const out = static_cast<O*>(g.out);
+    O* const out = static_cast<O*>(g.out) + (SPLIT ? static_cast<size_t>(tile / of_part) * g.I * g.J : 0);
+    // f(row, v) for the rows of eight of a lane's results of fragment i, from v0 on
+    auto rows = [&](auto check, int i, int v0, auto f) {
+      uint32_t first = m + i * 32;
+      // (no row's address or mask is kept through the steps)
+      asm volatile("" : "+v"(first));
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int v = v0; v < v0 + 8; ++v) {
+        const uint32_t r = first + 8 * (v / 4) + v % 4;
+        if (!decltype(check)::value || r < g.I) f(r, v);
+      }
+    };
+    auto both = [&](auto f) {
+      if (mw + MI * 32 <= g.I && nw + NJ * 32 <= g.J) f(std::false_type{});
+      else f(std::true_type{});
+    };
     if constexpr (TB) {
       // (no epilogue: a gradient) neighbouring lanes hold neighbouring columns
+      both([&](auto check) {
 #pragma unroll
-      for (int i = 0; i < MI; ++i) {
-        uint32_t first = m + i * 32;
-        asm volatile("" : "+v"(first));
-        __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-        for (int v = 0; v < 16; ++v) {
-          const uint32_t r = first + 8 * (v / 4) + v % 4;
-          O* const p = out + static_cast<size_t>(r) * g.J + n;
-          if (r < g.I) {
+        for (int q = 0; q < 2 * MI; ++q) {
+          const int i = q / 2;
+          rows(check, i, q % 2 * 8, [&](uint32_t r, int v) {
+            O* const p = out + static_cast<size_t>(r) * g.J + n;
 #pragma unroll
             for (int j = 0; j < NJ; ++j)
-              if (n + j * 32 < g.J) p[j * 32] = static_cast<O>(acc[i][j][v]);
-          }
+              if (!decltype(check)::value || n + j * 32 < g.J) p[j * 32] = static_cast<O>(acc[i][j][v]);
+          });
         }
-      }
+      });
     } else {
       float bias[NJ];
 #pragma unroll
-      for (uint32_t j = 0; j < NJ; ++j) bias[j] = g.bias && n + j < g.J ? g.bias[n + j] : 0.0f;
-      const bool whole = n + NJ <= g.J;
-      auto put_all = [&](O* p, const float (&y)[NJ]) {
-        if (whole) {
-          if constexpr (DT == PROFK_F32) {
-#pragma unroll
-            for (int j = 0; j < NJ; j += 2) *reinterpret_cast<f32x2u*>(p + j) = f32x2u{y[j], y[j + 1]};
-          } else if constexpr (NJ == 4) {
-            *reinterpret_cast<u32x2u*>(p) = u32x2u{pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3])};
-          } else {
-            *reinterpret_cast<u32u*>(p) = pack_bf16(y[0], y[1]);
-          }
-        } else {
-#pragma unroll
-          for (uint32_t j = 0; j < NJ - 1; ++j)
-            if (n + j < g.J) p[j] = static_cast<O>(y[j]);
-        }
-      };
-      if (n < g.J) {
-#pragma unroll
-        for (int i = 0; i < MI; ++i) {
-          uint32_t first = m + i * 32;
-          // (no row's address or mask is kept through the steps)
-          asm volatile("" : "+v"(first));
-          __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-          for (int v = 0; v < 16; ++v) {
-            const uint32_t r = first + 8 * (v / 4) + v % 4;
-            if (r < g.I) {
-              const size_t at = static_cast<size_t>(r) * g.J + n;
-              float z[NJ];
-#pragma unroll
-              for (int j = 0; j < NJ; ++j) z[j] = acc[i][j][v] + bias[j];
-              if (g.pre) put_all(static_cast<O*>(g.pre) + at, z);
-#pragma unroll
-              for (int j = 0; j < NJ; ++j) z[j] = act_of<ACT>(z[j]);
-              if (g.residual) {
-                const O* const q = static_cast<const O*>(g.residual) + r * g.residual_stride + n;
-                if (whole) {
-#pragma unroll
-                  for (int j = 0; j < NJ; j += 2) {
-                    if constexpr (DT == PROFK_F32) {
-                      const f32x2u u = *reinterpret_cast<const f32x2u*>(q + j);
-                      z[j] += u[0];
-                      z[j + 1] += u[1];
-                    } else {
-                      const uint32_t u = *reinterpret_cast<const u32u*>(q + j);
-                      z[j] += __uint_as_float(u << 16);
-                      z[j + 1] += __uint_as_float(u & 0xFFFF0000u);
-                    }
-                  }
-                } else {
-#pragma unroll
-                  for (uint32_t j = 0; j < NJ - 1; ++j)
-                    if (n + j < g.J) z[j] += static_cast<float>(q[j]);
-                }
-              }
-              put_all(out + at, z);
+      for (uint32_t j = 0; j < NJ; ++j) bias[j] = !SPLIT && g.bias && n + j < g.J ? g.bias[n + j] : 0.0f;
+      both([&](auto check) {
+        constexpr bool kCheck = decltype(check)::value;
+        if (kCheck && n >= g.J) return;
+        const bool whole = !kCheck || n + NJ <= g.J;
+        auto put_all = [&](O* p, const float (&y)[NJ]) {
+          if (whole) {
+            if constexpr (DT == PROFK_F32) {
+              if constexpr (NJ == 4) *reinterpret_cast<f32x4u*>(p) = f32x4u{y[0], y[1], y[2], y[3]};
+              else *reinterpret_cast<f32x2u*>(p) = f32x2u{y[0], y[1]};
+            } else if constexpr (NJ == 4) {
+              *reinterpret_cast<u32x2u*>(p) = u32x2u{pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3])};
+            } else {
+              *reinterpret_cast<u32u*>(p) = pack_bf16(y[0], y[1]);
             }
+          } else {
+#pragma unroll
+            for (uint32_t j = 0; j < NJ - 1; ++j)
+              if (n + j < g.J) p[j] = static_cast<O>(y[j]);
           }
+        };
+#pragma unroll
+        for (int h2 = 0; h2 < 2 * MI; ++h2) {
+          const int i = h2 / 2, v0 = h2 % 2 * 8;
+          // (eight rows' loads go out before the first is used)
+          float add[8][NJ];
+          if (!SPLIT && g.residual) {
+            rows(check, i, v0, [&](uint32_t r, int v) {
+              const O* const q = static_cast<const O*>(g.residual) + r * g.residual_stride + n;
+              if (whole) {
+#pragma unroll
+                for (int j = 0; j < NJ; j += 2) {
+                  if constexpr (DT == PROFK_F32) {
+                    const f32x2u u = *reinterpret_cast<const f32x2u*>(q + j);
+                    add[v - v0][j] = u[0];
+                    add[v - v0][j + 1] = u[1];
+                  } else {
+                    const uint32_t u = *reinterpret_cast<const u32u*>(q + j);
+                    add[v - v0][j] = __uint_as_float(u << 16);
+                    add[v - v0][j + 1] = __uint_as_float(u & 0xFFFF0000u);
+                  }
+                }
+              } else {
+#pragma unroll
+                for (uint32_t j = 0; j < NJ - 1; ++j) add[v - v0][j] = n + j < g.J ? static_cast<float>(q[j]) : 0.0f;
+                add[v - v0][NJ - 1] = 0.0f;
+              }
+            });
+          }
+          rows(check, i, v0, [&](uint32_t r, int v) {
+            const size_t at = static_cast<size_t>(r) * g.J + n;
+            float z[NJ];
+#pragma unroll
+            for (int j = 0; j < NJ; ++j) z[j] = acc[i][j][v] + bias[j];
+            if (!SPLIT && g.pre) put_all(static_cast<O*>(g.pre) + at, z);
+#pragma unroll
+            for (int j = 0; j < NJ; ++j) z[j] = act_of<ACT>(z[j]);
+            if (!SPLIT && g.residual) {
+#pragma unroll
+              for (int j = 0; j < NJ; ++j) z[j] += add[v - v0][j];
+            }
+            put_all(out + at, z);
+          });
         }
-      }
+      });
     }
   };
   start(tile0);
@@ -393,33 +424,85 @@ __device__ __forceinline__ void prod_body(const ProdArgs& g, uint32_t tiles_i, u
   prod_wait<0>();   // (no load may reach LDS after the workgroup's end)
 }
 
-template <bool TA, bool TB, int ACT, int DT, int WM, int WN, int MI, int NJ, int WAVES, bool WHOLE>
+template <bool TA, bool TB, int ACT, int DT, int WM, int WN, int MI, int NJ, int WAVES, bool WHOLE, bool SPLIT>
 __global__ __launch_bounds__(WM * WN * 64, WAVES) void k_prod(ProdArgs g, uint32_t tiles_i, uint32_t tiles) {
-  prod_body<TA, TB, ACT, DT, WM, WN, MI, NJ, WHOLE>(g, tiles_i, tiles);
+  prod_body<TA, TB, ACT, DT, WM, WN, MI, NJ, WHOLE, SPLIT>(g, tiles_i, tiles);
 }
 
 // PER: workgroups a CU holds.
-template <bool TA, bool TB, int ACT, int DT, int WM, int WN, int MI, int NJ, int PER>
+template <bool TA, bool TB, int ACT, int DT, int WM, int WN, int MI, int NJ, int PER, bool SPLIT>
 void launch_tiles(const ProdArgs& g, uint32_t cus, hipStream_t s) {
   using T = ProdTile<WM, WN, MI, NJ>;
-  const uint32_t ti = (g.I + T::BM - 1) / T::BM, tj = (g.J + T::BN - 1) / T::BN, tiles = ti * tj;
+  const uint32_t ti = (g.I + T::BM - 1) / T::BM, tj = (g.J + T::BN - 1) / T::BN, tiles = ti * tj * (SPLIT ? g.parts : 1);
   uint32_t grid = (tiles + kProdXcds - 1) / kProdXcds * kProdXcds;
   if (grid > PER * cus) grid = PER * cus / kProdXcds * kProdXcds;
   constexpr int kWaves = PER * WM * WN / 4;
-  if (g.K % (2 * kStageK) == 0) k_prod<TA, TB, ACT, DT, WM, WN, MI, NJ, kWaves, true><<<grid, T::BS, 0, s>>>(g, ti, tiles);
-  else k_prod<TA, TB, ACT, DT, WM, WN, MI, NJ, kWaves, false><<<grid, T::BS, 0, s>>>(g, ti, tiles);
+  if constexpr (SPLIT) {
+    k_prod<TA, TB, ACT, DT, WM, WN, MI, NJ, kWaves, false, true><<<grid, T::BS, 0, s>>>(g, ti, tiles);
+  } else if (g.K % (2 * kStageK) == 0) {
+    k_prod<TA, TB, ACT, DT, WM, WN, MI, NJ, kWaves, true, false><<<grid, T::BS, 0, s>>>(g, ti, tiles);
+  } else {
+    k_prod<TA, TB, ACT, DT, WM, WN, MI, NJ, kWaves, false, false><<<grid, T::BS, 0, s>>>(g, ti, tiles);
+  }
 }
 
-// Tiles of 256 x 256 where every CU has one, else two workgroups a CU of 128 x 128.
-template <bool TA, bool TB, int ACT, int DT> void launch_shape(const ProdArgs& g, uint32_t cus, hipStream_t s) {
-  const uint64_t large = static_cast<uint64_t>((g.I + 255) / 256) * ((g.J + 255) / 256);
-  if (g.I > 128 && large >= cus) launch_tiles<TA, TB, ACT, DT, 4, 2, 2, 4, 1>(g, cus, s);
-  else launch_tiles<TA, TB, ACT, DT, 2, 2, 2, 2, 2>(g, cus, s);
+template <bool TA, bool TB, int ACT, int DT, bool SPLIT>
+void launch_shape(const ProdArgs& g, const ProdPlan& p, uint32_t cus, hipStream_t s) {
+  if (p.large) launch_tiles<TA, TB, ACT, DT, 4, 2, 2, 4, 1, SPLIT>(g, cus, s);
+  else launch_tiles<TA, TB, ACT, DT, 2, 2, 2, 2, 2, SPLIT>(g, cus, s);
 }
 
 // Tiles are counted in 32 bits.
 inline bool tiles_fit(const ProdArgs& g) {
   return static_cast<uint64_t>((g.I + 127) / 128) * ((g.J + 127) / 128) < (uint64_t{1} << 31);
+}
+
+// The sums of K's parts, in their order, with the epilogue: 8 neighbours a
+// thread.
+template <int DT, int ACT> __global__ __launch_bounds__(256) void k_prod_join(ProdArgs g, const float* sums) {
+  const uint32_t per = (g.J + 7) / 8;
+  const uint64_t n = static_cast<uint64_t>(g.I) * per, size = static_cast<uint64_t>(g.I) * g.J;
+  for (uint64_t t = blockIdx.x * uint64_t{256} + threadIdx.x; t < n; t += gridDim.x * uint64_t{256}) {
+    const uint32_t i = static_cast<uint32_t>(t / per), j = static_cast<uint32_t>(t % per) * 8;
+    const uint64_t at = static_cast<uint64_t>(i) * g.J;
+    float z[8], v[8];
+    load8<PROFK_F32>(sums + at, j, g.J, z);
+    for (uint32_t p = 1; p < g.parts; ++p) {
+      load8<PROFK_F32>(sums + p * size + at, j, g.J, v);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) z[e] += v[e];
+    }
+    if (g.bias) {
+      load8<PROFK_F32>(g.bias, j, g.J, v);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) z[e] += v[e];
+    }
+    using O = std::conditional_t<DT == PROFK_F32, float, __bf16>;
+    if (g.pre) store8<DT>(static_cast<O*>(g.pre) + at, j, g.J, z);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) z[e] = act_of<ACT>(z[e]);
+    if (g.residual) {
+      load8<DT>(static_cast<const O*>(g.residual) + i * g.residual_stride, j, g.J, v);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) z[e] += v[e];
+    }
+    store8<DT>(static_cast<O*>(g.out) + at, j, g.J, z);
+  }
+}
+
+template <bool TA, bool TB, int ACT, int DT>
+void launch_planned(ProdArgs g, const ProdPlan& p, float* sums, uint32_t cus, hipStream_t s) {
+  if (p.parts == 1) {
+    launch_shape<TA, TB, ACT, DT, false>(g, p, cus, s);
+    return;
+  }
+  g.parts = p.parts;
+  g.part_k = p.part_k;
+  ProdArgs part = g;
+  part.out = sums;
+  launch_shape<TA, TB, PROFK_ACT_NONE, PROFK_F32, true>(part, p, cus, s);
+  const uint64_t blocks = (static_cast<uint64_t>(g.I) * ((g.J + 7) / 8) + 255) / 256;
+  k_prod_join<DT, ACT><<<blocks < 8192 ? static_cast<uint32_t>(blocks) : 8192, 256, 0, s>>>(g, sums);
 }
 
 }  // namespace
