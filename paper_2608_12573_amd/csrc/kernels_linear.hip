@@ -226,8 +226,10 @@ GradLayout grad_layout(int64_t M, int64_t N, int64_t K, int num_cus) {
 
 // Each way to go about a product costs the stages of the tiles that a CU takes
 // one after the other, and the join that writes and reads the parts' sums; the
-// least is taken.  A stage is of 64 of k: 1.35 us for a tile of 256 x 256, 1.0 for
-// two of 128 x 128, 0.64 for one.
+// least is taken.  A stage is of 64 of k: 1.5 us for a tile of 256 x 256, 0.95 for
+// two of 128 x 128, 0.55 for one (measured with K of 4096 and more; the choices are
+// close: 4096 x 12288 by 2048 takes 193 us as two parts with their join, 197 as
+// small tiles).
 ProdPlan plan_product(uint64_t I, uint64_t J, uint64_t K, uint32_t cus) {
   ProdPlan best{false, 1, 0};
   if (!I || !J || !K) return best;
@@ -239,7 +241,7 @@ ProdPlan plan_product(uint64_t I, uint64_t J, uint64_t K, uint32_t cus) {
       const uint64_t part_k = ((K + parts - 1) / parts + 127) / 128 * 128, used = (K + part_k - 1) / part_k;
       if (parts > 1 && (part_k < 256 || used != parts)) break;
       const uint64_t items = tiles * parts, slots = (large ? 1 : 2) * uint64_t{cus};
-      const double stage = large ? 1.35 : items <= cus ? 0.64 : 1.0;
+      const double stage = large ? 1.5 : items <= cus ? 0.55 : 0.95;
       double us = static_cast<double>((items + slots - 1) / slots) * static_cast<double>(part_k / 64) * stage;
       if (parts > 1) us += 4.0 + static_cast<double>(parts) * static_cast<double>(I) * static_cast<double>(J) * 8.0 / 6e6;
       if ((!large && parts == 1) || us < least) {

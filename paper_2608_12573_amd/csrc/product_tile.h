@@ -251,14 +251,17 @@ __device__ __forceinline__ void prod_body(const ProdArgs& g, uint32_t tiles_i, u
 #pragma unroll
     for (int i = 0; i < MI; ++i)
 #pragma unroll
-      for (int j = 0; j < NJ; ++j) asm volatile("" : "+v"(acc[i][j]));
+      for (int j = 0; j < NJ; ++j) {
+        if constexpr (MI * NJ == 16) asm volatile("" : "+a"(acc[i][j]));
+        else asm volatile("" : "+v"(acc[i][j]));
+      }
   };
   // LDS reads and loads between the matrix instructions of a quarter: the first
   // one waits for the reads before, and loads issued one after the other keep
   // the wave from its matrix instructions while they are taken
   constexpr int kReads = MI * (TA ? 2 : 1) + NJ * (TB ? 2 : 1);
-  auto weave = [&]() {
-    constexpr int M = MI * NJ, per = (kReads + M - 2) / (M - 1);
+  auto weave = [&](auto reads) {
+    constexpr int M = MI * NJ, per = (decltype(reads)::value + M - 2) / (M - 1);
     pin();
 #pragma unroll
     for (int i = 0; i < M; ++i) {
@@ -381,43 +384,49 @@ __device__ __forceinline__ void prod_body(const ProdArgs& g, uint32_t tiles_i, u
       });
     }
   };
+  using R0 = std::integral_constant<int, 0>;
+  using R1 = std::integral_constant<int, kReads>;
+  using R2 = std::integral_constant<int, 2 * kReads>;
   start(tile0);
   issue_a(s0);
   issue_b(s0);
   issue_a(s1);
-  Frag f0, f1;
-  prod_wait<T::QA>();
+  issue_b(s1);
+  Frag f0, f1, f2;
+  prod_wait<T::QA + T::QB>();
   prod_barrier();
   rd(s0, 0, f0);
-  // One stage; its first quarter's fragments are in f0, and the loads of a for
-  // the next have been issued.
-  auto stage = [&](uint4* cur, uint4* nxt, auto last) {
+  // One stage; its first quarter's fragments are in fa.  Its last two are read
+  // under the second, so that all waves are done with its part of LDS half way, and
+  // the loads of the stage after the next have a stage and a quarter to arrive.
+  auto stage = [&](uint4* cur, uint4* nxt, Frag& fa, Frag& fb, auto last) {
     __builtin_amdgcn_sched_barrier(0);
-    issue_b(nxt);
-    rd(cur, 1, f1);
-    mma(f0);
-    weave();
-    rd(cur, 2, f0);
-    mma(f1);
-    weave();
+    rd(cur, 1, fb);
+    mma(fa);
+    weave(R1{});
+    rd(cur, 2, fa);
+    rd(cur, 3, f2);
+    mma(fb);
+    weave(R2{});
     if (decltype(last)::value) turn();
-    rd(cur, 3, f1);
-    mma(f0);
-    weave();
-    // this wave has read its stage and its loads of the next have arrived; by
-    // the barrier, so have the others
-    prod_wait<0>();
+    prod_wait<63>();
     prod_barrier();
     issue_a(cur);
-    rd(nxt, 0, f0);
-    mma(f1);
-    weave();
+    mma(fa);
+    weave(R0{});
+    // the next stage has arrived
+    prod_wait<T::QA>();
+    prod_barrier();
+    issue_b(cur);
+    rd(nxt, 0, fb);
+    mma(f2);
+    weave(R1{});
   };
   for (uint32_t tile = tile0; tile < end; tile += per_xcd) {
     clear();
     for (uint32_t k = 0; k < stages; k += 2) {
-      stage(s0, s1, std::true_type{});     // (loads the tile's next odd stage)
-      stage(s1, s0, std::false_type{});
+      stage(s0, s1, f0, f1, std::true_type{});
+      stage(s1, s0, f1, f0, std::false_type{});
     }
     store(tile);
   }
