@@ -8,6 +8,8 @@
 //   y_v = u_v - [c_v > 0] presence - c_v frequency + bias_v, or -inf where the
 //         row's mask forbids v
 //   dx_v = dy_v (1 / repetition, repetition or 1), or 0 where it is forbidden.
+// The division is a product with repetition's reciprocal, rounded to fp32: 1.5
+// units in the last place at most.
 //
 // A workgroup takes a piece of a row.  It counts the history's tokens that fall
 // into its piece in LDS, a word a token (integer atomics: their order changes
@@ -25,7 +27,7 @@ namespace {
 constexpr uint32_t kAdjPrompt = 0x80000000u, kAdjBias = 0x40000000u;
 constexpr uint32_t kAdjList = 256;             // biases of a piece that are kept in LDS
 constexpr uint32_t kAdjChunks = 2;             // of 8 elements, of a thread
-constexpr uint32_t kAdjMaxPiece = 8192;        // elements (LDS: a word each)
+constexpr uint32_t kAdjPiece = 8192;           // most elements of a piece (LDS: a word each)
 
 __device__ __forceinline__ int64_t clamp64(int64_t x, int64_t lo, int64_t hi) { return x < lo ? lo : x > hi ? hi : x; }
 
@@ -48,22 +50,42 @@ template <int DT, bool GRAD> __global__ __launch_bounds__(512) void k_adjust(Adj
   const char* const x = static_cast<const char*>(a.x) + (row * a.stride + v0) * ES;
   const char* const src = GRAD ? static_cast<const char*>(a.dy) + (row * a.dy_stride + v0) * ES : x;
   char* const out = static_cast<char*>(a.out) + (row * a.out_stride + v0) * ES;
-  // the piece, loaded under the search of the lists
-  Raw8<DT> raw[kAdjChunks];
-#pragma unroll
-  for (uint32_t q = 0; q < kAdjChunks; ++q) raw[q] = load_raw8<DT>(src, (q * BS + tid) * 8, n);
+  const uint32_t* words = nullptr;
+  bool lost = false;                 // the row names a mask that is not there
+  if (a.allowed) {
+    const int64_t k = a.mask ? a.mask[row] : a.n_masks == 1 ? 0 : row;
+    lost = k >= a.n_masks;
+    if (k >= 0 && !lost) words = a.allowed + static_cast<uint64_t>(k) * a.allowed_stride;
+  }
   const bool hist = h1 > h0, bias = b1 > b0;
+  const int64_t made = h0 + (a.n_prompt && hist ? clamp64(a.n_prompt[row], 0, h1 - h0) : 0);
+  const float rep = a.repetition ? a.repetition[row] : 1.0f, inv = 1.0f / rep;
+  const float pres = !GRAD && a.presence ? a.presence[row] : 0.0f;
+  const float freq = !GRAD && a.frequency ? a.frequency[row] : 0.0f;
+  // the piece and its part of the mask, and the first of the lists, loaded
+  // together (a piece starts at a multiple of 32 tokens)
+  Raw8<DT> raw[kAdjChunks];
+  uint32_t ok[kAdjChunks];
+#pragma unroll
+  for (uint32_t q = 0; q < kAdjChunks; ++q) {
+    const uint32_t i = (q * BS + tid) * 8;
+    raw[q] = load_raw8<DT>(src, i, n);
+    ok[q] = words && i < n ? words[(v0 + i) / 32] >> (i % 32) : 0xFFu;
+  }
+  // (four tokens at a time: a load waits for none before it)
+  int64_t tok[4];
+  auto load_tokens = [&](int64_t i) {
+#pragma unroll
+    for (uint32_t q = 0; q < 4; ++q) tok[q] = i + q * BS < h1 ? a.tokens[i + q * BS] : -1;
+  };
+  load_tokens(h0 + tid);
+  int64_t id = b0 + tid < b1 ? a.bias_ids[b0 + tid] : -1;
   __shared__ uint32_t s_n, s_tok[kAdjList], s_at[kAdjList];
   if (hist || bias) {
     for (uint32_t i = tid * 4; i < a.piece; i += BS * 4) *reinterpret_cast<u32x4*>(s_word + i) = u32x4{};
     if (tid == 0) s_n = 0;
     __syncthreads();
-    const int64_t made = h0 + (a.n_prompt && hist ? clamp64(a.n_prompt[row], 0, h1 - h0) : 0);
-    // (four tokens at a time: a load waits for none before it)
     for (int64_t i = h0 + tid; i < h1; i += 4 * BS) {
-      int64_t tok[4];
-#pragma unroll
-      for (uint32_t q = 0; q < 4; ++q) tok[q] = i + q * BS < h1 ? a.tokens[i + q * BS] : -1;
 #pragma unroll
       for (uint32_t q = 0; q < 4; ++q) {
         const uint64_t v = static_cast<uint64_t>(tok[q]) - v0;
@@ -72,10 +94,11 @@ template <int DT, bool GRAD> __global__ __launch_bounds__(512) void k_adjust(Adj
           else atomicAdd(s_word + v, 1u);
         }
       }
+      load_tokens(i + 4 * BS);
     }
     for (int64_t i = b0 + tid; i < b1; i += BS) {
-      const uint64_t v = static_cast<uint64_t>(a.bias_ids[i]) - v0;
-      if (v < n) {
+      const uint64_t v = static_cast<uint64_t>(id) - v0;
+      if (id >= 0 && v < n) {
         atomicOr(s_word + v, kAdjBias);
         const uint32_t k = atomicAdd(&s_n, 1u);
         if (k < kAdjList) {
@@ -83,6 +106,7 @@ template <int DT, bool GRAD> __global__ __launch_bounds__(512) void k_adjust(Adj
           s_at[k] = static_cast<uint32_t>(i - b0);
         }
       }
+      id = i + BS < b1 ? a.bias_ids[i + BS] : -1;
     }
     __syncthreads();
   }
@@ -98,46 +122,35 @@ template <int DT, bool GRAD> __global__ __launch_bounds__(512) void k_adjust(Adj
     }
     return a.bias_values[b0 + at];
   };
-  const uint32_t* words = nullptr;
-  bool lost = false;                 // the row names a mask that is not there
-  if (a.allowed) {
-    const int64_t k = a.mask ? a.mask[row] : a.n_masks == 1 ? 0 : row;
-    lost = k >= a.n_masks;
-    if (k >= 0 && !lost) words = a.allowed + static_cast<uint64_t>(k) * a.allowed_stride;
-  }
-  const float rep = a.repetition ? a.repetition[row] : 1.0f;
-  const float pres = !GRAD && a.presence ? a.presence[row] : 0.0f;
-  const float freq = !GRAD && a.frequency ? a.frequency[row] : 0.0f;
-  const float nan = __builtin_nanf("");
 #pragma unroll
   for (uint32_t q = 0; q < kAdjChunks; ++q) {
     const uint32_t i = (q * BS + tid) * 8;
     if (i >= n) return;
     float y[8];
     to_f32<DT>(raw[q], y);
-    // (a piece starts at a multiple of 32 tokens)
-    const uint32_t ok = words ? words[(v0 + i) / 32] >> (i % 32) : 0xFFu;
-    // (the words past the row's end stay 0)
-    u32x4 c4[2] = {};
     if (hist || bias) {
-      c4[0] = *reinterpret_cast<const u32x4*>(s_word + i);
-      c4[1] = *reinterpret_cast<const u32x4*>(s_word + i + 4);
+      // (the words past the row's end stay 0)
+      const u32x4 c4[2] = {*reinterpret_cast<const u32x4*>(s_word + i), *reinterpret_cast<const u32x4*>(s_word + i + 4)};
+#pragma unroll
+      for (uint32_t e = 0; e < 8; ++e) {
+        const uint32_t c = c4[e / 4][e % 4];
+        if (c & ~kAdjBias) {
+          if constexpr (GRAD) {
+            y[e] *= load1(x, i + e, DT) > 0.0f ? inv : rep;
+          } else {
+            y[e] *= y[e] > 0.0f ? inv : rep;
+            const uint32_t m = c & ~(kAdjPrompt | kAdjBias);
+            y[e] -= m ? fmaf(static_cast<float>(m), freq, pres) : 0.0f;
+          }
+        }
+        if (!GRAD && (c & kAdjBias)) y[e] += bias_of(i + e);
+      }
     }
 #pragma unroll
-    for (uint32_t e = 0; e < 8; ++e) {
-      const uint32_t c = c4[e / 4][e % 4];
-      if (c & ~kAdjBias) {
-        if constexpr (GRAD) {
-          if (a.repetition) y[e] = load1(x, i + e, DT) > 0.0f ? y[e] / rep : y[e] * rep;
-        } else {
-          if (a.repetition) y[e] = y[e] > 0.0f ? y[e] / rep : y[e] * rep;
-          const uint32_t m = c & ~(kAdjPrompt | kAdjBias);
-          if (m) y[e] -= fmaf(static_cast<float>(m), freq, pres);
-        }
-      }
-      if (!GRAD && (c & kAdjBias)) y[e] += bias_of(i + e);
-      if (!(ok >> e & 1)) y[e] = GRAD ? 0.0f : -__builtin_inff();
-      if (lost) y[e] = nan;
+    for (uint32_t e = 0; e < 8; ++e) y[e] = ok[q] >> e & 1 ? y[e] : GRAD ? 0.0f : -__builtin_inff();
+    if (lost) {
+#pragma unroll
+      for (uint32_t e = 0; e < 8; ++e) y[e] = __builtin_nanf("");
     }
     store8<DT>(out, i, n, y);
   }
@@ -148,14 +161,16 @@ template <int DT, bool GRAD> __global__ __launch_bounds__(512) void k_adjust(Adj
 hipError_t launch_adjust(AdjustArgs a, int dtype, int64_t T, hipStream_t s) {
   const uint32_t cus = static_cast<uint32_t>(device_cu_count());
   // pieces of whole words of the mask; more of them where the rows are few
-  uint32_t piece = kAdjMaxPiece;
+  uint32_t piece = kAdjPiece;
   while (piece > 1024 && static_cast<uint64_t>(T) * ((a.V + piece - 1) / piece) < 2 * cus) piece /= 2;
   if (a.V < piece) piece = (a.V + 31) / 32 * 32;
   a.piece = piece;
   a.pieces = (a.V + piece - 1) / piece;
+  // threads for the piece, and no fewer than go through an average history in one
+  // step
+  const int64_t history = a.tokens ? a.n_tokens / T : 0;
   uint32_t bs = 512;
-  // (no fewer threads than go through an average history in one step)
-  while (bs > 64 && bs * 8 * kAdjChunks >= 2 * piece && (!a.tokens || bs * 4 >= 2 * (a.n_tokens / T))) bs /= 2;
+  while (bs > 64 && bs * 8 * kAdjChunks >= 2 * piece && bs * 4 >= 2 * history) bs /= 2;
   const uint32_t lds = a.tokens || (!a.dy && a.bias_ids) ? piece * 4 : 0;
   const int64_t step = ((int64_t{1} << 31) - 1) / bs / a.pieces < 1 ? 1 : ((int64_t{1} << 31) - 1) / bs / a.pieces;
   (void)hipGetLastError();
