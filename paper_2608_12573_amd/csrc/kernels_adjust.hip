@@ -38,14 +38,19 @@ template <int DT, bool GRAD> __global__ __launch_bounds__(512) void k_adjust(Adj
   constexpr uint32_t ES = DT == PROFK_F32 ? 4 : 2;
   const uint32_t tid = threadIdx.x, BS = blockDim.x;
   // (a list's offsets may be anything: none reaches past the list)
-  int64_t h0 = 0, h1 = 0, b0 = 0, b1 = 0;
+  const int64_t *tokens = nullptr, *ids = nullptr;
+  const float* values = nullptr;
+  uint32_t n_hist = 0, n_bias = 0;
   if (a.tokens) {
-    h0 = clamp64(a.offsets[row], 0, a.n_tokens);
-    h1 = clamp64(a.offsets[row + 1], h0, a.n_tokens);
+    const int64_t h0 = clamp64(a.offsets[row], 0, a.n_tokens);
+    n_hist = static_cast<uint32_t>(clamp64(a.offsets[row + 1], h0, a.n_tokens) - h0);
+    tokens = a.tokens + h0;
   }
   if (!GRAD && a.bias_ids) {
-    b0 = clamp64(a.bias_offsets[row], 0, a.n_bias);
-    b1 = clamp64(a.bias_offsets[row + 1], b0, a.n_bias);
+    const int64_t b0 = clamp64(a.bias_offsets[row], 0, a.n_bias);
+    n_bias = static_cast<uint32_t>(clamp64(a.bias_offsets[row + 1], b0, a.n_bias) - b0);
+    ids = a.bias_ids + b0;
+    values = a.bias_values + b0;
   }
   const char* const x = static_cast<const char*>(a.x) + (row * a.stride + v0) * ES;
   const char* const src = GRAD ? static_cast<const char*>(a.dy) + (row * a.dy_stride + v0) * ES : x;
@@ -57,8 +62,8 @@ template <int DT, bool GRAD> __global__ __launch_bounds__(512) void k_adjust(Adj
     lost = k >= a.n_masks;
     if (k >= 0 && !lost) words = a.allowed + static_cast<uint64_t>(k) * a.allowed_stride;
   }
-  const bool hist = h1 > h0, bias = b1 > b0;
-  const int64_t made = h0 + (a.n_prompt && hist ? clamp64(a.n_prompt[row], 0, h1 - h0) : 0);
+  const bool lists = n_hist || n_bias;
+  const uint32_t made = a.n_prompt && n_hist ? static_cast<uint32_t>(clamp64(a.n_prompt[row], 0, n_hist)) : 0;
   const float rep = a.repetition ? a.repetition[row] : 1.0f, inv = 1.0f / rep;
   const float pres = !GRAD && a.presence ? a.presence[row] : 0.0f;
   const float freq = !GRAD && a.frequency ? a.frequency[row] : 0.0f;
@@ -74,53 +79,55 @@ template <int DT, bool GRAD> __global__ __launch_bounds__(512) void k_adjust(Adj
   }
   // (four tokens at a time: a load waits for none before it)
   int64_t tok[4];
-  auto load_tokens = [&](int64_t i) {
+  auto load_tokens = [&](uint32_t i) {
 #pragma unroll
-    for (uint32_t q = 0; q < 4; ++q) tok[q] = i + q * BS < h1 ? a.tokens[i + q * BS] : -1;
+    for (uint32_t q = 0; q < 4; ++q) tok[q] = i + q * BS < n_hist ? tokens[i + q * BS] : -1;
   };
-  load_tokens(h0 + tid);
-  int64_t id = b0 + tid < b1 ? a.bias_ids[b0 + tid] : -1;
+  // an entry's place in the piece, n or more where it has none
+  auto in_piece = [&](int64_t v) { return v >> 32 == 0 ? static_cast<uint32_t>(v) - v0 : ~0u; };
+  load_tokens(tid);
+  int64_t id = tid < n_bias ? ids[tid] : -1;
   __shared__ uint32_t s_n, s_tok[kAdjList], s_at[kAdjList];
-  if (hist || bias) {
+  if (lists) {
     for (uint32_t i = tid * 4; i < a.piece; i += BS * 4) *reinterpret_cast<u32x4*>(s_word + i) = u32x4{};
     if (tid == 0) s_n = 0;
     __syncthreads();
-    for (int64_t i = h0 + tid; i < h1; i += 4 * BS) {
+    for (uint32_t i = tid; i < n_hist; i += 4 * BS) {
 #pragma unroll
       for (uint32_t q = 0; q < 4; ++q) {
-        const uint64_t v = static_cast<uint64_t>(tok[q]) - v0;
-        if (tok[q] >= 0 && v < n) {
+        const uint32_t v = in_piece(tok[q]);
+        if (v < n) {
           if (i + q * BS < made) atomicOr(s_word + v, kAdjPrompt);
           else atomicAdd(s_word + v, 1u);
         }
       }
       load_tokens(i + 4 * BS);
     }
-    for (int64_t i = b0 + tid; i < b1; i += BS) {
-      const uint64_t v = static_cast<uint64_t>(id) - v0;
-      if (id >= 0 && v < n) {
+    for (uint32_t i = tid; i < n_bias; i += BS) {
+      const uint32_t v = in_piece(id);
+      if (v < n) {
         atomicOr(s_word + v, kAdjBias);
         const uint32_t k = atomicAdd(&s_n, 1u);
         if (k < kAdjList) {
-          s_tok[k] = static_cast<uint32_t>(v);
-          s_at[k] = static_cast<uint32_t>(i - b0);
+          s_tok[k] = v;
+          s_at[k] = i;
         }
       }
-      id = i + BS < b1 ? a.bias_ids[i + BS] : -1;
+      id = i + BS < n_bias ? ids[i + BS] : -1;
     }
     __syncthreads();
   }
   // the last bias of token v of the piece: from the list in LDS, whose order may
   // be any, or, where that did not hold them all, from the row's
   auto bias_of = [&](uint32_t v) {
-    int64_t at = -1;
+    uint32_t at = 0;
     if (s_n <= kAdjList) {
       for (uint32_t k = 0; k < s_n; ++k)
-        if (s_tok[k] == v && static_cast<int64_t>(s_at[k]) > at) at = s_at[k];
+        if (s_tok[k] == v && s_at[k] > at) at = s_at[k];
     } else {
-      for (at = b1 - b0 - 1; a.bias_ids[b0 + at] != static_cast<int64_t>(v0) + v;) --at;
+      for (at = n_bias - 1; in_piece(ids[at]) != v;) --at;
     }
-    return a.bias_values[b0 + at];
+    return values[at];
   };
 #pragma unroll
   for (uint32_t q = 0; q < kAdjChunks; ++q) {
@@ -128,7 +135,7 @@ template <int DT, bool GRAD> __global__ __launch_bounds__(512) void k_adjust(Adj
     if (i >= n) return;
     float y[8];
     to_f32<DT>(raw[q], y);
-    if (hist || bias) {
+    if (lists) {
       // (the words past the row's end stay 0)
       const u32x4 c4[2] = {*reinterpret_cast<const u32x4*>(s_word + i), *reinterpret_cast<const u32x4*>(s_word + i + 4)};
 #pragma unroll
