@@ -15,7 +15,7 @@
 // into its piece in LDS, a word a token (integer atomics: their order changes
 // nothing), lists the biases of its tokens, and streams the piece once.  Every piece reads the whole history again, from the caches.
 #include "adjust.h"
-#include "elem8.h"
+#include "elems.h"
 #include "launch.h"
 
 namespace profk {
@@ -26,7 +26,7 @@ namespace {
 // the prompt.
 constexpr uint32_t kAdjPrompt = 0x80000000u, kAdjBias = 0x40000000u;
 constexpr uint32_t kAdjList = 256;             // biases of a piece that are kept in LDS
-constexpr uint32_t kAdjChunks = 2;             // of 8 elements, of a thread
+constexpr uint32_t kAdjElems = 16;             // of a thread, 16 bytes at a time
 constexpr uint32_t kAdjPiece = 8192;           // most elements of a piece (LDS: a word each)
 
 __device__ __forceinline__ int64_t clamp64(int64_t x, int64_t lo, int64_t hi) { return x < lo ? lo : x > hi ? hi : x; }
@@ -36,6 +36,7 @@ template <int DT, bool GRAD> __global__ __launch_bounds__(512) void k_adjust(Adj
   const uint32_t row = a.row + blockIdx.x / a.pieces, p = blockIdx.x % a.pieces;
   const uint32_t v0 = p * a.piece, n = min(a.piece, a.V - v0);
   constexpr uint32_t ES = DT == PROFK_F32 ? 4 : 2;
+  constexpr int E = 16 / ES, C = kAdjElems / E;
   const uint32_t tid = threadIdx.x, BS = blockDim.x;
   // (a list's offsets may be anything: none reaches past the list)
   const int64_t *tokens = nullptr, *ids = nullptr;
@@ -69,12 +70,12 @@ template <int DT, bool GRAD> __global__ __launch_bounds__(512) void k_adjust(Adj
   const float freq = !GRAD && a.frequency ? a.frequency[row] : 0.0f;
   // the piece and its part of the mask, and the first of the lists, loaded
   // together (a piece starts at a multiple of 32 tokens)
-  Raw8<DT> raw[kAdjChunks];
-  uint32_t ok[kAdjChunks];
+  Raw<DT, E> raw[C];
+  uint32_t ok[C];
 #pragma unroll
-  for (uint32_t q = 0; q < kAdjChunks; ++q) {
-    const uint32_t i = (q * BS + tid) * 8;
-    raw[q] = load_raw8<DT>(src, i, n);
+  for (uint32_t q = 0; q < C; ++q) {
+    const uint32_t i = (q * BS + tid) * E;
+    raw[q] = load_raw<DT, E>(src, i, n);
     ok[q] = words && i < n ? words[(v0 + i) / 32] >> (i % 32) : 0xFFu;
   }
   // (four tokens at a time: a load waits for none before it)
@@ -129,37 +130,59 @@ template <int DT, bool GRAD> __global__ __launch_bounds__(512) void k_adjust(Adj
     }
     return values[at];
   };
+  // (the words past the row's end stay 0)
+  auto words_of = [&](uint32_t i, uint32_t (&c)[E]) {
 #pragma unroll
-  for (uint32_t q = 0; q < kAdjChunks; ++q) {
-    const uint32_t i = (q * BS + tid) * 8;
+    for (uint32_t w = 0; w < E; w += 4) {
+      const u32x4 c4 = lists && i < n ? *reinterpret_cast<const u32x4*>(s_word + i + w) : u32x4{};
+#pragma unroll
+      for (uint32_t e = 0; e < 4; ++e) c[w + e] = c4[e];
+    }
+  };
+  // the gradient needs the logits of the history's tokens alone: all of a thread's
+  // are on their way before the first is used
+  float seen[C][E];
+  if constexpr (GRAD) {
+#pragma unroll
+    for (uint32_t q = 0; q < C; ++q) {
+      const uint32_t i = (q * BS + tid) * E;
+      uint32_t c[E];
+      words_of(i, c);
+#pragma unroll
+      for (uint32_t e = 0; e < E; ++e) {
+        seen[q][e] = 0.0f;
+        if (c[e]) seen[q][e] = load1(x, i + e, DT);
+      }
+    }
+  }
+#pragma unroll
+  for (uint32_t q = 0; q < C; ++q) {
+    const uint32_t i = (q * BS + tid) * E;
     if (i >= n) return;
-    float y[8];
-    to_f32<DT>(raw[q], y);
-    if (lists) {
-      // (the words past the row's end stay 0)
-      const u32x4 c4[2] = {*reinterpret_cast<const u32x4*>(s_word + i), *reinterpret_cast<const u32x4*>(s_word + i + 4)};
+    float y[E];
+    to_f32<DT, E>(raw[q], y);
+    uint32_t c[E];
+    words_of(i, c);
 #pragma unroll
-      for (uint32_t e = 0; e < 8; ++e) {
-        const uint32_t c = c4[e / 4][e % 4];
-        if (c & ~kAdjBias) {
-          if constexpr (GRAD) {
-            y[e] *= load1(x, i + e, DT) > 0.0f ? inv : rep;
-          } else {
-            y[e] *= y[e] > 0.0f ? inv : rep;
-            const uint32_t m = c & ~(kAdjPrompt | kAdjBias);
-            y[e] -= m ? fmaf(static_cast<float>(m), freq, pres) : 0.0f;
-          }
+    for (uint32_t e = 0; e < E; ++e) {
+      if constexpr (GRAD) {
+        y[e] *= c[e] ? (seen[q][e] > 0.0f ? inv : rep) : 1.0f;
+      } else {
+        if (c[e] & ~kAdjBias) {
+          y[e] *= y[e] > 0.0f ? inv : rep;
+          const uint32_t m = c[e] & ~(kAdjPrompt | kAdjBias);
+          y[e] -= m ? fmaf(static_cast<float>(m), freq, pres) : 0.0f;
         }
-        if (!GRAD && (c & kAdjBias)) y[e] += bias_of(i + e);
+        if (c[e] & kAdjBias) y[e] += bias_of(i + e);
       }
     }
 #pragma unroll
-    for (uint32_t e = 0; e < 8; ++e) y[e] = ok[q] >> e & 1 ? y[e] : GRAD ? 0.0f : -__builtin_inff();
+    for (uint32_t e = 0; e < E; ++e) y[e] = ok[q] >> e & 1 ? y[e] : GRAD ? 0.0f : -__builtin_inff();
     if (lost) {
 #pragma unroll
-      for (uint32_t e = 0; e < 8; ++e) y[e] = __builtin_nanf("");
+      for (uint32_t e = 0; e < E; ++e) y[e] = __builtin_nanf("");
     }
-    store8<DT>(out, i, n, y);
+    store<DT, E>(out, i, n, y);
   }
 }
 
@@ -177,7 +200,7 @@ hipError_t launch_adjust(AdjustArgs a, int dtype, int64_t T, hipStream_t s) {
   // step
   const int64_t history = a.tokens ? a.n_tokens / T : 0;
   uint32_t bs = 512;
-  while (bs > 64 && bs * 8 * kAdjChunks >= 2 * piece && bs * 4 >= 2 * history) bs /= 2;
+  while (bs > 64 && bs * kAdjElems >= 2 * piece && bs * 4 >= 2 * history) bs /= 2;
   const uint32_t lds = a.tokens || (!a.dy && a.bias_ids) ? piece * 4 : 0;
   const int64_t step = ((int64_t{1} << 31) - 1) / bs / a.pieces < 1 ? 1 : ((int64_t{1} << 31) - 1) / bs / a.pieces;
   (void)hipGetLastError();

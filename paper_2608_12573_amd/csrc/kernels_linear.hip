@@ -33,7 +33,7 @@ constexpr uint32_t kAnyB = 128, kAnyK = 32, kAnyRow = 40;
 
 // 8 neighbours in memory, those from `left` on 0.
 __device__ __forceinline__ u32x4 load_part8(const __bf16* p, uint32_t left) {
-  return load_raw8<PROFK_BF16>(p, 0, left).q[0];
+  return __builtin_bit_cast(u32x4, load_raw<PROFK_BF16, 8>(p, 0, left));
 }
 
 template <bool ACROSS> struct AnyTile {
@@ -145,17 +145,17 @@ template <int DT, int ACT> __global__ __launch_bounds__(256) void k_dz(DzArgs a)
   const uint32_t r1 = static_cast<uint32_t>(static_cast<uint64_t>(a.M) * (p + 1) / a.parts);
   float sum[8] = {}, d[8], z[8];
   for (uint32_t r = r0; r < r1; ++r) {
-    load8<DT>(static_cast<const char*>(a.dy) + r * a.dy_stride * ES, j, a.N, d);
+    load<DT, 8>(static_cast<const char*>(a.dy) + r * a.dy_stride * ES, j, a.N, d);
     if constexpr (ACT != PROFK_ACT_NONE) {
-      load8<DT>(static_cast<const char*>(a.pre) + static_cast<uint64_t>(r) * a.N * ES, j, a.N, z);
+      load<DT, 8>(static_cast<const char*>(a.pre) + static_cast<uint64_t>(r) * a.N * ES, j, a.N, z);
 #pragma unroll
       for (int e = 0; e < 8; ++e) d[e] *= slope_of<ACT>(z[e]);
     }
 #pragma unroll
     for (int e = 0; e < 8; ++e) sum[e] += d[e];
-    if (a.dz) store8<PROFK_BF16>(a.dz + r * a.dz_stride, j, static_cast<uint32_t>(a.dz_stride), d);   // (0 past N)
+    if (a.dz) store<PROFK_BF16, 8>(a.dz + r * a.dz_stride, j, static_cast<uint32_t>(a.dz_stride), d);   // (0 past N)
   }
-  if (a.part) store8<PROFK_F32>(a.part + static_cast<size_t>(p) * a.N, j, a.N, sum);
+  if (a.part) store<PROFK_F32, 8>(a.part + static_cast<size_t>(p) * a.N, j, a.N, sum);
 }
 
 __global__ __launch_bounds__(kJoinBS) void k_db_join(const float* part, uint32_t parts, uint32_t N, float* db) {
@@ -185,7 +185,7 @@ __global__ __launch_bounds__(256) void k_pad(PadArgs a) {
   const uint64_t n = static_cast<uint64_t>(a.R[m]) * per;
   for (uint64_t i = blockIdx.x * uint64_t{256} + threadIdx.x; i < n; i += gridDim.x * uint64_t{256}) {
     const uint32_t r = static_cast<uint32_t>(i / per), k = static_cast<uint32_t>(i % per) * 8;
-    reinterpret_cast<u32x4*>(a.out[m])[i] = load_raw8<PROFK_BF16>(a.x[m] + r * a.stride[m], k, a.K).q[0];
+    reinterpret_cast<u32x4*>(a.out[m])[i] = __builtin_bit_cast(u32x4, load_raw<PROFK_BF16, 8>(a.x[m] + r * a.stride[m], k, a.K));
   }
 }
 

@@ -13,7 +13,7 @@
 // which takes out of g its parts along 1 and along n, and over the rows
 //   dw = sum dy n,  db = sum dy.
 // All in fp32; every output is rounded once.
-#include "elem8.h"
+#include "elems.h"
 #include "join.h"
 #include "launch.h"
 #include "norm.h"
@@ -52,16 +52,28 @@ __device__ __forceinline__ float row_rstd(float sq, float d, float eps) {
   return 1.0f / sqrtf((var < 0.0f ? 0.0f : var) + eps);
 }
 
-__device__ __forceinline__ void load_param8(const void* p, int dtype, uint32_t i, uint32_t D, float none, float (&v)[8]) {
+template <int E>
+__device__ __forceinline__ void load_param(const void* p, int dtype, uint32_t i, uint32_t D, float none, float (&v)[E]) {
   if (!p) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = none;
+    for (int e = 0; e < E; ++e) v[e] = none;
   } else if (dtype == PROFK_F32) {
-    load8<PROFK_F32>(p, i, D, v);
+    if constexpr (E == 8) {
+      float lo[4], hi[4];
+      load<PROFK_F32, 4>(p, i, D, lo);
+      load<PROFK_F32, 4>(p, i + 4, D, hi);
+#pragma unroll
+      for (int e = 0; e < E; ++e) v[e] = e < 4 ? lo[e % 4] : hi[e % 4];
+    } else {
+      load<PROFK_F32, E>(p, i, D, v);
+    }
   } else {
-    load8<PROFK_BF16>(p, i, D, v);
+    load<PROFK_BF16, E>(p, i, D, v);
   }
 }
+
+// Elements of one of a thread's accesses.
+template <int XDT, int YDT> constexpr int kElems = XDT == PROFK_F32 || YDT == PROFK_F32 ? 4 : 8;
 
 template <int DT> __device__ __forceinline__ const void* row_at(const void* x, uint64_t stride, uint32_t r) {
   return static_cast<const char*>(x) + r * stride * (DT == PROFK_F32 ? 4 : 2);
@@ -70,47 +82,53 @@ template <int DT> __device__ __forceinline__ void* row_at(void* x, uint64_t stri
   return static_cast<char*>(x) + r * stride * (DT == PROFK_F32 ? 4 : 2);
 }
 
-// A row in the registers of GS threads, C chunks of 8 elements each, R rows a
+template <int E> __device__ __forceinline__ void store_sums(float* row, uint32_t i, uint32_t D, const float (&v)[E]) {
+#pragma unroll
+  for (int k = 0; k < E; k += 4) store<PROFK_F32, 4>(row, i + k, D, {v[k], v[k + 1], v[k + 2], v[k + 3]});
+}
+
+// A row in the registers of GS threads, C8 times 8 elements each, R rows a
 // workgroup; workgroups go through the rows, the scale and shift kept in
 // registers and the next row loaded under this one.
-template <int XDT, int YDT, int GS, int R, int C> __global__ __launch_bounds__(GS * R) void k_norm(NormArgs a) {
+template <int XDT, int YDT, int GS, int R, int C8> __global__ __launch_bounds__(GS * R) void k_norm(NormArgs a) {
   constexpr uint32_t BS = GS * R;
+  constexpr int E = kElems<XDT, YDT>, C = C8 * 8 / E;
   static_assert(GS == kWave || R == 1, "a row that is left out meets no barrier");
   __shared__ float s_red[BS / kWave][1], s_sq[BS / kWave][2];
   const uint32_t t = threadIdx.x % GS;
   const uint32_t step = gridDim.x * R;
   uint32_t row = blockIdx.x * R + threadIdx.x / GS;
   if (row >= a.T) return;      // (a whole wave, or the workgroup)
-  float w[C][8], b[C][8];
-  Raw8<XDT> next[C];
+  float w[C][E], b[C][E];
+  Raw<XDT, E> next[C];
 #pragma unroll
-  for (int c = 0; c < C; ++c) next[c] = load_raw8<XDT>(row_at<XDT>(a.x, a.stride, row), (c * GS + t) * 8, a.D);
+  for (int c = 0; c < C; ++c) next[c] = load_raw<XDT, E>(row_at<XDT>(a.x, a.stride, row), (c * GS + t) * E, a.D);
 #pragma unroll
   for (int c = 0; c < C; ++c) {
-    load_param8(a.w, a.p_dtype, (c * GS + t) * 8, a.D, 1.0f, w[c]);
-    load_param8(a.b, a.p_dtype, (c * GS + t) * 8, a.D, 0.0f, b[c]);
+    load_param(a.w, a.p_dtype, (c * GS + t) * E, a.D, 1.0f, w[c]);
+    load_param(a.b, a.p_dtype, (c * GS + t) * E, a.D, 0.0f, b[c]);
   }
   const float inv = 1.0f / static_cast<float>(a.D);
   for (; row < a.T; row += step) {
-    float v[C][8], s[1] = {0.0f};
+    float v[C][E], s[1] = {0.0f};
 #pragma unroll
     for (int c = 0; c < C; ++c) {
-      to_f32<XDT>(next[c], v[c]);
+      to_f32<XDT, E>(next[c], v[c]);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) s[0] += v[c][e];
+      for (int e = 0; e < E; ++e) s[0] += v[c][e];
     }
     if (a.T - row > step) {
 #pragma unroll
-      for (int c = 0; c < C; ++c) next[c] = load_raw8<XDT>(row_at<XDT>(a.x, a.stride, row + step), (c * GS + t) * 8, a.D);
+      for (int c = 0; c < C; ++c) next[c] = load_raw<XDT, E>(row_at<XDT>(a.x, a.stride, row + step), (c * GS + t) * E, a.D);
     }
     row_sum<GS>(s, s_red);
     const float m = s[0] * inv;
     float q[2] = {0.0f, 0.0f};
 #pragma unroll
     for (int c = 0; c < C; ++c) {
-      const uint32_t i = (c * GS + t) * 8;
+      const uint32_t i = (c * GS + t) * E;
 #pragma unroll
-      for (uint32_t e = 0; e < 8; ++e) {
+      for (uint32_t e = 0; e < E; ++e) {
         v[c][e] = i + e < a.D ? v[c][e] - m : 0.0f;
         q[0] += v[c][e];
         q[1] = fmaf(v[c][e], v[c][e], q[1]);
@@ -121,10 +139,10 @@ template <int XDT, int YDT, int GS, int R, int C> __global__ __launch_bounds__(G
     void* const out = row_at<YDT>(a.out, a.out_stride, row);
 #pragma unroll
     for (int c = 0; c < C; ++c) {
-      float y[8];
+      float y[E];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) y[e] = fmaf((v[c][e] - d) * r, w[c][e], b[c][e]);
-      store8<YDT>(out, (c * GS + t) * 8, a.D, y);
+      for (int e = 0; e < E; ++e) y[e] = fmaf((v[c][e] - d) * r, w[c][e], b[c][e]);
+      store<YDT, E>(out, (c * GS + t) * E, a.D, y);
     }
     if (t == 0) {
       if (a.mean) a.mean[row] = m + d;
@@ -137,23 +155,24 @@ template <int XDT, int YDT, int GS, int R, int C> __global__ __launch_bounds__(G
 // from the caches.
 template <int XDT, int YDT> __global__ __launch_bounds__(1024) void k_norm_long(NormArgs a) {
   constexpr uint32_t BS = 1024;
+  constexpr int E = kElems<XDT, YDT>;
   __shared__ float s_red[BS / kWave][1], s_sq[BS / kWave][2];
   const float inv = 1.0f / static_cast<float>(a.D);
   for (uint32_t row = blockIdx.x; row < a.T; row += gridDim.x) {
     const void* const x = row_at<XDT>(a.x, a.stride, row);
-    float s[1] = {0.0f}, v[8];
-    for (uint32_t i = threadIdx.x * 8; i < a.D; i += BS * 8) {
-      load8<XDT>(x, i, a.D, v);
+    float s[1] = {0.0f}, v[E];
+    for (uint32_t i = threadIdx.x * E; i < a.D; i += BS * E) {
+      load<XDT, E>(x, i, a.D, v);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) s[0] += v[e];
+      for (int e = 0; e < E; ++e) s[0] += v[e];
     }
     row_sum<BS>(s, s_red);
     const float m = s[0] * inv;
     float q[2] = {0.0f, 0.0f};
-    for (uint32_t i = threadIdx.x * 8; i < a.D; i += BS * 8) {
-      load8<XDT>(x, i, a.D, v);
+    for (uint32_t i = threadIdx.x * E; i < a.D; i += BS * E) {
+      load<XDT, E>(x, i, a.D, v);
 #pragma unroll
-      for (uint32_t e = 0; e < 8; ++e) {
+      for (uint32_t e = 0; e < E; ++e) {
         const float c = i + e < a.D ? v[e] - m : 0.0f;
         q[0] += c;
         q[1] = fmaf(c, c, q[1]);
@@ -162,14 +181,14 @@ template <int XDT, int YDT> __global__ __launch_bounds__(1024) void k_norm_long(
     row_sum<BS>(q, s_sq);
     const float d = q[0] * inv, r = row_rstd(q[1] * inv, d, a.eps);
     void* const out = row_at<YDT>(a.out, a.out_stride, row);
-    for (uint32_t i = threadIdx.x * 8; i < a.D; i += BS * 8) {
-      float w[8], b[8];
-      load8<XDT>(x, i, a.D, v);
-      load_param8(a.w, a.p_dtype, i, a.D, 1.0f, w);
-      load_param8(a.b, a.p_dtype, i, a.D, 0.0f, b);
+    for (uint32_t i = threadIdx.x * E; i < a.D; i += BS * E) {
+      float w[E], b[E];
+      load<XDT, E>(x, i, a.D, v);
+      load_param(a.w, a.p_dtype, i, a.D, 1.0f, w);
+      load_param(a.b, a.p_dtype, i, a.D, 0.0f, b);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] = fmaf((v[e] - m - d) * r, w[e], b[e]);
-      store8<YDT>(out, i, a.D, v);
+      for (int e = 0; e < E; ++e) v[e] = fmaf((v[e] - m - d) * r, w[e], b[e]);
+      store<YDT, E>(out, i, a.D, v);
     }
     if (threadIdx.x == 0) {
       if (a.mean) a.mean[row] = m + d;
@@ -181,23 +200,24 @@ template <int XDT, int YDT> __global__ __launch_bounds__(1024) void k_norm_long(
 // The gradients of rows in registers: one sum of two numbers a row, and the sums
 // of dy n and dy over a thread's rows kept in registers until its end, when the
 // workgroup's R rows of threads are added.
-template <int XDT, int YDT, int GS, int R, int C> __global__ __launch_bounds__(GS * R) void k_norm_grad(NormGradArgs a) {
+template <int XDT, int YDT, int GS, int R, int C8> __global__ __launch_bounds__(GS * R) void k_norm_grad(NormGradArgs a) {
   constexpr uint32_t BS = GS * R;
+  constexpr int E = kElems<XDT, YDT>, C = C8 * 8 / E;
   __shared__ float s_red[2][BS / kWave][2];
-  __shared__ float s_sum[R > 1 ? 2 * GS * C * 8 : 1];
+  __shared__ float s_sum[R > 1 ? 2 * GS * C * E : 1];
   const uint32_t t = threadIdx.x % GS, sub = threadIdx.x / GS;
   const uint32_t step = gridDim.x * R;
-  float w[C][8], dw[C][8] = {}, db[C][8] = {};
-  Raw8<XDT> nx[C];
-  Raw8<YDT> ny[C];
+  float w[C][E], dw[C][E] = {}, db[C][E] = {};
+  Raw<XDT, E> nx[C];
+  Raw<YDT, E> ny[C];
   float nm, nr;
   // (a row that is not there has a gradient of 0)
   auto load = [&](uint32_t r) {
     const uint32_t D = r < a.T ? a.D : 0;
 #pragma unroll
     for (int c = 0; c < C; ++c) {
-      nx[c] = load_raw8<XDT>(row_at<XDT>(a.x, a.stride, r), (c * GS + t) * 8, D);
-      ny[c] = load_raw8<YDT>(row_at<YDT>(a.dy, a.dy_stride, r), (c * GS + t) * 8, D);
+      nx[c] = load_raw<XDT, E>(row_at<XDT>(a.x, a.stride, r), (c * GS + t) * E, D);
+      ny[c] = load_raw<YDT, E>(row_at<YDT>(a.dy, a.dy_stride, r), (c * GS + t) * E, D);
     }
     nm = D ? a.mean[r] : 0.0f;
     nr = D ? a.rstd[r] : 0.0f;
@@ -205,19 +225,19 @@ template <int XDT, int YDT, int GS, int R, int C> __global__ __launch_bounds__(G
   uint32_t row0 = blockIdx.x * R;
   load(row0 + sub);
 #pragma unroll
-  for (int c = 0; c < C; ++c) load_param8(a.w, a.p_dtype, (c * GS + t) * 8, a.D, 1.0f, w[c]);
+  for (int c = 0; c < C; ++c) load_param(a.w, a.p_dtype, (c * GS + t) * E, a.D, 1.0f, w[c]);
   const float inv = 1.0f / static_cast<float>(a.D);
   uint32_t slot = 0;
   for (; row0 < a.T; row0 += step, slot ^= 1) {
     const uint32_t row = row0 + sub;
-    float n[C][8], g[C][8], s[2] = {0.0f, 0.0f};
+    float n[C][E], g[C][E], s[2] = {0.0f, 0.0f};
     const float m = nm, r = nr;
 #pragma unroll
     for (int c = 0; c < C; ++c) {
-      to_f32<XDT>(nx[c], n[c]);
-      to_f32<YDT>(ny[c], g[c]);
+      to_f32<XDT, E>(nx[c], n[c]);
+      to_f32<YDT, E>(ny[c], g[c]);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
+      for (int e = 0; e < E; ++e) {
         // (past the row's end dy is 0)
         n[c][e] = (n[c][e] - m) * r;
         dw[c][e] = fmaf(g[c][e], n[c][e], dw[c][e]);
@@ -237,8 +257,8 @@ template <int XDT, int YDT, int GS, int R, int C> __global__ __launch_bounds__(G
 #pragma unroll
         for (int c = 0; c < C; ++c) {
 #pragma unroll
-          for (int e = 0; e < 8; ++e) g[c][e] = r * (g[c][e] - s[0] - n[c][e] * s[1]);
-          store8<XDT>(out, (c * GS + t) * 8, a.D, g[c]);
+          for (int e = 0; e < E; ++e) g[c][e] = r * (g[c][e] - s[0] - n[c][e] * s[1]);
+          store<XDT, E>(out, (c * GS + t) * E, a.D, g[c]);
         }
       }
     }
@@ -252,10 +272,10 @@ template <int XDT, int YDT, int GS, int R, int C> __global__ __launch_bounds__(G
 #pragma unroll
         for (int c = 0; c < C; ++c)
 #pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            const uint32_t i = (c * 8 + e) * GS + t;
+          for (int e = 0; e < E; ++e) {
+            const uint32_t i = (c * E + e) * GS + t;
             s_sum[i] = k > 1 ? s_sum[i] + dw[c][e] : dw[c][e];
-            s_sum[GS * C * 8 + i] = k > 1 ? s_sum[GS * C * 8 + i] + db[c][e] : db[c][e];
+            s_sum[GS * C * E + i] = k > 1 ? s_sum[GS * C * E + i] + db[c][e] : db[c][e];
           }
       }
       __syncthreads();
@@ -264,15 +284,15 @@ template <int XDT, int YDT, int GS, int R, int C> __global__ __launch_bounds__(G
 #pragma unroll
     for (int c = 0; c < C; ++c)
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        dw[c][e] += s_sum[(c * 8 + e) * GS + t];
-        db[c][e] += s_sum[GS * C * 8 + (c * 8 + e) * GS + t];
+      for (int e = 0; e < E; ++e) {
+        dw[c][e] += s_sum[(c * E + e) * GS + t];
+        db[c][e] += s_sum[GS * C * E + (c * E + e) * GS + t];
       }
   }
 #pragma unroll
   for (int c = 0; c < C; ++c) {
-    store8<PROFK_F32>(part, (c * GS + t) * 8, a.D, dw[c]);
-    store8<PROFK_F32>(part + a.D, (c * GS + t) * 8, a.D, db[c]);
+    store_sums<E>(part, (c * GS + t) * E, a.D, dw[c]);
+    store_sums<E>(part + a.D, (c * GS + t) * E, a.D, db[c]);
   }
 }
 
@@ -280,6 +300,7 @@ template <int XDT, int YDT, int GS, int R, int C> __global__ __launch_bounds__(G
 // workgroups of 2048 columns and a part of the rows.
 template <int XDT, int YDT> __global__ __launch_bounds__(1024) void k_norm_grad_long(NormGradArgs a) {
   constexpr uint32_t BS = 1024;
+  constexpr int E = kElems<XDT, YDT>;
   __shared__ float s_red[2][BS / kWave][2];
   const float inv = 1.0f / static_cast<float>(a.D);
   uint32_t slot = 0;
@@ -288,13 +309,13 @@ template <int XDT, int YDT> __global__ __launch_bounds__(1024) void k_norm_grad_
     const void* const dy = row_at<YDT>(a.dy, a.dy_stride, row);
     void* const out = row_at<XDT>(a.dx, a.dx_stride, row);
     const float m = a.mean[row], r = a.rstd[row];
-    float s[2] = {0.0f, 0.0f}, n[8], g[8], w[8];
-    for (uint32_t i = threadIdx.x * 8; i < a.D; i += BS * 8) {
-      load8<XDT>(x, i, a.D, n);
-      load8<YDT>(dy, i, a.D, g);
-      load_param8(a.w, a.p_dtype, i, a.D, 1.0f, w);
+    float s[2] = {0.0f, 0.0f}, n[E], g[E], w[E];
+    for (uint32_t i = threadIdx.x * E; i < a.D; i += BS * E) {
+      load<XDT, E>(x, i, a.D, n);
+      load<YDT, E>(dy, i, a.D, g);
+      load_param(a.w, a.p_dtype, i, a.D, 1.0f, w);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
+      for (int e = 0; e < E; ++e) {
         const float q = g[e] * w[e];
         s[0] += q;
         s[1] = fmaf(q, (n[e] - m) * r, s[1]);
@@ -303,37 +324,38 @@ template <int XDT, int YDT> __global__ __launch_bounds__(1024) void k_norm_grad_
     row_sum<BS>(s, s_red[slot]);
     s[0] *= inv;
     s[1] *= inv;
-    for (uint32_t i = threadIdx.x * 8; i < a.D; i += BS * 8) {
-      load8<XDT>(x, i, a.D, n);
-      load8<YDT>(dy, i, a.D, g);
-      load_param8(a.w, a.p_dtype, i, a.D, 1.0f, w);
+    for (uint32_t i = threadIdx.x * E; i < a.D; i += BS * E) {
+      load<XDT, E>(x, i, a.D, n);
+      load<YDT, E>(dy, i, a.D, g);
+      load_param(a.w, a.p_dtype, i, a.D, 1.0f, w);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) g[e] = r * (g[e] * w[e] - s[0] - (n[e] - m) * r * s[1]);
-      store8<XDT>(out, i, a.D, g);
+      for (int e = 0; e < E; ++e) g[e] = r * (g[e] * w[e] - s[0] - (n[e] - m) * r * s[1]);
+      store<XDT, E>(out, i, a.D, g);
     }
   }
 }
 
 template <int XDT, int YDT> __global__ __launch_bounds__(256) void k_norm_cols(NormGradArgs a) {
-  const uint32_t i = (blockIdx.x * 256 + threadIdx.x) * 8;
+  constexpr int E = kElems<XDT, YDT>;
+  const uint32_t i = (blockIdx.x * 256 + threadIdx.x) * E;
   if (i >= a.D) return;
   const uint32_t p = blockIdx.y;
   const uint32_t r0 = static_cast<uint32_t>(static_cast<uint64_t>(a.T) * p / a.parts);
   const uint32_t r1 = static_cast<uint32_t>(static_cast<uint64_t>(a.T) * (p + 1) / a.parts);
-  float dw[8] = {}, db[8] = {}, n[8], g[8];
+  float dw[E] = {}, db[E] = {}, n[E], g[E];
   for (uint32_t row = r0; row < r1; ++row) {
-    load8<XDT>(row_at<XDT>(a.x, a.stride, row), i, a.D, n);
-    load8<YDT>(row_at<YDT>(a.dy, a.dy_stride, row), i, a.D, g);
+    load<XDT, E>(row_at<XDT>(a.x, a.stride, row), i, a.D, n);
+    load<YDT, E>(row_at<YDT>(a.dy, a.dy_stride, row), i, a.D, g);
     const float m = a.mean[row], r = a.rstd[row];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
+    for (int e = 0; e < E; ++e) {
       dw[e] = fmaf(g[e], (n[e] - m) * r, dw[e]);
       db[e] += g[e];
     }
   }
   float* const part = a.part + static_cast<size_t>(p) * 2 * a.D;
-  store8<PROFK_F32>(part, i, a.D, dw);
-  store8<PROFK_F32>(part + a.D, i, a.D, db);
+  store_sums<E>(part, i, a.D, dw);
+  store_sums<E>(part + a.D, i, a.D, db);
 }
 
 // The parts' sums to dw and db.
@@ -384,7 +406,7 @@ template <int XDT, int YDT> void norm_rows(const NormArgs& a, uint32_t cus, hipS
 template <int XDT, int YDT> void norm_grad_rows(const NormGradArgs& a, uint32_t cus, hipStream_t s) {
   if (a.D > kBlockD) {
     if (a.dx && a.T) k_norm_grad_long<XDT, YDT><<<a.T < 2 * cus ? a.T : 2 * cus, 1024, 0, s>>>(a);
-    if (a.part) k_norm_cols<XDT, YDT><<<dim3((a.D + 2047) / 2048, a.parts), 256, 0, s>>>(a);
+    if (a.part) k_norm_cols<XDT, YDT><<<dim3((a.D + 256 * kElems<XDT, YDT> - 1) / (256 * kElems<XDT, YDT>), a.parts), 256, 0, s>>>(a);
     return;
   }
   with_shape(a.D, [&](auto gs, auto c) {

@@ -3,7 +3,7 @@
 // kernels_linear.hip).
 #pragma once
 
-#include "elem8.h"
+#include "elems.h"
 
 namespace profk {
 

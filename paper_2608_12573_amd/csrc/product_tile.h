@@ -475,27 +475,27 @@ template <int DT, int ACT> __global__ __launch_bounds__(256) void k_prod_join(Pr
     const uint32_t i = static_cast<uint32_t>(t / per), j = static_cast<uint32_t>(t % per) * 8;
     const uint64_t at = static_cast<uint64_t>(i) * g.J;
     float z[8], v[8];
-    load8<PROFK_F32>(sums + at, j, g.J, z);
+    load<PROFK_F32, 8>(sums + at, j, g.J, z);
     for (uint32_t p = 1; p < g.parts; ++p) {
-      load8<PROFK_F32>(sums + p * size + at, j, g.J, v);
+      load<PROFK_F32, 8>(sums + p * size + at, j, g.J, v);
 #pragma unroll
       for (int e = 0; e < 8; ++e) z[e] += v[e];
     }
     if (g.bias) {
-      load8<PROFK_F32>(g.bias, j, g.J, v);
+      load<PROFK_F32, 8>(g.bias, j, g.J, v);
 #pragma unroll
       for (int e = 0; e < 8; ++e) z[e] += v[e];
     }
     using O = std::conditional_t<DT == PROFK_F32, float, __bf16>;
-    if (g.pre) store8<DT>(static_cast<O*>(g.pre) + at, j, g.J, z);
+    if (g.pre) store<DT, 8>(static_cast<O*>(g.pre) + at, j, g.J, z);
 #pragma unroll
     for (int e = 0; e < 8; ++e) z[e] = act_of<ACT>(z[e]);
     if (g.residual) {
-      load8<DT>(static_cast<const O*>(g.residual) + i * g.residual_stride, j, g.J, v);
+      load<DT, 8>(static_cast<const O*>(g.residual) + i * g.residual_stride, j, g.J, v);
 #pragma unroll
       for (int e = 0; e < 8; ++e) z[e] += v[e];
     }
-    store8<DT>(static_cast<O*>(g.out) + at, j, g.J, z);
+    store<DT, 8>(static_cast<O*>(g.out) + at, j, g.J, z);
   }
 }
 
