@@ -12,8 +12,19 @@
 // units in the last place at most.
 //
 // A workgroup takes a piece of a row.  It counts the history's tokens that fall
-// into its piece in LDS, a word a token (integer atomics: their order changes
-// nothing), lists the biases of its tokens, and streams the piece once.  Every piece reads the whole history again, from the caches.
+// into its piece in LDS (integer atomics: their order changes nothing), lists the
+// biases of its tokens, and streams the piece once, 64 bytes a thread, loaded
+// under the search of the lists.  Every piece reads the whole history again, from
+// the caches.  The piece in flight is what hides the search, so the table must not
+// limit the workgroups of a CU: it has 16 bits a token, a flag for the prompt, one
+// for a bias and 14 of count.  (With 32, 256 x 131072 bf16 with histories of up to
+// 4096 took 43 us, its inputs not in the caches.)  Rows with longer histories than
+// 14 bits count take their piece in two halves, 32 bits a token.
+//
+// The gradient needs no counts, but the sign of the history's logits, which it
+// reads when it comes upon their tokens and notes beside the flag.
+#include <type_traits>
+
 #include "adjust.h"
 #include "elems.h"
 #include "launch.h"
@@ -22,21 +33,23 @@ namespace profk {
 
 namespace {
 
-// Of a token's word: it is in the prompt, it has a bias; the rest counts it after
-// the prompt.
-constexpr uint32_t kAdjPrompt = 0x80000000u, kAdjBias = 0x40000000u;
+// Of a token's word, in its upper half where it has 32 bits: it is in the prompt
+// (of the gradient: in the history); it has a bias (its logit is above 0).
+constexpr uint32_t kAdjSeen = 0x8000u, kAdjBias = 0x4000u, kAdjCount = 0x3FFFu;
 constexpr uint32_t kAdjList = 256;             // biases of a piece that are kept in LDS
-constexpr uint32_t kAdjElems = 16;             // of a thread, 16 bytes at a time
-constexpr uint32_t kAdjPiece = 8192;           // most elements of a piece (LDS: a word each)
+constexpr uint32_t kAdjBytes = 64;             // of a thread's elements, 16 at a time
+constexpr uint32_t kAdjBS = 512;               // most threads
+
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
 __device__ __forceinline__ int64_t clamp64(int64_t x, int64_t lo, int64_t hi) { return x < lo ? lo : x > hi ? hi : x; }
 
-template <int DT, bool GRAD> __global__ __launch_bounds__(512) void k_adjust(AdjustArgs a) {
-  extern __shared__ __align__(16) uint32_t s_word[];     // [piece]
+template <int DT, bool GRAD> __global__ __launch_bounds__(kAdjBS) void k_adjust(AdjustArgs a) {
+  extern __shared__ __align__(16) uint32_t s_word[];     // 16 bits for each element of the threads
   const uint32_t row = a.row + blockIdx.x / a.pieces, p = blockIdx.x % a.pieces;
   const uint32_t v0 = p * a.piece, n = min(a.piece, a.V - v0);
   constexpr uint32_t ES = DT == PROFK_F32 ? 4 : 2;
-  constexpr int E = 16 / ES, C = kAdjElems / E;
+  constexpr int E = 16 / ES, C = kAdjBytes / 16;
   const uint32_t tid = threadIdx.x, BS = blockDim.x;
   // (a list's offsets may be anything: none reaches past the list)
   const int64_t *tokens = nullptr, *ids = nullptr;
@@ -89,35 +102,6 @@ template <int DT, bool GRAD> __global__ __launch_bounds__(512) void k_adjust(Adj
   load_tokens(tid);
   int64_t id = tid < n_bias ? ids[tid] : -1;
   __shared__ uint32_t s_n, s_tok[kAdjList], s_at[kAdjList];
-  if (lists) {
-    for (uint32_t i = tid * 4; i < a.piece; i += BS * 4) *reinterpret_cast<u32x4*>(s_word + i) = u32x4{};
-    if (tid == 0) s_n = 0;
-    __syncthreads();
-    for (uint32_t i = tid; i < n_hist; i += 4 * BS) {
-#pragma unroll
-      for (uint32_t q = 0; q < 4; ++q) {
-        const uint32_t v = in_piece(tok[q]);
-        if (v < n) {
-          if (i + q * BS < made) atomicOr(s_word + v, kAdjPrompt);
-          else atomicAdd(s_word + v, 1u);
-        }
-      }
-      load_tokens(i + 4 * BS);
-    }
-    for (uint32_t i = tid; i < n_bias; i += BS) {
-      const uint32_t v = in_piece(id);
-      if (v < n) {
-        atomicOr(s_word + v, kAdjBias);
-        const uint32_t k = atomicAdd(&s_n, 1u);
-        if (k < kAdjList) {
-          s_tok[k] = v;
-          s_at[k] = i;
-        }
-      }
-      id = i + BS < n_bias ? ids[i + BS] : -1;
-    }
-    __syncthreads();
-  }
   // the last bias of token v of the piece: from the list in LDS, whose order may
   // be any, or, where that did not hold them all, from the row's
   auto bias_of = [&](uint32_t v) {
@@ -130,59 +114,120 @@ template <int DT, bool GRAD> __global__ __launch_bounds__(512) void k_adjust(Adj
     }
     return values[at];
   };
-  // (the words past the row's end stay 0)
-  auto words_of = [&](uint32_t i, uint32_t (&c)[E]) {
+  // f(token's place, its new flags or count): to the table of the places from lo on
+  auto search = [&](auto wide, uint32_t lo, uint32_t len) {
+    constexpr bool kWide = decltype(wide)::value;
+    auto at_word = [&](uint32_t v) { return s_word + (kWide ? v : v / 2); };
+    auto flag = [&](uint32_t v, uint32_t f) { return kWide ? f << 16 : f << (v & 1) * 16; };
+    for (uint32_t i = tid * 4; i < BS * (kAdjBytes / ES) / 2; i += BS * 4) *reinterpret_cast<u32x4*>(s_word + i) = u32x4{};
+    if (tid == 0) s_n = 0;
+    __syncthreads();
+    for (uint32_t i = tid; i < n_hist; i += 4 * BS) {
+      uint32_t v[4];
+      [[maybe_unused]] float z[4];
 #pragma unroll
-    for (uint32_t w = 0; w < E; w += 4) {
-      const u32x4 c4 = lists && i < n ? *reinterpret_cast<const u32x4*>(s_word + i + w) : u32x4{};
-#pragma unroll
-      for (uint32_t e = 0; e < 4; ++e) c[w + e] = c4[e];
-    }
-  };
-  // the gradient needs the logits of the history's tokens alone: all of a thread's
-  // are on their way before the first is used
-  float seen[C][E];
-  if constexpr (GRAD) {
-#pragma unroll
-    for (uint32_t q = 0; q < C; ++q) {
-      const uint32_t i = (q * BS + tid) * E;
-      uint32_t c[E];
-      words_of(i, c);
-#pragma unroll
-      for (uint32_t e = 0; e < E; ++e) {
-        seen[q][e] = 0.0f;
-        if (c[e]) seen[q][e] = load1(x, i + e, DT);
-      }
-    }
-  }
-#pragma unroll
-  for (uint32_t q = 0; q < C; ++q) {
-    const uint32_t i = (q * BS + tid) * E;
-    if (i >= n) return;
-    float y[E];
-    to_f32<DT, E>(raw[q], y);
-    uint32_t c[E];
-    words_of(i, c);
-#pragma unroll
-    for (uint32_t e = 0; e < E; ++e) {
-      if constexpr (GRAD) {
-        y[e] *= c[e] ? (seen[q][e] > 0.0f ? inv : rep) : 1.0f;
-      } else {
-        if (c[e] & ~kAdjBias) {
-          y[e] *= y[e] > 0.0f ? inv : rep;
-          const uint32_t m = c[e] & ~(kAdjPrompt | kAdjBias);
-          y[e] -= m ? fmaf(static_cast<float>(m), freq, pres) : 0.0f;
+      for (uint32_t q = 0; q < 4; ++q) {
+        v[q] = in_piece(tok[q]);
+        v[q] = v[q] < n ? v[q] - lo : ~0u;
+        if constexpr (GRAD) {
+          z[q] = 0.0f;
+          if (v[q] < len) z[q] = load1(x, v[q] + lo, DT);
         }
-        if (c[e] & kAdjBias) y[e] += bias_of(i + e);
       }
+#pragma unroll
+      for (uint32_t q = 0; q < 4; ++q) {
+        if (v[q] < len) {
+          if constexpr (GRAD) {
+            atomicOr(at_word(v[q]), flag(v[q], kAdjSeen | (z[q] > 0.0f ? kAdjBias : 0u)));
+          } else if (i + q * BS < made) {
+            atomicOr(at_word(v[q]), flag(v[q], kAdjSeen));
+          } else {
+            atomicAdd(at_word(v[q]), kWide ? 1u : 1u << (v[q] & 1) * 16);
+          }
+        }
+      }
+      load_tokens(i + 4 * BS);
     }
+    for (uint32_t i = tid; i < n_bias; i += BS) {
+      const uint32_t p = in_piece(id), v = p < n ? p - lo : ~0u;
+      if (v < len) {
+        atomicOr(at_word(v), flag(v, kAdjBias));
+        const uint32_t k = atomicAdd(&s_n, 1u);
+        if (k < kAdjList) {
+          s_tok[k] = p;
+          s_at[k] = i;
+        }
+      }
+      id = i + BS < n_bias ? ids[i + BS] : -1;
+    }
+    __syncthreads();
+  };
+  // one element: its word's flags and count
+  auto adjust = [&](float y, uint32_t i, uint32_t flags, uint32_t count) {
+    if constexpr (GRAD) return y * (flags & kAdjSeen ? (flags & kAdjBias ? inv : rep) : 1.0f);
+    if (flags & kAdjSeen || count) {
+      y *= y > 0.0f ? inv : rep;
+      y -= count ? fmaf(static_cast<float>(count), freq, pres) : 0.0f;
+    }
+    if (flags & kAdjBias) y += bias_of(i);
+    return y;
+  };
+  auto finish = [&](uint32_t q, float (&y)[E]) {
 #pragma unroll
     for (uint32_t e = 0; e < E; ++e) y[e] = ok[q] >> e & 1 ? y[e] : GRAD ? 0.0f : -__builtin_inff();
     if (lost) {
 #pragma unroll
       for (uint32_t e = 0; e < E; ++e) y[e] = __builtin_nanf("");
     }
-    store<DT, E>(out, i, n, y);
+    store<DT, E>(out, (q * BS + tid) * E, n, y);
+  };
+  if (GRAD || n_hist <= kAdjCount) {
+    if (lists) search(std::false_type{}, 0, n);
+#pragma unroll
+    for (uint32_t q = 0; q < C; ++q) {
+      const uint32_t i = (q * BS + tid) * E;
+      if (i >= n) return;
+      float y[E];
+      to_f32<DT, E>(raw[q], y);
+      if (lists) {
+        // (the words past the row's end stay 0)
+        const u32x2 c2 = *reinterpret_cast<const u32x2*>(s_word + i / 2);
+        u32x2 c3 = {};
+        if constexpr (E == 8) c3 = *reinterpret_cast<const u32x2*>(s_word + i / 2 + 2);
+#pragma unroll
+        for (uint32_t e = 0; e < E; ++e) {
+          const uint32_t c = (e < 4 ? c2[e / 2 % 2] : c3[e / 2 % 2]) >> e % 2 * 16;
+          y[e] = adjust(y[e], i + e, c, c & kAdjCount);
+        }
+      }
+      finish(q, y);
+    }
+    return;
+  }
+  const uint32_t half = BS * E * (C / 2);
+#pragma unroll
+  for (uint32_t h = 0; h < 2; ++h) {
+    if (h * half >= n) return;            // (the whole workgroup)
+    if (h) {
+      __syncthreads();
+      load_tokens(tid);
+      id = tid < n_bias ? ids[tid] : -1;
+    }
+    search(std::true_type{}, h * half, min(half, n - h * half));
+#pragma unroll
+    for (uint32_t q = h * (C / 2); q < (h + 1) * (C / 2); ++q) {
+      const uint32_t i = (q * BS + tid) * E;
+      if (i < n) {
+        float y[E];
+        to_f32<DT, E>(raw[q], y);
+#pragma unroll
+        for (uint32_t e = 0; e < E; ++e) {
+          const uint32_t c = s_word[i - h * half + e];
+          y[e] = adjust(y[e], i + e, c >> 16, c & 0x3FFFFFFFu);
+        }
+        finish(q, y);
+      }
+    }
   }
 }
 
@@ -190,8 +235,9 @@ template <int DT, bool GRAD> __global__ __launch_bounds__(512) void k_adjust(Adj
 
 hipError_t launch_adjust(AdjustArgs a, int dtype, int64_t T, hipStream_t s) {
   const uint32_t cus = static_cast<uint32_t>(device_cu_count());
+  const uint32_t elems = kAdjBytes / (dtype == PROFK_F32 ? 4 : 2);      // of a thread
   // pieces of whole words of the mask; more of them where the rows are few
-  uint32_t piece = kAdjPiece;
+  uint32_t piece = kAdjBS * elems;
   while (piece > 1024 && static_cast<uint64_t>(T) * ((a.V + piece - 1) / piece) < 2 * cus) piece /= 2;
   if (a.V < piece) piece = (a.V + 31) / 32 * 32;
   a.piece = piece;
@@ -199,9 +245,9 @@ hipError_t launch_adjust(AdjustArgs a, int dtype, int64_t T, hipStream_t s) {
   // threads for the piece, and no fewer than go through an average history in one
   // step
   const int64_t history = a.tokens ? a.n_tokens / T : 0;
-  uint32_t bs = 512;
-  while (bs > 64 && bs * kAdjElems >= 2 * piece && bs * 4 >= 2 * history) bs /= 2;
-  const uint32_t lds = a.tokens || (!a.dy && a.bias_ids) ? piece * 4 : 0;
+  uint32_t bs = kAdjBS;
+  while (bs > 64 && bs * elems >= 2 * piece && bs * 4 >= 2 * history) bs /= 2;
+  const uint32_t lds = a.tokens || (!a.dy && a.bias_ids) ? bs * elems * 2 : 0;
   const int64_t step = ((int64_t{1} << 31) - 1) / bs / a.pieces < 1 ? 1 : ((int64_t{1} << 31) - 1) / bs / a.pieces;
   (void)hipGetLastError();
   for (int64_t r = 0; r < T; r += step) {

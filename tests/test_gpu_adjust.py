@@ -115,6 +115,24 @@ def test_histories(history, V):
     _check(pk.adjust_logits(x, **one), *_want(x, one), "f32")
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("V", [33, 5000, 40001])
+def test_histories_past_the_small_counts(V, dtype):
+    note(f"adjust_logits long histories of {V} {dtype}")
+    x, kw = _case(6, V, dtype, V, history=50000, masks=2, biases=400)
+    n = (kw["offsets"][1:] - kw["offsets"][:-1]).tolist()
+    assert max(n) > 16384 and any(0 < k < 16384 for k in n)
+    _check(pk.adjust_logits(x, **kw), *_want(x, kw), dtype)
+    # 16383 times, 16384 times and more, one token
+    at = torch.tensor([0, 16383, 16383 + 16384, 16383 + 16384 + 16385, 60000, 60000, 60001], device="cuda")
+    one = dict(kw, tokens=torch.full((60001,), V - 1, device="cuda"), offsets=at, n_prompt=None)
+    _check(pk.adjust_logits(x, **one), *_want(x, one), dtype)
+    g = {k: one[k] for k in ("tokens", "offsets", "repetition", "allowed", "mask")}
+    d = torch.randn((6, V), device="cuda").to(DT[dtype])
+    want = dense.adjust_grad(_np(d), _np(x), **{k: _np(v) for k, v in g.items()})
+    _check(pk.adjust_logits_grad(d, x, **g), want, 2 * U * np.abs(want), dtype)
+
+
 @pytest.mark.parametrize("V,n", [(40, 300), (3000, 900), (30000, 3000)])
 def test_many_biases(V, n):
     note(f"adjust_logits {n} biases of {V}")
