@@ -79,26 +79,39 @@ template <int DT, int E> __device__ __forceinline__ void load(const void* row, u
   to_f32<DT, E>(load_raw<DT, E>(row, i, D), v);
 }
 
-// Of E values those that lie in the row, each rounded once.
-template <int DT, int E> __device__ __forceinline__ void store(void* row, uint32_t i, uint32_t D, const float (&v)[E]) {
+// E values as they are in memory, each rounded once.
+template <int DT, int E> __device__ __forceinline__ Raw<DT, E> pack(const float (&v)[E]) {
+  Raw<DT, E> r;
+#pragma unroll
+  for (int w = 0; w < Raw<DT, E>::W; ++w)
+    r.q[w] = DT == PROFK_F32 ? __float_as_uint(v[w % E]) : pack_bf16(v[2 * w % E], v[(2 * w + 1) % E]);
+  return r;
+}
+
+// Of E elements as they are in memory those that lie in the row.
+template <int DT, int E> __device__ __forceinline__ void store_raw(void* row, uint32_t i, uint32_t D, const Raw<DT, E>& r) {
   constexpr int W = Raw<DT, E>::W, S = W < 4 ? W : 4;
   using V = typename Words<S>::type;
-  using O = std::conditional_t<DT == PROFK_F32, float, __bf16>;
+  using O = std::conditional_t<DT == PROFK_F32, uint32_t, uint16_t>;
   O* const p = static_cast<O*>(row) + i;
   if (i + E <= D) {
 #pragma unroll
     for (int w = 0; w < W; w += S) {
       V o;
 #pragma unroll
-      for (int s = 0; s < S; ++s)
-        o[s] = DT == PROFK_F32 ? __float_as_uint(v[(w + s) % E]) : pack_bf16(v[2 * (w + s) % E], v[(2 * (w + s) + 1) % E]);
-      *reinterpret_cast<V*>(p + w) = o;      // (of bf16 one store)
+      for (int s = 0; s < S; ++s) o[s] = r.q[w + s];
+      *reinterpret_cast<V*>(p + w * (DT == PROFK_F32 ? 1 : 2)) = o;
     }
   } else {
 #pragma unroll
     for (uint32_t e = 0; e < E; ++e)
-      if (i + e < D) p[e] = static_cast<O>(v[e]);
+      if (i + e < D) p[e] = static_cast<O>(DT == PROFK_F32 ? r.q[e % W] : r.q[e / 2] >> e % 2 * 16);
   }
+}
+
+// Of E values those that lie in the row, each rounded once.
+template <int DT, int E> __device__ __forceinline__ void store(void* row, uint32_t i, uint32_t D, const float (&v)[E]) {
+  store_raw<DT, E>(row, i, D, pack<DT, E>(v));
 }
 
 // Element i of a row, as fp32.

@@ -11,15 +11,20 @@
 // The division is a product with repetition's reciprocal, rounded to fp32: 1.5
 // units in the last place at most.
 //
-// A workgroup takes a piece of a row.  It counts the history's tokens that fall
-// into its piece in LDS (integer atomics: their order changes nothing), lists the
-// biases of its tokens, and streams the piece once, 64 bytes a thread, loaded
-// under the search of the lists.  Every piece reads the whole history again, from
-// the caches.  The piece in flight is what hides the search, so the table must not
-// limit the workgroups of a CU: it has 16 bits a token, a flag for the prompt, one
-// for a bias and 14 of count.  (With 32, 256 x 131072 bf16 with histories of up to
-// 4096 took 43 us, its inputs not in the caches.)  Rows with longer histories than
-// 14 bits count take their piece in two halves, 32 bits a token.
+// A workgroup takes a piece of a row, 64 bytes a thread, loaded under the search of
+// the lists.  It counts the history's tokens that fall into its piece in a table in
+// LDS (integer atomics: their order changes nothing), lists the biases of its
+// tokens, and marks both in a bitmap.  The marked tokens, few as a rule, are then
+// adjusted from their logits, and their values take the place of their counts, as
+// they are in memory; the piece goes by with two selections an element, by the
+// bitmap and by the mask.  (With each element looked up and adjusted in place, 256
+// x 131072 bf16 took 44 us, instructions.)  Every piece reads the whole history
+// again, from the caches.
+//
+// The table is as large as the piece, so that it does not limit the workgroups of
+// a CU: of 16-bit logits it has two flags and 14 bits of count, of 32-bit ones 30.
+// Rows with longer histories than 14 bits count take a piece of 16-bit logits in
+// two halves, 32 bits a token.
 //
 // The gradient needs no counts, but the sign of the history's logits, which it
 // reads when it comes upon their tokens and notes beside the flag.
@@ -40,12 +45,23 @@ constexpr uint32_t kAdjList = 256;             // biases of a piece that are kep
 constexpr uint32_t kAdjBytes = 64;             // of a thread's elements, 16 at a time
 constexpr uint32_t kAdjBS = 512;               // most threads
 
+// Bytes of the table for each element of a thread.
+template <int DT, bool GRAD> constexpr uint32_t kAdjWord = DT == PROFK_F32 && !GRAD ? 4 : 2;
+
+// All ones in the half of a pair, or the element, whose bit is set.
+template <int DT> __device__ __forceinline__ uint32_t mask_of(uint32_t bits, int w) {
+  if constexpr (DT == PROFK_F32) return static_cast<uint32_t>(__builtin_amdgcn_sbfe(bits, w, 1));
+  const uint32_t lo = __builtin_amdgcn_sbfe(bits, 2 * w, 1), hi = __builtin_amdgcn_sbfe(bits, 2 * w + 1, 1);
+  return (lo & 0xFFFFu) | (hi & 0xFFFF0000u);
+}
+
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
 __device__ __forceinline__ int64_t clamp64(int64_t x, int64_t lo, int64_t hi) { return x < lo ? lo : x > hi ? hi : x; }
 
 template <int DT, bool GRAD> __global__ __launch_bounds__(kAdjBS) void k_adjust(AdjustArgs a) {
-  extern __shared__ __align__(16) uint32_t s_word[];     // 16 bits for each element of the threads
+  extern __shared__ __align__(16) uint32_t s_word[];     // the table
+  __shared__ uint32_t s_bits[GRAD ? 1 : kAdjBS * kAdjBytes / (DT == PROFK_F32 ? 4 : 2) / 32];
   const uint32_t row = a.row + blockIdx.x / a.pieces, p = blockIdx.x % a.pieces;
   const uint32_t v0 = p * a.piece, n = min(a.piece, a.V - v0);
   constexpr uint32_t ES = DT == PROFK_F32 ? 4 : 2;
@@ -114,12 +130,20 @@ template <int DT, bool GRAD> __global__ __launch_bounds__(kAdjBS) void k_adjust(
     }
     return values[at];
   };
-  // f(token's place, its new flags or count): to the table of the places from lo on
+  // the lists' entries of the piece's places from lo on to the table, 32 bits a
+  // place or 16
   auto search = [&](auto wide, uint32_t lo, uint32_t len) {
     constexpr bool kWide = decltype(wide)::value;
     auto at_word = [&](uint32_t v) { return s_word + (kWide ? v : v / 2); };
     auto flag = [&](uint32_t v, uint32_t f) { return kWide ? f << 16 : f << (v & 1) * 16; };
-    for (uint32_t i = tid * 4; i < BS * (kAdjBytes / ES) / 2; i += BS * 4) *reinterpret_cast<u32x4*>(s_word + i) = u32x4{};
+    auto mark = [&](uint32_t v) {
+      if constexpr (!GRAD) atomicOr(s_bits + v / 32, 1u << v % 32);
+    };
+    for (uint32_t i = tid * 4; i < BS * (kAdjBytes / ES) * kAdjWord<DT, GRAD> / 4; i += BS * 4)
+      *reinterpret_cast<u32x4*>(s_word + i) = u32x4{};
+    if constexpr (!GRAD) {
+      for (uint32_t i = tid; i < BS * (kAdjBytes / ES) / 32; i += BS) s_bits[i] = 0;
+    }
     if (tid == 0) s_n = 0;
     __syncthreads();
     for (uint32_t i = tid; i < n_hist; i += 4 * BS) {
@@ -144,6 +168,7 @@ template <int DT, bool GRAD> __global__ __launch_bounds__(kAdjBS) void k_adjust(
           } else {
             atomicAdd(at_word(v[q]), kWide ? 1u : 1u << (v[q] & 1) * 16);
           }
+          mark(v[q]);
         }
       }
       load_tokens(i + 4 * BS);
@@ -152,6 +177,7 @@ template <int DT, bool GRAD> __global__ __launch_bounds__(kAdjBS) void k_adjust(
       const uint32_t p = in_piece(id), v = p < n ? p - lo : ~0u;
       if (v < len) {
         atomicOr(at_word(v), flag(v, kAdjBias));
+        mark(v);
         const uint32_t k = atomicAdd(&s_n, 1u);
         if (k < kAdjList) {
           s_tok[k] = p;
@@ -162,9 +188,8 @@ template <int DT, bool GRAD> __global__ __launch_bounds__(kAdjBS) void k_adjust(
     }
     __syncthreads();
   };
-  // one element: its word's flags and count
+  // one element: its flags and count
   auto adjust = [&](float y, uint32_t i, uint32_t flags, uint32_t count) {
-    if constexpr (GRAD) return y * (flags & kAdjSeen ? (flags & kAdjBias ? inv : rep) : 1.0f);
     if (flags & kAdjSeen || count) {
       y *= y > 0.0f ? inv : rep;
       y -= count ? fmaf(static_cast<float>(count), freq, pres) : 0.0f;
@@ -172,35 +197,67 @@ template <int DT, bool GRAD> __global__ __launch_bounds__(kAdjBS) void k_adjust(
     if (flags & kAdjBias) y += bias_of(i);
     return y;
   };
-  auto finish = [&](uint32_t q, float (&y)[E]) {
+  constexpr uint32_t kNan = DT == PROFK_F32 ? 0x7FC00000u : 0x7FC07FC0u;
+  constexpr uint32_t kForbidden = GRAD ? 0u : DT == PROFK_F32 ? 0xFF800000u : 0xFF80FF80u;
+  auto finish = [&](uint32_t q, Raw<DT, E>& y) {
 #pragma unroll
-    for (uint32_t e = 0; e < E; ++e) y[e] = ok[q] >> e & 1 ? y[e] : GRAD ? 0.0f : -__builtin_inff();
-    if (lost) {
-#pragma unroll
-      for (uint32_t e = 0; e < E; ++e) y[e] = __builtin_nanf("");
+    for (int w = 0; w < 4; ++w) {
+      const uint32_t m = mask_of<DT>(ok[q], w);
+      y.q[w] = lost ? kNan : (y.q[w] & m) | (kForbidden & ~m);
     }
-    store<DT, E>(out, (q * BS + tid) * E, n, y);
+    store_raw<DT, E>(out, (q * BS + tid) * E, n, y);
   };
-  if (GRAD || n_hist <= kAdjCount) {
+  if constexpr (GRAD) {
     if (lists) search(std::false_type{}, 0, n);
 #pragma unroll
     for (uint32_t q = 0; q < C; ++q) {
       const uint32_t i = (q * BS + tid) * E;
       if (i >= n) return;
-      float y[E];
-      to_f32<DT, E>(raw[q], y);
       if (lists) {
+        float y[E];
+        to_f32<DT, E>(raw[q], y);
         // (the words past the row's end stay 0)
-        const u32x2 c2 = *reinterpret_cast<const u32x2*>(s_word + i / 2);
-        u32x2 c3 = {};
-        if constexpr (E == 8) c3 = *reinterpret_cast<const u32x2*>(s_word + i / 2 + 2);
+        const uint32_t* const c = s_word + i / 2;
 #pragma unroll
         for (uint32_t e = 0; e < E; ++e) {
-          const uint32_t c = (e < 4 ? c2[e / 2 % 2] : c3[e / 2 % 2]) >> e % 2 * 16;
-          y[e] = adjust(y[e], i + e, c, c & kAdjCount);
+          const uint32_t f = c[e / 2] >> e % 2 * 16;
+          y[e] *= f & kAdjSeen ? (f & kAdjBias ? inv : rep) : 1.0f;
+        }
+        raw[q] = pack<DT, E>(y);
+      }
+      finish(q, raw[q]);
+    }
+    return;
+  }
+  if (DT == PROFK_F32 || n_hist <= kAdjCount) {
+    using O = std::conditional_t<DT == PROFK_F32, float, __bf16>;
+    if (lists) {
+      constexpr bool kWide = DT == PROFK_F32;
+      search(std::integral_constant<bool, kWide>{}, 0, n);
+      for (uint32_t w = tid; w < (n + 31) / 32; w += BS) {
+        for (uint32_t bits = s_bits[w]; bits; bits &= bits - 1) {
+          const uint32_t v = w * 32 + static_cast<uint32_t>(__builtin_ctz(bits));
+          const uint32_t c = kWide ? s_word[v] : s_word[v / 2] >> v % 2 * 16;
+          reinterpret_cast<O*>(s_word)[v] =
+              static_cast<O>(adjust(load1(x, v, DT), v, kWide ? c >> 16 : c, kWide ? c & 0x3FFFFFFFu : c & kAdjCount));
         }
       }
-      finish(q, y);
+      __syncthreads();
+    }
+#pragma unroll
+    for (uint32_t q = 0; q < C; ++q) {
+      const uint32_t i = (q * BS + tid) * E;
+      if (i >= n) return;
+      if (lists) {
+        const uint32_t bits = s_bits[i / 32] >> i % 32;
+        const u32x4 c = *reinterpret_cast<const u32x4*>(s_word + i * ES / 4);
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+          const uint32_t m = mask_of<DT>(bits, w);
+          raw[q].q[w] = (c[w] & m) | (raw[q].q[w] & ~m);
+        }
+      }
+      finish(q, raw[q]);
     }
     return;
   }
@@ -225,7 +282,8 @@ template <int DT, bool GRAD> __global__ __launch_bounds__(kAdjBS) void k_adjust(
           const uint32_t c = s_word[i - h * half + e];
           y[e] = adjust(y[e], i + e, c >> 16, c & 0x3FFFFFFFu);
         }
-        finish(q, y);
+        raw[q] = pack<DT, E>(y);
+        finish(q, raw[q]);
       }
     }
   }
@@ -247,7 +305,8 @@ hipError_t launch_adjust(AdjustArgs a, int dtype, int64_t T, hipStream_t s) {
   const int64_t history = a.tokens ? a.n_tokens / T : 0;
   uint32_t bs = kAdjBS;
   while (bs > 64 && bs * elems >= 2 * piece && bs * 4 >= 2 * history) bs /= 2;
-  const uint32_t lds = a.tokens || (!a.dy && a.bias_ids) ? bs * elems * 2 : 0;
+  const uint32_t word = dtype == PROFK_F32 ? (a.dy ? kAdjWord<PROFK_F32, true> : kAdjWord<PROFK_F32, false>) : 2;
+  const uint32_t lds = a.tokens || (!a.dy && a.bias_ids) ? bs * elems * word : 0;
   const int64_t step = ((int64_t{1} << 31) - 1) / bs / a.pieces < 1 ? 1 : ((int64_t{1} << 31) - 1) / bs / a.pieces;
   (void)hipGetLastError();
   for (int64_t r = 0; r < T; r += step) {
