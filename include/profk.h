@@ -502,7 +502,8 @@ int profk_linear_grad(int32_t dtype, const void* dy, int64_t dy_stride, const vo
  *         the history; x_v where it is not
  *   out_v = u_v - [c_v > 0] presence - c_v frequency + bias_v, or -inf where the
  *         row's mask forbids v
- * in fp32, rounded once to the logits' dtype.
+ * in fp32 (the division by the reciprocal of repetition, itself rounded), rounded
+ * once to the logits' dtype.
  *
  *   logits, out  fp32 or bf16 [T, V], rows x_stride and out_stride elements
  *             apart; out may be the logits (same stride), and must not overlap
@@ -522,6 +523,9 @@ int profk_linear_grad(int32_t dtype, const void* dy, int64_t dy_stride, const vo
  *             one (n_masks must be T or 1).
  *   NaN, inf  stay where they are allowed; where they are forbidden -inf.  A row
  *             that allows nothing is all -inf.
+ *   time      one read and one write of the logits; each piece of a row (64 KiB
+ *             at most) searches the row's history and biases again, and rows with
+ *             more than 256 biases in a piece search their list for each of them.
  *
  * profk_adjust_logits_grad: the gradient with respect to the logits, that of out
  * times 1 / repetition, repetition or 1 as above, and 0 where the mask forbids.

@@ -10,14 +10,14 @@ namespace {
 
 constexpr uint32_t kJoinCols = 16, kJoinRows = 64, kJoinBS = kJoinCols * kJoinRows;
 
-// part: [parts, cols].  Workgroup b has the columns from b kJoinCols on; threads
+// part: [parts, cols].  The workgroup has the columns from b kJoinCols on; threads
 // below kJoinCols return the sum of theirs, if it is below cols.  (With 64 columns
 // and 16 rows of threads, 1024 parts of 8192 columns took 18 us: a part after the
 // other.)
-__device__ __forceinline__ float join_parts(const float* part, uint32_t parts, uint32_t cols) {
+__device__ __forceinline__ float join_parts(const float* part, uint32_t parts, uint32_t cols, uint32_t b) {
   __shared__ float s[kJoinRows][kJoinCols], s8[8][kJoinCols];
   const uint32_t c = threadIdx.x % kJoinCols, k = threadIdx.x / kJoinCols;
-  const uint32_t col = blockIdx.x * kJoinCols + c;
+  const uint32_t col = b * kJoinCols + c;
   float sum = 0.0f;
   if (col < cols) {
 #pragma unroll 4

@@ -67,6 +67,13 @@ template <int DT, bool GRAD> __global__ __launch_bounds__(kAdjBS) void k_adjust(
   constexpr uint32_t ES = DT == PROFK_F32 ? 4 : 2;
   constexpr int E = 16 / ES, C = kAdjBytes / 16;
   const uint32_t tid = threadIdx.x, BS = blockDim.x;
+  const char* const x = static_cast<const char*>(a.x) + (row * a.stride + v0) * ES;
+  const char* const src = GRAD ? static_cast<const char*>(a.dy) + (row * a.dy_stride + v0) * ES : x;
+  char* const out = static_cast<char*>(a.out) + (row * a.out_stride + v0) * ES;
+  // the piece first: nothing of it waits for the lists
+  Raw<DT, E> raw[C];
+#pragma unroll
+  for (uint32_t q = 0; q < C; ++q) raw[q] = load_raw<DT, E>(src, (q * BS + tid) * E, n);
   // (a list's offsets may be anything: none reaches past the list)
   const int64_t *tokens = nullptr, *ids = nullptr;
   const float* values = nullptr;
@@ -82,9 +89,6 @@ template <int DT, bool GRAD> __global__ __launch_bounds__(kAdjBS) void k_adjust(
     ids = a.bias_ids + b0;
     values = a.bias_values + b0;
   }
-  const char* const x = static_cast<const char*>(a.x) + (row * a.stride + v0) * ES;
-  const char* const src = GRAD ? static_cast<const char*>(a.dy) + (row * a.dy_stride + v0) * ES : x;
-  char* const out = static_cast<char*>(a.out) + (row * a.out_stride + v0) * ES;
   const uint32_t* words = nullptr;
   bool lost = false;                 // the row names a mask that is not there
   if (a.allowed) {
@@ -97,21 +101,19 @@ template <int DT, bool GRAD> __global__ __launch_bounds__(kAdjBS) void k_adjust(
   const float rep = a.repetition ? a.repetition[row] : 1.0f, inv = 1.0f / rep;
   const float pres = !GRAD && a.presence ? a.presence[row] : 0.0f;
   const float freq = !GRAD && a.frequency ? a.frequency[row] : 0.0f;
-  // the piece and its part of the mask, and the first of the lists, loaded
-  // together (a piece starts at a multiple of 32 tokens)
-  Raw<DT, E> raw[C];
+  // (a piece starts at a multiple of 32 tokens)
   uint32_t ok[C];
 #pragma unroll
   for (uint32_t q = 0; q < C; ++q) {
     const uint32_t i = (q * BS + tid) * E;
-    raw[q] = load_raw<DT, E>(src, i, n);
     ok[q] = words && i < n ? words[(v0 + i) / 32] >> (i % 32) : 0xFFu;
   }
-  // (four tokens at a time: a load waits for none before it)
-  int64_t tok[4];
+  // (eight tokens at a time: a load waits for none before it)
+  constexpr uint32_t TB = 8;
+  int64_t tok[TB];
   auto load_tokens = [&](uint32_t i) {
 #pragma unroll
-    for (uint32_t q = 0; q < 4; ++q) tok[q] = i + q * BS < n_hist ? tokens[i + q * BS] : -1;
+    for (uint32_t q = 0; q < TB; ++q) tok[q] = i + q * BS < n_hist ? tokens[i + q * BS] : -1;
   };
   // an entry's place in the piece, n or more where it has none
   auto in_piece = [&](int64_t v) { return v >> 32 == 0 ? static_cast<uint32_t>(v) - v0 : ~0u; };
@@ -146,11 +148,11 @@ template <int DT, bool GRAD> __global__ __launch_bounds__(kAdjBS) void k_adjust(
     }
     if (tid == 0) s_n = 0;
     __syncthreads();
-    for (uint32_t i = tid; i < n_hist; i += 4 * BS) {
-      uint32_t v[4];
-      [[maybe_unused]] float z[4];
+    for (uint32_t i = tid; i < n_hist; i += TB * BS) {
+      uint32_t v[TB];
+      [[maybe_unused]] float z[TB];
 #pragma unroll
-      for (uint32_t q = 0; q < 4; ++q) {
+      for (uint32_t q = 0; q < TB; ++q) {
         v[q] = in_piece(tok[q]);
         v[q] = v[q] < n ? v[q] - lo : ~0u;
         if constexpr (GRAD) {
@@ -159,7 +161,7 @@ template <int DT, bool GRAD> __global__ __launch_bounds__(kAdjBS) void k_adjust(
         }
       }
 #pragma unroll
-      for (uint32_t q = 0; q < 4; ++q) {
+      for (uint32_t q = 0; q < TB; ++q) {
         if (v[q] < len) {
           if constexpr (GRAD) {
             atomicOr(at_word(v[q]), flag(v[q], kAdjSeen | (z[q] > 0.0f ? kAdjBias : 0u)));
@@ -171,7 +173,7 @@ template <int DT, bool GRAD> __global__ __launch_bounds__(kAdjBS) void k_adjust(
           mark(v[q]);
         }
       }
-      load_tokens(i + 4 * BS);
+      load_tokens(i + TB * BS);
     }
     for (uint32_t i = tid; i < n_bias; i += BS) {
       const uint32_t p = in_piece(id), v = p < n ? p - lo : ~0u;
@@ -304,7 +306,7 @@ hipError_t launch_adjust(AdjustArgs a, int dtype, int64_t T, hipStream_t s) {
   // step
   const int64_t history = a.tokens ? a.n_tokens / T : 0;
   uint32_t bs = kAdjBS;
-  while (bs > 64 && bs * elems >= 2 * piece && bs * 4 >= 2 * history) bs /= 2;
+  while (bs > 64 && bs * elems >= 2 * piece && bs * 8 >= 2 * history) bs /= 2;
   const uint32_t word = dtype == PROFK_F32 ? (a.dy ? kAdjWord<PROFK_F32, true> : kAdjWord<PROFK_F32, false>) : 2;
   const uint32_t lds = a.tokens || (!a.dy && a.bias_ids) ? bs * elems * word : 0;
   const int64_t step = ((int64_t{1} << 31) - 1) / bs / a.pieces < 1 ? 1 : ((int64_t{1} << 31) - 1) / bs / a.pieces;

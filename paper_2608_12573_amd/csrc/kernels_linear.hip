@@ -159,9 +159,11 @@ template <int DT, int ACT> __global__ __launch_bounds__(256) void k_dz(DzArgs a)
 }
 
 __global__ __launch_bounds__(kJoinBS) void k_db_join(const float* part, uint32_t parts, uint32_t N, float* db) {
-  const float sum = join_parts(part, parts, N);
-  const uint32_t j = blockIdx.x * kJoinCols + threadIdx.x;
-  if (threadIdx.x < kJoinCols && j < N) db[j] = sum;
+  for (uint32_t b = blockIdx.x; b < (N + kJoinCols - 1) / kJoinCols; b += gridDim.x) {
+    const float sum = join_parts(part, parts, N, b);
+    const uint32_t j = b * kJoinCols + threadIdx.x;
+    if (threadIdx.x < kJoinCols && j < N) db[j] = sum;
+  }
 }
 
 uint32_t dz_parts(int64_t M, int64_t N, int num_cus) {
@@ -317,7 +319,8 @@ hipError_t launch_linear_grad(const LinGradCall& c, hipStream_t s) {
     e = hipGetLastError();
   }
   if (e == hipSuccess && c.db && N) {
-    k_db_join<<<(N + kJoinCols - 1) / kJoinCols, kJoinBS, 0, s>>>(part, L.parts, N, c.db);
+    const uint32_t blocks = (N + kJoinCols - 1) / kJoinCols;   // (a launch holds fewer than 2^32 threads)
+    k_db_join<<<blocks < 65536 ? blocks : 65536, kJoinBS, 0, s>>>(part, L.parts, N, c.db);
     e = hipGetLastError();
   }
   float* const sums = reinterpret_cast<float*>(ws + L.sums);

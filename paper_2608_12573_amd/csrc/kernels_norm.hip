@@ -360,7 +360,7 @@ template <int XDT, int YDT> __global__ __launch_bounds__(256) void k_norm_cols(N
 
 // The parts' sums to dw and db.
 __global__ __launch_bounds__(kJoinBS) void k_norm_join(NormGradArgs a) {
-  const float sum = join_parts(a.part, a.parts, 2 * a.D);
+  const float sum = join_parts(a.part, a.parts, 2 * a.D, blockIdx.x);
   const uint32_t col = blockIdx.x * kJoinCols + threadIdx.x;
   if (threadIdx.x >= kJoinCols || col >= 2 * a.D) return;
   void* const out = col < a.D ? a.dw : a.db;

@@ -165,6 +165,39 @@ def test_residual_in_place_and_neighbours(M, K, N):
     assert torch.equal(out, want) and (buf[:32] == 7).all() and (buf[32 + M * N:] == 7).all()
 
 
+@pytest.mark.parametrize("M,K,N", [(2, 256, 65), (70, 256, 133), (300, 512, 261), (64, 4096, 515)])
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+def test_outputs_at_any_element(M, K, N, dt):
+    note(f"linear to odd places {M}x{K}x{N} {dt}")
+    x, w, b, g = _inputs(M, K, N, 16)
+    z = torch.empty((M, N), dtype=DT[dt], device="cuda")
+    want = pk.linear(x, w, b, "silu", dtype=DT[dt], pre=z)
+    bufs = [torch.full((M * N + 16,), 7.0, dtype=DT[dt], device="cuda") for _ in range(2)]
+    out, pre = (t[3:3 + M * N].view(M, N) for t in bufs)
+    pk.linear(x, w, b, "silu", out=out, pre=pre)
+    assert torch.equal(out, want) and torch.equal(pre, z)
+    for t in bufs:
+        assert (t[:3] == 7).all() and (t[3 + M * N:] == 7).all()
+    dy = torch.randn((M, N), generator=g).to(DT[dt]).cuda()
+    grads = pk.linear_grad(dy, x, w, z, "silu")
+    outs = [torch.full((t.numel() + 16,), 7.0, dtype=t.dtype, device="cuda") for t in grads]
+    views = tuple(o[5:5 + t.numel()].view(t.shape) for o, t in zip(outs, grads))
+    pk.linear_grad(dy, x, w, pre, "silu", out=views)
+    for v, t, o in zip(views, grads, outs):
+        assert torch.equal(v, t) and (o[:5] == 7).all() and (o[5 + t.numel():] == 7).all()
+
+
+@pytest.mark.parametrize("N,parts", [(70000, "many columns"), (1100000, "more than one launch's")])
+def test_wide_bias_gradients(N, parts):
+    note(f"linear_grad of {N} columns")
+    dy = torch.randn((3, N), generator=torch.Generator().manual_seed(N)).cuda()
+    x = torch.ones((3, 8), dtype=torch.bfloat16, device="cuda")
+    w = torch.ones((N, 8), dtype=torch.bfloat16, device="cuda")
+    db = pk.linear_grad(dy, x, w, need=(False, False, True))[2]
+    want = _np(dy).sum(axis=0)
+    _check(db, want, 23 * U * np.abs(_np(dy)).sum(axis=0) + U * np.abs(want), "dbias")
+
+
 def test_no_rows_no_columns():
     note("linear without rows or columns")
     w = torch.ones((5, 8), dtype=torch.bfloat16, device="cuda")
