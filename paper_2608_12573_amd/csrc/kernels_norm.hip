@@ -205,9 +205,11 @@ template <int XDT, int YDT, int GS, int R, int C8> __global__ __launch_bounds__(
   constexpr int E = kElems<XDT, YDT>, C = C8 * 8 / E;
   __shared__ float s_red[2][BS / kWave][2];
   __shared__ float s_sum[R > 1 ? 2 * GS * C * E : 1];
+  // (1024 threads have 128 registers each: no row ahead, the scale from the caches)
+  constexpr bool kLean = BS == 1024;
   const uint32_t t = threadIdx.x % GS, sub = threadIdx.x / GS;
   const uint32_t step = gridDim.x * R;
-  float w[C][E], dw[C][E] = {}, db[C][E] = {};
+  float w[kLean ? 1 : C][E], dw[C][E] = {}, db[C][E] = {};
   Raw<XDT, E> nx[C];
   Raw<YDT, E> ny[C];
   float nm, nr;
@@ -223,31 +225,35 @@ template <int XDT, int YDT, int GS, int R, int C8> __global__ __launch_bounds__(
     nr = D ? a.rstd[r] : 0.0f;
   };
   uint32_t row0 = blockIdx.x * R;
-  load(row0 + sub);
+  if constexpr (!kLean) {
+    load(row0 + sub);
 #pragma unroll
-  for (int c = 0; c < C; ++c) load_param(a.w, a.p_dtype, (c * GS + t) * E, a.D, 1.0f, w[c]);
+    for (int c = 0; c < C; ++c) load_param(a.w, a.p_dtype, (c * GS + t) * E, a.D, 1.0f, w[c]);
+  }
   const float inv = 1.0f / static_cast<float>(a.D);
   uint32_t slot = 0;
   for (; row0 < a.T; row0 += step, slot ^= 1) {
     const uint32_t row = row0 + sub;
     float n[C][E], g[C][E], s[2] = {0.0f, 0.0f};
+    if constexpr (kLean) load(row);
     const float m = nm, r = nr;
 #pragma unroll
     for (int c = 0; c < C; ++c) {
       to_f32<XDT, E>(nx[c], n[c]);
       to_f32<YDT, E>(ny[c], g[c]);
+      if constexpr (kLean) load_param(a.w, a.p_dtype, (c * GS + t) * E, a.D, 1.0f, w[0]);
 #pragma unroll
       for (int e = 0; e < E; ++e) {
         // (past the row's end dy is 0)
         n[c][e] = (n[c][e] - m) * r;
         dw[c][e] = fmaf(g[c][e], n[c][e], dw[c][e]);
         db[c][e] += g[c][e];
-        g[c][e] *= w[c][e];
+        g[c][e] *= w[kLean ? 0 : c][e];
         s[0] += g[c][e];
         s[1] = fmaf(g[c][e], n[c][e], s[1]);
       }
     }
-    if (a.T - row0 > step) load(row + step);
+    if (!kLean && a.T - row0 > step) load(row + step);
     if (a.dx) {       // (the same for all: the barrier is met by the whole workgroup)
       row_sum<GS>(s, s_red[slot]);
       s[0] *= inv;
@@ -373,14 +379,17 @@ __global__ __launch_bounds__(kJoinBS) void k_norm_join(NormGradArgs a) {
 // Longest rows that are kept in registers.
 constexpr uint32_t kBlockD = 16384;
 
-// f(threads of a row, chunks of a thread) for rows of D <= kBlockD.
+// f(threads of a row, chunks of a thread) for rows of D <= kBlockD.  (16384 x 6000
+// bf16 with 512 threads took 89 us, its gradient 183; with 384 .. and ..)
 template <class F> void with_shape(uint32_t D, F f) {
   using std::integral_constant;
   if (D <= 512) f(integral_constant<int, 64>{}, integral_constant<int, 1>{});
   else if (D <= 1024) f(integral_constant<int, 64>{}, integral_constant<int, 2>{});
   else if (D <= 2048) f(integral_constant<int, 256>{}, integral_constant<int, 1>{});
   else if (D <= 4096) f(integral_constant<int, 256>{}, integral_constant<int, 2>{});
+  else if (D <= 6144) f(integral_constant<int, 384>{}, integral_constant<int, 2>{});
   else if (D <= 8192) f(integral_constant<int, 512>{}, integral_constant<int, 2>{});
+  else if (D <= 12288) f(integral_constant<int, 768>{}, integral_constant<int, 2>{});
   else f(integral_constant<int, 1024>{}, integral_constant<int, 2>{});
 }
 

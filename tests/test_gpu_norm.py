@@ -57,7 +57,7 @@ def _forward_tol(x, y, w, b, r, dtype):
 
 
 SHAPES = [(1, 1), (3, 2), (5, 7), (1, 4096), (4, 511), (9, 512), (7, 513), (5, 1000), (6, 1024), (3, 1025), (5, 2048), (3, 2049),
-          (4, 4096), (3, 4097), (2, 8192), (3, 8193), (2, 16384), (3, 16385), (2, 50001), (2100, 96), (1500, 1536), (37, 777)]
+          (4, 4096), (3, 4097), (3, 6144), (2, 6145), (2, 8192), (3, 8193), (2, 12288), (3, 12289), (2, 16384), (3, 16385), (2, 50001), (2100, 96), (1500, 1536), (37, 777)]
 
 
 @pytest.mark.parametrize("T,D", SHAPES)
