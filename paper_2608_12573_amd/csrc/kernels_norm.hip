@@ -206,7 +206,7 @@ template <int XDT, int YDT, int GS, int R, int C8> __global__ __launch_bounds__(
   __shared__ float s_red[2][BS / kWave][2];
   __shared__ float s_sum[R > 1 ? 2 * GS * C * E : 1];
   // (1024 threads have 128 registers each: no row ahead, the scale from the caches)
-  constexpr bool kLean = BS == 1024;
+  constexpr bool kLean = BS == 1024 && C8 > 1;
   const uint32_t t = threadIdx.x % GS, sub = threadIdx.x / GS;
   const uint32_t step = gridDim.x * R;
   float w[kLean ? 1 : C][E], dw[C][E] = {}, db[C][E] = {};
@@ -393,9 +393,21 @@ template <class F> void with_shape(uint32_t D, F f) {
   else f(integral_constant<int, 1024>{}, integral_constant<int, 2>{});
 }
 
+template <class F> void with_grad_shape(uint32_t D, F f) {
+  using std::integral_constant;
+  if (D <= 512) f(integral_constant<int, 64>{}, integral_constant<int, 1>{});
+  else if (D <= 1024) f(integral_constant<int, 128>{}, integral_constant<int, 1>{});
+  else if (D <= 2048) f(integral_constant<int, 256>{}, integral_constant<int, 1>{});
+  else if (D <= 4096) f(integral_constant<int, 512>{}, integral_constant<int, 1>{});
+  else if (D <= 6144) f(integral_constant<int, 768>{}, integral_constant<int, 1>{});
+  else if (D <= 8192) f(integral_constant<int, 1024>{}, integral_constant<int, 1>{});
+  else if (D <= 12288) f(integral_constant<int, 768>{}, integral_constant<int, 2>{});
+  else f(integral_constant<int, 1024>{}, integral_constant<int, 2>{});
+}
+
 // Rows of a workgroup of the two kernels, and its workgroups a CU.
 constexpr int norm_rows_of(int gs) { return gs == 64 ? 4 : 1; }
-constexpr int grad_rows_of(int gs) { return gs == 64 ? 8 : gs == 256 ? 2 : 1; }
+constexpr int grad_rows_of(int gs) { return gs == 64 ? 8 : gs == 128 ? 4 : gs == 256 ? 2 : 1; }
 uint32_t row_grid(uint32_t T, uint32_t rows, uint32_t threads, uint32_t cus) {
   const uint32_t need = (T + rows - 1) / rows, most = (threads <= 256 ? 4 : threads <= 512 ? 2 : 1) * cus;
   return need < most ? need : most;
@@ -418,7 +430,7 @@ template <int XDT, int YDT> void norm_grad_rows(const NormGradArgs& a, uint32_t 
     if (a.part) k_norm_cols<XDT, YDT><<<dim3((a.D + 256 * kElems<XDT, YDT> - 1) / (256 * kElems<XDT, YDT>), a.parts), 256, 0, s>>>(a);
     return;
   }
-  with_shape(a.D, [&](auto gs, auto c) {
+  with_grad_shape(a.D, [&](auto gs, auto c) {
     constexpr int GS = decltype(gs)::value, R = grad_rows_of(GS);
     k_norm_grad<XDT, YDT, GS, R, decltype(c)::value><<<a.parts, GS * R, 0, s>>>(a);
   });
@@ -431,7 +443,7 @@ uint32_t norm_grad_parts(int64_t T, int64_t D, int num_cus) {
   if (T <= 0) return 1;
   if (D <= static_cast<int64_t>(kBlockD)) {
     uint32_t parts = 0;
-    with_shape(static_cast<uint32_t>(D), [&](auto gs, auto) {
+    with_grad_shape(static_cast<uint32_t>(D), [&](auto gs, auto) {
       constexpr int GS = decltype(gs)::value, R = grad_rows_of(GS);
       parts = row_grid(static_cast<uint32_t>(T), R, GS * R, cus);
     });
