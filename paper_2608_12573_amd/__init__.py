@@ -861,16 +861,19 @@ def mx4_linear(x, w_codes, w_scales, dtype=None, ws=None, out=None):
 
 # ------------------------------------------------------------- layer norm ---
 
-def _here(device):
-    """The calls below go to the current device's stream: a tensor of another
-    GPU is refused."""
-    if device.index != _torch()._C._cuda_getDevice():
+def _stream_on(device):
+    """The current stream's handle.  The calls below go to the current device's
+    stream: a tensor of another GPU is refused."""
+    C = _torch()._C
+    current = C._cuda_getDevice()
+    if device.index != current:
         raise ProfkError(f"the tensors are on {device}, which is not the current device")
+    return C._cuda_getCurrentRawStream(current)
 
 
 def _out_rows(out, name, R, C, dtype, device):
     """Checks an output matrix whose rows may be strided: its row stride."""
-    dt, oR, oC, stride = _rows(out, name)
+    _, oR, oC, stride = _rows(out, name)
     if oR != R or oC != C or (dtype is not None and out.dtype != dtype):
         raise ProfkError(f"{name} must be {dtype or out.dtype} of shape {(R, C)}, got {out.dtype} {(oR, oC)}")
     _on_device(out, name, device)
@@ -883,6 +886,13 @@ def _params(weight, bias, D, device):
     one = weight if weight is not None else bias
     if one is None:
         return F32
+    try:
+        if one.dtype is torch.float32 and one.shape == (D,) and one.is_contiguous() and one.device == device and \
+                (bias is None or bias is one or (bias.dtype is torch.float32 and bias.shape == (D,) and
+                                                 bias.is_contiguous() and bias.device == device)):
+            return F32
+    except AttributeError:
+        pass
     dt = _dtype_code(one) if isinstance(one, torch.Tensor) else F32
     if weight is not None:
         _vector(weight, "weight", one.dtype if isinstance(one, torch.Tensor) else None, (D,), device)
@@ -916,7 +926,7 @@ def layer_norm(x, weight=None, bias=None, eps=1e-5, dtype=None, out=None):
     if out is None and torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in (x, weight, bias)):
         return _differentiable("layer_norm").apply(x, weight, bias, eps, dtype)
     pdt = _params(weight, bias, D, dev)
-    _here(dev)
+    stream = _stream_on(dev)
     if out is None:
         out = layer_norm_outputs(T, D, dtype or x.dtype, dev)
     ostride = _out_rows(out[0], "out[0]", T, D, dtype, dev)
@@ -924,7 +934,7 @@ def layer_norm(x, weight=None, bias=None, eps=1e-5, dtype=None, out=None):
     _vector(out[2], "out[2]", torch.float32, (T,), dev)
     _check(lib().profk_layer_norm(dt, x.data_ptr(), T, D, stride, pdt, _ptr(weight), _ptr(bias), eps,
                                   _dtype_code(out[0]), out[0].data_ptr(), ostride, out[1].data_ptr(), out[2].data_ptr(),
-                                  _stream()))
+                                  stream))
     return out
 
 
@@ -949,7 +959,7 @@ def layer_norm_grad(dy, x, weight, mean, rstd, ws=None, out=None, need=(True, Tr
     pdt = _params(weight, None, D, dev)
     _vector(mean, "mean", f32, (T,), dev)
     _vector(rstd, "rstd", f32, (T,), dev)
-    _here(dev)
+    stream = _stream_on(dev)
     ptype = weight.dtype if weight is not None else f32
     if out is None:
         out = (torch.empty((T, D), dtype=x.dtype, device=dev) if need[0] else None,
@@ -967,7 +977,7 @@ def layer_norm_grad(dy, x, weight, mean, rstd, ws=None, out=None, need=(True, Tr
         ws = torch.empty(n, dtype=torch.uint8, device=dev)
     _check(L.profk_layer_norm_grad(dt, x.data_ptr(), T, D, stride, ddt, dy.data_ptr(), dstride, pdt, _ptr(weight),
                                    mean.data_ptr(), rstd.data_ptr(), _ptr(out[0]), ostride, _ptr(out[1]), _ptr(out[2]),
-                                   ws.data_ptr() if n else None, n, _stream()))
+                                   ws.data_ptr() if n else None, n, stream))
     return out
 
 
@@ -1024,7 +1034,7 @@ def linear(x, w, bias=None, activation=None, residual=None, dtype=None, ws=None,
         return _differentiable("linear").apply(x, w, bias, residual, activation, dtype, ws)
     if bias is not None:
         _vector(bias, "bias", torch.float32, (N,), dev)
-    _here(dev)
+    stream = _stream_on(dev)
     out, odt = _dense_out((M, N), dtype, torch.float32, out, dev)
     if pre is not None:
         _vector(pre, "pre", out.dtype, (M, N), dev)
@@ -1036,7 +1046,7 @@ def linear(x, w, bias=None, activation=None, residual=None, dtype=None, ws=None,
     elif n:
         ws = torch.empty(n, dtype=torch.uint8, device=dev)
     _check(L.profk_linear(x.data_ptr(), M, K, xs, w.data_ptr(), N, wstride, _ptr(bias), act, odt, _ptr(residual), rs,
-                          out.data_ptr(), _ptr(pre), ws.data_ptr() if n else None, n, _stream()))
+                          out.data_ptr(), _ptr(pre), ws.data_ptr() if n else None, n, stream))
     return out
 
 
@@ -1064,7 +1074,7 @@ def linear_grad(dy, x, w, pre=None, activation=None, ws=None, out=None, need=(Tr
         _vector(pre, "pre", dy.dtype, (M, N), dev)
     else:
         pre = None
-    _here(dev)
+    stream = _stream_on(dev)
     bf16 = torch.bfloat16
     if out is None:
         out = (torch.empty((M, K), dtype=bf16, device=dev) if need[0] else None,
@@ -1081,7 +1091,7 @@ def linear_grad(dy, x, w, pre=None, activation=None, ws=None, out=None, need=(Tr
         ws = torch.empty(n, dtype=torch.uint8, device=dev)
     _check(L.profk_linear_grad(ddt, dy.data_ptr(), dstride, _ptr(pre), act, x.data_ptr(), M, K, xs, w.data_ptr(), N,
                                wstride, _ptr(out[0]), _ptr(out[1]), _ptr(out[2]), ws.data_ptr() if n else None, n,
-                               _stream()))
+                               stream))
     return out
 
 
@@ -1164,14 +1174,14 @@ def adjust_logits(logits, tokens=None, offsets=None, n_prompt=None, repetition=N
         n_bias = _list(ids, "bias[0]", torch.int64, dev)
         _vector(values, "bias[1]", f32, (n_bias,), dev)
         _vector(at, "bias[2]", torch.int64, (T + 1,), dev)
-    _here(dev)
+    stream = _stream_on(dev)
     if out is None:
         out = torch.empty((T, V), dtype=logits.dtype, device=dev)
     ostride = _out_rows(out, "out", T, V, logits.dtype, dev)
     _check(lib().profk_adjust_logits(dt, logits.data_ptr(), T, V, stride, _ptr(tokens), _ptr(offsets), n_tokens,
                                      _ptr(n_prompt), _ptr(repetition), _ptr(presence), _ptr(frequency), _ptr(ids),
                                      _ptr(values), _ptr(at), n_bias, _ptr(allowed), n_masks, words, _ptr(mask),
-                                     out.data_ptr(), ostride, _stream()))
+                                     out.data_ptr(), ostride, stream))
     return out
 
 
@@ -1188,13 +1198,13 @@ def adjust_logits_grad(d_out, logits, tokens=None, offsets=None, n_prompt=None, 
     n_tokens, n_masks, words = _history(T, V, tokens, offsets, repetition, allowed, mask, dev)
     if n_prompt is not None:
         _vector(n_prompt, "n_prompt", torch.int64, (T,), dev)
-    _here(dev)
+    stream = _stream_on(dev)
     if out is None:
         out = torch.empty((T, V), dtype=logits.dtype, device=dev)
     ostride = _out_rows(out, "out", T, V, logits.dtype, dev)
     _check(lib().profk_adjust_logits_grad(dt, d_out.data_ptr(), dstride, logits.data_ptr(), T, V, stride, _ptr(tokens),
                                           _ptr(offsets), n_tokens, _ptr(repetition), _ptr(allowed), n_masks, words,
-                                          _ptr(mask), out.data_ptr(), ostride, _stream()))
+                                          _ptr(mask), out.data_ptr(), ostride, stream))
     return out
 
 

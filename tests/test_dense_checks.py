@@ -141,4 +141,4 @@ def test_binding_refusals():
     # no GPU is current here: tensors of another one are refused
     if not torch.cuda.is_available():
         return
-    _raises(lambda: pk._here(torch.device("cuda", 7)), "not the current device")
+    _raises(lambda: pk._stream_on(torch.device("cuda", 7)), "not the current device")
