@@ -127,24 +127,27 @@ template <bool TA, bool TB> hipError_t launch_any(ProdArgs g, hipStream_t s) {
 }
 
 // --------------------------------------------------------------------- dz ---
-// dz = dy act'(z) to bf16, and the sums of its columns over a part of the rows.
+// dz = dy act'(z) to bf16, and the sums of its columns over a part of the rows.  A
+// workgroup has cols threads for 8 columns each, and as many rows at a time as fit.
 struct DzArgs {
   const void *dy, *pre;
   uint64_t dy_stride;
-  uint32_t M, N, parts;
+  uint32_t M, N, cols, parts;       // cols: a power of two
   __bf16* dz;                       // rows dz_stride apart; null: only the sums
   uint64_t dz_stride;
   float* part;                      // [parts, N], or null
 };
+constexpr uint32_t kDzBS = 256;
 
-template <int DT, int ACT> __global__ __launch_bounds__(256) void k_dz(DzArgs a) {
-  const uint32_t j = (blockIdx.x * 256 + threadIdx.x) * 8, p = blockIdx.y;
-  if (j >= a.N) return;
+template <int DT, int ACT> __global__ __launch_bounds__(kDzBS) void k_dz(DzArgs a) {
+  __shared__ float s[kDzBS][8];
   constexpr uint32_t ES = DT == PROFK_F32 ? 4 : 2;
+  const uint32_t rows = kDzBS / a.cols, sub = threadIdx.x / a.cols;
+  const uint32_t j = (blockIdx.x * a.cols + threadIdx.x % a.cols) * 8, p = blockIdx.y;
   const uint32_t r0 = static_cast<uint32_t>(static_cast<uint64_t>(a.M) * p / a.parts);
   const uint32_t r1 = static_cast<uint32_t>(static_cast<uint64_t>(a.M) * (p + 1) / a.parts);
   float sum[8] = {}, d[8], z[8];
-  for (uint32_t r = r0; r < r1; ++r) {
+  for (uint32_t r = j < a.N ? r0 + sub : r1; r < r1; r += rows) {
     load<DT, 8>(static_cast<const char*>(a.dy) + r * a.dy_stride * ES, j, a.N, d);
     if constexpr (ACT != PROFK_ACT_NONE) {
       load<DT, 8>(static_cast<const char*>(a.pre) + static_cast<uint64_t>(r) * a.N * ES, j, a.N, z);
@@ -155,7 +158,19 @@ template <int DT, int ACT> __global__ __launch_bounds__(256) void k_dz(DzArgs a)
     for (int e = 0; e < 8; ++e) sum[e] += d[e];
     if (a.dz) store<PROFK_BF16, 8>(a.dz + r * a.dz_stride, j, static_cast<uint32_t>(a.dz_stride), d);   // (0 past N)
   }
-  if (a.part) store<PROFK_F32, 8>(a.part + static_cast<size_t>(p) * a.N, j, a.N, sum);
+  if (!a.part) return;
+  if (rows > 1) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) s[threadIdx.x][e] = sum[e];
+    __syncthreads();
+    if (sub == 0) {
+      for (uint32_t k = 1; k < rows; ++k) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) sum[e] += s[k * a.cols + threadIdx.x][e];
+      }
+    }
+  }
+  if (sub == 0 && j < a.N) store<PROFK_F32, 8>(a.part + static_cast<size_t>(p) * a.N, j, a.N, sum);
 }
 
 __global__ __launch_bounds__(kJoinBS) void k_db_join(const float* part, uint32_t parts, uint32_t N, float* db) {
@@ -166,9 +181,18 @@ __global__ __launch_bounds__(kJoinBS) void k_db_join(const float* part, uint32_t
   }
 }
 
+// Threads of 8 columns of a workgroup of k_dz.
+uint32_t dz_cols(int64_t N) {
+  uint32_t cols = 1;
+  while (cols < kDzBS && cols * 8 < N) cols *= 2;
+  return cols;
+}
+// Parts of the rows: each thread has a few of them, and no more workgroups than
+// the CUs hold.  (The sums of few rows are one part, and need no join.)
 uint32_t dz_parts(int64_t M, int64_t N, int num_cus) {
-  const int64_t slabs = N > 0 ? (N + 2047) / 2048 : 1, most = (static_cast<int64_t>(num_cus) * 8 + slabs - 1) / slabs;
-  const int64_t parts = M < most ? M : most;
+  const int64_t cols = dz_cols(N), rows = kDzBS / cols;
+  const int64_t slabs = N > 0 ? (N + cols * 8 - 1) / (cols * 8) : 1, most = (static_cast<int64_t>(num_cus) * 8 + slabs - 1) / slabs;
+  const int64_t want = (M + rows * 4 - 1) / (rows * 4), parts = want < most ? want : most;
   return parts < 1 ? 1u : static_cast<uint32_t>(parts);
 }
 
@@ -306,19 +330,20 @@ hipError_t launch_linear_grad(const LinGradCall& c, hipStream_t s) {
   // (without an activation, dy in bf16 is dz)
   const bool given = c.act == PROFK_ACT_NONE && c.dtype == PROFK_BF16 && granules(c.dy, c.dy_stride, N, false);
   const bool dx = c.dx && M, dw = c.dw && N;
-  const DzArgs d{c.dy, c.pre, c.dy_stride, M, N, L.parts, (dx || dw) && !given ? dz : nullptr, L.dz_stride,
-                 c.db ? part : nullptr};
+  const uint32_t cols = dz_cols(N);
+  const DzArgs d{c.dy, c.pre, c.dy_stride, M, N, cols, L.parts, (dx || dw) && !given ? dz : nullptr, L.dz_stride,
+                 !c.db ? nullptr : L.parts == 1 ? c.db : part};
   (void)hipGetLastError();
   hipError_t e = hipSuccess;
   if (N && (d.dz || d.part)) {
-    const dim3 grid((N + 2047) / 2048, L.parts);
+    const dim3 grid((N + cols * 8 - 1) / (cols * 8), L.parts);
     with_act(c.act, [&](auto act) {
-      if (c.dtype == PROFK_F32) k_dz<PROFK_F32, decltype(act)::value><<<grid, 256, 0, s>>>(d);
-      else k_dz<PROFK_BF16, decltype(act)::value><<<grid, 256, 0, s>>>(d);
+      if (c.dtype == PROFK_F32) k_dz<PROFK_F32, decltype(act)::value><<<grid, kDzBS, 0, s>>>(d);
+      else k_dz<PROFK_BF16, decltype(act)::value><<<grid, kDzBS, 0, s>>>(d);
     });
     e = hipGetLastError();
   }
-  if (e == hipSuccess && c.db && N) {
+  if (e == hipSuccess && c.db && N && L.parts > 1) {
     const uint32_t blocks = (N + kJoinCols - 1) / kJoinCols;   // (a launch holds fewer than 2^32 threads)
     k_db_join<<<blocks < 65536 ? blocks : 65536, kJoinBS, 0, s>>>(part, L.parts, N, c.db);
     e = hipGetLastError();

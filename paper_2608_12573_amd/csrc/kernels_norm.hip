@@ -87,6 +87,13 @@ template <int E> __device__ __forceinline__ void store_sums(float* row, uint32_t
   for (int k = 0; k < E; k += 4) store<PROFK_F32, 4>(row, i + k, D, {v[k], v[k + 1], v[k + 2], v[k + 3]});
 }
 
+template <int E>
+__device__ __forceinline__ void store_param(void* p, int dtype, uint32_t i, uint32_t D, const float (&v)[E]) {
+  if (!p) return;
+  if (dtype == PROFK_F32) store_sums<E>(static_cast<float*>(p), i, D, v);
+  else store<PROFK_BF16, E>(p, i, D, v);
+}
+
 // A row in the registers of GS threads, C8 times 8 elements each, R rows a
 // workgroup; workgroups go through the rows, the scale and shift kept in
 // registers and the next row loaded under this one.
@@ -297,8 +304,14 @@ template <int XDT, int YDT, int GS, int R, int C8> __global__ __launch_bounds__(
   }
 #pragma unroll
   for (int c = 0; c < C; ++c) {
-    store_sums<E>(part, (c * GS + t) * E, a.D, dw[c]);
-    store_sums<E>(part + a.D, (c * GS + t) * E, a.D, db[c]);
+    const uint32_t i = (c * GS + t) * E;
+    if (a.parts == 1) {           // (no join follows)
+      store_param<E>(a.dw, a.p_dtype, i, a.D, dw[c]);
+      store_param<E>(a.db, a.p_dtype, i, a.D, db[c]);
+    } else {
+      store_sums<E>(part, i, a.D, dw[c]);
+      store_sums<E>(part + a.D, i, a.D, db[c]);
+    }
   }
 }
 
@@ -360,8 +373,13 @@ template <int XDT, int YDT> __global__ __launch_bounds__(256) void k_norm_cols(N
     }
   }
   float* const part = a.part + static_cast<size_t>(p) * 2 * a.D;
-  store_sums<E>(part, i, a.D, dw);
-  store_sums<E>(part + a.D, i, a.D, db);
+  if (a.parts == 1) {
+    store_param<E>(a.dw, a.p_dtype, i, a.D, dw);
+    store_param<E>(a.db, a.p_dtype, i, a.D, db);
+  } else {
+    store_sums<E>(part, i, a.D, dw);
+    store_sums<E>(part + a.D, i, a.D, db);
+  }
 }
 
 // The parts' sums to dw and db.
@@ -477,7 +495,7 @@ hipError_t launch_norm_grad(const NormGradArgs& a, int dtype, int dy_dtype, hipS
     else norm_grad_rows<PROFK_BF16, PROFK_BF16>(a, cus, s);
   }
   hipError_t e = hipGetLastError();
-  if (e != hipSuccess || !a.part) return e;
+  if (e != hipSuccess || !a.part || a.parts == 1) return e;
   k_norm_join<<<(2 * a.D + kJoinCols - 1) / kJoinCols, kJoinBS, 0, s>>>(a);
   return hipGetLastError();
 }
