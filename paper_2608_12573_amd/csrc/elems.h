@@ -1,8 +1,7 @@
 // Neighbouring elements of a row to and from fp32, and sums over a wave.
 //
-// Lanes take 16 bytes each of the widest type at hand, so that a wave's access is
-// one run of memory: 4 elements where one of the tensors is fp32, else 8.  (With 8
-// fp32 a lane, two accesses of every other 16 bytes, .. )
+// Lanes take 16 bytes of the widest type at hand in an access, so that a wave's is
+// one run of memory: 4 elements where one of the tensors is fp32, else 8.
 #pragma once
 
 #include <type_traits>

@@ -83,9 +83,15 @@ struct ProdPlan {
 };
 ProdPlan plan_product(uint64_t I, uint64_t J, uint64_t K, uint32_t cus);
 
+// The rows that the kernel of few rows takes.  From 17 it reads a as often as b, and
+// is the faster one where the tiles of 128 columns do not fill the CUs (us, 32 rows
+// here and 33 there: 4096 x 4096 10.6 and 14.9; 4096 x 12288 31.4 and 27.0, 1024 x
+// 50000 36.0 and 25.8).
+inline bool few_rows(uint64_t I, uint64_t J, uint32_t cus) { return I <= 16 || (I <= 32 && J < 32 * cus); }
+
 // The product of few rows, and the tiled one; false: these operands are not
 // aligned as they need them.
-bool launch_product_few(const ProdArgs& g, uint32_t cus, hipStream_t s);                // A and B along k, I <= 32
+bool launch_product_few(const ProdArgs& g, uint32_t cus, hipStream_t s);                // A and B along k, few_rows
 bool launch_product_along(ProdArgs g, const ProdPlan& p, float* sums, uint32_t cus, hipStream_t s);   // A and B along k
 bool launch_product_grad(ProdArgs g, bool a_across, const ProdPlan& p, float* sums, uint32_t cus,
                          hipStream_t s);                                               // B across k, A as said
