@@ -170,8 +170,11 @@ template <int NG, int XL, bool KSPLIT> __global__ __launch_bounds__(kFewBS) void
 
 template <int NG, int XL> void few_launch(const ProdArgs& g, uint32_t cus, hipStream_t s) {
   const uint32_t groups = (g.J + NG * 16 - 1) / (NG * 16), steps = (g.K + kFewK - 1) / kFewK;
-  // (each wave has a step: all meet at the barriers, whose number is that of the groups)
-  if (steps >= 8) {
+  // The waves share K where the groups are few, and where K is long (1 x K x N, us,
+  // shared and not: 1024 x 12288 8.2 and 8.9, x 50000 22.9 and 23.0, x 131072 52.5 and
+  // 48.1; 512 x 131072 33.0 and 26.9; 2048 x 131072 90.7 and 110.0).  (Each then has a
+  // step: all meet at the barriers, whose number is that of the groups.)
+  if (steps >= 32 || (steps >= 8 && groups < 4 * cus)) {
     const uint32_t most = few_per_cu(NG, XL, true) * cus;
     k_prod_few<NG, XL, true><<<groups < most ? groups : most, kFewBS, 0, s>>>(g);
   } else {
