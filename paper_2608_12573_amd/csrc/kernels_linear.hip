@@ -140,11 +140,11 @@ struct DzArgs {
 };
 constexpr uint32_t kDzBS = 256;
 
-template <int DT, int ACT> __global__ __launch_bounds__(kDzBS) void k_dz(DzArgs a) {
+template <int DT, int ACT> __device__ __forceinline__ void dz_body(const DzArgs& a, uint32_t slab, uint32_t p) {
   __shared__ float s[kDzBS][8];
   constexpr uint32_t ES = DT == PROFK_F32 ? 4 : 2;
   const uint32_t rows = kDzBS / a.cols, sub = threadIdx.x / a.cols;
-  const uint32_t j = (blockIdx.x * a.cols + threadIdx.x % a.cols) * 8, p = blockIdx.y;
+  const uint32_t j = (slab * a.cols + threadIdx.x % a.cols) * 8;
   const uint32_t r0 = static_cast<uint32_t>(static_cast<uint64_t>(a.M) * p / a.parts);
   const uint32_t r1 = static_cast<uint32_t>(static_cast<uint64_t>(a.M) * (p + 1) / a.parts);
   float sum[8] = {}, d[8], z[8];
@@ -174,6 +174,36 @@ template <int DT, int ACT> __global__ __launch_bounds__(kDzBS) void k_dz(DzArgs 
   if (sub == 0 && j < a.N) store<PROFK_F32, 8>(a.part + static_cast<size_t>(p) * a.N, j, a.N, sum);
 }
 
+// Two matrices (either may have no rows) of any stride and alignment, to rows of
+// whole 16-byte granules, zeros past K.
+struct PadArgs {
+  const __bf16* x[2];
+  uint64_t stride[2];
+  uint32_t R[2], K;
+  __bf16* out[2];
+};
+__device__ __forceinline__ void pad_body(const PadArgs& a, uint32_t block, uint32_t blocks) {
+  const uint32_t per = (a.K + 7) / 8;
+#pragma unroll
+  for (int m = 0; m < 2; ++m) {
+    const uint64_t n = static_cast<uint64_t>(a.R[m]) * per;
+    for (uint64_t i = block * uint64_t{256} + threadIdx.x; i < n; i += blocks * uint64_t{256}) {
+      const uint32_t r = static_cast<uint32_t>(i / per), k = static_cast<uint32_t>(i % per) * 8;
+      reinterpret_cast<u32x4*>(a.out[m])[i] =
+          __builtin_bit_cast(u32x4, load_raw<PROFK_BF16, 8>(a.x[m] + r * a.stride[m], k, a.K));
+    }
+  }
+}
+__global__ __launch_bounds__(256) void k_pad(PadArgs a) { pad_body(a, blockIdx.x, gridDim.x); }
+
+// dz, in dz_blocks workgroups, and the copies beside it.
+template <int DT, int ACT> __global__ __launch_bounds__(kDzBS) void k_dz(DzArgs a, uint32_t slabs, uint32_t dz_blocks, PadArgs p) {
+  static_assert(kDzBS == 256, "pad_body");
+  if (blockIdx.x < dz_blocks) dz_body<DT, ACT>(a, blockIdx.x % slabs, blockIdx.x / slabs);
+  else pad_body(p, blockIdx.x - dz_blocks, gridDim.x - dz_blocks);
+}
+
+
 __global__ __launch_bounds__(kJoinBS) void k_db_join(const float* part, uint32_t parts, uint32_t N, float* db) {
   for (uint32_t b = blockIdx.x; b < (N + kJoinCols - 1) / kJoinCols; b += gridDim.x) {
     const float sum = join_parts(part, parts, N, b);
@@ -199,40 +229,23 @@ uint32_t dz_parts(int64_t M, int64_t N, int num_cus) {
 
 size_t align256(size_t n) { return (n + 255) / 256 * 256; }
 
-// Two matrices (either may have no rows) of any stride and alignment, to rows of
-// whole 16-byte granules, zeros past K.
-struct PadArgs {
-  const __bf16* x[2];
-  uint64_t stride[2];
-  uint32_t R[2], K;
-  __bf16* out[2];
-};
-__global__ __launch_bounds__(256) void k_pad(PadArgs a) {
-  const uint32_t per = (a.K + 7) / 8, m = blockIdx.y;
-  const uint64_t n = static_cast<uint64_t>(a.R[m]) * per;
-  for (uint64_t i = blockIdx.x * uint64_t{256} + threadIdx.x; i < n; i += gridDim.x * uint64_t{256}) {
-    const uint32_t r = static_cast<uint32_t>(i / per), k = static_cast<uint32_t>(i % per) * 8;
-    reinterpret_cast<u32x4*>(a.out[m])[i] = __builtin_bit_cast(u32x4, load_raw<PROFK_BF16, 8>(a.x[m] + r * a.stride[m], k, a.K));
-  }
-}
-
 uint64_t padded(int64_t K) { return (static_cast<uint64_t>(K) + 7) / 8 * 8; }
 size_t pad_bytes(int64_t R, int64_t K) { return K % 8 ? align256(static_cast<size_t>(R) * padded(K) * 2) : 0; }
 
 // Operands whose rows are not whole granules (K % 8) are copied, a pass over
 // them, for the tiled product (the product of any operands took 140 us for the
 // gradients of 509 x 1001 x 777 instead of 40).
-hipError_t pad(const void* x, uint64_t x_stride, int64_t M, __bf16* x_out, const void* w, uint64_t w_stride, int64_t N,
-               __bf16* w_out, int64_t K, hipStream_t s) {
-  const PadArgs a{{static_cast<const __bf16*>(x), static_cast<const __bf16*>(w)},
-                  {x_stride, w_stride},
-                  {static_cast<uint32_t>(M), static_cast<uint32_t>(N)},
-                  static_cast<uint32_t>(K),
-                  {x_out, w_out}};
-  const uint64_t blocks = (static_cast<uint64_t>(M > N ? M : N) * (padded(K) / 8) + 255) / 256;
-  if (blocks == 0) return hipSuccess;
-  k_pad<<<dim3(blocks < 8192 ? static_cast<uint32_t>(blocks) : 8192, 2), 256, 0, s>>>(a);
-  return hipGetLastError();
+PadArgs pad_args(const void* x, uint64_t x_stride, int64_t M, __bf16* x_out, const void* w, uint64_t w_stride, int64_t N,
+                 __bf16* w_out, int64_t K) {
+  return {{static_cast<const __bf16*>(x), static_cast<const __bf16*>(w)},
+          {x_stride, w_stride},
+          {static_cast<uint32_t>(M), static_cast<uint32_t>(N)},
+          static_cast<uint32_t>(K),
+          {x_out, w_out}};
+}
+uint32_t pad_blocks(const PadArgs& a) {
+  const uint64_t blocks = (static_cast<uint64_t>(a.R[0] > a.R[1] ? a.R[0] : a.R[1]) * ((a.K + 7) / 8) + 255) / 256;
+  return blocks < 8192 ? static_cast<uint32_t>(blocks) : 8192;
 }
 
 // Bytes of the sums of K's parts of an I x J product.
@@ -270,7 +283,7 @@ GradLayout grad_layout(int64_t M, int64_t N, int64_t K, int num_cus) {
 // close: 4096 x 12288 by 2048 takes 193 us as two parts with their join, 197 as
 // small tiles).
 ProdPlan plan_product(uint64_t I, uint64_t J, uint64_t K, uint32_t cus) {
-  ProdPlan best{false, 1, 0};
+  ProdPlan best{false, 1, 0, 0.0};
   if (!I || !J || !K) return best;
   double least = 0.0;
   for (int large = 0; large < 2; ++large) {
@@ -285,11 +298,22 @@ ProdPlan plan_product(uint64_t I, uint64_t J, uint64_t K, uint32_t cus) {
       if (parts > 1) us += 4.0 + static_cast<double>(parts) * static_cast<double>(I) * static_cast<double>(J) * 8.0 / 6e6;
       if ((!large && parts == 1) || us < least) {
         least = us;
-        best = {large == 1, parts, static_cast<uint32_t>(part_k)};
+        best = {large == 1, parts, static_cast<uint32_t>(part_k), us};
       }
     }
   }
   return best;
+}
+
+// The two products of a gradient whose small tiles the CUs hold all at once cost
+// the longer one's stages, and a launch less (3 us).
+bool plan_pair(uint64_t M, uint64_t N, uint64_t K, uint32_t cus) {
+  if (!M || !N || !K) return false;
+  const auto tiles = [](uint64_t a, uint64_t b) { return ((a + 127) / 128 + 7) / 8 * 8 * ((b + 127) / 128); };
+  const uint64_t items = tiles(M, K) + tiles(N, K);
+  if (items > 2 * uint64_t{cus}) return false;
+  const double pair = static_cast<double>(((M > N ? M : N) + 127) / 128 * 2) * (items <= cus ? 0.55 : 0.95);
+  return pair <= plan_product(M, K, N, cus).us + plan_product(N, K, M, cus).us + 3.0;
 }
 
 size_t lin_workspace(int64_t M, int64_t N, int64_t K, int num_cus) {
@@ -310,7 +334,9 @@ hipError_t launch_linear(const LinCall& c, hipStream_t s) {
   if (c.K % 8) {
     __bf16* const x = reinterpret_cast<__bf16*>(ws);
     __bf16* const w = reinterpret_cast<__bf16*>(ws + pad_bytes(c.M, c.K));
-    const hipError_t e = pad(c.x, c.x_stride, c.M, x, c.w, c.w_stride, c.N, w, c.K, s);
+    const PadArgs p = pad_args(c.x, c.x_stride, c.M, x, c.w, c.w_stride, c.N, w, c.K);
+    k_pad<<<pad_blocks(p), 256, 0, s>>>(p);
+    const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     g.a = x;
     g.b = w;
@@ -320,7 +346,7 @@ hipError_t launch_linear(const LinCall& c, hipStream_t s) {
   if (launch_product_few(g, cus, s)) return hipGetLastError();
   float* const sums = reinterpret_cast<float*>(ws + pad_bytes(c.M, c.K) + pad_bytes(c.N, c.K));
   // (few rows that are not aligned have no workspace for parts)
-  const ProdPlan p = few_rows(g.I, g.J, cus) ? ProdPlan{false, 1, 0} : plan_product(g.I, g.J, g.K, cus);
+  const ProdPlan p = few_rows(g.I, g.J, cus) ? ProdPlan{false, 1, 0, 0.0} : plan_product(g.I, g.J, g.K, cus);
   if (launch_product_along(g, p, sums, cus, s)) return hipGetLastError();
   return launch_any<false, false>(g, s);
 }
@@ -338,13 +364,16 @@ hipError_t launch_linear_grad(const LinGradCall& c, hipStream_t s) {
   const uint32_t cols = dz_cols(N);
   const DzArgs d{c.dy, c.pre, c.dy_stride, M, N, cols, L.parts, (dx || dw) && !given ? dz : nullptr, L.dz_stride,
                  !c.db ? nullptr : L.parts == 1 ? c.db : part};
+  // the copies of W and x, where their rows are not whole granules, beside dz
+  const PadArgs p = pad_args(c.x, c.x_stride, K % 8 && dw ? M : 0, reinterpret_cast<__bf16*>(ws + L.x), c.w, c.w_stride,
+                             K % 8 && dx ? N : 0, reinterpret_cast<__bf16*>(ws + L.w), K);
+  const uint32_t slabs = N && (d.dz || d.part) ? (N + cols * 8 - 1) / (cols * 8) : 0, dz_blocks = slabs * L.parts;
   (void)hipGetLastError();
   hipError_t e = hipSuccess;
-  if (N && (d.dz || d.part)) {
-    const dim3 grid((N + cols * 8 - 1) / (cols * 8), L.parts);
+  if (const uint32_t blocks = dz_blocks + pad_blocks(p)) {
     with_act(c.act, [&](auto act) {
-      if (c.dtype == PROFK_F32) k_dz<PROFK_F32, decltype(act)::value><<<grid, kDzBS, 0, s>>>(d);
-      else k_dz<PROFK_BF16, decltype(act)::value><<<grid, kDzBS, 0, s>>>(d);
+      if (c.dtype == PROFK_F32) k_dz<PROFK_F32, decltype(act)::value><<<blocks, kDzBS, 0, s>>>(d, slabs, dz_blocks, p);
+      else k_dz<PROFK_BF16, decltype(act)::value><<<blocks, kDzBS, 0, s>>>(d, slabs, dz_blocks, p);
     });
     e = hipGetLastError();
   }
@@ -363,28 +392,22 @@ hipError_t launch_linear_grad(const LinGradCall& c, hipStream_t s) {
   g.J = K;
   g.act = PROFK_ACT_NONE;
   g.out_dtype = PROFK_BF16;
-  // b: W or x, copied where its rows are not whole granules
-  if (e == hipSuccess && g.b_padded && (dx || dw))
-    e = pad(c.x, c.x_stride, dw ? M : 0, reinterpret_cast<__bf16*>(ws + L.x), c.w, c.w_stride, dx ? N : 0,
-            reinterpret_cast<__bf16*>(ws + L.w), K, s);
-  auto other = [&](const void* p, uint64_t stride, size_t copy) {
-    g.b = g.b_padded ? reinterpret_cast<const __bf16*>(ws + copy) : static_cast<const __bf16*>(p);
-    g.bs = g.b_padded ? padded(K) : stride;
+  // b: W or x, or its copy
+  auto product = [&](const void* b, uint64_t stride, size_t copy, uint32_t I, uint32_t k, void* out) {
+    ProdArgs o = g;
+    o.b = g.b_padded ? reinterpret_cast<const __bf16*>(ws + copy) : static_cast<const __bf16*>(b);
+    o.bs = g.b_padded ? padded(K) : stride;
+    o.I = I;
+    o.K = k;
+    o.out = out;
+    return o;
   };
-  if (e == hipSuccess && dx) {
-    other(c.w, c.w_stride, L.w);
-    g.I = M;
-    g.K = N;
-    g.out = c.dx;
-    e = launch_product_grad(g, false, plan_product(M, K, N, cus), sums, cus, s) ? hipGetLastError() : launch_any<false, true>(g, s);
-  }
-  if (e == hipSuccess && dw) {
-    other(c.x, c.x_stride, L.x);
-    g.I = N;
-    g.K = M;
-    g.out = c.dw;
-    e = launch_product_grad(g, true, plan_product(N, K, M, cus), sums, cus, s) ? hipGetLastError() : launch_any<true, true>(g, s);
-  }
+  const ProdArgs gx = product(c.w, c.w_stride, L.w, M, N, c.dx), gw = product(c.x, c.x_stride, L.x, N, M, c.dw);
+  if (e == hipSuccess && dx && dw && plan_pair(M, N, K, cus) && launch_product_pair(gx, gw, s)) return hipGetLastError();
+  if (e == hipSuccess && dx)
+    e = launch_product_grad(gx, false, plan_product(M, K, N, cus), sums, cus, s) ? hipGetLastError() : launch_any<false, true>(gx, s);
+  if (e == hipSuccess && dw)
+    e = launch_product_grad(gw, true, plan_product(N, K, M, cus), sums, cus, s) ? hipGetLastError() : launch_any<true, true>(gw, s);
   return e;
 }
 

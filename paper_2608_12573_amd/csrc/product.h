@@ -80,8 +80,11 @@ template <class F> void with_act(int act, F f) {
 struct ProdPlan {
   bool large;
   uint32_t parts, part_k;
+  double us;                        // its cost
 };
 ProdPlan plan_product(uint64_t I, uint64_t J, uint64_t K, uint32_t cus);
+// Both products of a gradient in one launch are the faster way.
+bool plan_pair(uint64_t M, uint64_t N, uint64_t K, uint32_t cus);
 
 // The rows that the kernel of few rows takes.  From 17 it reads a as often as b, and
 // is the faster one where the tiles of 128 columns do not fill the CUs (us, 32 rows
@@ -95,6 +98,9 @@ bool launch_product_few(const ProdArgs& g, uint32_t cus, hipStream_t s);        
 bool launch_product_along(ProdArgs g, const ProdPlan& p, float* sums, uint32_t cus, hipStream_t s);   // A and B along k
 bool launch_product_grad(ProdArgs g, bool a_across, const ProdPlan& p, float* sums, uint32_t cus,
                          hipStream_t s);                                               // B across k, A as said
+
+// ... B across k: dx (A along) and dW (A across) at once, unsplit, in small tiles.
+bool launch_product_pair(const ProdArgs& dx, const ProdArgs& dw, hipStream_t s);
 
 // Operands that the tiled product takes: rows of whole 16-byte granules.  `len`
 // is the length of a row.

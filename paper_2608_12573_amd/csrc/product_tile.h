@@ -175,18 +175,16 @@ template <bool ACROSS, int BW, int Q, int F, bool PERM, bool WHOLE> struct ProdS
 // g.part_k, a whole number of two stages (the last may hold less), each a tile of
 // its own whose sums go to g.out [parts, I, J].
 template <bool TA, bool TB, int ACT, int DT, int WM, int WN, int MI, int NJ, bool WHOLE, bool SPLIT>
-__device__ __forceinline__ void prod_body(const ProdArgs& g, uint32_t tiles_i, uint32_t tiles) {
+__device__ __forceinline__ void prod_body(const ProdArgs& g, uint32_t tiles_i, uint32_t tiles, uint32_t block,
+                                          uint32_t blocks, uint4* s0, uint4* s1) {
   static_assert(!SPLIT || (!WHOLE && ACT == PROFK_ACT_NONE && DT == PROFK_F32), "sums of parts");
   using T = ProdTile<WM, WN, MI, NJ>;
-  // distinct arrays, so that the compiler can tell the stage being read from
-  // the one being filled
-  __shared__ __align__(16) uint4 s0[T::kGran], s1[T::kGran];
   // workgroup b runs on XCD b % 8: each XCD takes a run of tiles, and goes through
   // panels of kPanel column tiles row by row, so that what it works on at a time
   // is near a square, which shares most in its L2
-  const uint32_t xcd = blockIdx.x % kProdXcds, per_xcd = gridDim.x / kProdXcds;   // (the grid is a multiple of 8)
+  const uint32_t xcd = block % kProdXcds, per_xcd = blocks / kProdXcds;   // (a multiple of 8)
   const uint32_t end = static_cast<uint32_t>(static_cast<uint64_t>(tiles) * (xcd + 1) / kProdXcds);
-  const uint32_t tile0 = static_cast<uint32_t>(static_cast<uint64_t>(tiles) * xcd / kProdXcds) + blockIdx.x / kProdXcds;
+  const uint32_t tile0 = static_cast<uint32_t>(static_cast<uint64_t>(tiles) * xcd / kProdXcds) + block / kProdXcds;
   if (tile0 >= end) return;
   // a tile takes an even number of stages, so that each starts at the same one
   const uint32_t tile_k = SPLIT ? g.part_k : g.K, of_part = SPLIT ? tiles / g.parts : tiles;
@@ -447,7 +445,17 @@ __device__ __forceinline__ void prod_body(const ProdArgs& g, uint32_t tiles_i, u
 
 template <bool TA, bool TB, int ACT, int DT, int WM, int WN, int MI, int NJ, int WAVES, bool WHOLE, bool SPLIT>
 __global__ __launch_bounds__(WM * WN * 64, WAVES) void k_prod(ProdArgs g, uint32_t tiles_i, uint32_t tiles) {
-  prod_body<TA, TB, ACT, DT, WM, WN, MI, NJ, WHOLE, SPLIT>(g, tiles_i, tiles);
+  using T = ProdTile<WM, WN, MI, NJ>;
+  // distinct arrays, so that the compiler can tell the stage being read from the
+  // one being filled
+  __shared__ __align__(16) uint4 s0[T::kGran], s1[T::kGran];
+  prod_body<TA, TB, ACT, DT, WM, WN, MI, NJ, WHOLE, SPLIT>(g, tiles_i, tiles, blockIdx.x, gridDim.x, s0, s1);
+}
+
+// Workgroups of a launch over `tiles`.
+inline uint32_t prod_grid(uint32_t tiles, uint32_t most) {
+  const uint32_t grid = (tiles + kProdXcds - 1) / kProdXcds * kProdXcds;
+  return grid > most ? most / kProdXcds * kProdXcds : grid;
 }
 
 // PER: workgroups a CU holds.
@@ -455,8 +463,7 @@ template <bool TA, bool TB, int ACT, int DT, int WM, int WN, int MI, int NJ, int
 void launch_tiles(const ProdArgs& g, uint32_t cus, hipStream_t s) {
   using T = ProdTile<WM, WN, MI, NJ>;
   const uint32_t ti = (g.I + T::BM - 1) / T::BM, tj = (g.J + T::BN - 1) / T::BN, tiles = ti * tj * (SPLIT ? g.parts : 1);
-  uint32_t grid = (tiles + kProdXcds - 1) / kProdXcds * kProdXcds;
-  if (grid > PER * cus) grid = PER * cus / kProdXcds * kProdXcds;
+  const uint32_t grid = prod_grid(tiles, PER * cus);
   constexpr int kWaves = PER * WM * WN / 4;
   if constexpr (SPLIT) {
     k_prod<TA, TB, ACT, DT, WM, WN, MI, NJ, kWaves, false, true><<<grid, T::BS, 0, s>>>(g, ti, tiles);

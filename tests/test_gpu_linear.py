@@ -122,6 +122,24 @@ def test_grad(M, K, N, act, dt):
     _grad(M, K, N, act, dt, M + K + N)
 
 
+@pytest.mark.parametrize("M,K,N", [(8, 8, 8), (1500, 1000, 24), (24, 1500, 1000), (1000, 24, 1500), (1024, 1024, 1024),
+                                   (2049, 1031, 515), (2304, 1032, 520), (3000, 2000, 128)])
+@pytest.mark.parametrize("need", [(True, True, True), (True, True, False), (True, False, True), (False, True, True)])
+def test_both_products_at_once_and_each_alone(M, K, N, need):
+    note(f"linear_grad {M}x{K}x{N} {need}")
+    x, w, b, g = _inputs(M, K, N, 12)
+    dy = torch.randn((M, N), generator=g).bfloat16().cuda()
+    got = pk.linear_grad(dy, x, w, need=need)
+    X, W, G = _np(x), _np(w), _np(dy)
+    ex, ew, eb, _ = dense.linear_grad(G, X, W, None)
+    for t, want, tol in ((got[0], ex, (N + 2) * U * (np.abs(G) @ np.abs(W)) + BF * np.abs(ex) + 1e-38),
+                         (got[1], ew, (M + 2) * U * (np.abs(G).T @ np.abs(X)) + BF * np.abs(ew) + 1e-38),
+                         (got[2], eb, (M + 20) * U * np.abs(G).sum(axis=0) + U * np.abs(eb) + 1e-38)):
+        if t is not None:
+            _check(t, want, tol, "gradient")
+    assert [t is not None for t in got] == list(need)
+
+
 @pytest.mark.parametrize("M,K,N", [(4096, 4096, 64), (72, 4200, 4104), (4200, 72, 4104), (4100, 4360, 40)])
 @pytest.mark.parametrize("act", [None, "gelu"])
 def test_grad_of_large_tiles(M, K, N, act):
