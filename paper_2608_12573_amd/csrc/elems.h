@@ -122,13 +122,17 @@ __device__ __forceinline__ float load1(const void* row, uint32_t i, int dtype) {
 template <int CTRL> __device__ __forceinline__ float dpp_add(float x) {
   return x + __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), CTRL, 0xF, 0xF, false));
 }
-// The sum over the wave, in every lane: exchanges inside each row of 16 lanes,
-// then the four rows'.
-__device__ __forceinline__ float wave_sum(float x) {
+// The sum over each row of 16 lanes, in every one of them: quad swaps, then half-row
+// and row mirrors.
+__device__ __forceinline__ float sum16(float x) {
   x = dpp_add<0xB1>(x);
   x = dpp_add<0x4E>(x);
   x = dpp_add<0x141>(x);
-  x = dpp_add<0x140>(x);
+  return dpp_add<0x140>(x);
+}
+// The sum over the wave, in every lane.
+__device__ __forceinline__ float wave_sum(float x) {
+  x = sum16(x);
   const int i = __float_as_int(x);
   return (__int_as_float(__builtin_amdgcn_readlane(i, 0)) + __int_as_float(__builtin_amdgcn_readlane(i, 16))) +
          (__int_as_float(__builtin_amdgcn_readlane(i, 32)) + __int_as_float(__builtin_amdgcn_readlane(i, 48)));

@@ -319,6 +319,7 @@ bool plan_pair(uint64_t M, uint64_t N, uint64_t K, uint32_t cus) {
 size_t lin_workspace(int64_t M, int64_t N, int64_t K, int num_cus) {
   const uint32_t cus = static_cast<uint32_t>(num_cus);
   const bool few = few_rows(static_cast<uint64_t>(M), static_cast<uint64_t>(N), cus);
+  if (M <= kFewAny) return 0;
   return pad_bytes(M, K) + pad_bytes(N, K) + (few ? 0 : sums_bytes(M, N, K, cus));
 }
 
@@ -331,6 +332,7 @@ hipError_t launch_linear(const LinCall& c, hipStream_t s) {
   const uint32_t cus = static_cast<uint32_t>(device_cu_count());
   (void)hipGetLastError();
   uint8_t* const ws = static_cast<uint8_t*>(c.ws);
+  if (launch_product_few(g, cus, s) || launch_product_few_any(g, cus, s)) return hipGetLastError();
   if (c.K % 8) {
     __bf16* const x = reinterpret_cast<__bf16*>(ws);
     __bf16* const w = reinterpret_cast<__bf16*>(ws + pad_bytes(c.M, c.K));

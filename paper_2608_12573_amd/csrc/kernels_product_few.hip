@@ -183,7 +183,87 @@ template <int NG, int XL> void few_launch(const ProdArgs& g, uint32_t cus, hipSt
   }
 }
 
+// Up to kFewAny rows of any stride and alignment, with nothing copied: a wave takes
+// four rows of b, its lanes neighbouring eights of k, so that each access is a run of
+// memory whatever it starts at, and sums over its lanes at the end.  The next eights
+// are on their way under the products of these.  Measured: 1 x 4097 x 12288 21 us, 1 x
+// 2049 x 131072 101 us (5.3 TB/s); on the matrix cores, whose fragments are 64 bytes
+// of 16 rows, 48 and 224, and with b copied first 55 and more.
+// L: lanes of a row; 16 where rows are short (1 x 101 x 50001 with 64 17 us).
+constexpr int kDotRows = 4;
+template <int M, int L> __global__ __launch_bounds__(kFewBS) void k_prod_dot(ProdArgs g) {
+  const uint32_t lane = threadIdx.x & (kWave - 1);
+  const uint32_t w = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  constexpr uint32_t kAt = kWave / L, kRows = kDotRows * kAt, kChunk = L * 8;   // rows of an access, of a wave; k of an access
+  const uint32_t quads = (g.J + kRows - 1) / kRows, chunks = (g.K + kChunk - 1) / kChunk, l = lane % L;
+  for (uint32_t q = blockIdx.x * kFewNW + w; q < quads; q += gridDim.x * kFewNW) {
+    const __bf16* b[kDotRows];
+#pragma unroll
+    for (uint32_t r = 0; r < kDotRows; ++r) b[r] = g.b + min(q * kRows + r * kAt + lane / L, g.J - 1) * g.bs;
+    Raw<PROFK_BF16, 8> nb[kDotRows], na[M];
+    auto fetch = [&](uint32_t p) {
+      const uint32_t k = (p * L + l) * 8;
+      // (only the last chunk may be a part: no check in the others, behind which loads
+      // would wait)
+      if ((p + 1) * kChunk <= g.K) {
+#pragma unroll
+        for (int r = 0; r < kDotRows; ++r) nb[r] = __builtin_bit_cast(Raw<PROFK_BF16, 8>, *reinterpret_cast<const u32x4h*>(b[r] + k));
+#pragma unroll
+        for (uint32_t m = 0; m < M; ++m)
+          na[m] = __builtin_bit_cast(Raw<PROFK_BF16, 8>, *reinterpret_cast<const u32x4h*>(g.a + m * g.as + k));
+      } else {
+#pragma unroll
+        for (int r = 0; r < kDotRows; ++r) nb[r] = load_raw<PROFK_BF16, 8>(b[r], k, g.K);
+#pragma unroll
+        for (uint32_t m = 0; m < M; ++m) na[m] = load_raw<PROFK_BF16, 8>(g.a + m * g.as, k, g.K);
+      }
+    };
+    float acc[kDotRows][M] = {};
+    fetch(0);
+    for (uint32_t p = 0; p < chunks; ++p) {
+      float vb[kDotRows][8], va[M][8];
+#pragma unroll
+      for (int r = 0; r < kDotRows; ++r) to_f32<PROFK_BF16, 8>(nb[r], vb[r]);
+#pragma unroll
+      for (int m = 0; m < M; ++m) to_f32<PROFK_BF16, 8>(na[m], va[m]);
+      if (p + 1 < chunks) fetch(p + 1);
+#pragma unroll
+      for (int r = 0; r < kDotRows; ++r)
+#pragma unroll
+        for (int m = 0; m < M; ++m)
+#pragma unroll
+          for (int e = 0; e < 8; ++e) acc[r][m] = fmaf(vb[r][e], va[m][e], acc[r][m]);
+    }
+#pragma unroll
+    for (uint32_t r = 0; r < kDotRows; ++r)
+#pragma unroll
+      for (uint32_t m = 0; m < M; ++m) {
+        const float sum = L == kWave ? wave_sum(acc[r][m]) : sum16(acc[r][m]);
+        const uint32_t j = q * kRows + r * kAt + lane / L;
+        if (l == r * M + m && j < g.J) put(g, m, j, sum);
+      }
+  }
+}
+
 }  // namespace
+
+bool launch_product_few_any(const ProdArgs& g, uint32_t cus, hipStream_t s) {
+  if (g.I > kFewAny) return false;
+  const auto launch = [&](auto m, auto lanes) {
+    constexpr uint32_t kRows = kDotRows * kWave / decltype(lanes)::value * kFewNW;
+    const uint32_t blocks = (g.J + kRows - 1) / kRows, most = 8 * cus;
+    k_prod_dot<decltype(m)::value, decltype(lanes)::value><<<blocks < most ? blocks : most, kFewBS, 0, s>>>(g);
+  };
+  const auto rows = [&](auto m) {
+    if (g.K <= 256) launch(m, std::integral_constant<int, 16>{});
+    else launch(m, std::integral_constant<int, 64>{});
+  };
+  if (g.I == 1) rows(std::integral_constant<int, 1>{});
+  else if (g.I == 2) rows(std::integral_constant<int, 2>{});
+  else if (g.I == 3) rows(std::integral_constant<int, 3>{});
+  else rows(std::integral_constant<int, 4>{});
+  return true;
+}
 
 bool launch_product_few(const ProdArgs& g, uint32_t cus, hipStream_t s) {
   if (!few_rows(g.I, g.J, cus) || !granules(g.a, g.as, g.K, g.a_padded) || !granules(g.b, g.bs, g.K, g.b_padded)) return false;

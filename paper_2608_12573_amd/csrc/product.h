@@ -92,6 +92,9 @@ bool plan_pair(uint64_t M, uint64_t N, uint64_t K, uint32_t cus);
 // 50000 36.0 and 25.8).
 inline bool few_rows(uint64_t I, uint64_t J, uint32_t cus) { return I <= 16 || (I <= 32 && J < 32 * cus); }
 
+// Up to kFewAny rows of operands along k of any stride and alignment; false: more.
+constexpr uint32_t kFewAny = 4;
+bool launch_product_few_any(const ProdArgs& g, uint32_t cus, hipStream_t s);
 // The product of few rows, and the tiled one; false: these operands are not
 // aligned as they need them.
 bool launch_product_few(const ProdArgs& g, uint32_t cus, hipStream_t s);                // A and B along k, few_rows

@@ -91,6 +91,14 @@ def test_many_groups_and_tiles(M, K, N, act, out):
     _linear(M, K, N, act, out, True, act is not None, M + K + N, pre=M < 1000)
 
 
+@pytest.mark.parametrize("M", [1, 2, 3, 4, 5, 16])
+@pytest.mark.parametrize("K,N", [(1, 3), (7, 100), (511, 65), (513, 1000), (1025, 33), (4097, 50), (101, 40003)])
+@pytest.mark.parametrize("act,out,pad", [("gelu", "bf16", 0), (None, "f32", 1)])
+def test_few_odd_rows(M, K, N, act, out, pad):
+    note(f"linear {M}x{K}x{N} {act} {out} rows {pad} longer")
+    _linear(M, K, N, act, out, True, act is not None, M + K + N, pad, pad)
+
+
 @pytest.mark.parametrize("M,K,N", [(1, 4096, 640), (2, 72, 40), (9, 264, 96), (40, 1000, 200), (200, 264, 300), (300, 64, 520)])
 @pytest.mark.parametrize("pad,off", [(1, 0), (0, 1), (3, 2), (8, 0), (8, 8), (4, 4)])
 def test_strides_and_alignment(M, K, N, pad, off):
