@@ -1170,6 +1170,8 @@ def adjust_logits(logits, tokens=None, offsets=None, n_prompt=None, repetition=N
     ids = values = at = None
     n_bias = 0
     if bias is not None:
+        if not isinstance(bias, (tuple, list)) or len(bias) != 3:
+            raise ProfkError("bias must be (ids, values, offsets)")
         ids, values, at = bias
         n_bias = _list(ids, "bias[0]", torch.int64, dev)
         _vector(values, "bias[1]", f32, (n_bias,), dev)

@@ -203,7 +203,6 @@ template <int DT, int ACT> __global__ __launch_bounds__(kDzBS) void k_dz(DzArgs 
   else pad_body(p, blockIdx.x - dz_blocks, gridDim.x - dz_blocks);
 }
 
-
 __global__ __launch_bounds__(kJoinBS) void k_db_join(const float* part, uint32_t parts, uint32_t N, float* db) {
   for (uint32_t b = blockIdx.x; b < (N + kJoinCols - 1) / kJoinCols; b += gridDim.x) {
     const float sum = join_parts(part, parts, N, b);
