@@ -130,6 +130,34 @@ def test_graph_replays(T, D, V):
             assert t.equal(a, b)
 
 
+def test_graph_of_autograd():
+    t = torch()
+    note("autograd's chain captured")
+    T, D, V = 70, 136, 333
+    d = _data(T, D, V, 9)
+    d["allowed"].fill_(-1)
+    g = t.randn(T, device="cuda")
+    leaves = {k: d[k].clone().requires_grad_() for k in ("x", "w", "b", "w1", "c1", "w2")}
+
+    def call():
+        out = _autograd(d, leaves)
+        return (out.detach(),) + t.autograd.grad(out, list(leaves.values()), g)
+
+    graph, out = _captured(call)
+    for seed in (9, 10):
+        fresh = _data(T, D, V, seed)
+        with t.no_grad():
+            for k, v in leaves.items():
+                v.copy_(fresh[k])
+                d[k].copy_(fresh[k])
+        lp, want = _by_hand(d, g)
+        graph.replay()
+        t.cuda.synchronize()
+        assert t.equal(out[0], lp)
+        for a, k in zip(out[1:], leaves):
+            assert t.equal(a, want[k]), k
+
+
 def test_two_streams_at_once():
     t = torch()
     note("chains on two streams")
