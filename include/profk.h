@@ -478,6 +478,9 @@ int profk_layer_norm_grad(int32_t dtype, const void* x, int64_t T, int64_t D, in
  *             be out itself (of stride N).
  *   dx, dW    contiguous bf16 [M, K], [N, K], from dz rounded to bf16; dbias
  *             fp32 [N].  Any of them may be NULL.
+ *   time      rows of x and W that start at multiples of 16 bytes are the fastest.
+ *             Where K is no multiple of 8 both are copied to such rows first (not
+ *             for M <= 4); others at odd places run at about half the rate.
  *   sizes     1 <= K <= 2^20, 0 <= M, N <= 2^31 - 1.  M = 0 sets dW and dbias to
  *             zero, N = 0 dx.
  *   ws        profk_linear_workspace_size(M, K, N) and
