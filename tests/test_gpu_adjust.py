@@ -143,6 +143,18 @@ def test_many_biases(V, n):
     _check(pk.adjust_logits(x, **few), *_want(x, few), "f32")
 
 
+@pytest.mark.parametrize("V", [1, 31, 64, 130, 256, 700, 3000, 9000])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_every_token_marked(V, dtype):
+    note(f"adjust_logits every token of {V} marked {dtype}")
+    x, kw = _case(5, V, dtype, V, masks=2, biases=40)
+    every = torch.arange(V, device="cuda")
+    kw["tokens"] = torch.cat([every, every.flip(0)[:V // 2]]).repeat(5)
+    kw["offsets"] = torch.arange(6, device="cuda") * (V + V // 2)
+    kw["n_prompt"] = torch.tensor([0, V // 3, V, 10 * V, 1], device="cuda")
+    _check(pk.adjust_logits(x, **kw), *_want(x, kw), dtype)
+
+
 @pytest.mark.parametrize("name", ["repetition", "presence", "frequency", "bias", "allowed", None])
 def test_each_alone(name):
     note(f"adjust_logits with {name} alone")
