@@ -290,7 +290,8 @@ def _input(x, name, dims, dtypes=(F32, BF16), layout="contiguous"):
         raise ProfkError(f"{name} must be {' or '.join('float32' if d == F32 else 'bfloat16' for d in dtypes)}")
     if layout == "contiguous" and not x.is_contiguous():
         raise ProfkError(f"{name} must be contiguous (strides {tuple(x.stride())})")
-    if layout == "rows" and (x.stride(1) != 1 or (x.shape[0] > 1 and x.stride(0) < x.shape[1])):
+    # (torch calls a column contiguous whatever the stride between its columns)
+    if layout == "rows" and ((x.shape[1] > 1 and x.stride(1) != 1) or (x.shape[0] > 1 and x.stride(0) < x.shape[1])):
         raise ProfkError(f"{name} must be [B, D] with unit column stride and rows at least D apart "
                          f"(strides {tuple(x.stride())})")
     _on_device(x, name, None)
@@ -600,7 +601,9 @@ def _rows(x, name):
     R, C = x.shape
     s0, s1 = x.stride()
     if s1 != 1 or s0 < C:
-        if R <= 1 and (s1 == 1 or C <= 1):
+        if C <= 1 and s0 >= C:
+            pass
+        elif R <= 1 and (s1 == 1 or C <= 1):
             s0 = C
         else:
             _input(x, name, 2, layout="rows")
