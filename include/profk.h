@@ -476,8 +476,12 @@ int profk_layer_norm_grad(int32_t dtype, const void* x, int64_t T, int64_t D, in
  *             pre contiguous.  pre, where it is not NULL, takes z, rounded, for
  *             the gradient (needed there but for PROFK_ACT_NONE).  residual may
  *             be out itself (of stride N).
- *   dx, dW    contiguous bf16 [M, K], [N, K], from dz rounded to bf16; dbias
- *             fp32 [N].  Any of them may be NULL.
+ *   dx, dW    contiguous bf16 [M, K], [N, K]; dbias fp32 [N].  Any of them may be
+ *             NULL.  Where dz is no bf16 number by itself (dy fp32, gelu, silu) the
+ *             products take it as the sum of two, within 2^-16 of itself.
+ *             PROFK_DZ_BF16, or-ed to the gradient's activation, rounds it to one,
+ *             within 2^-8: about half the products' time.  An infinity or NaN in x
+ *             or W leaves infinities or NaN in all that it enters.
  *   time      rows of x and W that start at multiples of 16 bytes are the fastest.
  *             Where K is no multiple of 8 both are copied to such rows first (not
  *             for M <= 4); others at odd places run at about half the rate.
@@ -488,6 +492,7 @@ int profk_layer_norm_grad(int32_t dtype, const void* x, int64_t T, int64_t D, in
  *             (NULL for 0).
  * Outputs must not overlap inputs otherwise (PROFK_EINVAL). */
 enum { PROFK_ACT_NONE = 0, PROFK_ACT_RELU = 1, PROFK_ACT_GELU = 2, PROFK_ACT_SILU = 3 };
+enum { PROFK_DZ_BF16 = 256 };       /* profk_linear_grad: activation | PROFK_DZ_BF16 */
 size_t profk_linear_workspace_size(int64_t M, int64_t K, int64_t N);
 int profk_linear(const void* x, int64_t M, int64_t K, int64_t x_stride, const void* w, int64_t N, int64_t w_stride,
                  const float* bias, int32_t activation, int32_t out_dtype, const void* residual,

@@ -987,6 +987,7 @@ def layer_norm_grad(dy, x, weight, mean, rstd, ws=None, out=None, need=(True, Tr
 # ----------------------------------------------------------- dense product ---
 
 ACTIVATIONS = {None: 0, "relu": 1, "gelu": 2, "silu": 3}
+DZ_BF16 = 256
 
 
 def _activation(name):
@@ -1014,7 +1015,7 @@ def linear_workspace(M, K, N, device="cuda"):
     return torch.empty(int(lib().profk_linear_workspace_size(M, K, N)), dtype=torch.uint8, device=device)
 
 
-def linear(x, w, bias=None, activation=None, residual=None, dtype=None, ws=None, out=None, pre=None):
+def linear(x, w, bias=None, activation=None, residual=None, dtype=None, ws=None, out=None, pre=None, round_dz=False):
     """act(x W^T + bias) + residual: bf16 x [M, K] and W [N, K] (rows of either
     may be strided), fp32 bias [N]; fp32 (the default) or bf16 [M, N], fp32 sums,
     rounded once.
@@ -1024,8 +1025,8 @@ def linear(x, w, bias=None, activation=None, residual=None, dtype=None, ws=None,
     x W^T + bias, of the output's type, for linear_grad.
 
     Where an input requires a gradient, a new output is differentiable with
-    respect to x, w, bias and residual.  Into a given `out` nothing is recorded:
-    the caller takes linear_grad."""
+    respect to x, w, bias and residual (round_dz: as linear_grad's).  Into a given
+    `out` nothing is recorded: the caller takes linear_grad."""
     torch = _torch()
     M, K, N, xs, wstride = _product(x, w)
     dev = x.device
@@ -1034,7 +1035,7 @@ def linear(x, w, bias=None, activation=None, residual=None, dtype=None, ws=None,
             any(t is not None and t.requires_grad for t in (x, w, bias, residual)):
         if pre is not None:
             raise ProfkError("pre is kept by the recorded call itself")
-        return _differentiable("linear").apply(x, w, bias, residual, activation, dtype, ws)
+        return _differentiable("linear").apply(x, w, bias, residual, activation, dtype, ws, round_dz)
     if bias is not None:
         _vector(bias, "bias", torch.float32, (N,), dev)
     stream = _stream_on(dev)
@@ -1059,12 +1060,14 @@ def linear_grad_workspace(M, K, N, device="cuda"):
     return torch.empty(int(lib().profk_linear_grad_workspace_size(M, K, N)), dtype=torch.uint8, device=device)
 
 
-def linear_grad(dy, x, w, pre=None, activation=None, ws=None, out=None, need=(True, True, True)):
+def linear_grad(dy, x, w, pre=None, activation=None, ws=None, out=None, need=(True, True, True), round_dz=False):
     """The gradients of linear's x, W and bias for dy [M, N] (fp32 or bf16, rows
     may be strided): (dx bf16 [M, K], dW bf16 [N, K], dbias fp32 [N]); the
     residual's is dy.  pre: linear's, of dy's type (not needed without an
     activation).  out: the three, given; a None among them, and what `need` (of
-    new ones) leaves out, is not computed."""
+    new ones) leaves out, is not computed.  round_dz: dz = dy act'(z) enters the
+    products rounded to bf16, within 2^-8 of itself, in about half their time;
+    else within 2^-16."""
     torch = _torch()
     M, K, N, xs, wstride = _product(x, w)
     dev = x.device
@@ -1092,9 +1095,9 @@ def linear_grad(dy, x, w, pre=None, activation=None, ws=None, out=None, need=(Tr
         _bytes_buffer(ws, "ws", n, dev)
     elif n:
         ws = torch.empty(n, dtype=torch.uint8, device=dev)
-    _check(L.profk_linear_grad(ddt, dy.data_ptr(), dstride, _ptr(pre), act, x.data_ptr(), M, K, xs, w.data_ptr(), N,
-                               wstride, _ptr(out[0]), _ptr(out[1]), _ptr(out[2]), ws.data_ptr() if n else None, n,
-                               stream))
+    _check(L.profk_linear_grad(ddt, dy.data_ptr(), dstride, _ptr(pre), act | (DZ_BF16 if round_dz else 0), x.data_ptr(), M,
+                               K, xs, w.data_ptr(), N, wstride, _ptr(out[0]), _ptr(out[1]), _ptr(out[2]),
+                               ws.data_ptr() if n else None, n, stream))
     return out
 
 
@@ -1247,13 +1250,13 @@ def _differentiable(name):
 
     class Linear(torch.autograd.Function):
         @staticmethod
-        def forward(ctx, x, w, bias, residual, activation, dtype, ws):
+        def forward(ctx, x, w, bias, residual, activation, dtype, ws, round_dz):
             pre = None
             if activation is not None and any(ctx.needs_input_grad[:3]):
                 pre = torch.empty((x.shape[0], w.shape[0]), dtype=dtype or torch.float32, device=x.device)
             out = linear(x, w, bias, activation, residual, dtype, ws=ws, pre=pre)
             ctx.save_for_backward(x, w, pre)
-            ctx.activation = activation
+            ctx.activation, ctx.round_dz = activation, round_dz
             return out
 
         @staticmethod
@@ -1263,8 +1266,8 @@ def _differentiable(name):
             need = ctx.needs_input_grad
             d = (None, None, None)
             if any(need[:3]):
-                d = linear_grad(rows(dy), x, w, pre, ctx.activation, need=need[:3])
-            return d + (dy if need[3] else None, None, None, None)
+                d = linear_grad(rows(dy), x, w, pre, ctx.activation, need=need[:3], round_dz=ctx.round_dz)
+            return d + (dy if need[3] else None, None, None, None, None)
 
     class AdjustLogits(torch.autograd.Function):
         @staticmethod

@@ -640,6 +640,8 @@ int profk_linear_grad(int32_t dtype, const void* dy, int64_t dy_stride, const vo
                       const void* x, int64_t M, int64_t K, int64_t x_stride, const void* w, int64_t N,
                       int64_t w_stride, void* dx, void* dw, float* dbias, void* ws, size_t ws_bytes, void* stream) {
   if (!dtype_ok(dtype)) return PROFK_EDTYPE;
+  const bool round_dz = activation >= 0 && activation & PROFK_DZ_BF16;
+  if (round_dz) activation &= ~PROFK_DZ_BF16;
   if (check_linear(M, K, x_stride, N, w_stride, activation) != PROFK_OK || !rows_ok(M, N, dy_stride)) return PROFK_EINVAL;
   if ((!dx || M == 0) && ((!dw && !dbias) || N == 0)) return PROFK_OK;
   if (M > 0 && N > 0 && (!dy || (activation != PROFK_ACT_NONE && !pre) || (dw && !x) || (dx && !w))) return PROFK_ENULL;
@@ -654,7 +656,7 @@ int profk_linear_grad(int32_t dtype, const void* dy, int64_t dy_stride, const vo
     if (overlap(o, sx) || overlap(o, sw) || overlap(o, sd) || overlap(o, sp)) return PROFK_EINVAL;
   if (overlap(s1, s2) || overlap(s1, s3) || overlap(s2, s3)) return PROFK_EINVAL;
   if (ws_bytes < need) return PROFK_EWORKSPACE;
-  const profk::LinGradCall c{dy, pre, static_cast<uint64_t>(dy_stride), dtype, activation, x, w,
+  const profk::LinGradCall c{dy, pre, static_cast<uint64_t>(dy_stride), dtype, activation, round_dz, x, w,
                              static_cast<uint64_t>(x_stride), static_cast<uint64_t>(w_stride), M, N, K, dx, dw, dbias,
                              ws};
   const hipError_t e = profk::launch_linear_grad(c, static_cast<hipStream_t>(stream));

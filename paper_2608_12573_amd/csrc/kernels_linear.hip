@@ -5,9 +5,11 @@
 //   dx = dz W,  dW = dz^T x,  db = sum over the rows of dz.
 // Products are exact in fp32 and summed in it on the matrix cores; bias,
 // activation and residual are fp32, and y (and z, where it is kept) is rounded
-// once.  dz is rounded to bf16 for the matrix cores: within 2^-8 of each term,
-// which the two products average over their sums.  db is summed from dz before
-// that.
+// once.  Where dz is no bf16 number by itself (dy in fp32, or the slope of gelu or
+// silu), it enters the two products as the sum of two, within 2^-16 of itself: as
+// many matrix instructions again.  A caller may have it rounded to one instead,
+// within 2^-8 of each term, which the products average over their sums (4096 x 2048 x
+// 12288 with gelu 826 us as two, 455 rounded).  db is summed from dz itself.
 //
 // All three products are P[i, j] = sum_k A(i, k) B(j, k) with either operand's k
 // neighbouring in memory ("along") or a whole row apart ("across").
@@ -74,14 +76,17 @@ template <bool TA, bool TB> __global__ __launch_bounds__(256) void k_prod_any(Pr
   f32x16 acc[2][2] = {};
   ta.load(g.a, g.as, i0, g.I, 0, g.K);
   tb.load(g.b, g.bs, j0, g.J, 0, g.K);
-  for (uint32_t k0 = 0; k0 < g.K; k0 += kAnyK) {
+  // (a second term of a: its steps of k follow)
+  const uint32_t steps = (g.K + kAnyK - 1) / kAnyK, all = g.a_low ? 2 * steps : steps;
+  for (uint32_t t = 0; t < all; ++t) {
     __syncthreads();
     ta.store(sa);
     tb.store(sb);
     __syncthreads();
-    if (k0 + kAnyK < g.K) {
-      ta.load(g.a, g.as, i0, g.I, k0 + kAnyK, g.K);
-      tb.load(g.b, g.bs, j0, g.J, k0 + kAnyK, g.K);
+    if (t + 1 < all) {
+      const uint32_t k = (t + 1 < steps ? t + 1 : t + 1 - steps) * kAnyK;
+      ta.load(t + 1 < steps ? g.a : g.a_low, g.as, i0, g.I, k, g.K);
+      tb.load(g.b, g.bs, j0, g.J, k, g.K);
     }
 #pragma unroll
     for (uint32_t q = 0; q < 2; ++q) {
@@ -128,17 +133,25 @@ template <bool TA, bool TB> hipError_t launch_any(ProdArgs g, hipStream_t s) {
 }
 
 // --------------------------------------------------------------------- dz ---
-// dz = dy act'(z) to bf16, and the sums of its columns over a part of the rows.  A
-// workgroup has cols threads for 8 columns each, and as many rows at a time as fit.
+// dz = dy act'(z) to bf16, or to a sum of two bf16 numbers, and the sums of its
+// columns over a part of the rows.  A workgroup has cols threads for 8 columns each,
+// and as many rows at a time as fit.
 struct DzArgs {
   const void *dy, *pre;
   uint64_t dy_stride;
   uint32_t M, N, cols, parts;       // cols: a power of two
-  __bf16* dz;                       // rows dz_stride apart; null: only the sums
+  __bf16 *dz, *low;                 // rows dz_stride apart; null: only the sums; low null: one number
   uint64_t dz_stride;
   float* part;                      // [parts, N], or null
 };
 constexpr uint32_t kDzBS = 256;
+
+// The bf16 number next to a finite x (the largest, where that is infinite), so that x
+// less it is finite; infinities and NaN as they are.
+__device__ __forceinline__ float top_term(float x) {
+  const float hi = static_cast<float>(static_cast<__bf16>(x));
+  return fabsf(hi) == INFINITY && fabsf(x) < INFINITY ? copysignf(0x1.FEp127f, x) : hi;
+}
 
 template <int DT, int ACT> __device__ __forceinline__ void dz_body(const DzArgs& a, uint32_t slab, uint32_t p) {
   __shared__ float s[kDzBS][8];
@@ -157,6 +170,16 @@ template <int DT, int ACT> __device__ __forceinline__ void dz_body(const DzArgs&
     }
 #pragma unroll
     for (int e = 0; e < 8; ++e) sum[e] += d[e];
+    if (a.low) {
+      float low[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float hi = top_term(d[e]);
+        low[e] = fabsf(d[e]) < INFINITY ? d[e] - hi : 0.0f;
+        d[e] = hi;
+      }
+      store<PROFK_BF16, 8>(a.low + r * a.dz_stride, j, static_cast<uint32_t>(a.dz_stride), low);
+    }
     if (a.dz) store<PROFK_BF16, 8>(a.dz + r * a.dz_stride, j, static_cast<uint32_t>(a.dz_stride), d);   // (0 past N)
   }
   if (!a.part) return;
@@ -255,7 +278,7 @@ size_t sums_bytes(int64_t I, int64_t J, int64_t K, uint32_t cus) {
 }
 
 struct GradLayout {
-  size_t dz, part, x, w, sums, bytes;   // offsets
+  size_t dz, low, part, x, w, sums, bytes;   // offsets
   uint64_t dz_stride;
   uint32_t parts;
 };
@@ -263,7 +286,8 @@ GradLayout grad_layout(int64_t M, int64_t N, int64_t K, int num_cus) {
   GradLayout L{};
   L.dz_stride = (static_cast<uint64_t>(N) + 7) / 8 * 8;
   L.parts = dz_parts(M, N, num_cus);
-  L.part = align256(static_cast<size_t>(M) * L.dz_stride * 2);
+  L.low = align256(static_cast<size_t>(M) * L.dz_stride * 2);
+  L.part = 2 * L.low;
   L.x = L.part + align256(static_cast<size_t>(L.parts) * N * 4);
   L.w = L.x + pad_bytes(M, K);
   L.sums = L.w + pad_bytes(N, K);
@@ -325,7 +349,7 @@ size_t lin_workspace(int64_t M, int64_t N, int64_t K, int num_cus) {
 size_t lin_grad_workspace(int64_t M, int64_t N, int64_t K, int num_cus) { return grad_layout(M, N, K, num_cus).bytes; }
 
 hipError_t launch_linear(const LinCall& c, hipStream_t s) {
-  ProdArgs g{static_cast<const __bf16*>(c.x), static_cast<const __bf16*>(c.w), c.x_stride, c.w_stride,
+  ProdArgs g{static_cast<const __bf16*>(c.x), static_cast<const __bf16*>(c.w), nullptr, c.x_stride, c.w_stride,
              static_cast<uint32_t>(c.M), static_cast<uint32_t>(c.N), static_cast<uint32_t>(c.K), c.bias, c.act,
              c.out_dtype, c.residual, c.residual_stride, c.out, c.pre, 0, 0, 1, 0, false, false};
   const uint32_t cus = static_cast<uint32_t>(device_cu_count());
@@ -358,13 +382,16 @@ hipError_t launch_linear_grad(const LinGradCall& c, hipStream_t s) {
   uint8_t* const ws = static_cast<uint8_t*>(c.ws);
   const uint32_t M = static_cast<uint32_t>(c.M), N = static_cast<uint32_t>(c.N), K = static_cast<uint32_t>(c.K);
   __bf16* const dz = reinterpret_cast<__bf16*>(ws + L.dz);
+  // (dz is a bf16 number where dy is and the slope is 0 or 1)
+  const bool slope = c.act == PROFK_ACT_GELU || c.act == PROFK_ACT_SILU;
+  __bf16* const low = !c.round_dz && (slope || c.dtype == PROFK_F32) ? reinterpret_cast<__bf16*>(ws + L.low) : nullptr;
   float* const part = reinterpret_cast<float*>(ws + L.part);
   // (without an activation, dy in bf16 is dz)
   const bool given = c.act == PROFK_ACT_NONE && c.dtype == PROFK_BF16 && granules(c.dy, c.dy_stride, N, false);
   const bool dx = c.dx && M, dw = c.dw && N;
   const uint32_t cols = dz_cols(N);
-  const DzArgs d{c.dy, c.pre, c.dy_stride, M, N, cols, L.parts, (dx || dw) && !given ? dz : nullptr, L.dz_stride,
-                 !c.db ? nullptr : L.parts == 1 ? c.db : part};
+  const DzArgs d{c.dy, c.pre, c.dy_stride, M, N, cols, L.parts, (dx || dw) && !given ? dz : nullptr,
+                 dx || dw ? low : nullptr, L.dz_stride, !c.db ? nullptr : L.parts == 1 ? c.db : part};
   // the copies of W and x, where their rows are not whole granules, beside dz
   const PadArgs p = pad_args(c.x, c.x_stride, K % 8 && dw ? M : 0, reinterpret_cast<__bf16*>(ws + L.x), c.w, c.w_stride,
                              K % 8 && dx ? N : 0, reinterpret_cast<__bf16*>(ws + L.w), K);
@@ -387,6 +414,7 @@ hipError_t launch_linear_grad(const LinGradCall& c, hipStream_t s) {
   ProdArgs g{};
   g.parts = 1;
   g.a = given ? static_cast<const __bf16*>(c.dy) : dz;
+  g.a_low = low;
   g.as = given ? c.dy_stride : L.dz_stride;
   g.a_padded = !given;
   g.b_padded = K % 8 != 0;

@@ -27,6 +27,7 @@ struct LinGradCall {
   const void *dy, *pre;             // [M, N] of dtype; pre null without an activation
   uint64_t dy_stride;
   int dtype, act;
+  bool round_dz;                    // dz to one bf16 number for the products
   const void *x, *w;
   uint64_t x_stride, w_stride;
   int64_t M, N, K;

@@ -11,6 +11,7 @@ namespace profk {
 // "across" it, a row of neighbouring i for each k.
 struct ProdArgs {
   const __bf16 *a, *b;
+  const __bf16* a_low;              // a second operand to be added to a, laid out as it is, or null
   uint64_t as, bs;                  // elements from row to row
   uint32_t I, J, K;
   const float* bias;                // [J]

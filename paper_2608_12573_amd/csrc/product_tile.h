@@ -139,11 +139,11 @@ template <bool ACROSS, int BW, int Q, int F, bool PERM, bool WHOLE> struct ProdS
     base += k * (ACROSS ? row_bytes : uint64_t{2});
     K = left;
   }
-  // stage `next` of the tile to LDS
-  __device__ __forceinline__ void issue(uint4* st, uint32_t next) const {
+  // stage `next` of the tile to LDS, of the operand `plane` bytes behind this one
+  __device__ __forceinline__ void issue(uint4* st, uint32_t next, int64_t plane = 0) const {
 #pragma unroll
     for (int q = 0; q < Q; ++q) {
-      const uint8_t* p = base + off[q];
+      const uint8_t* p = base + plane + off[q];
       if constexpr (!WHOLE) p = next * kStageK + k_of(q) < K ? p : reinterpret_cast<const uint8_t*>(&g_zero_granule);
       __builtin_amdgcn_global_load_lds(reinterpret_cast<const uint32_t*>(p), st + (w * Q + q) * kWave, 16, 0, 0);
     }
@@ -171,10 +171,11 @@ template <bool ACROSS, int BW, int Q, int F, bool PERM, bool WHOLE> struct ProdS
   }
 };
 
-// WHOLE: K is a multiple of two stages.  SPLIT: K is taken in g.parts parts of
-// g.part_k, a whole number of two stages (the last may hold less), each a tile of
-// its own whose sums go to g.out [parts, I, J].
-template <bool TA, bool TB, int ACT, int DT, int WM, int WN, int MI, int NJ, bool WHOLE, bool SPLIT>
+// WHOLE: K is a multiple of two stages (TWO: of one).  SPLIT: K is taken in g.parts
+// parts of g.part_k, a whole number of two stages (the last may hold less), each a
+// tile of its own whose sums go to g.out [parts, I, J].  TWO: a is the sum of g.a and
+// g.a_low; the 64 of k of a stage come by twice, first of g.a, then of g.a_low.
+template <bool TA, bool TB, int ACT, int DT, int WM, int WN, int MI, int NJ, bool WHOLE, bool SPLIT, bool TWO>
 __device__ __forceinline__ void prod_body(const ProdArgs& g, uint32_t tiles_i, uint32_t tiles, uint32_t block,
                                           uint32_t blocks, uint4* s0, uint4* s1) {
   static_assert(!SPLIT || (!WHOLE && ACT == PROFK_ACT_NONE && DT == PROFK_F32), "sums of parts");
@@ -188,7 +189,9 @@ __device__ __forceinline__ void prod_body(const ProdArgs& g, uint32_t tiles_i, u
   if (tile0 >= end) return;
   // a tile takes an even number of stages, so that each starts at the same one
   const uint32_t tile_k = SPLIT ? g.part_k : g.K, of_part = SPLIT ? tiles / g.parts : tiles;
-  const uint32_t stages = (tile_k + 2 * kStageK - 1) / (2 * kStageK) * 2;
+  const uint32_t stages =
+      TWO ? (tile_k + kStageK - 1) / kStageK * 2 : (tile_k + 2 * kStageK - 1) / (2 * kStageK) * 2;
+  const int64_t low = TWO ? reinterpret_cast<const uint8_t*>(g.a_low) - reinterpret_cast<const uint8_t*>(g.a) : 0;
   const uint32_t tid = threadIdx.x, lane = tid & (kWave - 1);
   const uint32_t w = __builtin_amdgcn_readfirstlane(tid / kWave);
   const uint32_t c = lane & 31, h = lane >> 5, wm = w / WN, wn = w % WN;
@@ -218,11 +221,13 @@ __device__ __forceinline__ void prod_body(const ProdArgs& g, uint32_t tiles_i, u
   };
   uint32_t next_k = 0, next_tile = tile0;
   // (past the last tile: its last stage again)
-  auto issue_a = [&](uint4* st) { sa.issue(st, next_k); };
+  auto of_k = [](uint32_t stage) { return TWO ? stage / 2 : stage; };
+  auto issue_a = [&](uint4* st) { sa.issue(st, of_k(next_k), next_k % 2 ? low : 0); };
   auto issue_b = [&](uint4* st) {
-    sb.issue(st + T::kB, next_k);
+    sb.issue(st + T::kB, of_k(next_k));
     ++next_k;
-    if (WHOLE ? next_k < stages : next_k < stages && next_k * kStageK < sa.K) {
+    if (TWO && next_k % 2) return;
+    if (next_k < stages && (WHOLE || of_k(next_k) * kStageK < sa.K)) {
       sa.base += sa.adv;
       sb.base += sb.adv;
     }
@@ -443,13 +448,13 @@ __device__ __forceinline__ void prod_body(const ProdArgs& g, uint32_t tiles_i, u
   prod_wait<0>();   // (no load may reach LDS after the workgroup's end)
 }
 
-template <bool TA, bool TB, int ACT, int DT, int WM, int WN, int MI, int NJ, int WAVES, bool WHOLE, bool SPLIT>
+template <bool TA, bool TB, int ACT, int DT, int WM, int WN, int MI, int NJ, int WAVES, bool WHOLE, bool SPLIT, bool TWO>
 __global__ __launch_bounds__(WM * WN * 64, WAVES) void k_prod(ProdArgs g, uint32_t tiles_i, uint32_t tiles) {
   using T = ProdTile<WM, WN, MI, NJ>;
   // distinct arrays, so that the compiler can tell the stage being read from the
   // one being filled
   __shared__ __align__(16) uint4 s0[T::kGran], s1[T::kGran];
-  prod_body<TA, TB, ACT, DT, WM, WN, MI, NJ, WHOLE, SPLIT>(g, tiles_i, tiles, blockIdx.x, gridDim.x, s0, s1);
+  prod_body<TA, TB, ACT, DT, WM, WN, MI, NJ, WHOLE, SPLIT, TWO>(g, tiles_i, tiles, blockIdx.x, gridDim.x, s0, s1);
 }
 
 // Workgroups of a launch over `tiles`.
@@ -459,25 +464,25 @@ inline uint32_t prod_grid(uint32_t tiles, uint32_t most) {
 }
 
 // PER: workgroups a CU holds.
-template <bool TA, bool TB, int ACT, int DT, int WM, int WN, int MI, int NJ, int PER, bool SPLIT>
+template <bool TA, bool TB, int ACT, int DT, int WM, int WN, int MI, int NJ, int PER, bool SPLIT, bool TWO>
 void launch_tiles(const ProdArgs& g, uint32_t cus, hipStream_t s) {
   using T = ProdTile<WM, WN, MI, NJ>;
   const uint32_t ti = (g.I + T::BM - 1) / T::BM, tj = (g.J + T::BN - 1) / T::BN, tiles = ti * tj * (SPLIT ? g.parts : 1);
   const uint32_t grid = prod_grid(tiles, PER * cus);
   constexpr int kWaves = PER * WM * WN / 4;
   if constexpr (SPLIT) {
-    k_prod<TA, TB, ACT, DT, WM, WN, MI, NJ, kWaves, false, true><<<grid, T::BS, 0, s>>>(g, ti, tiles);
-  } else if (g.K % (2 * kStageK) == 0) {
-    k_prod<TA, TB, ACT, DT, WM, WN, MI, NJ, kWaves, true, false><<<grid, T::BS, 0, s>>>(g, ti, tiles);
+    k_prod<TA, TB, ACT, DT, WM, WN, MI, NJ, kWaves, false, true, TWO><<<grid, T::BS, 0, s>>>(g, ti, tiles);
+  } else if (g.K % ((TWO ? 1 : 2) * kStageK) == 0) {
+    k_prod<TA, TB, ACT, DT, WM, WN, MI, NJ, kWaves, true, false, TWO><<<grid, T::BS, 0, s>>>(g, ti, tiles);
   } else {
-    k_prod<TA, TB, ACT, DT, WM, WN, MI, NJ, kWaves, false, false><<<grid, T::BS, 0, s>>>(g, ti, tiles);
+    k_prod<TA, TB, ACT, DT, WM, WN, MI, NJ, kWaves, false, false, TWO><<<grid, T::BS, 0, s>>>(g, ti, tiles);
   }
 }
 
-template <bool TA, bool TB, int ACT, int DT, bool SPLIT>
+template <bool TA, bool TB, int ACT, int DT, bool SPLIT, bool TWO>
 void launch_shape(const ProdArgs& g, const ProdPlan& p, uint32_t cus, hipStream_t s) {
-  if (p.large) launch_tiles<TA, TB, ACT, DT, 4, 2, 2, 4, 1, SPLIT>(g, cus, s);
-  else launch_tiles<TA, TB, ACT, DT, 2, 2, 2, 2, 2, SPLIT>(g, cus, s);
+  if (p.large) launch_tiles<TA, TB, ACT, DT, 4, 2, 2, 4, 1, SPLIT, TWO>(g, cus, s);
+  else launch_tiles<TA, TB, ACT, DT, 2, 2, 2, 2, 2, SPLIT, TWO>(g, cus, s);
 }
 
 // Tiles are counted in 32 bits.
@@ -518,17 +523,17 @@ template <int DT, int ACT> __global__ __launch_bounds__(256) void k_prod_join(Pr
   }
 }
 
-template <bool TA, bool TB, int ACT, int DT>
+template <bool TA, bool TB, int ACT, int DT, bool TWO>
 void launch_planned(ProdArgs g, const ProdPlan& p, float* sums, uint32_t cus, hipStream_t s) {
   if (p.parts == 1) {
-    launch_shape<TA, TB, ACT, DT, false>(g, p, cus, s);
+    launch_shape<TA, TB, ACT, DT, false, TWO>(g, p, cus, s);
     return;
   }
   g.parts = p.parts;
   g.part_k = p.part_k;
   ProdArgs part = g;
   part.out = sums;
-  launch_shape<TA, TB, PROFK_ACT_NONE, PROFK_F32, true>(part, p, cus, s);
+  launch_shape<TA, TB, PROFK_ACT_NONE, PROFK_F32, true, TWO>(part, p, cus, s);
   const uint64_t blocks = (static_cast<uint64_t>(g.I) * ((g.J + 7) / 8) + 255) / 256;
   k_prod_join<DT, ACT><<<blocks < 8192 ? static_cast<uint32_t>(blocks) : 8192, 256, 0, s>>>(g, sums);
 }
