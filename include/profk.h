@@ -532,8 +532,9 @@ int profk_linear_grad(int32_t dtype, const void* dy, int64_t dy_stride, const vo
  *   NaN, inf  stay where they are allowed; where they are forbidden -inf.  A row
  *             that allows nothing is all -inf.
  *   time      one read and one write of the logits; each piece of a row (64 KiB
- *             at most) searches the row's history and biases again, and rows with
- *             more than 256 biases in a piece search their list for each of them.
+ *             at most) goes through the row's history and biases again, twice where
+ *             it has more than 16 biases or, of bf16 logits, the history more than
+ *             16383 tokens.
  *
  * profk_adjust_logits_grad: the gradient with respect to the logits, that of out
  * times 1 / repetition, repetition or 1 as above, and 0 where the mask forbids.

@@ -23,8 +23,12 @@
 //
 // The table is as large as the piece, so that it does not limit the workgroups of
 // a CU: of 16-bit logits it has two flags and 14 bits of count, of 32-bit ones 30.
-// Rows with longer histories than 14 bits count take a piece of 16-bit logits in
-// two halves, 32 bits a token.
+// Rows with longer histories than 14 bits count, and pieces with more biases than
+// are listed, take a piece of 16-bit logits in two halves, 32 bits a token, each
+// element from its registers: first the counts, then, in the same table, the number
+// of each token's last bias, by an integer maximum.  Every step is a pass over a
+// list: no token searches a long one (256 x 131072 bf16 with 5000 biases a row 95 us,
+// with one for every token 985).
 //
 // The gradient needs no counts, but the sign of the history's logits, which it
 // reads when it comes upon their tokens and notes beside the flag.
@@ -41,7 +45,10 @@ namespace {
 // Of a token's word, in its upper half where it has 32 bits: it is in the prompt
 // (of the gradient: in the history); it has a bias (its logit is above 0).
 constexpr uint32_t kAdjSeen = 0x8000u, kAdjBias = 0x4000u, kAdjCount = 0x3FFFu;
-constexpr uint32_t kAdjList = 256;             // biases of a piece that are kept in LDS
+// Biases of a piece that are listed in LDS: each of their tokens goes through that
+// list (us, 256 x 131072 bf16, by the list and by element: 200 spread biases a row 38
+// and 52, 15 neighbouring ones 75 and 49, 50 of them 360 and 49).
+constexpr uint32_t kAdjList = 16;
 constexpr uint32_t kAdjBytes = 64;             // of a thread's elements, 16 at a time
 constexpr uint32_t kAdjBS = 512;               // most threads
 
@@ -120,29 +127,28 @@ template <int DT, bool GRAD> __global__ __launch_bounds__(kAdjBS) void k_adjust(
   load_tokens(tid);
   int64_t id = tid < n_bias ? ids[tid] : -1;
   __shared__ uint32_t s_n, s_tok[kAdjList], s_at[kAdjList];
-  // the last bias of token v of the piece: from the list in LDS, whose order may
-  // be any, or, where that did not hold them all, from the row's
+  // the last bias of token v of the piece, from the list in LDS, whose order may be
+  // any
   auto bias_of = [&](uint32_t v) {
     uint32_t at = 0;
-    if (s_n <= kAdjList) {
-      for (uint32_t k = 0; k < s_n; ++k)
-        if (s_tok[k] == v && s_at[k] > at) at = s_at[k];
-    } else {
-      for (at = n_bias - 1; in_piece(ids[at]) != v;) --at;
-    }
+    for (uint32_t k = 0; k < s_n; ++k)
+      if (s_tok[k] == v && s_at[k] > at) at = s_at[k];
     return values[at];
   };
-  // the lists' entries of the piece's places from lo on to the table, 32 bits a
-  // place or 16
-  auto search = [&](auto wide, uint32_t lo, uint32_t len) {
+  auto clear = [&]() {
+    for (uint32_t i = tid * 4; i < BS * (kAdjBytes / ES) * kAdjWord<DT, GRAD> / 4; i += BS * 4)
+      *reinterpret_cast<u32x4*>(s_word + i) = u32x4{};
+  };
+  // the history's tokens of the piece's places from lo on to the table, 32 bits a
+  // place or 16; and, where they are to be listed, the biases
+  auto search = [&](auto wide, uint32_t lo, uint32_t len, bool list) {
     constexpr bool kWide = decltype(wide)::value;
     auto at_word = [&](uint32_t v) { return s_word + (kWide ? v : v / 2); };
     auto flag = [&](uint32_t v, uint32_t f) { return kWide ? f << 16 : f << (v & 1) * 16; };
     auto mark = [&](uint32_t v) {
       if constexpr (!GRAD) atomicOr(s_bits + v / 32, 1u << v % 32);
     };
-    for (uint32_t i = tid * 4; i < BS * (kAdjBytes / ES) * kAdjWord<DT, GRAD> / 4; i += BS * 4)
-      *reinterpret_cast<u32x4*>(s_word + i) = u32x4{};
+    clear();
     if constexpr (!GRAD) {
       for (uint32_t i = tid; i < BS * (kAdjBytes / ES) / 32; i += BS) s_bits[i] = 0;
     }
@@ -175,14 +181,14 @@ template <int DT, bool GRAD> __global__ __launch_bounds__(kAdjBS) void k_adjust(
       }
       load_tokens(i + TB * BS);
     }
-    for (uint32_t i = tid; i < n_bias; i += BS) {
-      const uint32_t p = in_piece(id), v = p < n ? p - lo : ~0u;
-      if (v < len) {
+    for (uint32_t i = tid; list && i < n_bias; i += BS) {
+      const uint32_t v = in_piece(id);
+      if (v < n) {
         atomicOr(at_word(v), flag(v, kAdjBias));
         mark(v);
         const uint32_t k = atomicAdd(&s_n, 1u);
         if (k < kAdjList) {
-          s_tok[k] = p;
+          s_tok[k] = v;
           s_at[k] = i;
         }
       }
@@ -190,13 +196,12 @@ template <int DT, bool GRAD> __global__ __launch_bounds__(kAdjBS) void k_adjust(
     }
     __syncthreads();
   };
-  // one element: its flags and count
-  auto adjust = [&](float y, uint32_t i, uint32_t flags, uint32_t count) {
+  // one element's penalties: its flags and count
+  auto adjust = [&](float y, uint32_t flags, uint32_t count) {
     if (flags & kAdjSeen || count) {
       y *= y > 0.0f ? inv : rep;
       y -= count ? fmaf(static_cast<float>(count), freq, pres) : 0.0f;
     }
-    if (flags & kAdjBias) y += bias_of(i);
     return y;
   };
   constexpr uint32_t kNan = DT == PROFK_F32 ? 0x7FC00000u : 0x7FC07FC0u;
@@ -210,7 +215,7 @@ template <int DT, bool GRAD> __global__ __launch_bounds__(kAdjBS) void k_adjust(
     store_raw<DT, E>(out, (q * BS + tid) * E, n, y);
   };
   if constexpr (GRAD) {
-    if (lists) search(std::false_type{}, 0, n);
+    if (lists) search(std::false_type{}, 0, n, false);
 #pragma unroll
     for (uint32_t q = 0; q < C; ++q) {
       const uint32_t i = (q * BS + tid) * E;
@@ -231,11 +236,16 @@ template <int DT, bool GRAD> __global__ __launch_bounds__(kAdjBS) void k_adjust(
     }
     return;
   }
-  if (DT == PROFK_F32 || n_hist <= kAdjCount) {
+  // (more biases than all pieces could list: a pass over them less)
+  bool by_element = (DT != PROFK_F32 && n_hist > kAdjCount) || n_bias / kAdjList >= a.pieces;
+  constexpr bool kWide = DT == PROFK_F32;
+  if (lists && !by_element) {
+    search(std::integral_constant<bool, kWide>{}, 0, n, true);
+    by_element = s_n > kAdjList;
+  }
+  if (!by_element) {
     using O = std::conditional_t<DT == PROFK_F32, float, __bf16>;
     if (lists) {
-      constexpr bool kWide = DT == PROFK_F32;
-      search(std::integral_constant<bool, kWide>{}, 0, n);
       // a word of the bitmap a thread, or a part of one where the words are fewer:
       // marked tokens of a thread are adjusted one after the other (4 x 256 fp32, most
       // of them marked and 50 biases a row: 95 us by words, 15 so)
@@ -247,9 +257,10 @@ template <int DT, bool GRAD> __global__ __launch_bounds__(kAdjBS) void k_adjust(
         if (span < 32) bits &= (1u << span) - 1;
         for (; bits; bits &= bits - 1) {
           const uint32_t v = first + static_cast<uint32_t>(__builtin_ctz(bits));
-          const uint32_t c = kWide ? s_word[v] : s_word[v / 2] >> v % 2 * 16;
-          reinterpret_cast<O*>(s_word)[v] =
-              static_cast<O>(adjust(load1(x, v, DT), v, kWide ? c >> 16 : c, kWide ? c & 0x3FFFFFFFu : c & kAdjCount));
+          const uint32_t c = kWide ? s_word[v] : s_word[v / 2] >> v % 2 * 16, flags = kWide ? c >> 16 : c;
+          float y = adjust(load1(x, v, DT), flags, kWide ? c & 0x3FFFFFFFu : c & kAdjCount);
+          if (flags & kAdjBias) y += bias_of(v);
+          reinterpret_cast<O*>(s_word)[v] = static_cast<O>(y);
         }
       }
       __syncthreads();
@@ -271,30 +282,48 @@ template <int DT, bool GRAD> __global__ __launch_bounds__(kAdjBS) void k_adjust(
     }
     return;
   }
-  const uint32_t half = BS * E * (C / 2);
+  constexpr uint32_t kParts = kWide ? 1 : 2, CP = C / kParts;
+  const uint32_t part = BS * E * CP;
 #pragma unroll
-  for (uint32_t h = 0; h < 2; ++h) {
-    if (h * half >= n) return;            // (the whole workgroup)
-    if (h) {
-      __syncthreads();
-      load_tokens(tid);
-      id = tid < n_bias ? ids[tid] : -1;
+  for (uint32_t h = 0; h < kParts; ++h) {
+    const uint32_t lo = h * part;
+    if (lo >= n) return;                  // (the whole workgroup)
+    const uint32_t len = min(part, n - lo);
+    __syncthreads();
+    load_tokens(tid);
+    search(std::true_type{}, lo, len, false);
+    float y[CP][E];
+#pragma unroll
+    for (uint32_t q = 0; q < CP; ++q) {
+      to_f32<DT, E>(raw[h * CP + q], y[q]);
+#pragma unroll
+      for (uint32_t e = 0; e < E; ++e) {
+        const uint32_t c = s_word[(q * BS + tid) * E + e];
+        y[q][e] = adjust(y[q][e], c >> 16, c & 0x3FFFFFFFu);
+      }
     }
-    search(std::true_type{}, h * half, min(half, n - h * half));
+    if (n_bias) {
+      __syncthreads();
+      clear();
+      __syncthreads();
+      for (uint32_t i = tid; i < n_bias; i += BS) {
+        const uint32_t p = in_piece(ids[i]), v = p < n ? p - lo : ~0u;
+        if (v < len) atomicMax(s_word + v, i + 1);
+      }
+      __syncthreads();
 #pragma unroll
-    for (uint32_t q = h * (C / 2); q < (h + 1) * (C / 2); ++q) {
-      const uint32_t i = (q * BS + tid) * E;
-      if (i < n) {
-        float y[E];
-        to_f32<DT, E>(raw[q], y);
+      for (uint32_t q = 0; q < CP; ++q) {
 #pragma unroll
         for (uint32_t e = 0; e < E; ++e) {
-          const uint32_t c = s_word[i - h * half + e];
-          y[e] = adjust(y[e], i + e, c >> 16, c & 0x3FFFFFFFu);
+          const uint32_t c = s_word[(q * BS + tid) * E + e];
+          if (c) y[q][e] += values[c - 1];
         }
-        raw[q] = pack<DT, E>(y);
-        finish(q, raw[q]);
       }
+    }
+#pragma unroll
+    for (uint32_t q = 0; q < CP; ++q) {
+      raw[h * CP + q] = pack<DT, E>(y[q]);
+      if (lo + (q * BS + tid) * E < n) finish(h * CP + q, raw[h * CP + q]);
     }
   }
 }
