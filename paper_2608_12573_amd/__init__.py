@@ -321,6 +321,18 @@ def _bytes_buffer(t, name, nbytes, device):
     _on_device(t, name, device)
 
 
+def _given(*tensors):
+    """Outputs that the caller gave (None: not this one) are about to be written,
+    through their pointers: autograd's check of what it saved has to see that, and
+    what it records cannot be written behind its back."""
+    torch = _torch()
+    tensors = [t for t in tensors if t is not None]
+    if torch.is_grad_enabled() and any(t.requires_grad for t in tensors):
+        raise ProfkError("a given output requires a gradient, and the call would not be recorded: give a detached one, or "
+                         "call under torch.no_grad()")
+    torch.autograd.graph.increment_version(tensors)
+
+
 def _nbytes(t):
     return t.numel() * t.element_size()
 
@@ -334,6 +346,7 @@ def _outputs(x, n, out, info, n_info):
     else:
         _buffer(out[0], "out[0]", x.dtype, n, x.device)
         _buffer(out[1], "out[1]", torch.int64, n, x.device)
+        _given(out[0], out[1])
     if info is None:
         info = torch.empty(n_info * INFO_BYTES, dtype=torch.uint8, device=x.device)
     else:
@@ -502,6 +515,7 @@ def sae_encode_topk(x, w_enc, b_enc, k_row, eps=1e-6, recall=1.0, seed=0, p=None
     else:
         _buffer(out[0], "out[0]", torch.float32, K, x.device)
         _buffer(out[1], "out[1]", torch.int64, K, x.device)
+        _given(out[0], out[1])
     if info is None:
         info = torch.empty(INFO_BYTES, dtype=torch.uint8, device=x.device)
     else:
@@ -520,6 +534,7 @@ def sae_encode_dense(x, w_enc, b_enc, out=None):
         out = torch.empty((B, d_dict), dtype=torch.float32, device=x.device)
     else:
         _buffer(out, "out", torch.float32, B * d_dict, x.device)
+        _given(out)
     _check(lib().profk_sae_encode_dense(_ptr(x), _ptr(w_enc), _ptr(b_enc), B, d_model, d_dict, _ptr(out),
                                         _stream()))
     return out
@@ -543,6 +558,7 @@ def sae_decode(vals, flat_idx, w_dec, b_dec, B, out=None, ws=None):
         out = torch.empty((B, d_model), dtype=torch.float32, device=vals.device)
     else:
         _buffer(out, "out", torch.float32, B * d_model, vals.device)
+        _given(out)
     n = int(lib().profk_sae_decode_workspace_size(B, K))
     if ws is None:
         ws = torch.empty(max(n, 1), dtype=torch.uint8, device=vals.device)
@@ -652,6 +668,7 @@ def token_logprobs(logits, tokens, n_top=0, ws=None, out=None, lse_low=None):
         raise ProfkError(f"n_top must be from 0 to {MAX_TOP}, got {n_top}")
     if lse_low is not None:
         _vector(lse_low, "lse_low", torch.float32, (T,), dev)
+        _given(lse_low)
     L = lib()
     n = L.profk_token_logprobs_workspace_size(T, V, n_top)
     if ws is not None:
@@ -667,6 +684,7 @@ def token_logprobs(logits, tokens, n_top=0, ws=None, out=None, lse_low=None):
         _vector(out[2], "out[2]", f32, one, dev)
         _vector(out[3], "out[3]", f32, (T, n_top), dev)
         _vector(out[4], "out[4]", torch.int64, (T, n_top), dev)
+        _given(*out)
     _check(L.profk_token_logprobs_ex(dt, logits.data_ptr(), T, V, stride, tokens.data_ptr(), n_top, out[0].data_ptr(),
                                      out[1].data_ptr(), out[2].data_ptr(), _ptr(lse_low), out[3].data_ptr(),
                                      out[4].data_ptr(), ws.data_ptr() if n else None, n, _stream()))
@@ -706,12 +724,15 @@ def token_logprobs_grad(logits, tokens, lse, entropy, g_logprob, g_entropy=None,
         n = top_idx.shape[1]
         _vector(top_idx, "top_idx", torch.int64, (T, n), dev)
         _vector(g_top, "g_top", f32, (T, n), dev)
-    if out is None:
+    given = out is not None
+    if not given:
         out = torch.empty((T, V), dtype=logits.dtype, device=dev)
     ot, oT, oV, ostride = _rows(out, "out")
     if ot != dt or oT != T or oV != V:
         raise ProfkError("out must have the logits' dtype and shape")
     _on_device(out, "out", dev)
+    if given:
+        _given(out)
     _check(lib().profk_token_logprobs_grad_ex(dt, logits.data_ptr(), T, V, stride, tokens.data_ptr(), lse.data_ptr(),
                                               _ptr(lse_low), _ptr(entropy), _ptr(g_logprob), _ptr(g_entropy), _ptr(g_lse), n,
                                               top_idx.data_ptr() if n else None, g_top.data_ptr() if n else None,
@@ -799,6 +820,8 @@ def mx4_quantize(x, out=None):
         out = mx4_outputs(R, K, x.device)
     elif _mx4(out[0], out[1], "out", K, x.device) != R:
         raise ProfkError(f"out must have {R} rows")
+    else:
+        _given(out[0], out[1])
     _check(lib().profk_mx4_quantize(dt, x.data_ptr(), R, K, stride, out[0].data_ptr(), out[1].data_ptr(), _stream()))
     return out
 
@@ -806,13 +829,16 @@ def mx4_quantize(x, out=None):
 def _dense_out(shape, dtype, default, out, device):
     """A contiguous fp32 or bf16 output of `shape`, given or new: (out, code)."""
     torch = _torch()
-    if out is None:
+    given = out is not None
+    if not given:
         out = torch.empty(shape, dtype=dtype or default, device=device)
     elif not isinstance(out, torch.Tensor):
         raise ProfkError("out must be a torch tensor")
     elif dtype is not None and out.dtype != dtype:
         raise ProfkError(f"out is {out.dtype}, not {dtype}")
     _vector(out, "out", out.dtype, shape, device)
+    if given:
+        _given(out)
     return out, _dtype_code(out)
 
 
@@ -922,7 +948,9 @@ def layer_norm(x, weight=None, bias=None, eps=1e-5, dtype=None, out=None):
 
     Where x, weight or bias require a gradient, the new outputs are
     differentiable with respect to them (mean and rstd are not).  Into a given
-    `out` nothing is recorded: the caller takes layer_norm_grad."""
+    `out` nothing is recorded: the caller takes layer_norm_grad.  Autograd sees that
+    a given output, of any call, was written; one that requires a gradient itself is
+    refused where autograd records."""
     torch = _torch()
     dt, T, D, stride = _rows(x, "x")
     dev = x.device
@@ -930,11 +958,14 @@ def layer_norm(x, weight=None, bias=None, eps=1e-5, dtype=None, out=None):
         return _differentiable("layer_norm").apply(x, weight, bias, eps, dtype)
     pdt = _params(weight, bias, D, dev)
     stream = _stream_on(dev)
-    if out is None:
+    given = out is not None
+    if not given:
         out = layer_norm_outputs(T, D, dtype or x.dtype, dev)
     ostride = _out_rows(out[0], "out[0]", T, D, dtype, dev)
     _vector(out[1], "out[1]", torch.float32, (T,), dev)
     _vector(out[2], "out[2]", torch.float32, (T,), dev)
+    if given:
+        _given(*out)
     _check(lib().profk_layer_norm(dt, x.data_ptr(), T, D, stride, pdt, _ptr(weight), _ptr(bias), eps,
                                   _dtype_code(out[0]), out[0].data_ptr(), ostride, out[1].data_ptr(), out[2].data_ptr(),
                                   stream))
@@ -964,7 +995,8 @@ def layer_norm_grad(dy, x, weight, mean, rstd, ws=None, out=None, need=(True, Tr
     _vector(rstd, "rstd", f32, (T,), dev)
     stream = _stream_on(dev)
     ptype = weight.dtype if weight is not None else f32
-    if out is None:
+    given = out is not None
+    if not given:
         out = (torch.empty((T, D), dtype=x.dtype, device=dev) if need[0] else None,
                torch.empty(D, dtype=ptype, device=dev) if need[1] else None,
                torch.empty(D, dtype=ptype, device=dev) if need[2] else None)
@@ -972,6 +1004,8 @@ def layer_norm_grad(dy, x, weight, mean, rstd, ws=None, out=None, need=(True, Tr
     for i in (1, 2):
         if out[i] is not None:
             _vector(out[i], f"out[{i}]", ptype, (D,), dev)
+    if given:
+        _given(*out)
     L = lib()
     n = L.profk_layer_norm_grad_workspace_size(T, D) if out[1] is not None or out[2] is not None else 0
     if ws is not None:
@@ -1042,6 +1076,7 @@ def linear(x, w, bias=None, activation=None, residual=None, dtype=None, ws=None,
     out, odt = _dense_out((M, N), dtype, torch.float32, out, dev)
     if pre is not None:
         _vector(pre, "pre", out.dtype, (M, N), dev)
+        _given(pre)
     rs = _out_rows(residual, "residual", M, N, out.dtype, dev) if residual is not None else N
     L = lib()
     n = L.profk_linear_workspace_size(M, K, N)
@@ -1082,13 +1117,16 @@ def linear_grad(dy, x, w, pre=None, activation=None, ws=None, out=None, need=(Tr
         pre = None
     stream = _stream_on(dev)
     bf16 = torch.bfloat16
-    if out is None:
+    given = out is not None
+    if not given:
         out = (torch.empty((M, K), dtype=bf16, device=dev) if need[0] else None,
                torch.empty((N, K), dtype=bf16, device=dev) if need[1] else None,
                torch.empty(N, dtype=torch.float32, device=dev) if need[2] else None)
     for i, (t, shape) in enumerate(((bf16, (M, K)), (bf16, (N, K)), (torch.float32, (N,)))):
         if out[i] is not None:
             _vector(out[i], f"out[{i}]", t, shape, dev)
+    if given:
+        _given(*out)
     L = lib()
     n = L.profk_linear_grad_workspace_size(M, K, N)
     if ws is not None:
@@ -1183,9 +1221,12 @@ def adjust_logits(logits, tokens=None, offsets=None, n_prompt=None, repetition=N
         _vector(values, "bias[1]", f32, (n_bias,), dev)
         _vector(at, "bias[2]", torch.int64, (T + 1,), dev)
     stream = _stream_on(dev)
-    if out is None:
+    given = out is not None
+    if not given:
         out = torch.empty((T, V), dtype=logits.dtype, device=dev)
     ostride = _out_rows(out, "out", T, V, logits.dtype, dev)
+    if given:
+        _given(out)
     _check(lib().profk_adjust_logits(dt, logits.data_ptr(), T, V, stride, _ptr(tokens), _ptr(offsets), n_tokens,
                                      _ptr(n_prompt), _ptr(repetition), _ptr(presence), _ptr(frequency), _ptr(ids),
                                      _ptr(values), _ptr(at), n_bias, _ptr(allowed), n_masks, words, _ptr(mask),
@@ -1207,9 +1248,12 @@ def adjust_logits_grad(d_out, logits, tokens=None, offsets=None, n_prompt=None, 
     if n_prompt is not None:
         _vector(n_prompt, "n_prompt", torch.int64, (T,), dev)
     stream = _stream_on(dev)
-    if out is None:
+    given = out is not None
+    if not given:
         out = torch.empty((T, V), dtype=logits.dtype, device=dev)
     ostride = _out_rows(out, "out", T, V, logits.dtype, dev)
+    if given:
+        _given(out)
     _check(lib().profk_adjust_logits_grad(dt, d_out.data_ptr(), dstride, logits.data_ptr(), T, V, stride, _ptr(tokens),
                                           _ptr(offsets), n_tokens, _ptr(repetition), _ptr(allowed), n_masks, words,
                                           _ptr(mask), out.data_ptr(), ostride, stream))
