@@ -333,6 +333,17 @@ def _given(*tensors):
     torch.autograd.graph.increment_version(tensors)
 
 
+def _recorded(*tensors):
+    """Whether autograd records a call of these inputs (None: not this one).  There
+    are no forward-mode derivatives: a tangent, which would be lost, is refused."""
+    torch = _torch()
+    forward = torch.autograd.forward_ad
+    if forward._current_level >= 0:
+        if any(t is not None and forward.unpack_dual(t).tangent is not None for t in tensors):
+            raise ProfkError("an input has a forward-mode tangent, which this call would lose: take its gradient backwards")
+    return torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors)
+
+
 def _nbytes(t):
     return t.numel() * t.element_size()
 
@@ -661,7 +672,7 @@ def token_logprobs(logits, tokens, n_top=0, ws=None, out=None, lse_low=None):
     torch = _torch()
     dt, T, V, stride = _rows(logits, "logits")
     dev = logits.device
-    if logits.requires_grad and out is None and torch.is_grad_enabled():
+    if _recorded(logits) and out is None:
         return _differentiable_logprobs().apply(logits, tokens, n_top, ws, lse_low)
     _vector(tokens, "tokens", torch.int64, (T,), dev)
     if not 0 <= n_top <= MAX_TOP:
@@ -954,7 +965,7 @@ def layer_norm(x, weight=None, bias=None, eps=1e-5, dtype=None, out=None):
     torch = _torch()
     dt, T, D, stride = _rows(x, "x")
     dev = x.device
-    if out is None and torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in (x, weight, bias)):
+    if _recorded(x, weight, bias) and out is None:
         return _differentiable("layer_norm").apply(x, weight, bias, eps, dtype)
     pdt = _params(weight, bias, D, dev)
     stream = _stream_on(dev)
@@ -1065,8 +1076,7 @@ def linear(x, w, bias=None, activation=None, residual=None, dtype=None, ws=None,
     M, K, N, xs, wstride = _product(x, w)
     dev = x.device
     act = _activation(activation)
-    if out is None and torch.is_grad_enabled() and \
-            any(t is not None and t.requires_grad for t in (x, w, bias, residual)):
+    if _recorded(x, w, bias, residual) and out is None:
         if pre is not None:
             raise ProfkError("pre is kept by the recorded call itself")
         return _differentiable("linear").apply(x, w, bias, residual, activation, dtype, ws, round_dz)
@@ -1201,7 +1211,7 @@ def adjust_logits(logits, tokens=None, offsets=None, n_prompt=None, repetition=N
     torch = _torch()
     dt, T, V, stride = _rows(logits, "logits")
     dev, f32 = logits.device, torch.float32
-    if out is None and logits.requires_grad and torch.is_grad_enabled():
+    if _recorded(logits) and out is None:
         return _differentiable("adjust_logits").apply(logits, tokens, offsets, n_prompt, repetition, presence, frequency,
                                                       bias, allowed, mask)
     n_tokens, n_masks, words = _history(T, V, tokens, offsets, repetition, allowed, mask, dev)
