@@ -450,8 +450,8 @@ int profk_mx4_linear(int32_t dtype, const void* x, int64_t M, int64_t K, int64_t
  *   eps       finite, above 0 (a row of equal values has no direction without).
  *   NaN, inf  a row with either is NaN.
  * out may be x itself, of the same type and stride; else the memory from an
- * output's first element to its last must not overlap x's or dy's
- * (PROFK_EINVAL).  Any of dx, dweight and dbias may be NULL.  ws:
+ * output's first element to its last (mean, rstd, dweight, dbias and ws are
+ * outputs) must not overlap an input's or another output's (PROFK_EINVAL).  Any of dx, dweight and dbias may be NULL.  ws:
  * profk_layer_norm_grad_workspace_size(T, D) bytes, 16-byte aligned; NULL is
  * accepted without dweight and dbias. */
 int profk_layer_norm(int32_t dtype, const void* x, int64_t T, int64_t D, int64_t x_stride, int32_t param_dtype,
@@ -490,7 +490,8 @@ int profk_layer_norm_grad(int32_t dtype, const void* x, int64_t T, int64_t D, in
  *   ws        profk_linear_workspace_size(M, K, N) and
  *             profk_linear_grad_workspace_size(M, K, N) bytes, 16-byte aligned
  *             (NULL for 0).
- * Outputs must not overlap inputs otherwise (PROFK_EINVAL). */
+ * Outputs, ws among them, must not overlap inputs otherwise, nor each other
+ * (PROFK_EINVAL). */
 enum { PROFK_ACT_NONE = 0, PROFK_ACT_RELU = 1, PROFK_ACT_GELU = 2, PROFK_ACT_SILU = 3 };
 enum { PROFK_DZ_BF16 = 256 };       /* profk_linear_grad: activation | PROFK_DZ_BF16 */
 size_t profk_linear_workspace_size(int64_t M, int64_t K, int64_t N);
@@ -515,7 +516,7 @@ int profk_linear_grad(int32_t dtype, const void* dy, int64_t dy_stride, const vo
  *
  *   logits, out  fp32 or bf16 [T, V], rows x_stride and out_stride elements
  *             apart; out may be the logits (same stride), and must not overlap
- *             them otherwise (PROFK_EINVAL).  T = 0 is accepted, 1 <= V <= 2^31 - 1.
+ *             them otherwise, nor a list or mask (PROFK_EINVAL).  T = 0 is accepted, 1 <= V <= 2^31 - 1.
  *   tokens    int64 [n_tokens], row r's history at token_offsets[r] up to
  *             token_offsets[r + 1] (int64 [T + 1]); NULL: no history.  Tokens
  *             outside 0 .. V - 1 (padding) count nowhere.  n_prompt int64 [T] or

@@ -4,6 +4,7 @@
 
 #include <cmath>
 #include <cstdint>
+#include <initializer_list>
 #include <mutex>
 
 #include "adjust.h"
@@ -527,9 +528,21 @@ struct Span {
   Span(const void* p, int64_t R, int64_t C, int64_t stride, int32_t dtype)
       : at(reinterpret_cast<uintptr_t>(p)),
         bytes(p && R > 0 && C > 0 ? static_cast<uintptr_t>((R - 1) * stride + C) * elem_size(dtype) : 0) {}
+  Span(const void* p, size_t n) : at(reinterpret_cast<uintptr_t>(p)), bytes(p ? n : 0) {}
 };
 bool overlap(const Span& a, const Span& b) {
   return a.bytes && b.bytes && a.at < b.at + b.bytes && b.at < a.at + a.bytes;
+}
+
+// An output that overlaps an input or another output.
+bool any_overlap(std::initializer_list<Span> outs, std::initializer_list<Span> ins) {
+  for (const Span* o = outs.begin(); o != outs.end(); ++o) {
+    for (const Span& i : ins)
+      if (overlap(*o, i)) return true;
+    for (const Span* p = o + 1; p != outs.end(); ++p)
+      if (overlap(*o, *p)) return true;
+  }
+  return false;
 }
 
 bool norm_ok(int64_t T, int64_t D) { return T >= 0 && T <= static_cast<int64_t>(INT32_MAX) && D >= 1 && D <= profk::kNormMaxD; }
@@ -548,7 +561,9 @@ int profk_layer_norm(int32_t dtype, const void* x, int64_t T, int64_t D, int64_t
       !aligned(weight, elem_size(param_dtype)) || !aligned(bias, elem_size(param_dtype)))
     return PROFK_EINVAL;
   const bool same = x == out && dtype == out_dtype && (x_stride == out_stride || T == 1);
-  if (!same && overlap(Span(x, T, D, x_stride, dtype), Span(out, T, D, out_stride, out_dtype))) return PROFK_EINVAL;
+  const Span sx(x, T, D, x_stride, dtype), so(out, T, D, out_stride, out_dtype), sm(mean, 1, T, T, PROFK_F32),
+      sr(rstd, 1, T, T, PROFK_F32), sw(weight, 1, D, D, param_dtype), sb(bias, 1, D, D, param_dtype);
+  if ((!same && overlap(sx, so)) || any_overlap({so, sm, sr}, {sw, sb}) || any_overlap({sm, sr}, {sx})) return PROFK_EINVAL;
   const profk::NormArgs a{x, static_cast<uint64_t>(x_stride), static_cast<uint64_t>(out_stride),
                           static_cast<uint32_t>(T), static_cast<uint32_t>(D), weight, bias, param_dtype, eps, out,
                           mean, rstd};
@@ -578,7 +593,12 @@ int profk_layer_norm_grad(int32_t dtype, const void* x, int64_t T, int64_t D, in
   const Span out(dx, T, D, dx_stride, dtype);
   if (overlap(out, Span(x, T, D, x_stride, dtype)) || overlap(out, Span(dy, T, D, dy_stride, dy_dtype)))
     return PROFK_EINVAL;
-  if (sums && ws_bytes < profk_layer_norm_grad_workspace_size(T, D)) return PROFK_EWORKSPACE;
+  const size_t need = sums ? profk_layer_norm_grad_workspace_size(T, D) : 0;
+  if (ws_bytes < need) return PROFK_EWORKSPACE;
+  if (any_overlap({out, Span(dweight, 1, D, D, param_dtype), Span(dbias, 1, D, D, param_dtype), Span(ws, need)},
+                  {Span(x, T, D, x_stride, dtype), Span(dy, T, D, dy_stride, dy_dtype), Span(weight, 1, D, D, param_dtype),
+                   Span(mean, 1, T, T, PROFK_F32), Span(rstd, 1, T, T, PROFK_F32)}))
+    return PROFK_EINVAL;
   const profk::NormGradArgs a{x, dy, static_cast<uint64_t>(x_stride), static_cast<uint64_t>(dy_stride),
                               static_cast<uint64_t>(dx_stride), static_cast<uint32_t>(T), static_cast<uint32_t>(D),
                               weight, param_dtype, mean, rstd, dx, dweight, dbias,
@@ -621,10 +641,9 @@ int profk_linear(const void* x, int64_t M, int64_t K, int64_t x_stride, const vo
   const Span sx(x, M, K, x_stride, PROFK_BF16), sw(w, N, K, w_stride, PROFK_BF16), so(out, M, N, N, out_dtype),
       sp(pre, M, N, N, out_dtype), sr(residual, M, N, residual_stride, out_dtype), sb(bias, 1, N, N, PROFK_F32);
   const bool same = residual == out && (residual_stride == N || M == 1);
-  for (const Span& o : {so, sp})
-    if (overlap(o, sx) || overlap(o, sw) || overlap(o, sb)) return PROFK_EINVAL;
-  if (overlap(so, sp) || overlap(sp, sr) || (!same && overlap(so, sr))) return PROFK_EINVAL;
+  if (any_overlap({so, sp}, {sx, sw, sb}) || overlap(sp, sr) || (!same && overlap(so, sr))) return PROFK_EINVAL;
   if (ws_bytes < need) return PROFK_EWORKSPACE;
+  if (any_overlap({Span(ws, need)}, {sx, sw, sb, sr, so, sp})) return PROFK_EINVAL;
   const profk::LinCall c{x, w, static_cast<uint64_t>(x_stride), static_cast<uint64_t>(w_stride), M, N, K, bias,
                          activation, out_dtype, residual, static_cast<uint64_t>(residual_stride), out, pre, ws};
   const hipError_t e = profk::launch_linear(c, static_cast<hipStream_t>(stream));
@@ -652,10 +671,9 @@ int profk_linear_grad(int32_t dtype, const void* dy, int64_t dy_stride, const vo
     return PROFK_EINVAL;
   const Span sx(x, M, K, x_stride, PROFK_BF16), sw(w, N, K, w_stride, PROFK_BF16), sd(dy, M, N, dy_stride, dtype),
       sp(pre, M, N, N, dtype), s1(dx, M, K, K, PROFK_BF16), s2(dw, N, K, K, PROFK_BF16), s3(dbias, 1, N, N, PROFK_F32);
-  for (const Span& o : {s1, s2, s3})
-    if (overlap(o, sx) || overlap(o, sw) || overlap(o, sd) || overlap(o, sp)) return PROFK_EINVAL;
-  if (overlap(s1, s2) || overlap(s1, s3) || overlap(s2, s3)) return PROFK_EINVAL;
+  if (any_overlap({s1, s2, s3}, {sx, sw, sd, sp})) return PROFK_EINVAL;
   if (ws_bytes < need) return PROFK_EWORKSPACE;
+  if (any_overlap({Span(ws, need)}, {sx, sw, sd, sp, s1, s2, s3})) return PROFK_EINVAL;
   const profk::LinGradCall c{dy, pre, static_cast<uint64_t>(dy_stride), dtype, activation, round_dz, x, w,
                              static_cast<uint64_t>(x_stride), static_cast<uint64_t>(w_stride), M, N, K, dx, dw, dbias,
                              ws};
@@ -684,6 +702,13 @@ int check_adjust(int32_t dtype, const void* logits, int64_t T, int64_t V, int64_
   if (!logits || !out || (tokens && !token_offsets)) return PROFK_ENULL;
   if (!aligned(logits, elem_size(dtype)) || !aligned(out, elem_size(dtype)) || !aligned(tokens, 8) ||
       !aligned(token_offsets, 8) || !aligned(repetition, 4) || !aligned(allowed, 4) || !aligned(mask, 8))
+    return PROFK_EINVAL;
+  const size_t rows = static_cast<size_t>(T);
+  if (any_overlap({Span(out, T, V, out_stride, dtype)},
+                  {Span(tokens, static_cast<size_t>(n_tokens) * 8), Span(token_offsets, (rows + 1) * 8),
+                   Span(repetition, rows * 4), Span(mask, rows * 8),
+                   Span(allowed, allowed ? ((static_cast<size_t>(n_masks) - 1) * static_cast<size_t>(allowed_stride) +
+                                            (static_cast<size_t>(V) + 31) / 32) * 4 : 0)}))
     return PROFK_EINVAL;
   a->x = logits;
   a->out = const_cast<void*>(out);
@@ -720,7 +745,12 @@ int profk_adjust_logits(int32_t dtype, const void* logits, int64_t T, int64_t V,
       !aligned(bias_values, 4) || !aligned(bias_offsets, 8))
     return PROFK_EINVAL;
   const bool same = logits == out && (x_stride == out_stride || T == 1);
-  if (!same && overlap(Span(logits, T, V, x_stride, dtype), Span(out, T, V, out_stride, dtype))) return PROFK_EINVAL;
+  const Span so(out, T, V, out_stride, dtype);
+  const size_t rows = static_cast<size_t>(T), biases = bias_ids ? static_cast<size_t>(n_bias) : 0;
+  if ((!same && overlap(Span(logits, T, V, x_stride, dtype), so)) ||
+      any_overlap({so}, {Span(n_prompt, rows * 8), Span(presence, rows * 4), Span(frequency, rows * 4),
+                         Span(bias_ids, biases * 8), Span(bias_values, biases * 4), Span(bias_offsets, (rows + 1) * 8)}))
+    return PROFK_EINVAL;
   a.n_prompt = n_prompt;
   a.presence = presence;
   a.frequency = frequency;
