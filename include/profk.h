@@ -471,7 +471,8 @@ int profk_layer_norm_grad(int32_t dtype, const void* x, int64_t T, int64_t D, in
  * stride and alignment; products are exact, sums fp32; bias fp32 [N].
  *
  *   activation  PROFK_ACT_*: gelu is z/2 (1 + erf(z / sqrt 2)), silu z / (1 +
- *             e^-z).  An infinite z gives their limits; relu has slope 0 at 0.
+ *             e^-z), computed to 2^-19 of themselves (results below 2e-36: to
+ *             that).  An infinite z gives their limits; relu has slope 0 at 0.
  *   out, pre, residual, dy  fp32 or bf16 (`out_dtype`, `dtype`) [M, N]; out and
  *             pre contiguous.  pre, where it is not NULL, takes z, rounded, for
  *             the gradient (needed there but for PROFK_ACT_NONE).  residual may
