@@ -36,15 +36,6 @@ constexpr uint32_t few_per_cu(int ng, int xl, bool ksplit) {
   return kCuLds / few_lds(ng, xl, ksplit) < 8 ? kCuLds / few_lds(ng, xl, ksplit) : 8;
 }
 
-// s_waitcnt vmcnt(N) lgkmcnt(0): all but this wave's N newest loads are done,
-// and so are its LDS reads.
-template <int N> __device__ __forceinline__ void few_wait() {
-  static_assert(N >= 0 && N < 64, "vmcnt");
-  asm volatile("" ::: "memory");
-  __builtin_amdgcn_s_waitcnt((N & 0xF) | ((N >> 4) << 14) | (0x7 << 4));
-  asm volatile("" ::: "memory");
-}
-
 // XL: loads of a's rows, 8 each.
 template <int NG, int XL, bool KSPLIT> __global__ __launch_bounds__(kFewBS) void k_prod_few(ProdArgs g) {
   constexpr int MG = XL > 2 ? 2 : 1, kLoads = NG * 2 + XL;
@@ -136,7 +127,7 @@ template <int NG, int XL, bool KSPLIT> __global__ __launch_bounds__(kFewBS) void
   const uint32_t xr = XL == 1 ? c & 7 : c;      // (rows past a's last load are not stored)
   auto step = [&](uint4* cur, uint4* old) {
     // (this wave's own loads and reads: no barrier)
-    few_wait<2 * kLoads>();
+    prod_wait<2 * kLoads>();
     issue(old);
     const uint4* const st = cur + w * kQ;
 #pragma unroll
@@ -165,7 +156,7 @@ template <int NG, int XL, bool KSPLIT> __global__ __launch_bounds__(kFewBS) void
     if (t + 2 < total) step(s2, s1);
     if (t + 3 < total) step(s3, s2);
   }
-  few_wait<0>();   // (no load may reach LDS after the workgroup's end)
+  prod_wait<0>();   // (no load may reach LDS after the workgroup's end)
 }
 
 template <int NG, int XL> void few_launch(const ProdArgs& g, uint32_t cus, hipStream_t s) {

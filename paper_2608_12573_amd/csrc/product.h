@@ -24,6 +24,16 @@ struct ProdArgs {
   bool a_padded, b_padded;          // rows end in whole granules of 8, zeros past their end
 };
 
+// s_waitcnt vmcnt(N) lgkmcnt(0) (gfx9 encoding: vmcnt in bits 3:0 and 15:14,
+// expcnt in 6:4, lgkmcnt in 11:8): all but this wave's N newest loads are done,
+// and so are its LDS reads.
+template <int N> __device__ __forceinline__ void prod_wait() {
+  static_assert(N >= 0 && N < 64, "vmcnt");
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt((N & 0xF) | ((N >> 4) << 14) | (0x7 << 4));
+  asm volatile("" ::: "memory");
+}
+
 // ------------------------------------------------------------ activations ---
 // An infinite z gives the limit, NaN stays NaN.
 //

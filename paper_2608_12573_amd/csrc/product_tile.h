@@ -59,15 +59,6 @@ constexpr uint32_t kPanel = 8;      // column tiles of a panel
 
 __device__ const uint4 g_zero_granule = {0, 0, 0, 0};
 
-// s_waitcnt vmcnt(N) lgkmcnt(0) (gfx9 encoding: vmcnt in bits 3:0 and 15:14,
-// expcnt in 6:4, lgkmcnt in 11:8): all but this wave's N newest loads are done,
-// and so are its LDS reads.
-template <int N> __device__ __forceinline__ void prod_wait() {
-  static_assert(N >= 0 && N < 64, "vmcnt");
-  asm volatile("" ::: "memory");
-  __builtin_amdgcn_s_waitcnt((N & 0xF) | ((N >> 4) << 14) | (0x7 << 4));
-  asm volatile("" ::: "memory");
-}
 // A workgroup barrier that waits for nothing else, across which the compiler
 // moves no memory access.
 __device__ __forceinline__ void prod_barrier() {
@@ -266,10 +257,7 @@ __device__ __forceinline__ void prod_body(const ProdArgs& g, uint32_t tiles_i, u
 #pragma unroll
     for (int i = 0; i < MI; ++i)
 #pragma unroll
-      for (int j = 0; j < NJ; ++j) {
-        if constexpr (MI * NJ == 16) asm volatile("" : "+a"(acc[i][j]));
-        else asm volatile("" : "+v"(acc[i][j]));
-      }
+      for (int j = 0; j < NJ; ++j) asm volatile("" : "+v"(acc[i][j]));
   };
   // LDS reads and loads between the matrix instructions of a quarter: the first
   // one waits for the reads before, and loads issued one after the other keep
