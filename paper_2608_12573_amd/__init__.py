@@ -325,12 +325,18 @@ def _given(*tensors):
     """Outputs that the caller gave (None: not this one) are about to be written,
     through their pointers: autograd's check of what it saved has to see that, and
     what it records cannot be written behind its back."""
+    # (a plain loop, and torch's own function of autograd.graph.increment_version
+    # without the checks before it: a microsecond of each call less)
     torch = _torch()
-    tensors = [t for t in tensors if t is not None]
-    if torch.is_grad_enabled() and any(t.requires_grad for t in tensors):
-        raise ProfkError("a given output requires a gradient, and the call would not be recorded: give a detached one, or "
-                         "call under torch.no_grad()")
-    torch.autograd.graph.increment_version(tensors)
+    records = torch.is_grad_enabled()
+    left_out = False
+    for t in tensors:
+        if t is None:
+            left_out = True
+        elif records and t.requires_grad:
+            raise ProfkError("a given output requires a gradient, and the call would not be recorded: give a detached one, "
+                             "or call under torch.no_grad()")
+    torch._C._increment_version([t for t in tensors if t is not None] if left_out else tensors)
 
 
 def _recorded(*tensors):
@@ -341,7 +347,11 @@ def _recorded(*tensors):
     if forward._current_level >= 0:
         if any(t is not None and forward.unpack_dual(t).tangent is not None for t in tensors):
             raise ProfkError("an input has a forward-mode tangent, which this call would lose: take its gradient backwards")
-    return torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors)
+    if torch.is_grad_enabled():
+        for t in tensors:
+            if t is not None and t.requires_grad:
+                return True
+    return False
 
 
 def _nbytes(t):
