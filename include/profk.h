@@ -448,7 +448,10 @@ int profk_mx4_linear(int32_t dtype, const void* x, int64_t M, int64_t K, int64_t
  *   mean, rstd  fp32 [T]: m and r (outputs that may be NULL; the gradient's
  *             inputs).
  *   eps       finite, above 0 (a row of equal values has no direction without).
- *   NaN, inf  a row with either is NaN.
+ *   NaN, inf  a row with either is NaN.  A row whose sum of squares leaves fp32
+ *             (values about 2^64 / sqrt D and more) has rstd 0.
+ *   gradient  of the given, rounded m and r: where a row's mean is far larger than
+ *             its deviation, n is off by up to 2^-24 |m| r.
  * out may be x itself, of the same type and stride; else the memory from an
  * output's first element to its last (mean, rstd, dweight, dbias and ws are
  * outputs) must not overlap an input's or another output's (PROFK_EINVAL).  Any of dx, dweight and dbias may be NULL.  ws:
@@ -483,9 +486,12 @@ int profk_layer_norm_grad(int32_t dtype, const void* x, int64_t T, int64_t D, in
  *             PROFK_DZ_BF16, or-ed to the gradient's activation, rounds it to one,
  *             within 2^-8: about half the products' time.  An infinity or NaN in x
  *             or W leaves infinities or NaN in all that it enters.
- *   time      rows of x and W that start at multiples of 16 bytes are the fastest.
- *             Where K is no multiple of 8 both are copied to such rows first (not
- *             for M <= 4); others at odd places run at about half the rate.
+ *   time      rows of x and W that start at multiples of 16 bytes are the fastest;
+ *             up to 4 rows of x are as fast from any place.  Where K is no multiple
+ *             of 8 both are copied to such rows first (1.3 to 3 times the time).
+ *             Other views at odd places take a kernel of any operands: 2.2 to 2.5
+ *             times the time at 4096 x 4096 x 12288, four to eleven times at 5 to
+ *             256 rows, six to eight in the gradients.  A copy is faster there.
  *   sizes     1 <= K <= 2^20, 0 <= M, N <= 2^31 - 1.  M = 0 sets dW and dbias to
  *             zero, N = 0 dx.
  *   ws        profk_linear_workspace_size(M, K, N) and
@@ -533,7 +539,7 @@ int profk_linear_grad(int32_t dtype, const void* dy, int64_t dy_stride, const vo
  *             one (n_masks must be T or 1).
  *   NaN, inf  stay where they are allowed; where they are forbidden -inf.  A row
  *             that allows nothing is all -inf.
- *   time      one read and one write of the logits; each piece of a row (64 KiB
+ *   time      one read and one write of the logits; each piece of a row (32 KiB
  *             at most) goes through the row's history and biases again, twice where
  *             it has more than 16 biases or, of bf16 logits, the history more than
  *             16383 tokens.

@@ -30,8 +30,10 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
 // ------------------------------------------------- product of any operands ---
 // Any sizes, strides and alignments: tiles of 128 x 128 on four waves of 64 x 64, 32
-// of k at a time through registers to LDS, its rows 80 bytes apart (4096 x 4096 x
-// 12288 688 us, against 304 of the tiled product).
+// of k at a time through registers to LDS, its rows 80 bytes apart.  One workgroup a
+// tile takes all of k: 4096 x 4096 x 12288 742 us on rows at odd elements, against 296
+// of the tiled product on whole granules; where the tiles are few the more (8 x 4096 x
+// 4096 102 and 9.3, 256 rows 129 and 21; gradients of 64 x 4096 x 4096 257 and 33).
 constexpr uint32_t kAnyB = 128, kAnyK = 32, kAnyRow = 40;
 
 // 8 neighbours in memory, those from `left` on 0.

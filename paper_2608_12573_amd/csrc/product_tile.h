@@ -24,8 +24,8 @@
 //
 // 256 x 256 tiles on eight waves of 64 x 128: a stage moves 64 KB for 32 matrix
 // instructions a wave, of 32 cycles, two waves a SIMD.  Measured: 8192^3 to bf16
-// 772 us (1.42 PFLOP/s; the library's 697), 4096 x 4096 x 12288 304 us (1.36),
-// with silu and a residual 316.  At 8192^3 the matrix cores are busy for 84 % of
+// 774 us (1.42 PFLOP/s; the library's 669-700), 4096 x 4096 x 12288 296-330 us (1.25
+// to 1.39, by clock; the library's 272-325), with silu and a residual 326-341.  At 8192^3 the matrix cores are busy for 84 % of
 // the cycles (the library's for 88), at a clock that falls to 1.5 GHz under both;
 // this kernel reads LDS half as much again as a wave of 128 x 128 would.  What it
 // took: the last two fragments of a stage read ahead, which frees its LDS half way
